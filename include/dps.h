@@ -289,6 +289,154 @@ dps_status dps_linear_grouped(int mode, uint32_t flags, const uint16_t *x_sorted
                               uint16_t *y, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Paged KV cache: what a decode step runs between its QKV and O products, on
+ * the KV blocks that share the region with the residuals (Sec. IV-B "Shared
+ * Region"; block ids as dps_sum_alloc hands them out).
+ *   dps_kv_map       a step's block tables and slot maps from request lengths
+ *   dps_kv_store     head norms and rotation of queries and keys; keys and
+ *                    values written to their slots
+ *   dps_attn_decode  attention of one new token a row over the blocks
+ * Lengths, tables and slots live on the device and are read there only, so a
+ * captured graph serves every step; entries that point outside the cache, the
+ * tables or the rotation table are never followed.
+ * ------------------------------------------------------------------------ */
+
+/* Element types: FP16, BF16, and (cache only) OCP E4M3 with a scale. */
+enum { DPS_KV_F16 = 0, DPS_KV_BF16 = 1, DPS_KV_E4M3 = 2 };
+
+/* The blocks of one layer's cache.  Block b starts at pool + b * block_stride
+ * and holds T = block_tokens tokens:
+ *     K  [kv_heads][row_bytes / 64][T][64 bytes]   row_bytes = head_dim * element bytes
+ *     V  [kv_heads][T][head_dim]
+ * A key row lies in 64-byte segments, T of them side by side, so that what a
+ * matrix instruction takes of 16 tokens is contiguous.  Slot s is token s mod T
+ * of block s / T.
+ *   pool          device, 16-byte aligned.  A layer whose blocks hold other
+ *                 layers' too passes its own first byte.
+ *   pool_bytes    from pool to the end of the last block's bytes; the blocks
+ *                 that fit it count, ids from 0.
+ *   block_stride  bytes, a multiple of 16, at least a block's.
+ *   kv_heads      1..4096.   head_dim  64, 96, 128, 192 or 256 (E4M3: not 96).
+ *   block_tokens  a power of two, 16..256.
+ *   type          DPS_KV_*.  E4M3 holds value / scale, k_scale for keys and
+ *                 v_scale for values (positive; other types ignore their
+ *                 value, which still has to be positive). */
+typedef struct {
+    uint8_t *pool;
+    int64_t pool_bytes;
+    int64_t block_stride;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t block_tokens;
+    int32_t type;
+    float k_scale;
+    float v_scale;
+} dps_kv_cache;
+
+/* What dps_kv_map writes, device arrays.  The new tokens of all requests, in
+ * request order, are the rows of the step; rows is the room for them (a graph's
+ * batch).  Rows past the last token, and tokens past `rows`, are padding and
+ * left out. */
+typedef struct {
+    int64_t rows;
+    int32_t *q_start;  /* [requests + 1] first row of each request; last: rows in use */
+    int32_t *seq_len;  /* [requests] tokens after the step                            */
+    int32_t *counts;   /* [2] new tokens in all, blocks taken off `fresh` in all; the
+                          step fits if they are at most rows and n_fresh              */
+    int32_t *pos;      /* [rows] position (padding: 0)                                */
+    int64_t *slot;     /* [rows] slot (-1: padding, or a token without a block)       */
+    int32_t *req;      /* [rows] request (padding: -1)                                */
+    int32_t *kv_len;   /* [rows] pos + 1, the tokens the row attends (padding: 0)     */
+} dps_kv_step;
+
+/* Block tables and slot maps of a step.  With B(x) = ceil(x / block_tokens),
+ * request r takes the next B(ctx_len + new_len) - B(ctx_len) ids of `fresh`
+ * (requests in order) into table[r][B(ctx_len)...]; its i-th new token has
+ * position ctx_len + i and slot table[r][pos / T] * T + pos mod T.  Other table
+ * entries are not touched.  Past the end of `fresh` an entry becomes -1; blocks
+ * past table_cols are not taken.  Negative lengths count as 0.  The same
+ * arguments give the same results again.
+ *   ctx_len, new_len  device int32[requests]: tokens in the cache before the
+ *                     step, tokens of the step (0: idle; 1: decode; more: prompt).
+ *   requests          0..4096.
+ *   fresh             device int32[n_fresh]: free block ids.
+ *   table             device int32[requests][table_cols], fewer than 2^31 entries.
+ *   step              host pointer; its arrays are written. */
+dps_status dps_kv_map(const int32_t *ctx_len, const int32_t *new_len, int64_t requests,
+                      int32_t block_tokens, const int32_t *fresh, int64_t n_fresh, int32_t *table,
+                      int64_t table_cols, const dps_kv_step *step, void *stream);
+
+/* Arguments of dps_kv_store.  Strides are in elements, multiples of 8; rows
+ * are 16-byte aligned. */
+typedef struct {
+    int64_t rows;
+    int64_t heads;            /* query heads, 0..65536                                  */
+    const uint16_t *qkv;      /* [rows]: heads query, kv_heads key, kv_heads value heads */
+    int64_t qkv_stride;
+    const int64_t *slot;      /* [rows]; a slot outside the cache (-1) stores nothing   */
+    const int32_t *pos;       /* [rows] positions; NULL without a rotation              */
+    const float *rope;        /* [max_pos][rot]: rot / 2 cosines, rot / 2 sines; NULL: none */
+    int64_t max_pos;
+    int32_t rot;              /* leading values of a head that turn, a multiple of 16    */
+    int32_t adjacent;         /* pairs (2i, 2i + 1); 0: pairs (i, i + rot / 2)           */
+    const uint16_t *q_weight; /* [head_dim] norm weights of query and key heads; both    */
+    const uint16_t *k_weight; /* NULL: no norm                                           */
+    float eps;
+    int32_t type;             /* DPS_KV_F16 or DPS_KV_BF16: of qkv, weights and outputs  */
+    uint16_t *q_out;          /* [rows][heads * head_dim]; may be qkv itself             */
+    int64_t q_out_stride;
+    uint16_t *k_out;          /* [rows][kv_heads * head_dim] keys as stored in a 16-bit  */
+    int64_t k_out_stride;     /* cache, or NULL; may be qkv's own key columns            */
+} dps_kv_store_args;
+
+/* Head norms, rotation and store, in one pass over the QKV product.  A query or
+ * key head x becomes x * rsqrt(mean(x^2) + eps) * w (with weights), then each
+ * pair (a, b) of its leading rot values becomes (a cos - b sin, b cos + a sin)
+ * at the row's position; values are stored as they are.  fp32 arithmetic, one
+ * rounding (nearest even; E4M3: of value / scale clamped to +-448).  A row whose
+ * position is outside the rotation table gets NaN in what turns.  A 16-bit cache
+ * has the type of the activations; an E4M3 cache goes with either.  Rows with
+ * the same slot: one of them is stored. */
+dps_status dps_kv_store(const dps_kv_store_args *args, const dps_kv_cache *cache, void *stream);
+
+/* Arguments of dps_attn_decode.  Strides are in elements, multiples of 8. */
+typedef struct {
+    int64_t rows;
+    int64_t heads;          /* query heads, a multiple of kv_heads, up to 65536           */
+    const uint16_t *q;      /* [rows][heads][head_dim]                                    */
+    int64_t q_stride;
+    const int32_t *table;   /* [requests][table_cols] block ids                           */
+    int64_t requests;
+    int64_t table_cols;
+    const int32_t *req;     /* [rows] table row of each row; NULL: its own index          */
+    const int32_t *kv_len;  /* [rows] tokens attended: positions 0 .. kv_len - 1          */
+    int32_t window;         /* > 0: only the last `window` of them                        */
+    int32_t type;           /* DPS_KV_F16 or DPS_KV_BF16: of q and out                    */
+    float scale;            /* of the products q . k                                      */
+    uint16_t *out;          /* [rows][heads][head_dim]                                    */
+    int64_t out_stride;
+    float *lse;             /* [rows][heads] log of the sum of exponentials, or NULL      */
+} dps_attn_args;
+
+/* Workspace bytes of dps_attn_decode on the current device.  Contents on entry
+ * do not matter. */
+size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t kv_heads, int64_t head_dim);
+
+/* One new token a row over the paged cache: softmax(scale * q K^T) V, query head
+ * h on key/value head h / (heads / kv_heads), fp32 softmax and sums, one
+ * rounding.  The work is split over the length of every row alike and joined in
+ * a second launch; results do not depend on timing.  Tokens in a block outside
+ * the cache (a table entry of -1) are left out; a length past the table's
+ * columns is cut there; a row that attends nothing (length 0, req outside the
+ * table, no block) gives zeros and lse -inf.  Cache bytes outside the attended
+ * tokens may hold anything.  Several rows may share a request (kv_len then says
+ * what each sees).
+ *   ws  device scratch of ws_bytes >= dps_attn_workspace_bytes(...), 256-byte
+ *       aligned. */
+dps_status dps_attn_decode(const dps_attn_args *args, const dps_kv_cache *cache, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * SUM manager (Sec. IV-B "SUM manager"; Sec. IV-D, Algorithm 1): host-side
  * bookkeeping of the shared region's physical units.  A unit holds either
  * one residual tensor (BACKED) or KV blocks (AVAIL: some free, FULL: none

@@ -710,3 +710,286 @@ DPS_EXPORT dps_status dps_linear_static(int mode, uint32_t flags, const uint16_t
     return run_linear(mode, flags, x, nullptr, m, w, y, ws, DPS_STATIC_SCRATCH_BYTES,
                       (hipStream_t)stream, false);
 }
+
+// ---- paged KV cache -------------------------------------------------------------
+
+namespace {
+
+// Cache descriptor checks shared by the store and the attention.
+dps_status check_cache(const dps_kv_cache *c, dps::KvCacheView *out)
+{
+    REQUIRE(c != nullptr, DPS_ERR_INVALID_ARG, "cache descriptor is NULL");
+    REQUIRE(c->type == DPS_KV_F16 || c->type == DPS_KV_BF16 || c->type == DPS_KV_E4M3,
+            DPS_ERR_INVALID_ARG, "unknown cache type");
+    const int elt = c->type == DPS_KV_E4M3 ? 1 : 2;
+    REQUIRE(c->kv_heads >= 1 && c->kv_heads <= 4096, DPS_ERR_INVALID_ARG,
+            "kv_heads must be in 1..4096");
+    REQUIRE(c->block_tokens >= 16 && c->block_tokens <= 256 &&
+                (c->block_tokens & (c->block_tokens - 1)) == 0,
+            DPS_ERR_UNSUPPORTED, "block_tokens must be a power of two in 16..256");
+    REQUIRE(c->head_dim == 64 || c->head_dim == 96 || c->head_dim == 128 || c->head_dim == 192 ||
+                c->head_dim == 256,
+            DPS_ERR_UNSUPPORTED, "head_dim must be 64, 96, 128, 192 or 256");
+    REQUIRE(c->head_dim * elt % 64 == 0, DPS_ERR_UNSUPPORTED,
+            "an E4M3 cache needs a head_dim that is a multiple of 64");
+    const int64_t bytes = 2 * (int64_t)c->kv_heads * c->block_tokens * c->head_dim * elt;
+    // the kernels address a block with 32-bit offsets (4096 heads: 2^30 bytes)
+    REQUIRE(c->block_stride >= bytes, DPS_ERR_INVALID_ARG,
+            "block_stride is smaller than one block");
+    REQUIRE(c->pool != nullptr, DPS_ERR_INVALID_ARG, "cache pool is NULL");
+    REQUIRE(aligned(c->pool, 16) && c->block_stride % 16 == 0, DPS_ERR_ALIGNMENT,
+            "cache pool or block_stride is not 16-byte aligned");
+    REQUIRE(c->pool_bytes >= bytes, DPS_ERR_INVALID_ARG, "pool_bytes is smaller than one block");
+    REQUIRE(c->k_scale > 0.0f && c->v_scale > 0.0f && c->k_scale <= 3.4e38f &&
+                c->v_scale <= 3.4e38f,
+            DPS_ERR_INVALID_ARG, "k_scale and v_scale must be positive and finite");
+    out->pool = c->pool;
+    out->block_stride = c->block_stride;
+    out->n_blocks = (c->pool_bytes - bytes) / c->block_stride + 1;
+    out->log2_tokens = __builtin_ctz((unsigned)c->block_tokens);
+    out->kv_heads = c->kv_heads;
+    out->dim = c->head_dim;
+    out->k_scale = c->type == DPS_KV_E4M3 ? c->k_scale : 1.0f;
+    out->v_scale = c->type == DPS_KV_E4M3 ? c->v_scale : 1.0f;
+    return DPS_OK;
+}
+
+// The 16-bit type of the activations beside a cache of `type`.
+dps_status check_act(int act, int type)
+{
+    REQUIRE(act == DPS_KV_F16 || act == DPS_KV_BF16, DPS_ERR_INVALID_ARG,
+            "activations must be FP16 or BF16");
+    REQUIRE(type == DPS_KV_E4M3 || type == act, DPS_ERR_INVALID_ARG,
+            "a 16-bit cache holds the type of the activations");
+    return DPS_OK;
+}
+
+// Launch shape and workspace of an attention call.
+struct AttnPlan {
+    int groups, step;  // passes over a key/value head, query heads of a pass
+    int blocks;        // ranges of the work line
+    size_t out_bytes, stat_bytes, unit_bytes;
+    size_t bytes() const { return out_bytes + stat_bytes + unit_bytes; }
+};
+
+AttnPlan plan_attn(int64_t rows, int64_t heads, int64_t kv_heads, int64_t dim)
+{
+    AttnPlan a;
+    const int64_t group = heads / kv_heads;
+    a.groups = (int)cdiv(group, 16);
+    a.step = (int)cdiv(group, a.groups);
+    a.groups = (int)cdiv(group, a.step);
+    const int64_t lines = kv_heads * a.groups;
+    // two blocks of four waves a CU over all lines
+    const int64_t blocks = 2 * (int64_t)current_cu_count() / lines;
+    a.blocks = (int)(blocks < 1 ? 1 : blocks);
+    const int64_t parts = 2 * a.blocks * lines * a.step;
+    a.out_bytes = align256(parts * dim * 4);
+    a.stat_bytes = align256(parts * 8);
+    a.unit_bytes = align256((rows + 1) * 4);
+    return a;
+}
+
+}  // namespace
+
+DPS_EXPORT dps_status dps_kv_map(const int32_t *ctx_len, const int32_t *new_len, int64_t requests,
+                                 int32_t block_tokens, const int32_t *fresh, int64_t n_fresh,
+                                 int32_t *table, int64_t table_cols, const dps_kv_step *step,
+                                 void *stream)
+{
+    g_err[0] = 0;
+    REQUIRE(requests >= 0 && table_cols >= 0 && n_fresh >= 0, DPS_ERR_INVALID_ARG,
+            "requests, table_cols or n_fresh is negative");
+    REQUIRE(requests <= 4096, DPS_ERR_UNSUPPORTED, "more than 4096 requests in one call");
+    REQUIRE(block_tokens >= 16 && block_tokens <= 256 && (block_tokens & (block_tokens - 1)) == 0,
+            DPS_ERR_UNSUPPORTED, "block_tokens must be a power of two in 16..256");
+    REQUIRE(table_cols <= 0x7fffffff && requests * table_cols <= 0x7fffffff, DPS_ERR_UNSUPPORTED,
+            "table of 2^31 entries or more");
+    REQUIRE(step != nullptr, DPS_ERR_INVALID_ARG, "step descriptor is NULL");
+    REQUIRE(step->rows >= 0 && step->rows <= 0x7fffffff, DPS_ERR_INVALID_ARG,
+            "rows must be in 0..2^31-1");
+    REQUIRE(requests == 0 || (ctx_len != nullptr && new_len != nullptr), DPS_ERR_INVALID_ARG,
+            "ctx_len or new_len is NULL");
+    REQUIRE(requests * table_cols == 0 || table != nullptr, DPS_ERR_INVALID_ARG, "table is NULL");
+    REQUIRE(n_fresh == 0 || fresh != nullptr, DPS_ERR_INVALID_ARG, "fresh is NULL");
+    REQUIRE(step->q_start != nullptr && step->counts != nullptr &&
+                (requests == 0 || step->seq_len != nullptr),
+            DPS_ERR_INVALID_ARG, "q_start, seq_len or counts is NULL");
+    REQUIRE(step->rows == 0 || (step->pos != nullptr && step->slot != nullptr &&
+                                step->req != nullptr && step->kv_len != nullptr),
+            DPS_ERR_INVALID_ARG, "pos, slot, req or kv_len is NULL");
+    REQUIRE(aligned(ctx_len, 4) && aligned(new_len, 4) && aligned(fresh, 4) && aligned(table, 4) &&
+                aligned(step->q_start, 4) && aligned(step->seq_len, 4) &&
+                aligned(step->counts, 4) && aligned(step->pos, 4) && aligned(step->slot, 8) &&
+                aligned(step->req, 4) && aligned(step->kv_len, 4),
+            DPS_ERR_ALIGNMENT, "an array is off the alignment of its entries");
+    dps::KvMapProblem p;
+    p.ctx_len = ctx_len;
+    p.new_len = new_len;
+    p.requests = (int32_t)requests;
+    p.log2_tokens = __builtin_ctz((unsigned)block_tokens);
+    p.fresh = fresh;
+    p.n_fresh = n_fresh;
+    p.table = table;
+    p.table_cols = table_cols;
+    p.rows = (int32_t)step->rows;
+    p.q_start = step->q_start;
+    p.seq_len = step->seq_len;
+    p.counts = step->counts;
+    p.pos = step->pos;
+    p.slot = step->slot;
+    p.req = step->req;
+    p.kv_len = step->kv_len;
+    return launched(dps::launch_kv_map(p, (hipStream_t)stream));
+}
+
+DPS_EXPORT dps_status dps_kv_store(const dps_kv_store_args *a, const dps_kv_cache *cache,
+                                   void *stream)
+{
+    g_err[0] = 0;
+    REQUIRE(a != nullptr, DPS_ERR_INVALID_ARG, "store arguments are NULL");
+    dps::KvStoreProblem p;
+    dps_status s = check_cache(cache, &p.cache);
+    if (s != DPS_OK)
+        return s;
+    s = check_act(a->type, cache->type);
+    if (s != DPS_OK)
+        return s;
+    const int64_t dim = cache->head_dim, kv_heads = cache->kv_heads;
+    REQUIRE(a->rows >= 0 && a->rows <= 0x7fffffff, DPS_ERR_INVALID_ARG,
+            "rows must be in 0..2^31-1");
+    REQUIRE(a->heads >= 0 && a->heads <= 65536, DPS_ERR_INVALID_ARG, "heads must be in 0..65536");
+    REQUIRE(a->rows <= 1 || a->qkv_stride >= (a->heads + 2 * kv_heads) * dim, DPS_ERR_INVALID_ARG,
+            "qkv_stride is smaller than a row");
+    REQUIRE(a->rows <= 1 || a->q_out_stride >= a->heads * dim, DPS_ERR_INVALID_ARG,
+            "q_out_stride is smaller than a row");
+    REQUIRE(a->rows <= 1 || a->k_out == nullptr || a->k_out_stride >= kv_heads * dim,
+            DPS_ERR_INVALID_ARG, "k_out_stride is smaller than a row");
+    if (a->rope != nullptr) {
+        REQUIRE(a->rot >= 16 && a->rot <= dim && a->rot % 16 == 0, DPS_ERR_INVALID_ARG,
+                "rot must be a multiple of 16, at most head_dim");
+        REQUIRE(a->max_pos >= 1, DPS_ERR_INVALID_ARG, "max_pos must be positive");
+    }
+    REQUIRE((a->q_weight == nullptr) == (a->k_weight == nullptr) || a->heads == 0,
+            DPS_ERR_INVALID_ARG, "q_weight and k_weight are given together");
+    REQUIRE(a->eps >= 0.0f && a->eps <= 3.4e38f, DPS_ERR_INVALID_ARG,
+            "eps must be finite and not negative");
+    if (a->rows == 0)
+        return DPS_OK;
+    REQUIRE(a->qkv != nullptr && a->slot != nullptr && (a->heads == 0 || a->q_out != nullptr),
+            DPS_ERR_INVALID_ARG, "qkv, slot or q_out is NULL");
+    REQUIRE(a->rope == nullptr || a->pos != nullptr, DPS_ERR_INVALID_ARG,
+            "a rotation needs positions");
+    REQUIRE(aligned(a->qkv, 16) && aligned(a->q_out, 16) && aligned(a->k_out, 16) &&
+                aligned(a->rope, 16) && aligned(a->q_weight, 16) && aligned(a->k_weight, 16),
+            DPS_ERR_ALIGNMENT, "qkv, q_out, k_out, rope or a weight is not 16-byte aligned");
+    REQUIRE((a->rows <= 1 || (a->qkv_stride % 8 == 0 && a->q_out_stride % 8 == 0 &&
+                              (a->k_out == nullptr || a->k_out_stride % 8 == 0))) &&
+                aligned(a->slot, 8) && aligned(a->pos, 4),
+            DPS_ERR_ALIGNMENT, "a row is not 16-byte aligned, or slot or pos is off its alignment");
+    p.qkv = a->qkv;
+    p.qkv_stride = a->qkv_stride;
+    p.rows = a->rows;
+    p.heads = (int32_t)a->heads;
+    p.slot = a->slot;
+    p.pos = a->pos;
+    p.rope = a->rope;
+    p.max_pos = a->max_pos;
+    p.rot = a->rope ? a->rot : 0;
+    p.adjacent = a->adjacent != 0;
+    p.q_weight = a->q_weight;
+    p.k_weight = a->k_weight;
+    p.eps = a->eps;
+    p.q_out = a->q_out;
+    p.q_out_stride = a->q_out_stride;
+    p.k_out = a->k_out;
+    p.k_out_stride = a->k_out_stride;
+    return launched(
+        dps::launch_kv_store(p, a->type, cache->type == DPS_KV_E4M3, (hipStream_t)stream));
+}
+
+DPS_EXPORT size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t kv_heads,
+                                           int64_t head_dim)
+{
+    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || head_dim <= 0 || heads % kv_heads != 0)
+        return 0;
+    return plan_attn(rows, heads, kv_heads, head_dim).bytes();
+}
+
+DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache *cache, void *ws,
+                                      size_t ws_bytes, void *stream)
+{
+    g_err[0] = 0;
+    REQUIRE(a != nullptr, DPS_ERR_INVALID_ARG, "attention arguments are NULL");
+    dps::KvCacheView c;
+    dps_status s = check_cache(cache, &c);
+    if (s != DPS_OK)
+        return s;
+    s = check_act(a->type, cache->type);
+    if (s != DPS_OK)
+        return s;
+    const int64_t dim = cache->head_dim, kv_heads = cache->kv_heads;
+    REQUIRE(a->rows >= 0 && a->requests >= 0 && a->table_cols >= 0, DPS_ERR_INVALID_ARG,
+            "rows, requests or table_cols is negative");
+    REQUIRE(a->heads >= 1 && a->heads <= 65536 && a->heads % kv_heads == 0, DPS_ERR_INVALID_ARG,
+            "heads must be a multiple of kv_heads, at most 65536");
+    REQUIRE(a->window >= 0, DPS_ERR_INVALID_ARG, "window is negative");
+    REQUIRE(a->scale == a->scale && a->scale >= -3.4e38f && a->scale <= 3.4e38f,
+            DPS_ERR_INVALID_ARG, "scale must be finite");
+    REQUIRE(a->rows <= 1 || (a->q_stride >= a->heads * dim && a->out_stride >= a->heads * dim),
+            DPS_ERR_INVALID_ARG, "q_stride or out_stride is smaller than a row");
+    if (a->rows == 0)
+        return DPS_OK;
+    REQUIRE(a->q != nullptr && a->out != nullptr && a->kv_len != nullptr, DPS_ERR_INVALID_ARG,
+            "q, out or kv_len is NULL");
+    REQUIRE(a->requests * a->table_cols == 0 || a->table != nullptr, DPS_ERR_INVALID_ARG,
+            "table is NULL");
+    REQUIRE(a->req != nullptr || a->requests >= a->rows, DPS_ERR_INVALID_ARG,
+            "without req every row needs a table row");
+    REQUIRE(aligned(a->q, 16) && aligned(a->out, 16) &&
+                (a->rows <= 1 || (a->q_stride % 8 == 0 && a->out_stride % 8 == 0)),
+            DPS_ERR_ALIGNMENT, "q or out, or a row of them, is not 16-byte aligned");
+    REQUIRE(aligned(a->table, 4) && aligned(a->req, 4) && aligned(a->kv_len, 4) &&
+                aligned(a->lse, 4),
+            DPS_ERR_ALIGNMENT, "table, req, kv_len or lse is not 4-byte aligned");
+    // rows, work units and threads of a launch are counted in 32 bits
+    const int64_t room = a->table_cols > (0x7fffffff >> c.log2_tokens)
+                             ? 0x7fffffff
+                             : a->table_cols << c.log2_tokens;
+    const AttnPlan plan = plan_attn(a->rows, a->heads, kv_heads, dim);
+    REQUIRE(a->rows <= 0x7fffffff / (room / 128 + 2) &&
+                a->rows * kv_heads * plan.groups <= (int64_t)(0xffffffffu / 256),
+            DPS_ERR_UNSUPPORTED, "too many rows for one call");
+    REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
+            "workspace is smaller than dps_attn_workspace_bytes()");
+    REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");
+    dps::AttnProblem p;
+    p.q = a->q;
+    p.q_stride = a->q_stride;
+    p.out = a->out;
+    p.out_stride = a->out_stride;
+    p.lse = a->lse;
+    p.pool = c.pool;
+    p.block_stride = c.block_stride;
+    p.n_blocks = c.n_blocks;
+    p.log2_tokens = c.log2_tokens;
+    p.kv_heads = c.kv_heads;
+    p.group = (int32_t)(a->heads / kv_heads);
+    p.head_groups = plan.groups;
+    p.group_step = plan.step;
+    p.table = a->table;
+    p.table_cols = a->table_cols;
+    p.requests = a->requests;
+    p.req = a->req;
+    p.kv_len = a->kv_len;
+    p.rows = a->rows;
+    p.window = a->window;
+    p.score_scale = a->scale * c.k_scale;
+    p.value_scale = c.v_scale;
+    uint8_t *at = static_cast<uint8_t *>(ws);
+    p.part_out = reinterpret_cast<float *>(at);
+    p.part_stat = reinterpret_cast<float *>(at + plan.out_bytes);
+    p.first_unit = reinterpret_cast<int32_t *>(at + plan.out_bytes + plan.stat_bytes);
+    return launched(dps::launch_attn(p, a->type, cache->type == DPS_KV_E4M3, (int)dim, plan.blocks,
+                                     (hipStream_t)stream));
+}

@@ -116,4 +116,81 @@ hipError_t launch_gemm_fp8(int enc, const uint8_t *xq, const float *scale, const
                            int64_t m, int64_t experts, int64_t n, int64_t k, const uint8_t *hi,
                            uint16_t *y, const LinearPlan &plan, float *partial, hipStream_t stream);
 
+// ---- paged KV cache -------------------------------------------------------------
+enum { KV_F16 = 0, KV_BF16 = 1, KV_E4M3 = 2 };
+
+// Blocks of 2^log2_tokens tokens: K [kv_heads][row bytes / 64][tokens][64 B],
+// then V [kv_heads][tokens][head_dim].
+struct KvCacheView {
+    uint8_t *pool;
+    int64_t block_stride;
+    int64_t n_blocks;
+    int32_t log2_tokens, kv_heads, dim;
+    float k_scale, v_scale;
+};
+
+struct KvMapProblem {
+    const int32_t *ctx_len, *new_len;
+    int32_t requests;
+    int32_t log2_tokens;
+    const int32_t *fresh;
+    int64_t n_fresh;
+    int32_t *table;
+    int64_t table_cols;
+    int32_t rows;
+    int32_t *q_start, *seq_len, *counts, *pos;
+    int64_t *slot;
+    int32_t *req, *kv_len;
+};
+hipError_t launch_kv_map(const KvMapProblem &p, hipStream_t stream);
+
+struct KvStoreProblem {
+    const uint16_t *qkv;
+    int64_t qkv_stride;
+    int64_t rows;
+    int32_t heads;
+    KvCacheView cache;
+    const int64_t *slot;
+    const int32_t *pos;
+    const float *rope;      // [max_pos][rot]: cos, then sin; nullptr: no rotation
+    int64_t max_pos;
+    int32_t rot;
+    bool adjacent;          // pairs (2i, 2i + 1) instead of (i, i + rot / 2)
+    const uint16_t *q_weight, *k_weight;  // nullptr: no norm
+    float eps;
+    uint16_t *q_out;
+    int64_t q_out_stride;
+    uint16_t *k_out;        // nullptr: keys go to the cache only
+    int64_t k_out_stride;
+};
+// type: KV_F16 or KV_BF16 of qkv; fp8: the cache holds E4M3, else `type`.
+hipError_t launch_kv_store(const KvStoreProblem &p, int type, bool fp8, hipStream_t stream);
+
+struct AttnProblem {
+    const void *q;
+    int64_t q_stride;       // elements
+    void *out;
+    int64_t out_stride;
+    float *lse;             // [rows][heads] or nullptr
+    const uint8_t *pool;
+    int64_t block_stride;
+    int64_t n_blocks;
+    int32_t log2_tokens, kv_heads;
+    int32_t group;          // query heads per key/value head
+    int32_t head_groups;    // passes of group_step <= 16 query heads over it
+    int32_t group_step;
+    const int32_t *table;
+    int64_t table_cols, requests;
+    const int32_t *req, *kv_len;
+    int64_t rows;
+    int32_t window;
+    float score_scale, value_scale;
+    // workspace: partial rows [2 blocks][heads of a pass][head_dim], their
+    // reference score and sum, and the first work unit of every row
+    float *part_out, *part_stat;
+    int32_t *first_unit;
+};
+hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
+                       hipStream_t stream);
+
 }  // namespace dps

@@ -5,6 +5,7 @@ torch tensors into device pointers, passes torch's current HIP stream, and
 turns status codes into exceptions.  PyTorch provides device memory and
 streams, nothing else.  If libdps.so is not built, the first call raises.
 """
+import collections
 import ctypes
 import functools
 import os
@@ -36,7 +37,8 @@ EXPORTED = ("dps_select_enc", "dps_split", "dps_merge", "dps_restore", "dps_back
             "dps_vmm_map_residual", "dps_vmm_remap", "dps_vmm_unmap_residual", "dps_vmm_destroy",
             "dps_vmm_last_error", "dps_restore_worker_create", "dps_restore_worker_kick",
             "dps_restore_worker_wait_idle", "dps_restore_worker_restored",
-            "dps_restore_worker_destroy", "dps_restore_worker_last_error")
+            "dps_restore_worker_destroy", "dps_restore_worker_last_error",
+            "dps_kv_map", "dps_kv_store", "dps_attn_workspace_bytes", "dps_attn_decode")
 
 
 class DpsError(RuntimeError):
@@ -59,6 +61,41 @@ class CRestoreTarget(ctypes.Structure):
 class CWeight(ctypes.Structure):
     _fields_ = [("hi", ctypes.c_void_p), ("res", CResidual), ("experts", ctypes.c_int64),
                 ("n", ctypes.c_int64), ("k", ctypes.c_int64), ("enc", ctypes.c_int32)]
+
+
+class CKvCache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("pool_bytes", ctypes.c_int64),
+                ("block_stride", ctypes.c_int64), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("k_scale", ctypes.c_float),
+                ("v_scale", ctypes.c_float)]
+
+
+class CKvStep(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("q_start", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p), ("counts", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("req", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p)]
+
+
+class CKvStoreArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("heads", ctypes.c_int64), ("qkv", ctypes.c_void_p),
+                ("qkv_stride", ctypes.c_int64), ("slot", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("rope", ctypes.c_void_p), ("max_pos", ctypes.c_int64),
+                ("rot", ctypes.c_int32), ("adjacent", ctypes.c_int32),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("type", ctypes.c_int32), ("q_out", ctypes.c_void_p),
+                ("q_out_stride", ctypes.c_int64), ("k_out", ctypes.c_void_p),
+                ("k_out_stride", ctypes.c_int64)]
+
+
+class CAttnArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("heads", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("requests", ctypes.c_int64), ("table_cols", ctypes.c_int64),
+                ("req", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("window", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("scale", ctypes.c_float), ("out", ctypes.c_void_p),
+                ("out_stride", ctypes.c_int64), ("lse", ctypes.c_void_p)]
 
 
 _lib = None
@@ -152,6 +189,15 @@ def load_library(path=LIB_PATH):
     lib.dps_restore_worker_destroy.restype = None
     lib.dps_restore_worker_last_error.argtypes = []
     lib.dps_restore_worker_last_error.restype = ctypes.c_char_p
+    lib.dps_kv_map.argtypes = [P, P, I64, I32, P, I64, P, I64, ctypes.POINTER(CKvStep), P]
+    lib.dps_kv_map.restype = ST
+    lib.dps_kv_store.argtypes = [ctypes.POINTER(CKvStoreArgs), ctypes.POINTER(CKvCache), P]
+    lib.dps_kv_store.restype = ST
+    lib.dps_attn_workspace_bytes.argtypes = [I64, I64, I64, I64]
+    lib.dps_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.dps_attn_decode.argtypes = [ctypes.POINTER(CAttnArgs), ctypes.POINTER(CKvCache), P,
+                                    ctypes.c_size_t, P]
+    lib.dps_attn_decode.restype = ST
     lib.dps_status_str.argtypes = [ST]
     lib.dps_status_str.restype = ctypes.c_char_p
     lib.dps_last_error.argtypes = []
@@ -432,6 +478,209 @@ def make_residual(numel, log2_chunk, device, slots=None, pool=None):
         pool = torch.zeros(max(n_chunks, int(slots.max().item()) + 1) * c, dtype=torch.uint8,
                            device=device)
     return Residual(pool, slots, log2_chunk)
+
+
+# ---- paged KV cache ---------------------------------------------------------------
+
+KV_F16, KV_BF16, KV_E4M3 = 0, 1, 2
+_KV_TYPES = {torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3}
+
+
+def _require(cond, what):
+    if not cond:
+        raise ValueError(what)
+
+
+def _require_int(name, t, dtype, dim):
+    """An index array as the kernels take it: dtype, contiguous, on the device."""
+    if not (t.dtype == dtype and t.dim() == dim and t.is_cuda and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %d-d %s device tensor" % (name, dim, dtype))
+
+
+class KvCache:
+    """One layer's paged KV cache over `pool` (a contiguous device tensor, e.g.
+    VmmRegion.kv): block b at byte offset + b * block_stride, block_tokens tokens of
+    kv_heads key and value heads of head_dim (block_bytes in all; layout as
+    dps_kv_cache in include/dps.h).  dtype: torch.float16, bfloat16 or
+    float8_e4m3fn (values / k_scale and v_scale).  By default blocks follow
+    one another from the pool's start."""
+
+    def __init__(self, pool, block_tokens, kv_heads, head_dim, dtype, k_scale=1.0, v_scale=1.0,
+                 offset=0, block_stride=None):
+        _require(dtype in _KV_TYPES, "dtype must be float16, bfloat16 or float8_e4m3fn")
+        _require(pool.is_cuda and pool.is_contiguous(), "pool must be a contiguous device tensor")
+        _require(0 < block_tokens <= 256 and 0 < kv_heads <= 4096 and 0 < head_dim <= 256,
+                 "block_tokens, kv_heads or head_dim is out of range")
+        self.pool = pool
+        self.block_tokens, self.kv_heads = int(block_tokens), int(kv_heads)
+        self.head_dim, self.dtype = int(head_dim), dtype
+        self.type = _KV_TYPES[dtype]
+        self.block_bytes = 2 * self.kv_heads * self.block_tokens * self.head_dim * dtype.itemsize
+        self.block_stride = self.block_bytes if block_stride is None else int(block_stride)
+        nbytes = pool.numel() * pool.element_size()
+        _require(0 <= offset <= nbytes, "offset is outside the pool")
+        self.n_blocks = 0
+        if self.block_stride > 0 and nbytes - offset >= self.block_bytes:
+            self.n_blocks = (nbytes - offset - self.block_bytes) // self.block_stride + 1
+        self.c = CKvCache(pool.data_ptr() + offset, nbytes - offset, self.block_stride,
+                          self.kv_heads, self.head_dim, self.block_tokens, self.type,
+                          float(k_scale), float(v_scale))
+        self.ref = ctypes.byref(self.c)
+
+
+class KvMap(collections.namedtuple("KvMap", "q_start seq_len counts pos slot req kv_len")):
+    """What kv_map writes: int32 q_start [requests + 1], seq_len [requests], counts
+    [2] (new tokens, blocks taken), and per row of the step int32 pos, int64 slot,
+    int32 req and kv_len (see dps_kv_step in include/dps.h)."""
+    __slots__ = ()
+
+
+def make_kv_map(requests, rows, device):
+    """Buffers for kv_map of up to `rows` rows; a graph's step keeps them."""
+    i32 = functools.partial(torch.empty, dtype=torch.int32, device=device)
+    return KvMap(i32(requests + 1), i32(requests), i32(2), i32(rows),
+                 torch.empty(rows, dtype=torch.int64, device=device), i32(rows), i32(rows))
+
+
+def kv_map(ctx_len, new_len, fresh, table, block_tokens, rows=None, out=None):
+    """Block tables and slot maps of a step (dps_kv_map): every request of ctx_len
+    cached and new_len new tokens (int32 device tensors) takes the blocks it needs
+    from `fresh` (int32 block ids) into its row of `table` (int32 [requests][columns],
+    updated in place).  rows: room for new tokens (without out); returns a KvMap."""
+    lib = _lib or load_library()
+    for name, t in (("ctx_len", ctx_len), ("new_len", new_len), ("fresh", fresh)):
+        _require_int(name, t, torch.int32, 1)
+    _require_int("table", table, torch.int32, 2)
+    requests = ctx_len.shape[0]
+    _require(0 < block_tokens <= 256, "block_tokens is out of range")
+    _require(new_len.shape[0] == requests and table.shape[0] == requests,
+             "ctx_len, new_len and table differ in requests")
+    if out is None:
+        _require(rows is not None and rows >= 0, "rows (or out) is needed")
+        out = make_kv_map(requests, rows, ctx_len.device)
+    else:
+        for name, t in zip(out._fields, out):
+            _require_int(name, t, torch.int64 if name == "slot" else torch.int32, 1)
+        rows = out.pos.shape[0]
+        _require(out.q_start.shape[0] == requests + 1 and out.seq_len.shape[0] == requests and
+                 out.counts.shape[0] == 2 and out.slot.shape[0] == rows and
+                 out.req.shape[0] == rows and out.kv_len.shape[0] == rows,
+                 "out does not fit the requests, or its rows differ")
+    step = CKvStep(rows, *[t.data_ptr() for t in out])
+    status = lib.dps_kv_map(ctx_len.data_ptr(), new_len.data_ptr(), requests, block_tokens,
+                            fresh.data_ptr(), fresh.shape[0], table.data_ptr(), table.shape[1],
+                            ctypes.byref(step), _stream())
+    if status:
+        _check(status)
+    return out
+
+
+def _rows_2d(name, t, width, rows, dtype):
+    """Rows of a [rows][width] (or [rows][heads][dim]) tensor whose rows are
+    contiguous: the row stride in elements."""
+    inner = t.stride(-1) == 1 or t.shape[-1] <= 1
+    if t.dim() == 3:
+        inner = inner and (t.shape[1] <= 1 or t.stride(1) == t.shape[2])
+        got = t.shape[1] * t.shape[2]
+    else:
+        got = t.shape[-1] if t.dim() == 2 else -1
+    if not (t.is_cuda and t.dtype == dtype and inner and got == width and t.shape[0] == rows):
+        raise ValueError("%s must be %d device rows of %d contiguous %s" % (name, rows, width,
+                                                                            dtype))
+    return t.stride(0) if rows > 1 else width
+
+
+def kv_store(qkv, cache, slot, heads, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6,
+             adjacent=False, q_out=None, k_out=None):
+    """Head norms (with q_weight and k_weight, [head_dim]) and rotation of the query
+    and key heads of qkv ([rows][(heads + 2 kv_heads) * head_dim], FP16 or BF16), keys
+    and values into `cache` at int64 `slot` [rows] (negative: not stored), in one pass
+    (dps_kv_store).  rope: float32 [max_pos][rot], rot / 2 cosines then sines, at the
+    int32 positions `pos`; adjacent: pairs (2i, 2i + 1) instead of (i, i + rot / 2).
+    Returns the queries [rows][heads][head_dim] (q_out).  k_out: the finished keys
+    [rows][kv_heads][head_dim] as well."""
+    lib = _lib or load_library()
+    rows, dim = qkv.shape[0], cache.head_dim
+    dtype = qkv.dtype
+    _require(dtype in (torch.float16, torch.bfloat16), "qkv must be float16 or bfloat16")
+    stride = _rows_2d("qkv", qkv, (heads + 2 * cache.kv_heads) * dim, rows, dtype)
+    _require_int("slot", slot, torch.int64, 1)
+    _require(slot.shape[0] == rows, "slot and qkv differ in rows")
+    max_pos = rot = 0
+    if rope is not None:
+        _require(rope.is_cuda and rope.dtype == torch.float32 and rope.dim() == 2 and
+                 rope.is_contiguous(), "rope must be a contiguous float32 [max_pos][rot]")
+        _require(pos is not None, "a rotation needs positions")
+        _require_int("pos", pos, torch.int32, 1)
+        _require(pos.shape[0] == rows, "pos and qkv differ in rows")
+        max_pos, rot = rope.shape
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _require(w.is_cuda and w.dtype == dtype and w.is_contiguous() and w.shape == (dim,),
+                     "%s must be [head_dim] of qkv's dtype" % name)
+    if q_out is None:
+        q_out = torch.empty((rows, heads, dim), dtype=dtype, device=qkv.device)
+    q_stride = _rows_2d("q_out", q_out, heads * dim, rows, dtype)
+    k_stride = 0
+    if k_out is not None:
+        k_stride = _rows_2d("k_out", k_out, cache.kv_heads * dim, rows, dtype)
+    args = CKvStoreArgs(rows, heads, qkv.data_ptr(), stride, slot.data_ptr(),
+                        pos.data_ptr() if rope is not None else None, _ptr(rope), max_pos, rot,
+                        1 if adjacent else 0, _ptr(q_weight), _ptr(k_weight), eps,
+                        _KV_TYPES[dtype], q_out.data_ptr(), q_stride, _ptr(k_out), k_stride)
+    status = lib.dps_kv_store(ctypes.byref(args), cache.ref, _stream())
+    if status:
+        _check(status)
+    return q_out
+
+
+def attn_workspace_bytes(cache, rows, heads):
+    """Workspace of attn_decode for up to `rows` rows of `heads` query heads."""
+    lib = _lib or load_library()
+    return lib.dps_attn_workspace_bytes(rows, heads, cache.kv_heads, cache.head_dim)
+
+
+def attn_decode(q, cache, table, kv_len, req=None, scale=None, window=0, out=None, lse=None,
+                workspace=None):
+    """Attention of one new token a row over the paged cache (dps_attn_decode): row j
+    of q ([rows][heads][head_dim]) attends positions 0 .. kv_len[j] - 1 (the last
+    `window` of them if window > 0) of request req[j] (j without req), whose blocks
+    are table[req[j]].  scale: of the scores, 1 / sqrt(head_dim) by default.  lse:
+    float32 [rows][heads] for the log of the sums.  Returns out (q's shape)."""
+    lib = _lib or load_library()
+    _require(q.dim() == 3, "q must be [rows][heads][head_dim]")
+    rows, heads, dim = q.shape
+    dtype = q.dtype
+    _require(dtype in (torch.float16, torch.bfloat16), "q must be float16 or bfloat16")
+    _require(dim == cache.head_dim, "q and cache differ in head_dim")
+    q_stride = _rows_2d("q", q, heads * dim, rows, dtype)
+    _require_int("table", table, torch.int32, 2)
+    _require_int("kv_len", kv_len, torch.int32, 1)
+    _require(kv_len.shape[0] == rows, "kv_len and q differ in rows")
+    if req is not None:
+        _require_int("req", req, torch.int32, 1)
+        _require(req.shape[0] == rows, "req and q differ in rows")
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=dtype, device=q.device)
+    out_stride = _rows_2d("out", out, heads * dim, rows, dtype)
+    if lse is not None:
+        _require(lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and
+                 lse.shape == (rows, heads), "lse must be a contiguous float32 [rows][heads]")
+    if scale is None:
+        scale = dim ** -0.5
+    window = min(window, 0x7fffffff)  # no length is beyond
+    _require(window >= 0, "window is negative")
+    if workspace is None:
+        need = lib.dps_attn_workspace_bytes(rows, heads, cache.kv_heads, dim)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    args = CAttnArgs(rows, heads, q.data_ptr(), q_stride, table.data_ptr(), table.shape[0],
+                     table.shape[1], _ptr(req), kv_len.data_ptr(), window, _KV_TYPES[dtype], scale,
+                     out.data_ptr(), out_stride, _ptr(lse))
+    status = lib.dps_attn_decode(ctypes.byref(args), cache.ref, workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream())
+    if status:
+        _check(status)
+    return out
 
 
 class SumManager:
