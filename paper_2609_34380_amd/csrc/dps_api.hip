@@ -768,11 +768,11 @@ dps_status check_act(int act, int type)
 struct AttnPlan {
     int groups, step;  // passes over a key/value head, query heads of a pass
     int blocks;        // ranges of the work line
-    size_t out_bytes, stat_bytes, unit_bytes;
-    size_t bytes() const { return out_bytes + stat_bytes + unit_bytes; }
+    size_t out_bytes, stat_bytes, join_bytes;
+    size_t bytes() const { return out_bytes + stat_bytes + join_bytes; }
 };
 
-AttnPlan plan_attn(int64_t rows, int64_t heads, int64_t kv_heads, int64_t dim)
+AttnPlan plan_attn(int64_t heads, int64_t kv_heads, int64_t dim, bool fp8)
 {
     AttnPlan a;
     const int64_t group = heads / kv_heads;
@@ -780,13 +780,13 @@ AttnPlan plan_attn(int64_t rows, int64_t heads, int64_t kv_heads, int64_t dim)
     a.step = (int)cdiv(group, a.groups);
     a.groups = (int)cdiv(group, a.step);
     const int64_t lines = kv_heads * a.groups;
-    // two blocks of four waves a CU over all lines
-    const int64_t blocks = 2 * (int64_t)current_cu_count() / lines;
+    const int64_t blocks =
+        (int64_t)dps::attn_blocks_per_cu(fp8, (int)dim) * current_cu_count() / lines;
     a.blocks = (int)(blocks < 1 ? 1 : blocks);
     const int64_t parts = 2 * a.blocks * lines * a.step;
     a.out_bytes = align256(parts * dim * 4);
     a.stat_bytes = align256(parts * 8);
-    a.unit_bytes = align256((rows + 1) * 4);
+    a.join_bytes = align256((int64_t)a.blocks * 32);
     return a;
 }
 
@@ -913,7 +913,10 @@ DPS_EXPORT size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t 
 {
     if (rows <= 0 || heads <= 0 || kv_heads <= 0 || head_dim <= 0 || heads % kv_heads != 0)
         return 0;
-    return plan_attn(rows, heads, kv_heads, head_dim).bytes();
+    // the type of the cache is not known here: room for either
+    const size_t wide = plan_attn(heads, kv_heads, head_dim, false).bytes();
+    const size_t fp8 = plan_attn(heads, kv_heads, head_dim, true).bytes();
+    return wide > fp8 ? wide : fp8;
 }
 
 DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache *cache, void *ws,
@@ -952,14 +955,13 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
     REQUIRE(aligned(a->table, 4) && aligned(a->req, 4) && aligned(a->kv_len, 4) &&
                 aligned(a->lse, 4),
             DPS_ERR_ALIGNMENT, "table, req, kv_len or lse is not 4-byte aligned");
-    // rows, work units and threads of a launch are counted in 32 bits
+    // every block sums the rows' tiles, in 32 bits
     const int64_t room = a->table_cols > (0x7fffffff >> c.log2_tokens)
                              ? 0x7fffffff
                              : a->table_cols << c.log2_tokens;
-    const AttnPlan plan = plan_attn(a->rows, a->heads, kv_heads, dim);
-    REQUIRE(a->rows <= 0x7fffffff / (room / 128 + 2) &&
-                a->rows * kv_heads * plan.groups <= (int64_t)(0xffffffffu / 256),
-            DPS_ERR_UNSUPPORTED, "too many rows for one call");
+    const AttnPlan plan = plan_attn(a->heads, kv_heads, dim, cache->type == DPS_KV_E4M3);
+    REQUIRE(a->rows <= (1 << 20) && a->rows <= 0x7fffffff / (room / 32 + 2), DPS_ERR_UNSUPPORTED,
+            "too many rows for one call");
     REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
             "workspace is smaller than dps_attn_workspace_bytes()");
     REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");
@@ -989,7 +991,7 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
     uint8_t *at = static_cast<uint8_t *>(ws);
     p.part_out = reinterpret_cast<float *>(at);
     p.part_stat = reinterpret_cast<float *>(at + plan.out_bytes);
-    p.first_unit = reinterpret_cast<int32_t *>(at + plan.out_bytes + plan.stat_bytes);
+    p.join = reinterpret_cast<int32_t *>(at + plan.out_bytes + plan.stat_bytes);
     return launched(dps::launch_attn(p, a->type, cache->type == DPS_KV_E4M3, (int)dim, plan.blocks,
                                      (hipStream_t)stream));
 }

@@ -17,11 +17,14 @@
 //   - Token 4 r + c of 16 sits in operand row 4 c + r.  With the cache's
 //     64-byte key segments every load of a wave is then contiguous (1 KiB at
 //     16 bytes a lane) for K and for V.
-//   - The tokens of all rows, in units of 128 (32 a wave), form one line per
-//     key/value head, cut into as many equal ranges as there are blocks:
-//     ragged lengths load every CU alike, and a block writes at most two
-//     partial rows however long a row is.  attn_join_kernel combines a row's
-//     partials in their order, so results do not depend on timing.
+//   - The tokens of all rows, in tiles of 32, form one line per key/value head,
+//     cut into equal ranges, one per wave: ragged lengths load every CU alike.
+//     A wave finishes the rows that lie inside its range by itself; what the
+//     four waves of a block share is joined in LDS, what blocks share (at most
+//     two partial rows a block, however long a row is) in attn_join_kernel.
+//     Partials are joined in their order, so results do not depend on timing.
+//   - Block ids come through scalar loads one tile ahead: a vector load of them
+//     would wait for every value load issued before it.
 //
 // Precision: products and softmax in fp32.  The weights P enter the matrix
 // cores as two 16-bit terms (value and remainder), which keeps them to about
@@ -38,7 +41,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kTile = 32;               // tokens a wave takes at a time
-constexpr int kUnit = kTile * kWaves;   // tokens of a work unit
+constexpr int kJoinThreads = 512;
 constexpr int64_t kLongest = 0x7fffff00;  // tokens of a row (a tile past it still fits 31 bits)
 constexpr float kNone = -1e30f;         // reference score before any token
 constexpr float kLog2e = 1.4426950408889634f;
@@ -92,6 +95,15 @@ __device__ __forceinline__ void split2(float p0, float p1, uint32_t &hi, uint32_
     }
 }
 
+// Two fp32 values rounded to 16 bits, nearest even.
+template <int TYPE>
+__device__ __forceinline__ uint32_t narrow2(float a, float b)
+{
+    if (TYPE == KV_BF16)
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    return __builtin_bit_cast(uint32_t, half2v{(_Float16)a, (_Float16)b});
+}
+
 // Largest value over the four 16-lane quarters that share a head.
 __device__ __forceinline__ float quarters_ref(float x)
 {
@@ -120,18 +132,19 @@ __device__ __forceinline__ T stream(const uint8_t *p)
     return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
 }
 
-// The live tokens [lo, hi) of row r and its table row; hi = 0: none.
+// The live tokens [lo, hi) of a row and its table row; hi = 0: none.
 struct RowSpan {
     int32_t lo, hi;
     int32_t req;
 };
 
-__device__ __forceinline__ RowSpan row_span(const AttnProblem &p, int64_t r)
+__device__ __forceinline__ RowSpan row_span(const AttnProblem &p, const int32_t *__restrict__ req,
+                                            const int32_t *__restrict__ kv_len, int32_t r)
 {
     RowSpan s;
-    s.req = p.req ? p.req[r] : (int32_t)r;
+    s.req = req ? req[r] : r;
     const int64_t room = min(p.table_cols << p.log2_tokens, kLongest);
-    int64_t n = p.kv_len[r];
+    int64_t n = kv_len[r];
     if (s.req < 0 || s.req >= p.requests)
         n = 0;
     n = n < 0 ? 0 : (n > room ? room : n);
@@ -140,21 +153,43 @@ __device__ __forceinline__ RowSpan row_span(const AttnProblem &p, int64_t r)
     return s;
 }
 
-// Work units of a row (its live tokens on the grid of kUnit tokens).
-__device__ __forceinline__ int32_t row_units(const RowSpan &s)
+// Tiles of a row (its live tokens on the grid of kTile tokens).
+__device__ __forceinline__ int32_t row_tiles(const RowSpan &s)
 {
-    return s.hi == 0 ? 0 : (int32_t)(((uint32_t)s.hi + kUnit - 1) / kUnit) - s.lo / kUnit;
+    return s.hi == 0 ? 0 : (int32_t)(((uint32_t)s.hi + kTile - 1) / kTile) - s.lo / kTile;
 }
 
-// Range of block w of `parts` over `units` work units.
-__device__ __forceinline__ int32_t range_begin(int32_t w, int32_t units, int32_t parts)
+// The work line of a key/value head cut into `waves` ranges of `each` tiles, the
+// first `more` of them one longer.
+struct WorkLine {
+    uint32_t waves, each, more;
+
+    __device__ __forceinline__ WorkLine(uint32_t tiles, uint32_t most)
+        : waves(min(tiles, most)), each(tiles / max(waves, 1u)), more(tiles - each * waves)
+    {
+    }
+    __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ uint32_t count(uint32_t w) const
+    {
+        return w < waves ? each + (w < more ? 1 : 0) : 0;
+    }
+    // the wave that has tile t
+    __device__ __forceinline__ uint32_t of(uint32_t t) const
+    {
+        const uint32_t cut = more * (each + 1);
+        return t < cut ? t / (each + 1) : more + (t - cut) / each;
+    }
+};
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int32_t wave_scan(int32_t x, int lane)
 {
-    return (int32_t)((int64_t)w * units / parts);
-}
-// The block whose range holds unit u: the last w with w * units / parts <= u.
-__device__ __forceinline__ int32_t range_of(int32_t u, int32_t units, int32_t parts)
-{
-    return (int32_t)((((int64_t)u + 1) * parts - 1) / units);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t up = __shfl_up(x, d);
+        x += lane >= d ? up : 0;
+    }
+    return x;
 }
 
 // Four values of a finished row's head: o / sum, rounded once, and its lse.
@@ -163,16 +198,9 @@ __device__ __forceinline__ void attn_store(const AttnProblem &p, int64_t row, in
                                            int d, f32x4 o, float ref, float sum)
 {
     const float scale = sum == 0.0f ? 0.0f : p.value_scale / sum;
-    uint16_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float v = o[i] * scale;
-        h[i] = TYPE == KV_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v)
-                               : __builtin_bit_cast(uint16_t, (_Float16)v);
-    }
     uint16_t *at = static_cast<uint16_t *>(p.out) + row * p.out_stride + (int64_t)head * dim + d;
     *reinterpret_cast<u32x2 *>(at) =
-        u32x2{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
+        u32x2{narrow2<TYPE>(o[0] * scale, o[1] * scale), narrow2<TYPE>(o[2] * scale, o[3] * scale)};
     if (d == 0 && p.lse)
         p.lse[row * (p.kv_heads * p.group) + head] =
             sum == 0.0f ? -__builtin_inff() : (ref + log2f(sum)) * kLn2;
@@ -188,10 +216,36 @@ struct Shape {
     static constexpr int kP8 = D / 128;
     static constexpr int kP4 = (D % 128) / 64;
     static constexpr int kP2 = (D % 64) / 32;
-    // 16-bit keys of 256: two tiles' keys and a tile's values do not fit the
-    // registers beside the output, so loads wait for the piece they replace and
-    // the query stays in LDS (where the waves' outputs are joined later).
-    static constexpr bool kTight = D * kElt >= 512;
+    // Blocks of four waves a CU, as their registers allow.
+    static constexpr int kPerCu = attn_blocks_per_cu(FP8, D);
+};
+
+// A wave's output of one row: acc (value d of a head in the lane and register
+// that the matrix instruction leaves it), reference score and sum per head.
+template <int KACC>
+struct Partial {
+    f32x4 acc[KACC];
+    float ref, sum;
+
+    __device__ __forceinline__ void clear()
+    {
+        ref = kNone;
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KACC; ++i)
+            acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // Joins a partial that lies in LDS, a register of all lanes at a time.
+    __device__ __forceinline__ void join(const f32x4 *at, const float *stat, int lane)
+    {
+        const float r = stat[lane], to = fmaxf(ref, r);
+        const float a = __builtin_amdgcn_exp2f(ref - to), b = __builtin_amdgcn_exp2f(r - to);
+        sum = sum * a + stat[64 + lane] * b;
+        ref = to;
+#pragma unroll
+        for (int i = 0; i < KACC; ++i)
+            acc[i] = acc[i] * a + at[i * 64 + lane] * b;
+    }
 };
 
 // One piece of V (16 lanes x W values of head_dim from d0 on) of a tile's 32
@@ -212,102 +266,194 @@ struct VPiece {
 };
 
 template <int TYPE, bool FP8, int D>
-__global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
+__global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_kernel(
+    const AttnProblem p, const int32_t *__restrict__ tables, const int32_t *__restrict__ reqs,
+    const int32_t *__restrict__ kv_len)
 {
     typedef Shape<TYPE, FP8, D> S;
-    constexpr int kRow = D + 4;  // LDS floats of a head's output (padded off the banks)
-    __shared__ __align__(16) float s_out[kWaves * 16 * kRow];
-    __shared__ float s_ref[kWaves][16], s_sum[kWaves][16];
-    __shared__ int32_t s_wave_units[kWaves];
-    __shared__ int32_t s_row, s_row_first;
+    __shared__ f32x4 s_head[kWaves][S::kAcc * 64];  // rows that began before the wave
+    __shared__ float s_stat[kWaves][128];
+    __shared__ int32_t s_first[kThreads];
+    __shared__ int32_t s_sums[kWaves];
+    __shared__ int32_t s_state[kWaves];
+    __shared__ int32_t s_join[8];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15;   // query head of the pass (matrix column)
     const int quarter = lane >> 4;
-    const int32_t w = blockIdx.x;
     const int hv = blockIdx.y;   // (key/value head, group of at most 16 query heads)
     const int kvh = hv / p.head_groups;
     const int sub = hv % p.head_groups;
     const int first_head = kvh * p.group + sub * p.group_step;
     const int n_heads = min(p.group_step, p.group - sub * p.group_step);
+    const int rows = (int)p.rows;
 
-    // ---- this block's range of the work line --------------------------------
-    // thread i sums rows [i * per, (i + 1) * per)
-    const int32_t per = (int32_t)((p.rows + kThreads - 1) / kThreads);
-    const int32_t r0 = min(tid * per, (int32_t)p.rows), r1 = min(r0 + per, (int32_t)p.rows);
-    int32_t mine = 0;
-    for (int32_t r = r0; r < r1; ++r)
-        mine += row_units(row_span(p, r));
-    int32_t incl = mine;
+    // ---- this wave's range of the work line ----------------------------------
+    // up to 64 rows: a row a lane; above, thread i sums rows [i * per, (i + 1) * per)
+    int32_t tiles, chunk = 0, chunk_first = 0;
+    const int32_t per = rows <= 64 ? 64 : (rows + kThreads - 1) / kThreads;
+    RowSpan span;
+    int32_t mine = 0, incl = 0;
+    if (rows <= 64) {
+        span = RowSpan{0, 0, 0};
+        if (lane < rows)
+            span = row_span(p, reqs, kv_len, lane);
+        mine = row_tiles(span);
+        incl = wave_scan(mine, lane);
+        tiles = __builtin_amdgcn_readlane(incl, 63);
+    } else {
+        const int32_t r1 = min((tid + 1) * per, rows);
+        for (int32_t r = tid * per; r < r1; ++r)
+            mine += row_tiles(row_span(p, reqs, kv_len, r));
+        incl = wave_scan(mine, lane);
+        if (lane == 63)
+            s_sums[wave] = incl;
+        __syncthreads();
+        tiles = 0;
+        int32_t before = incl - mine;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int32_t up = __shfl_up(incl, d);
-        incl += lane >= d ? up : 0;
-    }
-    if (lane == 63)
-        s_wave_units[wave] = incl;
-    __syncthreads();
-    int32_t units = 0, before = incl - mine;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        before += i < wave ? s_wave_units[i] : 0;
-        units += s_wave_units[i];
-    }
-    const int32_t parts = min((int32_t)gridDim.x, units);
-    if (w == 0 && hv == 0) {  // the work line for the join
-        int32_t at = before;
-        for (int32_t r = r0; r < r1; ++r) {
-            p.first_unit[r] = at;
-            at += row_units(row_span(p, r));
+        for (int i = 0; i < kWaves; ++i) {
+            before += i < wave ? s_sums[i] : 0;
+            tiles += s_sums[i];
         }
-        if (tid == 0)
-            p.first_unit[p.rows] = units;
+        tiles = __builtin_amdgcn_readfirstlane(tiles);
+        s_first[tid] = before;
+        __syncthreads();
     }
-    if (w >= parts)
+    const WorkLine line((uint32_t)tiles, gridDim.x * kWaves);
+    const uint32_t me = blockIdx.x * kWaves + wave;
+    const int32_t begin = (int32_t)line.begin(me);
+    int left = (int)line.count(me);
+    if (tid < 8) {
+        s_join[tid] = 0;
+        if (hv == 0 && line.waves <= blockIdx.x * kWaves)
+            p.join[blockIdx.x * 8 + tid] = 0;
+    }
+    if (line.waves <= blockIdx.x * kWaves)  // no tile for the whole block
         return;
-    const int32_t begin = range_begin(w, units, parts), end = range_begin(w + 1, units, parts);
-    if (begin >= before && begin < before + mine) {
-        int32_t at = before, r = r0;
-        for (;; ++r) {
-            const int32_t n = row_units(row_span(p, r));
-            if (begin < at + n)
-                break;
-            at += n;
+    int row = 0, skip = 0;  // the row of the range's first tile, and that tile's index in it
+    if (left > 0) {
+        if (rows > 64) {
+            int below = 0;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i)
+                below += __popcll(__ballot(s_first[i * 64 + lane] <= begin));
+            chunk = __builtin_amdgcn_readfirstlane(below - 1);
+            chunk_first = __builtin_amdgcn_readfirstlane(s_first[chunk]);
         }
-        s_row = r;
-        s_row_first = at;
+        const int32_t r1 = min((chunk + 1) * per, rows);
+        for (int32_t r = chunk * per;; r += 64) {
+            if (rows > 64) {
+                span = RowSpan{0, 0, 0};
+                if (r + lane < r1)
+                    span = row_span(p, reqs, kv_len, r + lane);
+                mine = row_tiles(span);
+                incl = wave_scan(mine, lane);
+            }
+            const uint64_t past = __ballot(chunk_first + incl > begin);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                row = r + at;
+                skip = begin - (chunk_first + __builtin_amdgcn_readlane(incl - mine, at));
+                span.lo = __builtin_amdgcn_readlane(span.lo, at);
+                span.hi = __builtin_amdgcn_readlane(span.hi, at);
+                span.req = __builtin_amdgcn_readlane(span.req, at);
+                break;
+            }
+            chunk_first += __builtin_amdgcn_readlane(incl, 63);
+            if (r + 64 >= r1) {  // not reached: the range's first tile is in the chunk
+                left = 0;
+                break;
+            }
+        }
     }
-    __syncthreads();
-    // wave-uniform values, kept in scalar registers
-    int row = __builtin_amdgcn_readfirstlane(s_row);
-    int skip = __builtin_amdgcn_readfirstlane(begin - s_row_first);  // units of the row
-    int left = __builtin_amdgcn_readfirstlane(end - begin);
+    int lo = __builtin_amdgcn_readfirstlane(span.lo);
+    int hi = __builtin_amdgcn_readfirstlane(span.hi);
+    int req = __builtin_amdgcn_readfirstlane(span.req);
 
     const uint32_t tokens = 1u << p.log2_tokens;
     const uint32_t key_lane = (4 * (col & 3) + (col >> 2)) * 64 + quarter * 16;
     const uint32_t key_head = (uint32_t)kvh * S::kKeyLoads * tokens * 64;
     const uint32_t val_head = (uint32_t)(p.kv_heads + kvh) * tokens * (D * S::kElt);
     const float to_log2 = p.score_scale * kLog2e;
+    const int32_t last_col = (int32_t)p.table_cols - 1;
 
-    while (left > 0 && row < p.rows) {
-        const RowSpan span = row_span(p, row);
-        const int lo = __builtin_amdgcn_readfirstlane(span.lo);
-        const int hi = __builtin_amdgcn_readfirstlane(span.hi);
-        const int req = __builtin_amdgcn_readfirstlane(span.req);
-        const int row_n = hi == 0 ? 0 : (int)(((uint32_t)hi + kUnit - 1) / kUnit) - lo / kUnit;
-        const int n_units = min(row_n - skip, left);
-        if (n_units <= 0) {  // an empty row
-            ++row;
-            continue;
+    // values d .. d + W - 1 of a head, one piece register by register
+    const auto each_piece = [&](const auto &put) {
+#pragma unroll
+        for (int i = 0; i < S::kP8; ++i)
+            put(std::integral_constant<int, 8>(), 128 * i, 8 * i);
+        if (S::kP4)
+            put(std::integral_constant<int, 4>(), 128 * S::kP8, 8 * S::kP8);
+        if (S::kP2)
+            put(std::integral_constant<int, 2>(), 128 * S::kP8 + 64 * S::kP4,
+                8 * S::kP8 + 4 * S::kP4);
+    };
+    Partial<S::kAcc> o;
+    const auto finish = [&](const Partial<S::kAcc> &f, int r) {
+        if (col >= n_heads)
+            return;
+        const float scale = f.sum == 0.0f ? 0.0f : p.value_scale / f.sum;
+        uint16_t *at = static_cast<uint16_t *>(p.out) + r * p.out_stride +
+                       (int64_t)(first_head + col) * D;
+        each_piece([&](auto width, int d0, int tile) {
+            constexpr int W = width;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t v[W / 2];
+#pragma unroll
+                for (int k = 0; k < W / 2; ++k)
+                    v[k] = narrow2<TYPE>(f.acc[tile + 2 * k][i] * scale,
+                                         f.acc[tile + 2 * k + 1][i] * scale);
+                typedef typename Piece<2 * W>::T Vec;
+                Vec x;
+                __builtin_memcpy(&x, v, sizeof(x));
+                *reinterpret_cast<Vec *>(at + d0 + W * (4 * quarter + i)) = x;
+            }
+        });
+        if (quarter == 0 && p.lse)
+            p.lse[(int64_t)r * (p.kv_heads * p.group) + first_head + col] =
+                f.sum == 0.0f ? -__builtin_inff() : (f.ref + log2f(f.sum)) * kLn2;
+    };
+    // a partial row for the join: slot 0 of the block began before it, slot 1 in it
+    const auto hand_on = [&](const Partial<S::kAcc> &f, int which) {
+        if (col >= n_heads)
+            return;
+        const int64_t slot =
+            ((int64_t)(blockIdx.x * 2 + which) * gridDim.y + hv) * p.group_step + col;
+        float *at = p.part_out + slot * D;
+        each_piece([&](auto width, int d0, int tile) {
+            constexpr int W = width;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[W];
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+                    v[k] = f.acc[tile + k][i];
+                __builtin_memcpy(at + d0 + W * (4 * quarter + i), v, sizeof(v));
+            }
+        });
+        if (quarter == 0) {
+            p.part_stat[slot * 2] = f.ref;
+            p.part_stat[slot * 2 + 1] = f.sum;
         }
-        const int32_t *__restrict__ table = p.table + (int64_t)req * p.table_cols;
-        const int unit0 = lo / kUnit + skip;
+    };
+
+    // kHead: a row that began before the range, in s_head; kEnds: and ended in it;
+    // kOpen: a row that began in the range and did not end, in registers
+    enum { kHead = 1, kEnds = 2, kOpen = 4 };
+    int state = 0;
+    int row_n = row_tiles(RowSpan{lo, hi, req}), row_first = begin - skip;  // on the line
+    const int head_row = row, head_n = row_n, head_first = row_first;
+    while (left > 0) {
+        const int n_tiles = min(row_n - skip, left);
+        if (n_tiles > 0) {
+        const int32_t *__restrict__ table = tables + (int64_t)req * p.table_cols;
 
         // ---- query fragments ------------------------------------------------
-        u32x4 q[S::kTight ? 1 : S::kSteps];
-        u32x4 *q_lds = reinterpret_cast<u32x4 *>(&s_out[wave * 16 * kRow]) + lane;
+        u32x4 q[S::kSteps];
         {
             const uint8_t *qp = static_cast<const uint8_t *>(p.q) +
                                 ((int64_t)row * p.q_stride + (int64_t)(first_head + col) * D) * 2;
@@ -316,30 +462,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
                 // 8-bit keys hold 16 values a lane: two steps' operands side by side
                 const int d = FP8 ? 64 * (s >> 1) + 16 * quarter + 8 * (s & 1)
                                   : 32 * s + 8 * quarter;
-                u32x4 v = {0u, 0u, 0u, 0u};
+                q[s] = u32x4{0u, 0u, 0u, 0u};
                 if (col < n_heads)
-                    v = load16(qp + d * 2);
-                if (S::kTight)
-                    q_lds[64 * s] = v;
-                else
-                    q[s] = v;
+                    q[s] = load16(qp + d * 2);
             }
         }
+        o.clear();
 
-        float ref = kNone, sum = 0.0f;
-        f32x4 acc[S::kAcc];
+        // ids of the blocks of a tile's two halves of 16 tokens
+        const auto ids_of = [&](int t0, int32_t *id) {
 #pragma unroll
-        for (int i = 0; i < S::kAcc; ++i)
-            acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-        // Base of the block that holds token t0 (a multiple of 16), at the
-        // token's place in it; a block outside the pool is never read.
-        const auto block_of = [&](int t0, bool &ok) -> const uint8_t * {
-            int64_t c = (int64_t)((uint32_t)t0 >> p.log2_tokens);
-            c = min(c, p.table_cols - 1);
-            const int32_t b = table[c];
-            ok = b >= 0 && b < p.n_blocks;
-            return p.pool + (int64_t)(ok ? b : 0) * p.block_stride;
+            for (int h = 0; h < 2; ++h)
+                id[h] = table[min((int32_t)(((uint32_t)t0 + 16 * h) >> p.log2_tokens), last_col)];
         };
 
         u32x4 key[2][S::kKeyLoads];
@@ -347,12 +481,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
         VPiece<TYPE, FP8, 4> v4[1];
         VPiece<TYPE, FP8, (FP8 ? 4 : 2)> v2[1];
         const uint8_t *base[2];
-        bool ok[2];
+        bool ok[2];  // a block outside the cache is never read: the first one stands in
+        int32_t id[2];
 
         const auto load_keys = [&](int t0) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                base[h] = block_of(t0 + 16 * h, ok[h]);
+                ok[h] = id[h] >= 0 && id[h] < p.n_blocks;
+                base[h] = p.pool + (int64_t)(ok[h] ? id[h] : 0) * p.block_stride;
                 const uint32_t at = key_head + (((uint32_t)t0 + 16 * h) & (tokens - 1)) * 64;
 #pragma unroll
                 for (int s = 0; s < S::kKeyLoads; ++s)
@@ -370,26 +506,24 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
                                        (quarter * D + col * width) * S::kElt);
             }
         };
-        const auto load_values = [&](int t0, int first, int last) {
+        const auto load_values = [&](int t0) {
 #pragma unroll
             for (int i = 0; i < S::kP8; ++i)
-                if (i >= first && i < last)
-                    load_piece(v8[i], t0, 128 * i, 8);
-            if (S::kP4 && last > S::kP8)
+                load_piece(v8[i], t0, 128 * i, 8);
+            if (S::kP4)
                 load_piece(v4[0], t0, 128 * S::kP8, 4);
-            if (S::kP2 && last > S::kP8)
+            if (S::kP2)
                 load_piece(v2[0], t0, 128 * S::kP8 + 64 * S::kP4, 2);
         };
 
-        const int tile0 = unit0 * kUnit + wave * kTile;
+        const int tile0 = (lo / kTile + skip) * kTile;
+        ids_of(tile0, id);
         load_keys(tile0);
-        if (S::kTight)
-            load_values(tile0, 0, 1);
-        for (int u = 0; u < n_units; ++u) {
-            const int t0 = tile0 + u * kUnit;
+        ids_of(tile0 + kTile, id);
+        // one tile; with more to come, its softmax runs under the next one's key loads
+        const auto take = [&](int t0, auto more) {
             const bool ok0 = ok[0], ok1 = ok[1];
-            if (!S::kTight)
-                load_values(t0, 0, 9);
+            load_values(t0);
 
             // ---- S^T = K Q^T -------------------------------------------------
             f32x4 s2[2];
@@ -407,51 +541,49 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
                     } else {
                         a = key[h][s];
                     }
-                    s2[h] = mfma32<TYPE>(a, S::kTight ? q_lds[64 * s] : q[S::kTight ? 0 : s], s2[h]);
+                    s2[h] = mfma32<TYPE>(a, q[s], s2[h]);
                 }
             }
-            if (S::kTight) {
-                __builtin_amdgcn_sched_barrier(0);
-                load_values(t0, 1, 9);
-            } else if (u + 1 < n_units) {
-                load_keys(t0 + kUnit);
+            if (more) {
+                load_keys(t0 + kTile);
+                ids_of(t0 + 2 * kTile, id);
             }
 
             // ---- softmax over this lane's 8 tokens ----------------------------
             float x[8];
-            bool live[8];
-            const bool edge = t0 < lo || t0 + kTile > hi || !ok0 || !ok1;
+            uint32_t keep[8];  // of V: whatever a place past the row holds must not meet a zero weight
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 x[j] = s2[j >> 2][j & 3] * to_log2;
-                live[j] = true;
+                keep[j] = ~0u;
             }
-            if (edge) {
+            if (t0 < lo || t0 + kTile > hi || !ok0 || !ok1) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int t = t0 + 16 * (j >> 2) + 4 * (j & 3) + quarter;
-                    live[j] = t >= lo && t < hi && (j < 4 ? ok0 : ok1);
-                    x[j] = live[j] ? x[j] : -__builtin_inff();
+                    const bool live = t >= lo && t < hi && (j < 4 ? ok0 : ok1);
+                    x[j] = live ? x[j] : -__builtin_inff();
+                    keep[j] = live ? ~0u : 0u;
                 }
             }
             float m = x[0];
 #pragma unroll
             for (int j = 1; j < 8; ++j)
                 m = fmaxf(m, x[j]);
-            if (__any(m > ref + kRoom)) {
-                m = fmaxf(quarters_ref(m) - kLift, ref);
-                const float shrink = __builtin_amdgcn_exp2f(ref - m);
-                ref = m;
-                sum *= shrink;
+            if (__any(m > o.ref + kRoom)) {
+                m = fmaxf(quarters_ref(m) - kLift, o.ref);
+                const float shrink = __builtin_amdgcn_exp2f(o.ref - m);
+                o.ref = m;
+                o.sum *= shrink;
 #pragma unroll
                 for (int i = 0; i < S::kAcc; ++i)
-                    acc[i] *= shrink;
+                    o.acc[i] *= shrink;
             }
             u32x4 p_hi, p_lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                x[j] = __builtin_amdgcn_exp2f(x[j] - ref);
-                sum += x[j];
+                x[j] = __builtin_amdgcn_exp2f(x[j] - o.ref);
+                o.sum += x[j];
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -464,13 +596,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
             // ---- O^T += V^T P^T -----------------------------------------------
             int tile = 0;
             const auto turn = [&](auto &v, int width) {
-                if (edge) {
-                    // whatever a place past the row holds must not meet a zero weight
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (!live[j])
-                            v.raw[j] = 0;
-                }
+                for (int j = 0; j < 8; ++j)
+                    v.raw[j] &= keep[j];
 #pragma unroll
                 for (int i = 0; i < width / 2; ++i) {
                     uint32_t d[8];
@@ -483,135 +611,180 @@ __global__ __launch_bounds__(kThreads, 2) void attn_kernel(const AttnProblem p)
                         even[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x05040100u);
                         odd[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x07060302u);
                     }
-                    acc[tile] = mfma32<TYPE>(even, p_hi, acc[tile]);
-                    acc[tile] = mfma32<TYPE>(even, p_lo, acc[tile]);
-                    acc[tile + 1] = mfma32<TYPE>(odd, p_hi, acc[tile + 1]);
-                    acc[tile + 1] = mfma32<TYPE>(odd, p_lo, acc[tile + 1]);
+                    o.acc[tile] = mfma32<TYPE>(even, p_hi, o.acc[tile]);
+                    o.acc[tile] = mfma32<TYPE>(even, p_lo, o.acc[tile]);
+                    o.acc[tile + 1] = mfma32<TYPE>(odd, p_hi, o.acc[tile + 1]);
+                    o.acc[tile + 1] = mfma32<TYPE>(odd, p_lo, o.acc[tile + 1]);
                     tile += 2;
                 }
             };
 #pragma unroll
-            for (int i = 0; i < S::kP8; ++i) {
+            for (int i = 0; i < S::kP8; ++i)
                 turn(v8[i], 8);
-                if (S::kTight && i == 0) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (u + 1 < n_units)
-                        load_keys(t0 + kUnit);
-                }
-            }
             if (S::kP4)
                 turn(v4[0], 4);
             if (S::kP2)
                 turn(v2[0], 2);
-            if (S::kTight) {
-                __builtin_amdgcn_sched_barrier(0);
-                if (u + 1 < n_units)
-                    load_values(t0 + kUnit, 0, 1);
-            }
+        };
+        for (int u = 0; u < n_tiles - 1; ++u)
+            take(tile0 + u * kTile, std::true_type());
+        take(tile0 + (n_tiles - 1) * kTile, std::false_type());
+        o.sum = quarters_sum(o.sum);
+        left -= n_tiles;
+        const bool ends = skip + n_tiles == row_n;
+        if (skip > 0) {
+            state |= kHead | (ends ? kEnds : 0);
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i)
+                s_head[wave][i * 64 + lane] = o.acc[i];
+            s_stat[wave][lane] = o.ref;
+            s_stat[wave][64 + lane] = o.sum;
+        } else if (ends) {
+            finish(o, row);
+        } else {
+            state |= kOpen;
         }
-
-        // ---- join the four waves -------------------------------------------
-        sum = quarters_sum(sum);
-        if (quarter == 0) {
-            s_ref[wave][col] = ref;
-            s_sum[wave][col] = sum;
         }
-        __syncthreads();
-        float all = fmaxf(fmaxf(s_ref[0][col], s_ref[1][col]), fmaxf(s_ref[2][col], s_ref[3][col]));
-        const float shrink = __builtin_amdgcn_exp2f(ref - all);
-        {
-            float *o = &s_out[(wave * 16 + col) * kRow];
-            int tile = 0;
-            const auto put = [&](int d0, int width) {
-                // lane's rows 4 quarter + r hold values d0 + width * row + i
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int i = 0; i < width; ++i)
-                        o[d0 + width * (4 * quarter + r) + i] = acc[tile + i][r] * shrink;
-                tile += width;
-            };
-#pragma unroll
-            for (int i = 0; i < S::kP8; ++i)
-                put(128 * i, 8);
-            if (S::kP4)
-                put(128 * S::kP8, 4);
-            if (S::kP2)
-                put(128 * S::kP8 + 64 * S::kP4, 2);
-        }
-        __syncthreads();
-        const bool whole = skip == 0 && n_units == row_n;
-        // at most one partial begins inside its row and one at its start
-        const int64_t slot = ((int64_t)(w * 2 + (skip > 0 ? 0 : 1)) * gridDim.y + hv) * p.group_step;
-        for (int i = tid; i < n_heads * (D / 4); i += kThreads) {
-            const int head = i / (D / 4), d = (i % (D / 4)) * 4;
-            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-            float m = s_ref[0][head], l = 0.0f;
-#pragma unroll
-            for (int k = 1; k < kWaves; ++k)
-                m = fmaxf(m, s_ref[k][head]);
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-                o += *reinterpret_cast<const f32x4 *>(&s_out[(k * 16 + head) * kRow + d]);
-                l += s_sum[k][head] * __builtin_amdgcn_exp2f(s_ref[k][head] - m);
-            }
-            if (whole) {
-                attn_store<TYPE>(p, row, first_head + head, D, d, o, m, l);
-            } else {
-                *reinterpret_cast<f32x4 *>(p.part_out + (slot + head) * D + d) = o;
-                if (d == 0) {
-                    p.part_stat[(slot + head) * 2] = m;
-                    p.part_stat[(slot + head) * 2 + 1] = l;
-                }
-            }
-        }
-        __syncthreads();
-        left -= n_units;
+        if (left == 0 || row + 1 >= rows)
+            break;
         ++row;
         skip = 0;
+        row_first += row_n;
+        const RowSpan next = row_span(p, reqs, kv_len, row);
+        lo = next.lo;
+        hi = next.hi;
+        req = next.req;
+        row_n = row_tiles(next);
+    }
+
+    // ---- what the block's waves share ------------------------------------------
+    if (lane == 0)
+        s_state[wave] = state;
+    __syncthreads();
+    const auto state_of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_state[i]); };
+    // the last block of the row whose tiles begin at `first`
+    const auto last_block = [&](int first, int n) { return (int)line.of(first + n - 1) / kWaves; };
+    if (state & kOpen) {
+        bool ends = false;
+        for (int i = wave + 1; i < kWaves && !ends; ++i) {
+            o.join(s_head[i], s_stat[i], lane);
+            ends = state_of(i) & kEnds;
+        }
+        if (ends) {
+            finish(o, row);
+        } else {
+            hand_on(o, 1);
+            s_join[3] = row;
+            s_join[4] = last_block(row_first, row_n) - (int)blockIdx.x + 1;
+        }
+    }
+    if (wave == 0 && (state & kHead)) {  // a row that began in an earlier block
+        o.clear();
+        bool ends = false;
+        for (int i = 0; i < kWaves && !ends && (state_of(i) & kHead); ++i) {
+            o.join(s_head[i], s_stat[i], lane);
+            ends = state_of(i) & kEnds;
+        }
+        hand_on(o, 0);
+        const int first_block = (int)line.of(head_first) / kWaves;
+        s_join[0] = head_row;
+        s_join[1] = first_block;
+        s_join[2] = last_block(head_first, head_n) - first_block + 1;
+    }
+    if (hv == 0) {
+        __syncthreads();
+        if (tid < 8)
+            p.join[blockIdx.x * 8 + tid] = s_join[tid];
     }
 }
 
-// Combines a row's partials, one block per (row, head group), in the order of
-// the blocks that made them; rows without tokens get zeros.  A row that one
-// block finished is left as it is.
+// Joins the rows that several blocks share, and gives rows without tokens their
+// zeros.  Block w of the attention left in join[w]: the row it continued from an
+// earlier block (row, first block of the row, blocks of the row), and the row it
+// began and handed on (row, blocks).  A row's (head, 4 values) items are dealt to
+// as many of its blocks as gives a thread about four partials; threads that
+// share an item combine through LDS, in a fixed order.
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void attn_join_kernel(const AttnProblem p, int blocks,
-                                                             int dim)
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
+    const AttnProblem p, const int32_t *__restrict__ reqs, const int32_t *__restrict__ kv_len,
+    int dim)
 {
-    const int64_t row = blockIdx.x;
+    __shared__ f32x4 s_out[kJoinThreads];
+    __shared__ float s_ref[kJoinThreads], s_sum[kJoinThreads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int w = blockIdx.x, blocks = gridDim.x;
     const int hv = blockIdx.y;
     const int kvh = hv / p.head_groups;
     const int sub = hv % p.head_groups;
     const int first_head = kvh * p.group + sub * p.group_step;
     const int n_heads = min(p.group_step, p.group - sub * p.group_step);
-    const int32_t units = p.first_unit[p.rows];
-    const int32_t parts = min(blocks, units);
-    const int32_t u0 = p.first_unit[row], u1 = p.first_unit[row + 1];
-    int32_t w0 = 0, count = 0;
-    if (u1 > u0) {
-        w0 = range_of(u0, units, parts);
-        count = range_of(u1 - 1, units, parts) - w0 + 1;
-        if (count == 1)
-            return;
+    const int items = n_heads * (dim / 4);
+    const int32_t *join = p.join + w * 8;
+
+    for (int64_t r0 = w + (int64_t)wave * 64 * blocks; r0 < p.rows;
+         r0 += (int64_t)kJoinThreads * blocks) {
+        const int64_t r = r0 + (int64_t)lane * blocks;
+        uint64_t none = __ballot(r < p.rows && row_span(p, reqs, kv_len, (int32_t)r).hi == 0);
+        for (; none; none &= none - 1) {
+            const int64_t row = r0 + (int64_t)__builtin_ctzll(none) * blocks;
+            for (int i = lane; i < items; i += 64)
+                attn_store<TYPE>(p, row, first_head + i / (dim / 4), dim, i % (dim / 4) * 4,
+                                 f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f, 0.0f);
+        }
     }
-    for (int i = threadIdx.x; i < n_heads * (dim / 4); i += kThreads) {
-        const int head = i / (dim / 4), d = (i % (dim / 4)) * 4;
+
+    for (int began = 0; began < 2; ++began) {
+        const int row = join[began ? 3 : 0], count = join[began ? 4 : 2];
+        const int w0 = began ? w : join[1];
+        // the w - w0-th of the row's blocks takes that slice of the items: at most
+        // one a thread (16 heads of 256 are two slices, and count is at least 2)
+        const int slices =
+            min(count, max((count * items + 4 * kJoinThreads - 1) / (4 * kJoinThreads),
+                           (items + kJoinThreads - 1) / kJoinThreads));
+        if (w - w0 >= slices)
+            continue;
+        const int each = (items + slices - 1) / slices;
+        const int i0 = (w - w0) * each, n = min(each, items - i0);
+        if (n <= 0)
+            continue;
+        int groups = 1;  // threads an item
+        while (2 * groups * n <= kJoinThreads && groups < count)
+            groups *= 2;
+        const int g = tid / n, item = i0 + tid % n;
+        const int head = item / (dim / 4), d = item % (dim / 4) * 4;
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
         float ref = kNone, sum = 0.0f;
-        for (int k = 0; k < count; ++k) {
-            // the row's first partial begins at its start, the others inside it
-            const int64_t slot =
-                ((int64_t)((w0 + k) * 2 + (k == 0 ? 1 : 0)) * gridDim.y + hv) * p.group_step + head;
-            const f32x4 part = *reinterpret_cast<const f32x4 *>(p.part_out + slot * dim + d);
-            const float r = p.part_stat[slot * 2], l = p.part_stat[slot * 2 + 1];
+        const auto add = [&](f32x4 part, float r, float l) {
             const float to = fmaxf(ref, r);
             const float a = __builtin_amdgcn_exp2f(ref - to), b = __builtin_amdgcn_exp2f(r - to);
             o = o * a + part * b;
             sum = sum * a + l * b;
             ref = to;
+        };
+        if (g < groups) {
+#pragma unroll 4
+            for (int k = g; k < count; k += groups) {
+                // the row's first partial is what its block began, the others what theirs continued
+                const int64_t slot =
+                    ((int64_t)((w0 + k) * 2 + (k == 0 ? 1 : 0)) * gridDim.y + hv) * p.group_step +
+                    head;
+                add(*reinterpret_cast<const f32x4 *>(p.part_out + slot * dim + d),
+                    p.part_stat[slot * 2], p.part_stat[slot * 2 + 1]);
+            }
         }
-        attn_store<TYPE>(p, row, first_head + head, dim, d, o, ref, sum);
+        for (int half = groups / 2; half > 0; half /= 2) {
+            if (g >= half && g < 2 * half) {
+                s_out[tid] = o;
+                s_ref[tid] = ref;
+                s_sum[tid] = sum;
+            }
+            __syncthreads();
+            if (g < half)
+                add(s_out[tid + half * n], s_ref[tid + half * n], s_sum[tid + half * n]);
+            __syncthreads();
+        }
+        if (g == 0)
+            attn_store<TYPE>(p, row, first_head + head, dim, d, o, ref, sum);
     }
 }
 
@@ -620,12 +793,12 @@ hipError_t launch(const AttnProblem &p, int blocks, hipStream_t stream)
 {
     const int heads = p.kv_heads * p.head_groups;
     hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D>), dim3((unsigned)blocks, (unsigned)heads),
-                       dim3(kThreads), 0, stream, p);
+                       dim3(kThreads), 0, stream, p, p.table, p.req, p.kv_len);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL((attn_join_kernel<TYPE>), dim3((unsigned)p.rows, (unsigned)heads),
-                       dim3(kThreads), 0, stream, p, blocks, D);
+    hipLaunchKernelGGL((attn_join_kernel<TYPE>), dim3((unsigned)blocks, (unsigned)heads),
+                       dim3(kJoinThreads), 0, stream, p, p.req, p.kv_len, D);
     return hipGetLastError();
 }
 

@@ -186,10 +186,16 @@ struct AttnProblem {
     int32_t window;
     float score_scale, value_scale;
     // workspace: partial rows [2 blocks][heads of a pass][head_dim], their
-    // reference score and sum, and the first work unit of every row
+    // reference score and sum, and what the join finds of every block
     float *part_out, *part_stat;
-    int32_t *first_unit;
+    int32_t *join;
 };
+// Blocks of four waves that a CU holds at once: the registers of a wave take
+// its output, a tile's values and two tiles' keys.
+constexpr int attn_blocks_per_cu(bool fp8, int dim)
+{
+    return (fp8 ? 1 : 2) * dim >= 512 ? 1 : 2;
+}
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream);
 
