@@ -104,16 +104,27 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b)
     return __builtin_bit_cast(uint32_t, half2v{(_Float16)a, (_Float16)b});
 }
 
-// Largest value over the four 16-lane quarters that share a head.
-__device__ __forceinline__ float quarters_ref(float x)
+// Over the four 16-lane quarters that share a head: each swap leaves a lane and
+// its partner's value in the two results.
+template <typename F>
+__device__ __forceinline__ float over_quarters(float x, const F &f)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t a0 = a[0], a1 = a[1];
+    const uint32_t v = __builtin_bit_cast(
+        uint32_t, f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    return f(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+__device__ __forceinline__ float quarters_max(float x)
+{
+    return over_quarters(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float quarters_sum(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    return over_quarters(x, [](float a, float b) { return a + b; });
 }
 
 template <int BYTES>
@@ -181,14 +192,16 @@ struct WorkLine {
     }
 };
 
-// Inclusive sum over the wave's lanes.
-__device__ __forceinline__ int32_t wave_scan(int32_t x, int lane)
+// Inclusive sum over the wave's lanes: within rows of 16 by shifts, then the last
+// lane of each row (or pair of rows) into the following ones.
+__device__ __forceinline__ int32_t wave_scan(int32_t x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int32_t up = __shfl_up(x, d);
-        x += lane >= d ? up : 0;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // row_shr:2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);  // row_shr:4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);  // row_shr:8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
     return x;
 }
 
@@ -203,7 +216,7 @@ __device__ __forceinline__ void attn_store(const AttnProblem &p, int64_t row, in
         u32x2{narrow2<TYPE>(o[0] * scale, o[1] * scale), narrow2<TYPE>(o[2] * scale, o[3] * scale)};
     if (d == 0 && p.lse)
         p.lse[row * (p.kv_heads * p.group) + head] =
-            sum == 0.0f ? -__builtin_inff() : (ref + log2f(sum)) * kLn2;
+            sum == 0.0f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int TYPE, bool FP8, int D>
@@ -216,8 +229,9 @@ struct Shape {
     static constexpr int kP8 = D / 128;
     static constexpr int kP4 = (D % 128) / 64;
     static constexpr int kP2 = (D % 64) / 32;
-    // Blocks of four waves a CU, as their registers allow.
-    static constexpr int kPerCu = attn_blocks_per_cu(FP8, D);
+    // Waves a SIMD is compiled for: 256 registers a lane, all 512 where two tiles'
+    // keys and a tile's values beside the output need them.
+    static constexpr int kWavesPerSimd = D * kElt >= 512 ? 1 : 2;
 };
 
 // A wave's output of one row: acc (value d of a head in the lane and register
@@ -255,18 +269,25 @@ struct VPiece {
     typedef typename Piece<W * (FP8 ? 1 : 2)>::T Raw;
     Raw raw[8];
 
-    __device__ __forceinline__ uint32_t dword(int j, int i) const
+    // values 2i (even) and 2i + 1 (odd) of tokens 2j and 2j + 1, side by side
+    __device__ __forceinline__ void turn(int i, int j, uint32_t &even, uint32_t &odd) const
     {
-        // values 2i and 2i + 1 of token j as two 16-bit values
-        const uint32_t *d = reinterpret_cast<const uint32_t *>(&raw[j]);
-        if (!FP8)
-            return d[i];
-        return i & 1 ? wide2<TYPE, true>(d[i >> 1]) : wide2<TYPE, false>(d[i >> 1]);
+        const uint32_t *a = reinterpret_cast<const uint32_t *>(&raw[2 * j]);
+        const uint32_t *b = reinterpret_cast<const uint32_t *>(&raw[2 * j + 1]);
+        if (FP8) {
+            const uint32_t t = __builtin_amdgcn_perm(b[i >> 1], a[i >> 1],
+                                                     i & 1 ? 0x07030602u : 0x05010400u);
+            even = wide2<TYPE, false>(t);
+            odd = wide2<TYPE, true>(t);
+        } else {
+            even = __builtin_amdgcn_perm(b[i], a[i], 0x05040100u);
+            odd = __builtin_amdgcn_perm(b[i], a[i], 0x07060302u);
+        }
     }
 };
 
 template <int TYPE, bool FP8, int D>
-__global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_kernel(
+__global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) void attn_kernel(
     const AttnProblem p, const int32_t *__restrict__ tables, const int32_t *__restrict__ reqs,
     const int32_t *__restrict__ kv_len)
 {
@@ -291,7 +312,8 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
     const int rows = (int)p.rows;
 
     // ---- this wave's range of the work line ----------------------------------
-    // up to 64 rows: a row a lane; above, thread i sums rows [i * per, (i + 1) * per)
+    // up to 64 rows: a row a lane, in every wave; above, thread i sums rows
+    // [i * per, (i + 1) * per)
     int32_t tiles, chunk = 0, chunk_first = 0;
     const int32_t per = rows <= 64 ? 64 : (rows + kThreads - 1) / kThreads;
     RowSpan span;
@@ -301,13 +323,13 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
         if (lane < rows)
             span = row_span(p, reqs, kv_len, lane);
         mine = row_tiles(span);
-        incl = wave_scan(mine, lane);
+        incl = wave_scan(mine);
         tiles = __builtin_amdgcn_readlane(incl, 63);
     } else {
         const int32_t r1 = min((tid + 1) * per, rows);
         for (int32_t r = tid * per; r < r1; ++r)
             mine += row_tiles(row_span(p, reqs, kv_len, r));
-        incl = wave_scan(mine, lane);
+        incl = wave_scan(mine);
         if (lane == 63)
             s_sums[wave] = incl;
         __syncthreads();
@@ -340,32 +362,34 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
 #pragma unroll
             for (int i = 0; i < kWaves; ++i)
                 below += __popcll(__ballot(s_first[i * 64 + lane] <= begin));
-            chunk = __builtin_amdgcn_readfirstlane(below - 1);
+            chunk = below - 1;
             chunk_first = __builtin_amdgcn_readfirstlane(s_first[chunk]);
         }
-        const int32_t r1 = min((chunk + 1) * per, rows);
-        for (int32_t r = chunk * per;; r += 64) {
-            if (rows > 64) {
-                span = RowSpan{0, 0, 0};
-                if (r + lane < r1)
-                    span = row_span(p, reqs, kv_len, r + lane);
-                mine = row_tiles(span);
-                incl = wave_scan(mine, lane);
-            }
-            const uint64_t past = __ballot(chunk_first + incl > begin);
-            if (past) {
-                const int at = __builtin_ctzll(past);
-                row = r + at;
-                skip = begin - (chunk_first + __builtin_amdgcn_readlane(incl - mine, at));
-                span.lo = __builtin_amdgcn_readlane(span.lo, at);
-                span.hi = __builtin_amdgcn_readlane(span.hi, at);
-                span.req = __builtin_amdgcn_readlane(span.req, at);
-                break;
-            }
-            chunk_first += __builtin_amdgcn_readlane(incl, 63);
-            if (r + 64 >= r1) {  // not reached: the range's first tile is in the chunk
-                left = 0;
-                break;
+        if (per == 1) {
+            row = chunk;
+            skip = begin - chunk_first;
+            span = row_span(p, reqs, kv_len, row);
+        } else {
+            const int32_t r1 = min((chunk + 1) * per, rows);
+            for (int32_t r = chunk * per; r < r1; r += 64) {
+                if (rows > 64) {
+                    span = RowSpan{0, 0, 0};
+                    if (r + lane < r1)
+                        span = row_span(p, reqs, kv_len, r + lane);
+                    mine = row_tiles(span);
+                    incl = wave_scan(mine);
+                }
+                const uint64_t past = __ballot(chunk_first + incl > begin);
+                if (past) {
+                    const int at = __builtin_ctzll(past);
+                    row = r + at;
+                    skip = begin - (chunk_first + __builtin_amdgcn_readlane(incl - mine, at));
+                    span.lo = __builtin_amdgcn_readlane(span.lo, at);
+                    span.hi = __builtin_amdgcn_readlane(span.hi, at);
+                    span.req = __builtin_amdgcn_readlane(span.req, at);
+                    break;
+                }
+                chunk_first += __builtin_amdgcn_readlane(incl, 63);
             }
         }
     }
@@ -415,7 +439,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
         });
         if (quarter == 0 && p.lse)
             p.lse[(int64_t)r * (p.kv_heads * p.group) + first_head + col] =
-                f.sum == 0.0f ? -__builtin_inff() : (f.ref + log2f(f.sum)) * kLn2;
+                f.sum == 0.0f ? -__builtin_inff() : (f.ref + __builtin_amdgcn_logf(f.sum)) * kLn2;
     };
     // a partial row for the join: slot 0 of the block began before it, slot 1 in it
     const auto hand_on = [&](const Partial<S::kAcc> &f, int which) {
@@ -495,7 +519,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
                     key[h][s] = stream<u32x4>(base[h] + (at + s * tokens * 64) + key_lane);
             }
         };
-        // values of piece i: [i * 128, ...) of head_dim, the last ones narrower
+        // values d0 ... of the lane's 8 tokens, `width` of them a lane
         const auto load_piece = [&](auto &v, int t0, int d0, int width) {
             typedef typename std::remove_reference<decltype(v)>::type::Raw Raw;
 #pragma unroll
@@ -515,7 +539,6 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
             if (S::kP2)
                 load_piece(v2[0], t0, 128 * S::kP8 + 64 * S::kP4, 2);
         };
-
         const int tile0 = (lo / kTile + skip) * kTile;
         ids_of(tile0, id);
         load_keys(tile0);
@@ -550,39 +573,46 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
             }
 
             // ---- softmax over this lane's 8 tokens ----------------------------
-            float x[8];
-            uint32_t keep[8];  // of V: whatever a place past the row holds must not meet a zero weight
+            float to_ref = to_log2;
+            float x[8];        // score - ref, in powers of two
+            uint32_t keep[8];  // of V: what lies in a dead token's place may be no number
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = s2[j >> 2][j & 3] * to_log2;
+            for (int j = 0; j < 8; ++j)
                 keep[j] = ~0u;
-            }
             if (t0 < lo || t0 + kTile > hi || !ok0 || !ok1) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int t = t0 + 16 * (j >> 2) + 4 * (j & 3) + quarter;
                     const bool live = t >= lo && t < hi && (j < 4 ? ok0 : ok1);
-                    x[j] = live ? x[j] : -__builtin_inff();
+                    s2[j >> 2][j & 3] = live ? s2[j >> 2][j & 3] * to_log2 : -__builtin_inff();
                     keep[j] = live ? ~0u : 0u;
                 }
+                to_ref = 1.0f;
             }
-            float m = x[0];
+            const auto weigh = [&](float ref) {
 #pragma unroll
-            for (int j = 1; j < 8; ++j)
-                m = fmaxf(m, x[j]);
-            if (__any(m > o.ref + kRoom)) {
-                m = fmaxf(quarters_ref(m) - kLift, o.ref);
-                const float shrink = __builtin_amdgcn_exp2f(o.ref - m);
-                o.ref = m;
+                for (int j = 0; j < 8; ++j)
+                    x[j] = __builtin_fmaf(s2[j >> 2][j & 3], to_ref, -ref);
+                float m = x[0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j)
+                    m = fmaxf(m, x[j]);
+                return m;
+            };
+            if (__any(weigh(o.ref) > kRoom)) {
+                const float ref = fmaxf(quarters_max(weigh(0.0f)) - kLift, o.ref);
+                const float shrink = __builtin_amdgcn_exp2f(o.ref - ref);
+                o.ref = ref;
                 o.sum *= shrink;
 #pragma unroll
                 for (int i = 0; i < S::kAcc; ++i)
                     o.acc[i] *= shrink;
+                weigh(ref);
             }
             u32x4 p_hi, p_lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                x[j] = __builtin_amdgcn_exp2f(x[j] - o.ref);
+                x[j] = __builtin_amdgcn_exp2f(x[j]);
                 o.sum += x[j];
             }
 #pragma unroll
@@ -601,15 +631,13 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
                     v.raw[j] &= keep[j];
 #pragma unroll
                 for (int i = 0; i < width / 2; ++i) {
-                    uint32_t d[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        d[j] = v.dword(j, i);
                     u32x4 even, odd;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        even[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x05040100u);
-                        odd[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x07060302u);
+                        uint32_t e, d;
+                        v.turn(i, j, e, d);
+                        even[j] = e;
+                        odd[j] = d;
                     }
                     o.acc[tile] = mfma32<TYPE>(even, p_hi, o.acc[tile]);
                     o.acc[tile] = mfma32<TYPE>(even, p_lo, o.acc[tile]);
@@ -661,21 +689,21 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
     if (lane == 0)
         s_state[wave] = state;
     __syncthreads();
-    const auto state_of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_state[i]); };
-    // the last block of the row whose tiles begin at `first`
-    const auto last_block = [&](int first, int n) { return (int)line.of(first + n - 1) / kWaves; };
+    const int states = s_state[lane & (kWaves - 1)];
+    const auto state_of = [&](int i) { return __builtin_amdgcn_readlane(states, i); };
     if (state & kOpen) {
         bool ends = false;
         for (int i = wave + 1; i < kWaves && !ends; ++i) {
             o.join(s_head[i], s_stat[i], lane);
             ends = state_of(i) & kEnds;
         }
-        if (ends) {
+        if (ends)
             finish(o, row);
-        } else {
+        else
             hand_on(o, 1);
+        if (!ends && hv == 0) {
             s_join[3] = row;
-            s_join[4] = last_block(row_first, row_n) - (int)blockIdx.x + 1;
+            s_join[4] = (int)line.of(row_first + row_n - 1) / kWaves - (int)blockIdx.x + 1;
         }
     }
     if (wave == 0 && (state & kHead)) {  // a row that began in an earlier block
@@ -686,10 +714,12 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kPerCu)) void attn_
             ends = state_of(i) & kEnds;
         }
         hand_on(o, 0);
-        const int first_block = (int)line.of(head_first) / kWaves;
-        s_join[0] = head_row;
-        s_join[1] = first_block;
-        s_join[2] = last_block(head_first, head_n) - first_block + 1;
+        if (hv == 0) {
+            const int first_block = (int)line.of(head_first) / kWaves;
+            s_join[0] = head_row;
+            s_join[1] = first_block;
+            s_join[2] = (int)line.of(head_first + head_n - 1) / kWaves - first_block + 1;
+        }
     }
     if (hv == 0) {
         __syncthreads();

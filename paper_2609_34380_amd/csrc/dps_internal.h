@@ -190,12 +190,10 @@ struct AttnProblem {
     float *part_out, *part_stat;
     int32_t *join;
 };
-// Blocks of four waves that a CU holds at once: the registers of a wave take
-// its output, a tile's values and two tiles' keys.
-constexpr int attn_blocks_per_cu(bool fp8, int dim)
-{
-    return (fp8 ? 1 : 2) * dim >= 512 ? 1 : 2;
-}
+// Blocks of four waves a CU gets: one keeps enough bytes in flight (16 KiB a wave
+// at 128 16-bit values) and leaves the fewest partial rows; rows of 64 bytes take
+// two.
+constexpr int attn_blocks_per_cu(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim <= 64 ? 2 : 1; }
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream);
 
