@@ -9,6 +9,7 @@ import collections
 import ctypes
 import functools
 import os
+import struct
 
 import torch
 
@@ -189,14 +190,14 @@ def load_library(path=LIB_PATH):
     lib.dps_restore_worker_destroy.restype = None
     lib.dps_restore_worker_last_error.argtypes = []
     lib.dps_restore_worker_last_error.restype = ctypes.c_char_p
-    lib.dps_kv_map.argtypes = [P, P, I64, I32, P, I64, P, I64, ctypes.POINTER(CKvStep), P]
+    # descriptors as pointers: a structure by reference, or its bytes
+    lib.dps_kv_map.argtypes = [P, P, I64, I32, P, I64, P, I64, P, P]
     lib.dps_kv_map.restype = ST
-    lib.dps_kv_store.argtypes = [ctypes.POINTER(CKvStoreArgs), ctypes.POINTER(CKvCache), P]
+    lib.dps_kv_store.argtypes = [P, ctypes.POINTER(CKvCache), P]
     lib.dps_kv_store.restype = ST
     lib.dps_attn_workspace_bytes.argtypes = [I64, I64, I64, I64]
     lib.dps_attn_workspace_bytes.restype = ctypes.c_size_t
-    lib.dps_attn_decode.argtypes = [ctypes.POINTER(CAttnArgs), ctypes.POINTER(CKvCache), P,
-                                    ctypes.c_size_t, P]
+    lib.dps_attn_decode.argtypes = [P, ctypes.POINTER(CKvCache), P, ctypes.c_size_t, P]
     lib.dps_attn_decode.restype = ST
     lib.dps_status_str.argtypes = [ST]
     lib.dps_status_str.restype = ctypes.c_char_p
@@ -528,18 +529,45 @@ class KvCache:
         self.ref = ctypes.byref(self.c)
 
 
+def _packer(cls):
+    """The bytes of a C structure from its fields in order: filling a ctypes
+    structure costs several times as much, on calls that take microseconds."""
+    codes = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
+    made = struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0q")
+    assert made.size == ctypes.sizeof(cls)
+    return made.pack
+
+
+_pack_step, _pack_store, _pack_attn = (_packer(c) for c in (CKvStep, CKvStoreArgs, CAttnArgs))
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+_ACT_TYPES = {torch.float16: KV_F16, torch.bfloat16: KV_BF16}
+
+
 class KvMap(collections.namedtuple("KvMap", "q_start seq_len counts pos slot req kv_len")):
     """What kv_map writes: int32 q_start [requests + 1], seq_len [requests], counts
     [2] (new tokens, blocks taken), and per row of the step int32 pos, int64 slot,
     int32 req and kv_len (see dps_kv_step in include/dps.h)."""
-    __slots__ = ()
+
+    def step(self, requests):
+        """The descriptor (bytes) of these buffers, checked and made once."""
+        if self.__dict__.get("_requests") != requests:
+            for name, t in zip(self._fields, self):
+                _require_int(name, t, _I64 if name == "slot" else _I32, 1)
+            rows = self.pos.shape[0]
+            _require(self.q_start.shape[0] == requests + 1 and self.counts.shape[0] == 2 and
+                     self.seq_len.shape[0] == requests and self.slot.shape[0] == rows and
+                     self.req.shape[0] == rows and self.kv_len.shape[0] == rows,
+                     "out does not fit the requests, or its rows differ")
+            self._step = _pack_step(rows, *[t.data_ptr() for t in self])
+            self._requests = requests
+        return self._step
 
 
 def make_kv_map(requests, rows, device):
     """Buffers for kv_map of up to `rows` rows; a graph's step keeps them."""
-    i32 = functools.partial(torch.empty, dtype=torch.int32, device=device)
+    i32 = functools.partial(torch.empty, dtype=_I32, device=device)
     return KvMap(i32(requests + 1), i32(requests), i32(2), i32(rows),
-                 torch.empty(rows, dtype=torch.int64, device=device), i32(rows), i32(rows))
+                 torch.empty(rows, dtype=_I64, device=device), i32(rows), i32(rows))
 
 
 def kv_map(ctx_len, new_len, fresh, table, block_tokens, rows=None, out=None):
@@ -548,42 +576,40 @@ def kv_map(ctx_len, new_len, fresh, table, block_tokens, rows=None, out=None):
     from `fresh` (int32 block ids) into its row of `table` (int32 [requests][columns],
     updated in place).  rows: room for new tokens (without out); returns a KvMap."""
     lib = _lib or load_library()
-    for name, t in (("ctx_len", ctx_len), ("new_len", new_len), ("fresh", fresh)):
-        _require_int(name, t, torch.int32, 1)
-    _require_int("table", table, torch.int32, 2)
+    for t, dim in ((ctx_len, 1), (new_len, 1), (fresh, 1), (table, 2)):
+        if not (t.dtype is _I32 and t.is_cuda and t.is_contiguous() and t.dim() == dim):
+            _require_int("ctx_len, new_len and fresh (1-d) and table (2-d)", t, _I32, dim)
     requests = ctx_len.shape[0]
-    _require(0 < block_tokens <= 256, "block_tokens is out of range")
-    _require(new_len.shape[0] == requests and table.shape[0] == requests,
-             "ctx_len, new_len and table differ in requests")
+    held, cols = table.shape
+    if not (new_len.shape[0] == requests == held):
+        raise ValueError("ctx_len, new_len and table differ in requests")
+    if not 0 < block_tokens <= 256:
+        raise ValueError("block_tokens is out of range")
     if out is None:
         _require(rows is not None and rows >= 0, "rows (or out) is needed")
         out = make_kv_map(requests, rows, ctx_len.device)
-    else:
-        for name, t in zip(out._fields, out):
-            _require_int(name, t, torch.int64 if name == "slot" else torch.int32, 1)
-        rows = out.pos.shape[0]
-        _require(out.q_start.shape[0] == requests + 1 and out.seq_len.shape[0] == requests and
-                 out.counts.shape[0] == 2 and out.slot.shape[0] == rows and
-                 out.req.shape[0] == rows and out.kv_len.shape[0] == rows,
-                 "out does not fit the requests, or its rows differ")
-    step = CKvStep(rows, *[t.data_ptr() for t in out])
     status = lib.dps_kv_map(ctx_len.data_ptr(), new_len.data_ptr(), requests, block_tokens,
-                            fresh.data_ptr(), fresh.shape[0], table.data_ptr(), table.shape[1],
-                            ctypes.byref(step), _stream())
+                            fresh.data_ptr(), fresh.shape[0], table.data_ptr(), cols,
+                            out.step(requests), _stream())
     if status:
         _check(status)
     return out
 
 
-def _rows_2d(name, t, width, rows, dtype):
-    """Rows of a [rows][width] (or [rows][heads][dim]) tensor whose rows are
-    contiguous: the row stride in elements."""
+def _row_stride(name, t, rows, heads, dim, dtype):
+    """The row stride in elements of a [rows][heads * dim] or [rows][heads][dim]
+    device tensor whose rows are contiguous."""
+    width = heads * dim
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == rows * width and \
+            (rows == 0 or t.shape[0] == rows):
+        return width
     inner = t.stride(-1) == 1 or t.shape[-1] <= 1
+    got = -1
     if t.dim() == 3:
         inner = inner and (t.shape[1] <= 1 or t.stride(1) == t.shape[2])
         got = t.shape[1] * t.shape[2]
-    else:
-        got = t.shape[-1] if t.dim() == 2 else -1
+    elif t.dim() == 2:
+        got = t.shape[1]
     if not (t.is_cuda and t.dtype == dtype and inner and got == width and t.shape[0] == rows):
         raise ValueError("%s must be %d device rows of %d contiguous %s" % (name, rows, width,
                                                                             dtype))
@@ -600,35 +626,41 @@ def kv_store(qkv, cache, slot, heads, pos=None, rope=None, q_weight=None, k_weig
     Returns the queries [rows][heads][head_dim] (q_out).  k_out: the finished keys
     [rows][kv_heads][head_dim] as well."""
     lib = _lib or load_library()
-    rows, dim = qkv.shape[0], cache.head_dim
+    rows, dim, kv_heads = qkv.shape[0], cache.head_dim, cache.kv_heads
     dtype = qkv.dtype
-    _require(dtype in (torch.float16, torch.bfloat16), "qkv must be float16 or bfloat16")
-    stride = _rows_2d("qkv", qkv, (heads + 2 * cache.kv_heads) * dim, rows, dtype)
-    _require_int("slot", slot, torch.int64, 1)
-    _require(slot.shape[0] == rows, "slot and qkv differ in rows")
+    kind = _ACT_TYPES.get(dtype)
+    if kind is None:
+        raise ValueError("qkv must be float16 or bfloat16")
+    stride = _row_stride("qkv", qkv, rows, heads + 2 * kv_heads, dim, dtype)
+    if not (slot.dtype is _I64 and slot.is_cuda and slot.is_contiguous() and slot.shape == (rows,)):
+        raise ValueError("slot must be a contiguous int64 device tensor, one entry a row")
+    at = table = None
     max_pos = rot = 0
     if rope is not None:
-        _require(rope.is_cuda and rope.dtype == torch.float32 and rope.dim() == 2 and
-                 rope.is_contiguous(), "rope must be a contiguous float32 [max_pos][rot]")
-        _require(pos is not None, "a rotation needs positions")
-        _require_int("pos", pos, torch.int32, 1)
-        _require(pos.shape[0] == rows, "pos and qkv differ in rows")
+        if not (rope.is_cuda and rope.dtype is _F32 and rope.dim() == 2 and rope.is_contiguous()):
+            raise ValueError("rope must be a contiguous float32 device tensor [max_pos][rot]")
+        if not (pos is not None and pos.dtype is _I32 and pos.is_cuda and pos.is_contiguous() and
+                pos.shape == (rows,)):
+            raise ValueError("a rotation needs pos, contiguous int32, one entry a row")
         max_pos, rot = rope.shape
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _require(w.is_cuda and w.dtype == dtype and w.is_contiguous() and w.shape == (dim,),
-                     "%s must be [head_dim] of qkv's dtype" % name)
+        at, table = pos.data_ptr(), rope.data_ptr()
+    wq = wk = None
+    if q_weight is not None or k_weight is not None:
+        for w in (q_weight, k_weight):
+            if not (w is not None and w.is_cuda and w.dtype is dtype and w.is_contiguous() and
+                    w.shape == (dim,)):
+                raise ValueError("q_weight and k_weight must be [head_dim] of qkv's dtype, both")
+        wq, wk = q_weight.data_ptr(), k_weight.data_ptr()
     if q_out is None:
         q_out = torch.empty((rows, heads, dim), dtype=dtype, device=qkv.device)
-    q_stride = _rows_2d("q_out", q_out, heads * dim, rows, dtype)
-    k_stride = 0
+    q_stride = _row_stride("q_out", q_out, rows, heads, dim, dtype)
+    kp, k_stride = None, 0
     if k_out is not None:
-        k_stride = _rows_2d("k_out", k_out, cache.kv_heads * dim, rows, dtype)
-    args = CKvStoreArgs(rows, heads, qkv.data_ptr(), stride, slot.data_ptr(),
-                        pos.data_ptr() if rope is not None else None, _ptr(rope), max_pos, rot,
-                        1 if adjacent else 0, _ptr(q_weight), _ptr(k_weight), eps,
-                        _KV_TYPES[dtype], q_out.data_ptr(), q_stride, _ptr(k_out), k_stride)
-    status = lib.dps_kv_store(ctypes.byref(args), cache.ref, _stream())
+        kp, k_stride = k_out.data_ptr(), _row_stride("k_out", k_out, rows, kv_heads, dim, dtype)
+    args = _pack_store(rows, heads, qkv.data_ptr(), stride, slot.data_ptr(), at or 0, table or 0,
+                       max_pos, rot, 1 if adjacent else 0, wq or 0, wk or 0, eps, kind,
+                       q_out.data_ptr(), q_stride, kp or 0, k_stride)
+    status = lib.dps_kv_store(args, cache.ref, _stream())
     if status:
         _check(status)
     return q_out
@@ -648,35 +680,44 @@ def attn_decode(q, cache, table, kv_len, req=None, scale=None, window=0, out=Non
     are table[req[j]].  scale: of the scores, 1 / sqrt(head_dim) by default.  lse:
     float32 [rows][heads] for the log of the sums.  Returns out (q's shape)."""
     lib = _lib or load_library()
-    _require(q.dim() == 3, "q must be [rows][heads][head_dim]")
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][heads][head_dim]")
     rows, heads, dim = q.shape
     dtype = q.dtype
-    _require(dtype in (torch.float16, torch.bfloat16), "q must be float16 or bfloat16")
-    _require(dim == cache.head_dim, "q and cache differ in head_dim")
-    q_stride = _rows_2d("q", q, heads * dim, rows, dtype)
-    _require_int("table", table, torch.int32, 2)
-    _require_int("kv_len", kv_len, torch.int32, 1)
-    _require(kv_len.shape[0] == rows, "kv_len and q differ in rows")
+    kind = _ACT_TYPES.get(dtype)
+    if kind is None or dim != cache.head_dim:
+        raise ValueError("q must be float16 or bfloat16, of the cache's head_dim")
+    q_stride = _row_stride("q", q, rows, heads, dim, dtype)
+    if not (table.dtype is _I32 and table.is_cuda and table.is_contiguous() and table.dim() == 2):
+        raise ValueError("table must be a contiguous int32 device tensor [requests][columns]")
+    if not (kv_len.dtype is _I32 and kv_len.is_cuda and kv_len.is_contiguous() and
+            kv_len.shape == (rows,)):
+        raise ValueError("kv_len must be a contiguous int32 device tensor, one entry a row")
+    rp = lp = 0
     if req is not None:
-        _require_int("req", req, torch.int32, 1)
-        _require(req.shape[0] == rows, "req and q differ in rows")
+        if not (req.dtype is _I32 and req.is_cuda and req.is_contiguous() and req.shape == (rows,)):
+            raise ValueError("req must be a contiguous int32 device tensor, one entry a row")
+        rp = req.data_ptr()
     if out is None:
         out = torch.empty((rows, heads, dim), dtype=dtype, device=q.device)
-    out_stride = _rows_2d("out", out, heads * dim, rows, dtype)
+    out_stride = _row_stride("out", out, rows, heads, dim, dtype)
     if lse is not None:
-        _require(lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and
-                 lse.shape == (rows, heads), "lse must be a contiguous float32 [rows][heads]")
-    if scale is None:
-        scale = dim ** -0.5
-    window = min(window, 0x7fffffff)  # no length is beyond
-    _require(window >= 0, "window is negative")
+        if not (lse.dtype is _F32 and lse.is_cuda and lse.is_contiguous() and
+                lse.shape == (rows, heads)):
+            raise ValueError("lse must be a contiguous float32 device tensor [rows][heads]")
+        lp = lse.data_ptr()
+    if window < 0:
+        raise ValueError("window is negative")
     if workspace is None:
         need = lib.dps_attn_workspace_bytes(rows, heads, cache.kv_heads, dim)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    args = CAttnArgs(rows, heads, q.data_ptr(), q_stride, table.data_ptr(), table.shape[0],
-                     table.shape[1], _ptr(req), kv_len.data_ptr(), window, _KV_TYPES[dtype], scale,
-                     out.data_ptr(), out_stride, _ptr(lse))
-    status = lib.dps_attn_decode(ctypes.byref(args), cache.ref, workspace.data_ptr(),
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    requests, cols = table.shape
+    args = _pack_attn(rows, heads, q.data_ptr(), q_stride, table.data_ptr(), requests, cols, rp,
+                      kv_len.data_ptr(), min(window, 0x7fffffff), kind,
+                      dim ** -0.5 if scale is None else scale, out.data_ptr(), out_stride, lp)
+    status = lib.dps_attn_decode(args, cache.ref, workspace.data_ptr(),
                                  workspace.numel() * workspace.element_size(), _stream())
     if status:
         _check(status)
