@@ -874,6 +874,9 @@ DPS_EXPORT dps_status dps_kv_store(const dps_kv_store_args *a, const dps_kv_cach
             DPS_ERR_INVALID_ARG, "q_weight and k_weight are given together");
     REQUIRE(a->eps >= 0.0f && a->eps <= 3.4e38f, DPS_ERR_INVALID_ARG,
             "eps must be finite and not negative");
+    // a launch counts its threads (up to 16 a head) in 32 bits
+    REQUIRE(a->rows * (a->heads + 2 * kv_heads) <= (1 << 28) - 64, DPS_ERR_UNSUPPORTED,
+            "too many rows for one call");
     if (a->rows == 0)
         return DPS_OK;
     REQUIRE(a->qkv != nullptr && a->slot != nullptr && (a->heads == 0 || a->q_out != nullptr),

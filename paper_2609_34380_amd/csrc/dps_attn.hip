@@ -192,19 +192,6 @@ struct WorkLine {
     }
 };
 
-// Inclusive sum over the wave's lanes: within rows of 16 by shifts, then the last
-// lane of each row (or pair of rows) into the following ones.
-__device__ __forceinline__ int32_t wave_scan(int32_t x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // row_shr:2
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);  // row_shr:4
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);  // row_shr:8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
-    return x;
-}
-
 // Four values of a finished row's head: o / sum, rounded once, and its lse.
 template <int TYPE>
 __device__ __forceinline__ void attn_store(const AttnProblem &p, int64_t row, int head, int dim,

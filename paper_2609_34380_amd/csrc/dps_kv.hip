@@ -8,8 +8,6 @@ namespace dps {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr int kMapRows = 1024;  // rows of a block of kv_map_kernel
 
 // ---- step maps ------------------------------------------------------------------
 // With c = ctx_len, n = new_len of a request and B(x) = ceil(x / T): it takes
@@ -19,27 +17,33 @@ constexpr int kMapRows = 1024;  // rows of a block of kv_map_kernel
 // bisection.
 //
 // Bound: latency (20 bytes a row; a step of 256 rows moves 12 KB).  One launch:
-// every block sums the requests anew into its LDS, which costs it two reads of
-// the length arrays from L2, instead of a second launch that would wait for
-// the first.
+// every block sums the requests anew into its LDS, which costs it a read of the
+// length arrays from L2, instead of a second launch that would wait for the
+// first; a thread then has one row.  Past 256 requests the blocks are of 1024
+// threads, so that a thread sums 4 requests at most.
 
 struct Lengths {
-    int32_t have;  // blocks held before the step
-    int32_t need;  // blocks to take
+    int32_t have;        // blocks held before the step
+    int32_t need;        // blocks to take
     int32_t ctx, fresh;  // tokens before the step, new tokens
 };
 
-__device__ __forceinline__ Lengths lengths(const KvMapProblem &p, int r)
+// Blocks of n tokens, as far as a table row holds them.
+__device__ __forceinline__ int32_t held(const KvMapProblem &p, int64_t n)
 {
     const int64_t round = (int64_t(1) << p.log2_tokens) - 1;
+    return (int32_t)min((n + round) >> p.log2_tokens, p.table_cols);
+}
+
+__device__ __forceinline__ Lengths lengths(const KvMapProblem &p, int r)
+{
     const int64_t c = max(p.ctx_len[r], 0);
     const int64_t n = min((int64_t)max(p.new_len[r], 0), (int64_t)0x7fffffff - c);
     Lengths l;
     l.ctx = (int32_t)c;
     l.fresh = (int32_t)n;
-    // a table row holds table_cols blocks: none are taken past them
-    l.have = (int32_t)min((c + round) >> p.log2_tokens, p.table_cols);
-    l.need = (int32_t)min((c + n + round) >> p.log2_tokens, p.table_cols) - l.have;
+    l.have = held(p, c);
+    l.need = held(p, c + n) - l.have;
     return l;
 }
 
@@ -57,59 +61,67 @@ __device__ __forceinline__ int last_from(const int32_t *first, int n, int32_t x)
     return lo;
 }
 
-__global__ __launch_bounds__(kThreads) void kv_map_kernel(const KvMapProblem p)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void kv_map_kernel(const KvMapProblem p)
 {
-    extern __shared__ int32_t s_first[];
-    int32_t *s_row = s_first;                  // [requests + 1] first row
-    int32_t *s_block = s_first + p.requests + 1;  // [requests + 1] first new block
-    __shared__ int64_t s_rows[kWaves];
-    __shared__ int32_t s_blocks[kWaves];
+    constexpr int kWaves = THREADS / 64;
+    constexpr int kMost = THREADS == 256 ? 1 : 4;  // requests a thread
+    __shared__ int32_t s_row[THREADS * kMost];    // first row of a request
+    __shared__ int32_t s_block[THREADS * kMost];  // its first new block
+    __shared__ int32_t s_ctx[THREADS * kMost];
+    __shared__ int32_t s_low[kWaves], s_high[kWaves], s_blocks[kWaves];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (p.requests + kThreads - 1) / kThreads;
-    const int r0 = min(tid * per, p.requests), r1 = min(r0 + per, p.requests);
-    int64_t rows = 0;
-    int32_t blocks = 0;
-    for (int r = r0; r < r1; ++r) {
-        const Lengths l = lengths(p, r);
-        rows += l.fresh;
-        blocks += l.need;
-    }
-    int64_t row_incl = rows;
-    int32_t block_incl = blocks;
+    // thread i has requests [i * per, (i + 1) * per)
+    const int per = (p.requests + THREADS - 1) / THREADS;
+    const int r0 = tid * per;
+    Lengths l[kMost];
+    int32_t low = 0, high = 0, blocks = 0;  // new tokens in two halves: their sum passes 32 bits
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t a = __shfl_up(row_incl, d);
-        const int32_t b = __shfl_up(block_incl, d);
-        if (lane >= d) {
-            row_incl += a;
-            block_incl += b;
-        }
+    for (int i = 0; i < kMost; ++i) {
+        l[i] = Lengths{0, 0, 0, 0};
+        if (i < per && r0 + i < p.requests)
+            l[i] = lengths(p, r0 + i);
+        low += l[i].fresh & 0xffff;
+        high += l[i].fresh >> 16;
+        blocks += l[i].need;
     }
+    const int32_t low_incl = wave_scan(low), high_incl = wave_scan(high);
+    const int32_t block_incl = wave_scan(blocks);
     if (lane == 63) {
-        s_rows[wave] = row_incl;
+        s_low[wave] = low_incl;
+        s_high[wave] = high_incl;
         s_blocks[wave] = block_incl;
     }
     __syncthreads();
-    int64_t row_at = row_incl - rows, all_rows = 0;
-    int32_t block_at = block_incl - blocks, all_blocks = 0;
+    int32_t low_at = low_incl - low, high_at = high_incl - high;
+    int32_t block_at = block_incl - blocks, all_low = 0, all_high = 0, all_blocks = 0;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-        row_at += i < wave ? s_rows[i] : 0;
+        low_at += i < wave ? s_low[i] : 0;
+        high_at += i < wave ? s_high[i] : 0;
         block_at += i < wave ? s_blocks[i] : 0;
-        all_rows += s_rows[i];
+        all_low += s_low[i];
+        all_high += s_high[i];
         all_blocks += s_blocks[i];
     }
-    for (int r = r0; r < r1; ++r) {
-        const Lengths l = lengths(p, r);
-        s_row[r] = (int32_t)min(row_at, (int64_t)p.rows);
-        s_block[r] = block_at;
-        if (blockIdx.x == 0) {
-            p.q_start[r] = s_row[r];
-            p.seq_len[r] = l.ctx + l.fresh;
+    int64_t row_at = ((int64_t)high_at << 16) + low_at;
+    const int64_t all_rows = ((int64_t)all_high << 16) + all_low;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int r = r0 + i;
+        if (i < per && r < p.requests) {
+            const int32_t first = (int32_t)min(row_at, (int64_t)p.rows);
+            s_row[r] = first;
+            s_block[r] = block_at;
+            s_ctx[r] = l[i].ctx;
+            if (blockIdx.x == 0) {
+                p.q_start[r] = first;
+                p.seq_len[r] = l[i].ctx + l[i].fresh;
+            }
+            row_at += l[i].fresh;
+            block_at += l[i].need;
         }
-        row_at += l.fresh;
-        block_at += l.need;
     }
     if (blockIdx.x == 0 && tid == 0) {
         p.q_start[p.requests] = (int32_t)min(all_rows, (int64_t)p.rows);
@@ -119,28 +131,28 @@ __global__ __launch_bounds__(kThreads) void kv_map_kernel(const KvMapProblem p)
     __syncthreads();
 
     // new blocks into the tables
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < all_blocks;
-         i += (int64_t)gridDim.x * kThreads) {
+    for (int64_t i = (int64_t)blockIdx.x * THREADS + tid; i < all_blocks;
+         i += (int64_t)gridDim.x * THREADS) {
         const int r = last_from(s_block, p.requests, (int32_t)i);
-        const int64_t col = lengths(p, r).have + (i - s_block[r]);
+        const int64_t col = held(p, s_ctx[r]) + (i - s_block[r]);
         p.table[(int64_t)r * p.table_cols + col] = i < p.n_fresh ? p.fresh[i] : -1;
     }
 
     // rows
-    const int64_t first = (int64_t)blockIdx.x * kMapRows;
-    for (int64_t j = first + tid; j < min(first + kMapRows, (int64_t)p.rows); j += kThreads) {
+    const int64_t j = (int64_t)blockIdx.x * THREADS + tid;
+    if (j < p.rows) {
         int32_t pos = 0, req = -1;
         int64_t slot = -1;
         if (j < all_rows) {
             req = last_from(s_row, p.requests, (int32_t)j);
-            const Lengths l = lengths(p, req);
-            pos = l.ctx + ((int32_t)j - s_row[req]);
+            const int32_t ctx = s_ctx[req], have = held(p, ctx);
+            pos = ctx + ((int32_t)j - s_row[req]);
             const int32_t col = pos >> p.log2_tokens;
             int32_t block = -1;
-            if (col < l.have) {  // a block the request held before
+            if (col < have) {  // a block the request held before
                 block = p.table[(int64_t)req * p.table_cols + col];
             } else if (col < p.table_cols) {
-                const int64_t i = (int64_t)s_block[req] + (col - l.have);
+                const int64_t i = (int64_t)s_block[req] + (col - have);
                 block = i < p.n_fresh ? p.fresh[i] : -1;
             }
             if (block >= 0)
@@ -163,6 +175,11 @@ __global__ __launch_bounds__(kThreads) void kv_map_kernel(const KvMapProblem p)
 // up to a power of two), 16 values a lane in two 16-byte chunks.  With pairs
 // (i, i + rot / 2) a lane takes chunks j and j + rot / 16, so both values of
 // every pair are its own and the only exchange is the sum of squares.
+// Results are stored past the caches' retention, and the QKV rows, which the
+// product before has just written, loaded through them: 8192 rows of 32 + 16
+// heads of 128 40.5 us (206 MB, 5.1 TB/s, the rate of a plain copy), 43.3 with
+// plain stores, 41.0 with nontemporal loads too (and 4038 rows of 32 + 32 heads,
+// partly in the Infinity Cache, 26.0, 31.6 and 32.3).
 
 template <int TYPE>
 __device__ __forceinline__ float wide(uint16_t v)
@@ -219,6 +236,13 @@ __device__ __forceinline__ u32x2 codes8(const float *x, float inv_scale)
     return r;
 }
 
+// Stored past the caches' retention.
+template <typename V>
+__device__ __forceinline__ void put(void *p, V v)
+{
+    __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
+}
+
 template <int TYPE, bool FP8, int D>
 __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem p)
 {
@@ -226,32 +250,48 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
     constexpr int kGroup = kLanes <= 4 ? 4 : (kLanes <= 8 ? 8 : 16);
     constexpr int kElt = FP8 ? 1 : 2;
     const int j = threadIdx.x % kGroup;
-    const int kv_heads = p.cache.kv_heads;
-    const int64_t per_row = p.heads + 2 * (int64_t)kv_heads;
-    const int64_t items = p.rows * per_row;
-    const int64_t step = (int64_t)gridDim.x * (kThreads / kGroup);
-    for (int64_t it = (int64_t)blockIdx.x * (kThreads / kGroup) + threadIdx.x / kGroup; it < items;
-         it += step) {
-        const int64_t row = it / per_row;
-        const int head = (int)(it - row * per_row);
-        const bool is_q = head < p.heads, is_v = head >= p.heads + kv_heads;
-        const bool works = j < kLanes;
-        const bool turns = !is_v && p.rope && 16 * j < p.rot;
-        // the lane's two chunks of eight values
-        const bool split = turns && !p.adjacent;
-        const int c0 = split ? j : 2 * j, c1 = split ? j + p.rot / 16 : 2 * j + 1;
-        float x[16];
-        if (works) {
-            const uint16_t *src = p.qkv + row * p.qkv_stride + (int64_t)head * D;
-            widen8<TYPE>(load16(src + 8 * c0), x);
-            widen8<TYPE>(load16(src + 8 * c1), x + 8);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                x[i] = 0.0f;
-        }
+    const uint32_t q_heads = (uint32_t)p.heads, kv_heads = (uint32_t)p.cache.kv_heads;
+    const uint32_t heads = q_heads + 2 * kv_heads;
+    const uint32_t item = blockIdx.x * (kThreads / kGroup) + threadIdx.x / kGroup;
+    const uint32_t row = item / heads, head = item - row * heads;
+    if (row >= (uint32_t)p.rows)
+        return;
+    const bool is_q = head < q_heads, is_v = head >= q_heads + kv_heads;
+    const bool works = j < kLanes;
+    const bool turns = !is_v && 16 * j < p.rot;
+    // the lane's two chunks of eight values
+    const bool split = turns && !p.adjacent;
+    const int c0 = split ? j : 2 * j, c1 = split ? j + p.rot / 16 : 2 * j + 1;
+    u32x4 a = {0u, 0u, 0u, 0u}, b = a;
+    if (works) {
+        const uint16_t *src = p.qkv + row * p.qkv_stride + head * D;
+        a = load16(src + 8 * c0);
+        b = load16(src + 8 * c1);
+    }
+    const int64_t slot = is_q ? 0 : p.slot[row];
+    float x[16];
+    if (!is_v) {
         const uint16_t *weight = is_q ? p.q_weight : p.k_weight;
-        if (!is_v && weight) {
+        u32x4 wa, wb;
+        if (weight && works) {
+            wa = load16(weight + 8 * c0);
+            wb = load16(weight + 8 * c1);
+        }
+        f32x4 cs[2], sn[2];
+        if (turns) {
+            const int64_t pos = p.pos[row];
+            const bool known = pos >= 0 && pos < p.max_pos;
+            const float *at = p.rope + (known ? pos : 0) * p.rot + 8 * j;
+            cs[0] = *reinterpret_cast<const f32x4 *>(at);
+            cs[1] = *reinterpret_cast<const f32x4 *>(at + 4);
+            sn[0] = *reinterpret_cast<const f32x4 *>(at + p.rot / 2);
+            sn[1] = *reinterpret_cast<const f32x4 *>(at + p.rot / 2 + 4);
+            if (!known)  // no such angle: the row is not a number rather than wrong
+                cs[0] = cs[1] = sn[0] = sn[1] = __builtin_nanf("");
+        }
+        widen8<TYPE>(a, x);
+        widen8<TYPE>(b, x + 8);
+        if (weight) {
             float ss = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -262,78 +302,73 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
             const float inv = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
             if (works) {
                 float w[16];
-                widen8<TYPE>(load16(weight + 8 * c0), w);
-                widen8<TYPE>(load16(weight + 8 * c1), w + 8);
+                widen8<TYPE>(wa, w);
+                widen8<TYPE>(wb, w + 8);
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     x[i] = x[i] * inv * w[i];
             }
         }
         if (turns) {
-            const int64_t pos = p.pos[row];
-            float cs[8], sn[8];
-            if (pos >= 0 && pos < p.max_pos) {
-                const float *at = p.rope + pos * p.rot + 8 * j;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    cs[i] = at[i];
-                    sn[i] = at[i + p.rot / 2];
-                }
-            } else {  // no such angle: the row is not a number rather than wrong
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    cs[i] = sn[i] = __builtin_nanf("");
-            }
             if (p.adjacent) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float a = x[2 * i], b = x[2 * i + 1];
-                    x[2 * i] = a * cs[i] - b * sn[i];
-                    x[2 * i + 1] = b * cs[i] + a * sn[i];
+                    const float c = cs[i / 4][i % 4], s = sn[i / 4][i % 4];
+                    const float u = x[2 * i], v = x[2 * i + 1];
+                    x[2 * i] = u * c - v * s;
+                    x[2 * i + 1] = v * c + u * s;
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float a = x[i], b = x[i + 8];
-                    x[i] = a * cs[i] - b * sn[i];
-                    x[i + 8] = b * cs[i] + a * sn[i];
+                    const float c = cs[i / 4][i % 4], s = sn[i / 4][i % 4];
+                    const float u = x[i], v = x[i + 8];
+                    x[i] = u * c - v * s;
+                    x[i + 8] = v * c + u * s;
                 }
             }
         }
-        if (!works)
-            continue;
-        if (is_q) {
-            uint16_t *dst = p.q_out + row * p.q_out_stride + (int64_t)head * D;
-            *reinterpret_cast<u32x4 *>(dst + 8 * c0) = narrow8<TYPE>(x);
-            *reinterpret_cast<u32x4 *>(dst + 8 * c1) = narrow8<TYPE>(x + 8);
-            continue;
-        }
-        const int kvh = head - p.heads - (is_v ? kv_heads : 0);
-        if (!is_v && p.k_out) {
-            uint16_t *dst = p.k_out + row * p.k_out_stride + (int64_t)kvh * D;
-            *reinterpret_cast<u32x4 *>(dst + 8 * c0) = narrow8<TYPE>(x);
-            *reinterpret_cast<u32x4 *>(dst + 8 * c1) = narrow8<TYPE>(x + 8);
-        }
-        const int64_t slot = p.slot[row];
-        const int64_t tokens = int64_t(1) << p.cache.log2_tokens;
-        const int64_t block = slot >> p.cache.log2_tokens;
-        if (slot < 0 || block >= p.cache.n_blocks)
-            continue;
-        const int64_t t = slot & (tokens - 1);
-        uint8_t *base = p.cache.pool + block * p.cache.block_stride;
-        const float inv_scale = FP8 ? 1.0f / (is_v ? p.cache.v_scale : p.cache.k_scale) : 1.0f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int at = 8 * kElt * (h ? c1 : c0);  // byte in the row
-            uint8_t *dst =
-                is_v ? base + ((kv_heads + kvh) * tokens + t) * (D * kElt) + at
-                     : base + ((int64_t)kvh * (D * kElt / 64) + at / 64) * tokens * 64 + t * 64 +
-                           at % 64;
-            if (FP8)
-                *reinterpret_cast<u32x2 *>(dst) = codes8(x + 8 * h, inv_scale);
-            else
-                *reinterpret_cast<u32x4 *>(dst) = narrow8<TYPE>(x + 8 * h);
-        }
+        a = narrow8<TYPE>(x);
+        b = narrow8<TYPE>(x + 8);
+    } else if (FP8) {
+        widen8<TYPE>(a, x);
+        widen8<TYPE>(b, x + 8);
+    }
+    if (!works)
+        return;
+    const uint32_t kvh = head - q_heads - (is_v ? kv_heads : 0);
+    if (is_q || (!is_v && p.k_out)) {
+        uint16_t *dst = is_q ? p.q_out + row * p.q_out_stride + head * D
+                             : p.k_out + row * p.k_out_stride + kvh * D;
+        put(dst + 8 * c0, a);
+        put(dst + 8 * c1, b);
+        if (is_q)
+            return;
+    }
+    const int64_t block = slot >> p.cache.log2_tokens;
+    if (slot < 0 || block >= p.cache.n_blocks)
+        return;
+    // places inside a block fit 32 bits
+    const uint32_t tokens = 1u << p.cache.log2_tokens, t = (uint32_t)slot & (tokens - 1);
+    uint8_t *base = p.cache.pool + block * p.cache.block_stride;
+    const uint32_t at0 = 8 * kElt * c0, at1 = 8 * kElt * c1;  // bytes in the row
+    uint32_t to0, to1;
+    if (is_v) {
+        const uint32_t first = ((kv_heads + kvh) * tokens + t) * (D * kElt);
+        to0 = first + at0;
+        to1 = first + at1;
+    } else {
+        const uint32_t first = kvh * (D * kElt / 64);
+        to0 = ((first + at0 / 64) * tokens + t) * 64 + at0 % 64;
+        to1 = ((first + at1 / 64) * tokens + t) * 64 + at1 % 64;
+    }
+    if (FP8) {
+        const float inv_scale = 1.0f / (is_v ? p.cache.v_scale : p.cache.k_scale);
+        put(base + to0, codes8(x, inv_scale));
+        put(base + to1, codes8(x + 8, inv_scale));
+    } else {
+        put(base + to0, a);
+        put(base + to1, b);
     }
 }
 
@@ -342,9 +377,7 @@ hipError_t store(const KvStoreProblem &p, hipStream_t stream)
 {
     constexpr int lanes = D / 16, group = lanes <= 4 ? 4 : (lanes <= 8 ? 8 : 16);
     const int64_t items = p.rows * (p.heads + 2 * (int64_t)p.cache.kv_heads);
-    int64_t blocks = (items * group + kThreads - 1) / kThreads;
-    if (blocks > (1 << 20))
-        blocks = 1 << 20;
+    const int64_t blocks = (items * group + kThreads - 1) / kThreads;
     hipLaunchKernelGGL((kv_store_kernel<TYPE, FP8, D>), dim3((unsigned)blocks), dim3(kThreads), 0,
                        stream, p);
     return hipGetLastError();
@@ -367,9 +400,13 @@ hipError_t store_type(const KvStoreProblem &p, bool fp8, hipStream_t stream)
 
 hipError_t launch_kv_map(const KvMapProblem &p, hipStream_t stream)
 {
-    const int64_t blocks = p.rows > kMapRows ? ((int64_t)p.rows + kMapRows - 1) / kMapRows : 1;
-    hipLaunchKernelGGL(kv_map_kernel, dim3((unsigned)blocks), dim3(kThreads),
-                       2 * (p.requests + 1) * sizeof(int32_t), stream, p);
+    const int threads = p.requests <= 256 ? 256 : 1024;
+    const int64_t blocks = p.rows > 0 ? ((int64_t)p.rows + threads - 1) / threads : 1;
+    const dim3 grid((unsigned)blocks), block((unsigned)threads);
+    if (threads == 256)
+        hipLaunchKernelGGL(kv_map_kernel<256>, grid, block, 0, stream, p);
+    else
+        hipLaunchKernelGGL(kv_map_kernel<1024>, grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
