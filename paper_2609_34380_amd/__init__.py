@@ -9,7 +9,7 @@ package does not load the library; the first call into ``dps`` does, and
 fails loudly if it is not built.
 """
 
-__all__ = ["dps", "graphs", "workloads"]
+__all__ = ["decode", "dps", "graphs", "workloads"]
 
 
 def __getattr__(name):

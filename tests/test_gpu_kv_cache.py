@@ -124,6 +124,18 @@ def test_map(requests, tokens, new, pad):
     run_map(ctx, n, fresh, table, tokens, int(n.sum()) + pad)
 
 
+@pytest.mark.parametrize("requests", [256, 257, 1024, 1025, 2047, 4096])
+def test_map_many_requests(requests):
+    """One and more requests a thread, in blocks of 256 and of 1024 threads."""
+    rng = np.random.default_rng(requests)
+    ctx = rng.integers(0, 50, requests)
+    n = rng.integers(0, 3, requests)
+    n[requests // 2] = 70000          # a count of more than 16 bits
+    ids = rng.permutation(requests * 4 + 5000)
+    table = np.full((requests, 4), -1)
+    run_map(ctx, n, ids, table, 16, int(n.sum()) + 3)
+
+
 def test_map_edges():
     t16 = [[5, -1, -1, -1], [7, 8, -1, -1]]
     run_map([0, 0], [0, 0], [3], t16, 16, 4)                 # nothing to do
@@ -429,6 +441,23 @@ def test_attn_work_line(shape):
         lens = [0] * 700 + [400] + [0] * 90 + [10] + [0] * 300
     cache, table, q = build(F16, F16, 64, 1, 2, 16, lens)
     run_attn(cache, table, q, lens)
+
+
+@pytest.mark.parametrize("rows", [63, 64, 65, 200, 256, 257, 600])
+def test_attn_row_counts(rows):
+    """Rows a lane, a thread and several a thread in the search of the work line."""
+    lens = [(29 * i + rows) % 97 for i in range(rows)]
+    lens[rows // 2] = 0
+    cache, table, q = build(BF16, BF16, 64, 1, 3, 32, lens, seed=rows)
+    run_attn(cache, table, q, lens)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(16, 1, 256), (48, 1, 128), (32, 1, 64), (7, 7, 192)])
+def test_attn_long_chains(heads, kv_heads, dim):
+    """One row over most blocks of the grid: joined by slices of its heads."""
+    n = 30011
+    cache, table, q = build(F16, E4M3, dim, kv_heads, heads // kv_heads, 64, [n, 5])
+    run_attn(cache, table, q, [n, 5])
 
 
 @pytest.mark.parametrize("case", ["rising", "falling", "large", "flat", "negative_scale"])
