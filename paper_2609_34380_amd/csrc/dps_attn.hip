@@ -480,11 +480,18 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
         }
         o.clear();
 
-        // ids of the blocks of a tile's two halves of 16 tokens
-        const auto ids_of = [&](int t0, int32_t *id) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                id[h] = table[min((int32_t)(((uint32_t)t0 + 16 * h) >> p.log2_tokens), last_col)];
+        // Places in their blocks of a tile's two halves of 16 tokens, and the blocks' ids.
+        // A half without live tokens reads the other one's bytes again, from the cache,
+        // instead of its own from memory.
+        uint32_t place[2];
+        int32_t id[2];
+        const auto find = [&](int t0) {
+            const uint32_t first = (uint32_t)t0 + (t0 + 16 > lo ? 0 : 16);
+            const uint32_t second = (uint32_t)t0 + (t0 + 16 < hi ? 16 : 0);
+            place[0] = first & (tokens - 1);
+            place[1] = second & (tokens - 1);
+            id[0] = table[min((int32_t)(first >> p.log2_tokens), last_col)];
+            id[1] = table[min((int32_t)(second >> p.log2_tokens), last_col)];
         };
 
         u32x4 key[2][S::kKeyLoads];
@@ -493,47 +500,48 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
         VPiece<TYPE, FP8, (FP8 ? 4 : 2)> v2[1];
         const uint8_t *base[2];
         bool ok[2];  // a block outside the cache is never read: the first one stands in
-        int32_t id[2];
+        uint32_t at[2];
 
-        const auto load_keys = [&](int t0) {
+        const auto load_keys = [&] {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 ok[h] = id[h] >= 0 && id[h] < p.n_blocks;
                 base[h] = p.pool + (int64_t)(ok[h] ? id[h] : 0) * p.block_stride;
-                const uint32_t at = key_head + (((uint32_t)t0 + 16 * h) & (tokens - 1)) * 64;
+                at[h] = place[h];
 #pragma unroll
                 for (int s = 0; s < S::kKeyLoads; ++s)
-                    key[h][s] = stream<u32x4>(base[h] + (at + s * tokens * 64) + key_lane);
+                    key[h][s] = stream<u32x4>(
+                        base[h] + (key_head + at[h] * 64 + s * tokens * 64) + key_lane);
             }
         };
         // values d0 ... of the lane's 8 tokens, `width` of them a lane
-        const auto load_piece = [&](auto &v, int t0, int d0, int width) {
+        const auto load_piece = [&](auto &v, int d0, int width) {
             typedef typename std::remove_reference<decltype(v)>::type::Raw Raw;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int h = j >> 2;
-                const uint32_t t = (((uint32_t)t0 + 16 * h) & (tokens - 1)) + 4 * (j & 3);
+                const uint32_t t = at[h] + 4 * (j & 3);
                 v.raw[j] = stream<Raw>(base[h] + (val_head + (t * D + d0) * S::kElt) +
                                        (quarter * D + col * width) * S::kElt);
             }
         };
-        const auto load_values = [&](int t0) {
+        const auto load_values = [&] {
 #pragma unroll
             for (int i = 0; i < S::kP8; ++i)
-                load_piece(v8[i], t0, 128 * i, 8);
+                load_piece(v8[i], 128 * i, 8);
             if (S::kP4)
-                load_piece(v4[0], t0, 128 * S::kP8, 4);
+                load_piece(v4[0], 128 * S::kP8, 4);
             if (S::kP2)
-                load_piece(v2[0], t0, 128 * S::kP8 + 64 * S::kP4, 2);
+                load_piece(v2[0], 128 * S::kP8 + 64 * S::kP4, 2);
         };
         const int tile0 = (lo / kTile + skip) * kTile;
-        ids_of(tile0, id);
-        load_keys(tile0);
-        ids_of(tile0 + kTile, id);
+        find(tile0);
+        load_keys();
+        find(tile0 + kTile);
         // one tile; with more to come, its softmax runs under the next one's key loads
         const auto take = [&](int t0, auto more) {
             const bool ok0 = ok[0], ok1 = ok[1];
-            load_values(t0);
+            load_values();
 
             // ---- S^T = K Q^T -------------------------------------------------
             f32x4 s2[2];
@@ -555,8 +563,8 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
                 }
             }
             if (more) {
-                load_keys(t0 + kTile);
-                ids_of(t0 + 2 * kTile, id);
+                load_keys();
+                find(t0 + 2 * kTile);
             }
 
             // ---- softmax over this lane's 8 tokens ----------------------------
