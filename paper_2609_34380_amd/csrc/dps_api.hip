@@ -810,7 +810,8 @@ DPS_EXPORT dps_status dps_kv_map(const int32_t *ctx_len, const int32_t *new_len,
             "rows must be in 0..2^31-1");
     REQUIRE(requests == 0 || (ctx_len != nullptr && new_len != nullptr), DPS_ERR_INVALID_ARG,
             "ctx_len or new_len is NULL");
-    REQUIRE(requests * table_cols == 0 || table != nullptr, DPS_ERR_INVALID_ARG, "table is NULL");
+    REQUIRE(requests == 0 || table_cols == 0 || table != nullptr, DPS_ERR_INVALID_ARG,
+            "table is NULL");
     REQUIRE(n_fresh == 0 || fresh != nullptr, DPS_ERR_INVALID_ARG, "fresh is NULL");
     REQUIRE(step->q_start != nullptr && step->counts != nullptr &&
                 (requests == 0 || step->seq_len != nullptr),
@@ -948,7 +949,8 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
         return DPS_OK;
     REQUIRE(a->q != nullptr && a->out != nullptr && a->kv_len != nullptr, DPS_ERR_INVALID_ARG,
             "q, out or kv_len is NULL");
-    REQUIRE(a->requests * a->table_cols == 0 || a->table != nullptr, DPS_ERR_INVALID_ARG,
+    REQUIRE(a->table_cols <= 0x7fffffff, DPS_ERR_UNSUPPORTED, "table of 2^31 columns or more");
+    REQUIRE(a->requests == 0 || a->table_cols == 0 || a->table != nullptr, DPS_ERR_INVALID_ARG,
             "table is NULL");
     REQUIRE(a->req != nullptr || a->requests >= a->rows, DPS_ERR_INVALID_ARG,
             "without req every row needs a table row");

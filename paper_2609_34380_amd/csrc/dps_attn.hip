@@ -43,7 +43,7 @@ constexpr int kWaves = 4;
 constexpr int kTile = 32;               // tokens a wave takes at a time
 constexpr int kJoinThreads = 512;
 constexpr int64_t kLongest = 0x7fffff00;  // tokens of a row (a tile past it still fits 31 bits)
-constexpr float kNone = -1e30f;         // reference score before any token
+constexpr float kNone = -3e38f;         // reference score before any token
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // Weights are 2^(score - ref).  ref is set kLift below the largest score so far,
@@ -584,10 +584,13 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
                 }
                 to_ref = 1.0f;
             }
+            // the product is rounded before the difference: the largest score, which the
+            // reference came from, is then kLift above it whatever its size
             const auto weigh = [&](float ref) {
+#pragma clang fp contract(off)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    x[j] = __builtin_fmaf(s2[j >> 2][j & 3], to_ref, -ref);
+                    x[j] = s2[j >> 2][j & 3] * to_ref - ref;
                 float m = x[0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j)

@@ -502,6 +502,25 @@ def test_attn_small_weights_count():
     assert abs(float(got.float().mean()) - 19999 / (19999 + math.exp(17))) < 2e-6
 
 
+def test_attn_values_that_are_no_numbers_stay_with_their_heads():
+    """An infinity or NaN in one key/value head's live tokens, or in one query, leaves
+    every other head's result as it is; scores of BF16's whole range are taken."""
+    lens = [100, 40]
+    cache, table, q = build(BF16, BF16, 64, 2, 2, 16, lens)
+    clean, _ = run_attn(cache, table, q, lens)
+    k, v = cache.places(table[0, 2].long()[None] * 16 + 3)    # token 35 of request 0
+    cache.host[k[0, 1, :2]] = torch.tensor([0x80, 0x7F], dtype=torch.uint8)   # +inf
+    cache.host[v[0, 1, 4:6]] = torch.tensor([0xC0, 0x7F], dtype=torch.uint8)  # NaN
+    q2 = q.clone()
+    q2[1, 0, 0] = float("nan")
+    got = dps.attn_decode(q2.to(DEV), cache.up(), table.to(DEV),
+                          torch.tensor(lens, dtype=torch.int32, device=DEV))
+    assert torch.equal(got[0, :2], clean[0, :2]) and torch.equal(got[1, 1:], clean[1, 1:])
+    assert bool(got[0, 2:, 2].isnan().all()) and bool(got[1, 0].isnan().all())
+    cache, table, q = build(BF16, BF16, 64, 1, 2, 16, [50], qmul=1e17, kmul=1e15)
+    run_attn(cache, table, q, [50])
+
+
 def test_attn_strides_offset_and_streams():
     lens = [70, 1, 260]
     cache, table, q = build(F16, F16, 128, 2, 4, 16, lens, offset=1 << 12, gap=4096)

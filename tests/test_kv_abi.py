@@ -102,6 +102,7 @@ def test_store_refuses(lib, kw, status):
     (dict(table=0x20002), ALIGNMENT), (dict(req=0x30001), ALIGNMENT),
     (dict(rows=1 << 24, requests=1 << 24), UNSUPPORTED),
     (dict(rows=4000, requests=4000, table_cols=1 << 27), UNSUPPORTED),
+    (dict(rows=1, table_cols=1 << 31), UNSUPPORTED), (dict(rows=1, table_cols=1 << 62), UNSUPPORTED),
 ])
 def test_attn_refuses(lib, kw, status):
     got = lib.dps_attn_decode(ctypes.byref(attn(**kw)), ctypes.byref(cache()), 0x100, 1 << 40, None)
