@@ -54,7 +54,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLift = 6.0f, kRoom = 14.0f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 template <int TYPE>
 __device__ __forceinline__ f32x4 mfma32(u32x4 a, u32x4 b, f32x4 c)
@@ -93,15 +92,6 @@ __device__ __forceinline__ void split2(float p0, float p1, uint32_t &hi, uint32_
         lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p0 - (float)h[0],
                                                                      p1 - (float)h[1]));
     }
-}
-
-// Two fp32 values rounded to 16 bits, nearest even.
-template <int TYPE>
-__device__ __forceinline__ uint32_t narrow2(float a, float b)
-{
-    if (TYPE == KV_BF16)
-        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    return __builtin_bit_cast(uint32_t, half2v{(_Float16)a, (_Float16)b});
 }
 
 // Over the four 16-lane quarters that share a head: each swap leaves a lane and

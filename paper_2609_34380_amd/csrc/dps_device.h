@@ -227,6 +227,20 @@ __device__ __forceinline__ f32x4 mfma16x16x128_fp8(i32x8 a, i32x8 b, f32x4 c)
                                                              0, 0, 0, 0);
 }
 
+// Element types of the paged KV cache and the activations beside it.
+enum { KV_F16 = 0, KV_BF16 = 1, KV_E4M3 = 2 };
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two fp32 values rounded to 16 bits, nearest even.
+template <int TYPE>
+__device__ __forceinline__ uint32_t narrow2(float a, float b)
+{
+    if (TYPE == KV_BF16)
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    return __builtin_bit_cast(uint32_t, half2v{(_Float16)a, (_Float16)b});
+}
+
 // Inclusive sum over the wave's lanes: within rows of 16 by shifts, then the last
 // lane of each row (or pair of rows) into the following ones.
 __device__ __forceinline__ int32_t wave_scan(int32_t x)

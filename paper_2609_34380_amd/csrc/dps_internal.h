@@ -117,8 +117,6 @@ hipError_t launch_gemm_fp8(int enc, const uint8_t *xq, const float *scale, const
                            uint16_t *y, const LinearPlan &plan, float *partial, hipStream_t stream);
 
 // ---- paged KV cache -------------------------------------------------------------
-enum { KV_F16 = 0, KV_BF16 = 1, KV_E4M3 = 2 };
-
 // Blocks of 2^log2_tokens tokens: K [kv_heads][row bytes / 64][tokens][64 B],
 // then V [kv_heads][tokens][head_dim].
 struct KvCacheView {

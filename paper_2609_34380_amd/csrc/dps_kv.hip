@@ -190,13 +190,6 @@ __device__ __forceinline__ float wide(uint16_t v)
 }
 
 template <int TYPE>
-__device__ __forceinline__ uint16_t narrow(float v)
-{
-    return TYPE == KV_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v)
-                           : __builtin_bit_cast(uint16_t, (_Float16)v);
-}
-
-template <int TYPE>
 __device__ __forceinline__ void widen8(u32x4 raw, float *x)
 {
 #pragma unroll
@@ -212,7 +205,7 @@ __device__ __forceinline__ u32x4 narrow8(const float *x)
     u32x4 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        r[i] = (uint32_t)narrow<TYPE>(x[2 * i]) | (uint32_t)narrow<TYPE>(x[2 * i + 1]) << 16;
+        r[i] = narrow2<TYPE>(x[2 * i], x[2 * i + 1]);
     return r;
 }
 
@@ -223,7 +216,7 @@ __device__ __forceinline__ u32x2 codes8(const float *x, float inv_scale)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float v = x[i] * inv_scale;
-        y[i] = v > 448.0f ? 448.0f : (v < -448.0f ? -448.0f : v);
+        y[i] = v != v ? v : __builtin_amdgcn_fmed3f(v, -448.0f, 448.0f);
     }
     u32x2 r;
 #pragma unroll
@@ -236,6 +229,28 @@ __device__ __forceinline__ u32x2 codes8(const float *x, float inv_scale)
     return r;
 }
 
+template <int CONTROL>
+__device__ __forceinline__ float moved(float x)
+{
+    return __builtin_bit_cast(
+        float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, false));
+}
+
+// Sum over each group of 4, 8 or 16 lanes, in every lane of it.  Quads swap
+// lanes; then a half row, then a row of 16 is mirrored, which meets the other
+// quad's, the other half's sum.
+template <int GROUP>
+__device__ __forceinline__ float group_sum(float x)
+{
+    x += moved<0xB1>(x);  // quad_perm 1 0 3 2
+    x += moved<0x4E>(x);  // quad_perm 2 3 0 1
+    if (GROUP >= 8)
+        x += moved<0x141>(x);  // row_half_mirror
+    if (GROUP >= 16)
+        x += moved<0x140>(x);  // row_mirror
+    return x;
+}
+
 // Stored past the caches' retention.
 template <typename V>
 __device__ __forceinline__ void put(void *p, V v)
@@ -243,7 +258,7 @@ __device__ __forceinline__ void put(void *p, V v)
     __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
 }
 
-template <int TYPE, bool FP8, int D>
+template <int TYPE, bool FP8, int D, bool ADJACENT>
 __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem p)
 {
     constexpr int kLanes = D / 16;  // lanes with work in a group
@@ -260,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
     const bool works = j < kLanes;
     const bool turns = !is_v && 16 * j < p.rot;
     // the lane's two chunks of eight values
-    const bool split = turns && !p.adjacent;
+    const bool split = turns && !ADJACENT;
     const int c0 = split ? j : 2 * j, c1 = split ? j + p.rot / 16 : 2 * j + 1;
     u32x4 a = {0u, 0u, 0u, 0u}, b = a;
     if (works) {
@@ -269,6 +284,7 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
         b = load16(src + 8 * c1);
     }
     const int64_t slot = is_q ? 0 : p.slot[row];
+    const int64_t pos = turns ? p.pos[row] : 0;
     float x[16];
     if (!is_v) {
         const uint16_t *weight = is_q ? p.q_weight : p.k_weight;
@@ -279,7 +295,6 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
         }
         f32x4 cs[2], sn[2];
         if (turns) {
-            const int64_t pos = p.pos[row];
             const bool known = pos >= 0 && pos < p.max_pos;
             const float *at = p.rope + (known ? pos : 0) * p.rot + 8 * j;
             cs[0] = *reinterpret_cast<const f32x4 *>(at);
@@ -296,10 +311,7 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 ss += x[i] * x[i];
-#pragma unroll
-            for (int d = 1; d < kGroup; d <<= 1)
-                ss += __shfl_xor(ss, d, kGroup);
-            const float inv = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
+            const float inv = __builtin_amdgcn_rsqf(group_sum<kGroup>(ss) * (1.0f / D) + p.eps);
             if (works) {
                 float w[16];
                 widen8<TYPE>(wa, w);
@@ -310,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(const KvStoreProblem
             }
         }
         if (turns) {
-            if (p.adjacent) {
+            if (ADJACENT) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float c = cs[i / 4][i % 4], s = sn[i / 4][i % 4];
@@ -378,8 +390,12 @@ hipError_t store(const KvStoreProblem &p, hipStream_t stream)
     constexpr int lanes = D / 16, group = lanes <= 4 ? 4 : (lanes <= 8 ? 8 : 16);
     const int64_t items = p.rows * (p.heads + 2 * (int64_t)p.cache.kv_heads);
     const int64_t blocks = (items * group + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL((kv_store_kernel<TYPE, FP8, D>), dim3((unsigned)blocks), dim3(kThreads), 0,
-                       stream, p);
+    if (p.adjacent)
+        hipLaunchKernelGGL((kv_store_kernel<TYPE, FP8, D, true>), dim3((unsigned)blocks),
+                           dim3(kThreads), 0, stream, p);
+    else
+        hipLaunchKernelGGL((kv_store_kernel<TYPE, FP8, D, false>), dim3((unsigned)blocks),
+                           dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
