@@ -776,7 +776,7 @@ AttnPlan plan_attn(int64_t heads, int64_t kv_heads, int64_t dim, bool fp8)
 {
     AttnPlan a;
     const int64_t group = heads / kv_heads;
-    a.groups = (int)cdiv(group, 16);
+    a.groups = (int)cdiv(group, dps::attn_heads_a_pass(fp8, (int)dim));
     a.step = (int)cdiv(group, a.groups);
     a.groups = (int)cdiv(group, a.step);
     const int64_t lines = kv_heads * a.groups;

@@ -10,7 +10,8 @@
 // is built to keep loads in flight and never to move a byte twice:
 //   - A wave takes 32 tokens of one key/value head at a time.  S^T = K Q^T and
 //     O^T = V^T P^T run on 16 x 16 x 32 matrix instructions, up to 16 query
-//     heads as the columns.  The lane that holds S^T of (token, head) is the
+//     heads as the columns, or 17 to 32 in two column tiles (HT) that share
+//     every load and permute.  The lane that holds S^T of (token, head) is the
 //     lane whose P^T operand needs it, so P never crosses lanes; V is turned
 //     in registers (one byte permute per two values); the main loop has no LDS
 //     and no barrier.
@@ -28,8 +29,18 @@
 //
 // Precision: products and softmax in fp32.  The weights P enter the matrix
 // cores as two 16-bit terms (value and remainder), which keeps them to about
-// 2^-16 or better; one 16-bit term would add an error as large as the
-// rounding of the output.
+// 2^-16 or better; one term would add an error of the size of the output's own
+// rounding (relative error 2.1e-4 -> 2.9e-4 in FP16 over an E4M3 cache, 1.7e-3 ->
+// 2.1e-3 in BF16) and save 0-1% of the time.
+//
+// Measured on MI355X, both launches replayed from a graph, 32 query and 8
+// key/value heads of 128: one row of 131000 tokens beside 16 short ones (598 MB)
+// 98.5 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 48.0; 256 BF16 rows of
+// up to 600, 64 query heads (305 MB) 57.4; 16 rows of 30000 in E4M3 (930 MB) 143,
+// 6.5 TB/s, where a nontemporal read of memory reaches 6.6-6.9.  Every byte is
+// fetched once (FETCH_SIZE).  With loads that caches retain the first three take
+// 112, 52 and 65 us (kernel alone) against 99, 46 and 57.  The second launch and
+// its join cost about 4 us, a block's start and end about 5.
 #include <type_traits>
 
 #include "dps_internal.h"
@@ -196,7 +207,7 @@ __device__ __forceinline__ void attn_store(const AttnProblem &p, int64_t row, in
             sum == 0.0f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <int TYPE, bool FP8, int D>
+template <int TYPE, bool FP8, int D, int HT>
 struct Shape {
     static constexpr int kElt = FP8 ? 1 : 2;
     static constexpr int kSteps = D / 32;              // matrix steps over head_dim
@@ -208,7 +219,7 @@ struct Shape {
     static constexpr int kP2 = (D % 64) / 32;
     // Waves a SIMD is compiled for: 256 registers a lane, all 512 where two tiles'
     // keys and a tile's values beside the output need them.
-    static constexpr int kWavesPerSimd = D * kElt >= 512 ? 1 : 2;
+    static constexpr int kWavesPerSimd = D * kElt >= (HT == 1 ? 512 : 192) ? 1 : 2;
 };
 
 // A wave's output of one row: acc (value d of a head in the lane and register
@@ -263,14 +274,14 @@ struct VPiece {
     }
 };
 
-template <int TYPE, bool FP8, int D>
-__global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) void attn_kernel(
+template <int TYPE, bool FP8, int D, int HT>
+__global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd)) void attn_kernel(
     const AttnProblem p, const int32_t *__restrict__ tables, const int32_t *__restrict__ reqs,
     const int32_t *__restrict__ kv_len)
 {
-    typedef Shape<TYPE, FP8, D> S;
-    __shared__ f32x4 s_head[kWaves][S::kAcc * 64];  // rows that began before the wave
-    __shared__ float s_stat[kWaves][128];
+    typedef Shape<TYPE, FP8, D, HT> S;
+    __shared__ f32x4 s_head[kWaves][HT][S::kAcc * 64];  // rows that began before the wave
+    __shared__ float s_stat[kWaves][HT][128];
     __shared__ int32_t s_first[kThreads];
     __shared__ int32_t s_sums[kWaves];
     __shared__ int32_t s_state[kWaves];
@@ -279,9 +290,9 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15;   // query head of the pass (matrix column)
+    const int col = lane & 15;   // query head of a column tile (matrix column)
     const int quarter = lane >> 4;
-    const int hv = blockIdx.y;   // (key/value head, group of at most 16 query heads)
+    const int hv = blockIdx.y;   // (key/value head, pass over its query heads)
     const int kvh = hv / p.head_groups;
     const int sub = hv % p.head_groups;
     const int first_head = kvh * p.group + sub * p.group_step;
@@ -392,13 +403,15 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
             put(std::integral_constant<int, 2>(), 128 * S::kP8 + 64 * S::kP4,
                 8 * S::kP8 + 4 * S::kP4);
     };
-    Partial<S::kAcc> o;
-    const auto finish = [&](const Partial<S::kAcc> &f, int r) {
-        if (col >= n_heads)
+    Partial<S::kAcc> o[HT];
+    const auto finish = [&](int c, int r) {
+        const Partial<S::kAcc> &f = o[c];
+        const int head = 16 * c + col;
+        if (head >= n_heads)
             return;
         const float scale = f.sum == 0.0f ? 0.0f : p.value_scale / f.sum;
         uint16_t *at = static_cast<uint16_t *>(p.out) + r * p.out_stride +
-                       (int64_t)(first_head + col) * D;
+                       (int64_t)(first_head + head) * D;
         each_piece([&](auto width, int d0, int tile) {
             constexpr int W = width;
 #pragma unroll
@@ -415,15 +428,17 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
             }
         });
         if (quarter == 0 && p.lse)
-            p.lse[(int64_t)r * (p.kv_heads * p.group) + first_head + col] =
+            p.lse[(int64_t)r * (p.kv_heads * p.group) + first_head + head] =
                 f.sum == 0.0f ? -__builtin_inff() : (f.ref + __builtin_amdgcn_logf(f.sum)) * kLn2;
     };
     // a partial row for the join: slot 0 of the block began before it, slot 1 in it
-    const auto hand_on = [&](const Partial<S::kAcc> &f, int which) {
-        if (col >= n_heads)
+    const auto hand_on = [&](int c, int which) {
+        const Partial<S::kAcc> &f = o[c];
+        const int head = 16 * c + col;
+        if (head >= n_heads)
             return;
         const int64_t slot =
-            ((int64_t)(blockIdx.x * 2 + which) * gridDim.y + hv) * p.group_step + col;
+            ((int64_t)(blockIdx.x * 2 + which) * gridDim.y + hv) * p.group_step + head;
         float *at = p.part_out + slot * D;
         each_piece([&](auto width, int d0, int tile) {
             constexpr int W = width;
@@ -454,21 +469,23 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
         const int32_t *__restrict__ table = tables + (int64_t)req * p.table_cols;
 
         // ---- query fragments ------------------------------------------------
-        u32x4 q[S::kSteps];
-        {
+        u32x4 q[HT][S::kSteps];
+#pragma unroll
+        for (int c = 0; c < HT; ++c) {
+            const int head = 16 * c + col;
             const uint8_t *qp = static_cast<const uint8_t *>(p.q) +
-                                ((int64_t)row * p.q_stride + (int64_t)(first_head + col) * D) * 2;
+                                ((int64_t)row * p.q_stride + (int64_t)(first_head + head) * D) * 2;
 #pragma unroll
             for (int s = 0; s < S::kSteps; ++s) {
                 // 8-bit keys hold 16 values a lane: two steps' operands side by side
                 const int d = FP8 ? 64 * (s >> 1) + 16 * quarter + 8 * (s & 1)
                                   : 32 * s + 8 * quarter;
-                q[s] = u32x4{0u, 0u, 0u, 0u};
-                if (col < n_heads)
-                    q[s] = load16(qp + d * 2);
+                q[c][s] = u32x4{0u, 0u, 0u, 0u};
+                if (head < n_heads)
+                    q[c][s] = load16(qp + d * 2);
             }
+            o[c].clear();
         }
-        o.clear();
 
         // Places in their blocks of a tile's two halves of 16 tokens, and the blocks' ids.
         // A half without live tokens reads the other one's bytes again, from the cache,
@@ -534,10 +551,12 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
             load_values();
 
             // ---- S^T = K Q^T -------------------------------------------------
-            f32x4 s2[2];
+            f32x4 scores[HT][2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                s2[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < HT; ++c)
+                    scores[c][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int s = 0; s < S::kSteps; ++s) {
                     u32x4 a;
@@ -549,7 +568,9 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
                     } else {
                         a = key[h][s];
                     }
-                    s2[h] = mfma32<TYPE>(a, q[s], s2[h]);
+#pragma unroll
+                    for (int c = 0; c < HT; ++c)
+                        scores[c][h] = mfma32<TYPE>(a, q[c][s], scores[c][h]);
                 }
             }
             if (more) {
@@ -559,7 +580,6 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
 
             // ---- softmax over this lane's 8 tokens ----------------------------
             float to_ref = to_log2;
-            float x[8];        // score - ref, in powers of two
             uint32_t keep[8];  // of V: what lies in a dead token's place may be no number
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -569,46 +589,54 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
                 for (int j = 0; j < 8; ++j) {
                     const int t = t0 + 16 * (j >> 2) + 4 * (j & 3) + quarter;
                     const bool live = t >= lo && t < hi && (j < 4 ? ok0 : ok1);
-                    s2[j >> 2][j & 3] = live ? s2[j >> 2][j & 3] * to_log2 : -__builtin_inff();
+#pragma unroll
+                    for (int c = 0; c < HT; ++c) {
+                        float &x = reinterpret_cast<float *>(&scores[c][j >> 2])[j & 3];
+                        x = live ? x * to_log2 : -__builtin_inff();
+                    }
                     keep[j] = live ? ~0u : 0u;
                 }
                 to_ref = 1.0f;
             }
-            // the product is rounded before the difference: the largest score, which the
-            // reference came from, is then kLift above it whatever its size
-            const auto weigh = [&](float ref) {
+            u32x4 p_hi[HT], p_lo[HT];
+#pragma unroll
+            for (int c = 0; c < HT; ++c) {
+                float x[8];  // score - ref, in powers of two
+                // the product is rounded before the difference: the largest score, which
+                // the reference came from, is then kLift above it whatever its size
+                const auto weigh = [&](float ref) {
 #pragma clang fp contract(off)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] = s2[j >> 2][j & 3] * to_ref - ref;
-                float m = x[0];
+                    for (int j = 0; j < 8; ++j)
+                        x[j] = scores[c][j >> 2][j & 3] * to_ref - ref;
+                    float m = x[0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j)
-                    m = fmaxf(m, x[j]);
-                return m;
-            };
-            if (__any(weigh(o.ref) > kRoom)) {
-                const float ref = fmaxf(quarters_max(weigh(0.0f)) - kLift, o.ref);
-                const float shrink = __builtin_amdgcn_exp2f(o.ref - ref);
-                o.ref = ref;
-                o.sum *= shrink;
+                    for (int j = 1; j < 8; ++j)
+                        m = fmaxf(m, x[j]);
+                    return m;
+                };
+                if (__any(weigh(o[c].ref) > kRoom)) {
+                    const float ref = fmaxf(quarters_max(weigh(0.0f)) - kLift, o[c].ref);
+                    const float shrink = __builtin_amdgcn_exp2f(o[c].ref - ref);
+                    o[c].ref = ref;
+                    o[c].sum *= shrink;
 #pragma unroll
-                for (int i = 0; i < S::kAcc; ++i)
-                    o.acc[i] *= shrink;
-                weigh(ref);
-            }
-            u32x4 p_hi, p_lo;
+                    for (int i = 0; i < S::kAcc; ++i)
+                        o[c].acc[i] *= shrink;
+                    weigh(ref);
+                }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = __builtin_amdgcn_exp2f(x[j]);
-                o.sum += x[j];
-            }
+                for (int j = 0; j < 8; ++j) {
+                    x[j] = __builtin_amdgcn_exp2f(x[j]);
+                    o[c].sum += x[j];
+                }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t hi2, lo2;
-                split2<TYPE>(x[2 * j], x[2 * j + 1], hi2, lo2);
-                p_hi[j] = hi2;
-                p_lo[j] = lo2;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t hi2, lo2;
+                    split2<TYPE>(x[2 * j], x[2 * j + 1], hi2, lo2);
+                    p_hi[c][j] = hi2;
+                    p_lo[c][j] = lo2;
+                }
             }
 
             // ---- O^T += V^T P^T -----------------------------------------------
@@ -627,10 +655,14 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
                         even[j] = e;
                         odd[j] = d;
                     }
-                    o.acc[tile] = mfma32<TYPE>(even, p_hi, o.acc[tile]);
-                    o.acc[tile] = mfma32<TYPE>(even, p_lo, o.acc[tile]);
-                    o.acc[tile + 1] = mfma32<TYPE>(odd, p_hi, o.acc[tile + 1]);
-                    o.acc[tile + 1] = mfma32<TYPE>(odd, p_lo, o.acc[tile + 1]);
+#pragma unroll
+                    for (int c = 0; c < HT; ++c) {
+                        f32x4 &x = o[c].acc[tile], &y = o[c].acc[tile + 1];
+                        x = mfma32<TYPE>(even, p_hi[c], x);
+                        x = mfma32<TYPE>(even, p_lo[c], x);
+                        y = mfma32<TYPE>(odd, p_hi[c], y);
+                        y = mfma32<TYPE>(odd, p_lo[c], y);
+                    }
                     tile += 2;
                 }
             };
@@ -645,20 +677,21 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
         for (int u = 0; u < n_tiles - 1; ++u)
             take(tile0 + u * kTile, std::true_type());
         take(tile0 + (n_tiles - 1) * kTile, std::false_type());
-        o.sum = quarters_sum(o.sum);
         left -= n_tiles;
         const bool ends = skip + n_tiles == row_n;
-        if (skip > 0) {
-            state |= kHead | (ends ? kEnds : 0);
+        state |= skip > 0 ? kHead | (ends ? kEnds : 0) : ends ? 0 : kOpen;
 #pragma unroll
-            for (int i = 0; i < S::kAcc; ++i)
-                s_head[wave][i * 64 + lane] = o.acc[i];
-            s_stat[wave][lane] = o.ref;
-            s_stat[wave][64 + lane] = o.sum;
-        } else if (ends) {
-            finish(o, row);
-        } else {
-            state |= kOpen;
+        for (int c = 0; c < HT; ++c) {
+            o[c].sum = quarters_sum(o[c].sum);
+            if (skip > 0) {
+#pragma unroll
+                for (int i = 0; i < S::kAcc; ++i)
+                    s_head[wave][c][i * 64 + lane] = o[c].acc[i];
+                s_stat[wave][c][lane] = o[c].ref;
+                s_stat[wave][c][64 + lane] = o[c].sum;
+            } else if (ends) {
+                finish(c, row);
+            }
         }
         }
         if (left == 0 || row + 1 >= rows)
@@ -682,26 +715,37 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D>::kWavesPerSimd)) voi
     if (state & kOpen) {
         bool ends = false;
         for (int i = wave + 1; i < kWaves && !ends; ++i) {
-            o.join(s_head[i], s_stat[i], lane);
+#pragma unroll
+            for (int c = 0; c < HT; ++c)
+                o[c].join(s_head[i][c], s_stat[i][c], lane);
             ends = state_of(i) & kEnds;
         }
-        if (ends)
-            finish(o, row);
-        else
-            hand_on(o, 1);
+#pragma unroll
+        for (int c = 0; c < HT; ++c) {
+            if (ends)
+                finish(c, row);
+            else
+                hand_on(c, 1);
+        }
         if (!ends && hv == 0) {
             s_join[3] = row;
             s_join[4] = (int)line.of(row_first + row_n - 1) / kWaves - (int)blockIdx.x + 1;
         }
     }
     if (wave == 0 && (state & kHead)) {  // a row that began in an earlier block
-        o.clear();
         bool ends = false;
+#pragma unroll
+        for (int c = 0; c < HT; ++c)
+            o[c].clear();
         for (int i = 0; i < kWaves && !ends && (state_of(i) & kHead); ++i) {
-            o.join(s_head[i], s_stat[i], lane);
+#pragma unroll
+            for (int c = 0; c < HT; ++c)
+                o[c].join(s_head[i][c], s_stat[i][c], lane);
             ends = state_of(i) & kEnds;
         }
-        hand_on(o, 0);
+#pragma unroll
+        for (int c = 0; c < HT; ++c)
+            hand_on(c, 0);
         if (hv == 0) {
             const int first_block = (int)line.of(head_first) / kWaves;
             s_join[0] = head_row;
@@ -754,17 +798,14 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
     for (int began = 0; began < 2; ++began) {
         const int row = join[began ? 3 : 0], count = join[began ? 4 : 2];
         const int w0 = began ? w : join[1];
-        // the w - w0-th of the row's blocks takes that slice of the items: at most
-        // one a thread (16 heads of 256 are two slices, and count is at least 2)
-        const int slices =
-            min(count, max((count * items + 4 * kJoinThreads - 1) / (4 * kJoinThreads),
-                           (items + kJoinThreads - 1) / kJoinThreads));
+        // the w - w0-th of the row's blocks takes that slice of the items
+        const int slices = min(count, (count * items + 4 * kJoinThreads - 1) / (4 * kJoinThreads));
         if (w - w0 >= slices)
             continue;
         const int each = (items + slices - 1) / slices;
-        const int i0 = (w - w0) * each, n = min(each, items - i0);
-        if (n <= 0)
-            continue;
+        const int end = min((w - w0 + 1) * each, items);
+        for (int i0 = (w - w0) * each; i0 < end; i0 += kJoinThreads) {
+        const int n = min(end - i0, kJoinThreads);
         int groups = 1;  // threads an item
         while (2 * groups * n <= kJoinThreads && groups < count)
             groups *= 2;
@@ -803,6 +844,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
         }
         if (g == 0)
             attn_store<TYPE>(p, row, first_head + head, dim, d, o, ref, sum);
+        }
     }
 }
 
@@ -810,8 +852,14 @@ template <int TYPE, bool FP8, int D>
 hipError_t launch(const AttnProblem &p, int blocks, hipStream_t stream)
 {
     const int heads = p.kv_heads * p.head_groups;
-    hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D>), dim3((unsigned)blocks, (unsigned)heads),
-                       dim3(kThreads), 0, stream, p, p.table, p.req, p.kv_len);
+    const dim3 grid((unsigned)blocks, (unsigned)heads);
+    constexpr int most = attn_heads_a_pass(FP8, D) / 16;
+    if (p.group_step > 16)
+        hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D, most>), grid, dim3(kThreads), 0, stream, p,
+                           p.table, p.req, p.kv_len);
+    else
+        hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D, 1>), grid, dim3(kThreads), 0, stream, p,
+                           p.table, p.req, p.kv_len);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;

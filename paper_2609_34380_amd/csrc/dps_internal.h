@@ -175,7 +175,7 @@ struct AttnProblem {
     int64_t n_blocks;
     int32_t log2_tokens, kv_heads;
     int32_t group;          // query heads per key/value head
-    int32_t head_groups;    // passes of group_step <= 16 query heads over it
+    int32_t head_groups;    // passes of group_step <= 32 query heads over it
     int32_t group_step;
     const int32_t *table;
     int64_t table_cols, requests;
@@ -190,8 +190,16 @@ struct AttnProblem {
 };
 // Blocks of four waves a CU gets: one keeps enough bytes in flight (16 KiB a wave
 // at 128 16-bit values) and leaves the fewest partial rows; rows of 64 bytes take
-// two.
+// two.  MI355X, one / two blocks: 256 BF16 rows of up to 600 tokens, heads of 128
+// 58.7 / 62 us, 16 rows of 30000 in E4M3 143.7 / 146.7, 3 BF16 rows of 34002,
+// heads of 64 24.8 / 26.5; 16 rows of 11911 in E4M3, heads of 64 46.4 / 38.2.
 constexpr int attn_blocks_per_cu(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim <= 64 ? 2 : 1; }
+// Query heads of a key/value head that share one pass over its tokens: two column
+// tiles of 16.  MI355X, 24 query heads a key/value head, against two passes: 13
+// rows of 13830 tokens, 8 heads of 64 in FP16 62.9 / 82.0 us, 21 rows of 20609 in
+// E4M3 82.0 / 108.8.  16-bit rows of 192 and 256 leave no registers for the
+// second tile (21 rows of 267 tokens, 16 heads of 192 32.7 / 28.1).
+constexpr int attn_heads_a_pass(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim >= 384 ? 16 : 32; }
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream);
 

@@ -393,6 +393,16 @@ def test_attn_lengths(dtype, cdtype, dim, kv_heads, group, tokens):
     run_attn(cache, table, q, LENS)
 
 
+@pytest.mark.parametrize("group", [16, 17, 23, 32, 33, 64, 71])
+def test_attn_head_groups(group):
+    """One and two column tiles, and several passes over a key/value head."""
+    for dtype, cdtype, dim in ((F16, F16, 64), (BF16, E4M3, 128), (F16, F16, 256), (F16, F16, 192),
+                               (BF16, BF16, 96), (F16, E4M3, 256)):
+        lens = [300, 1, 0, 17, 700]
+        cache, table, q = build(dtype, cdtype, dim, 2, group, 32, lens, seed=group)
+        run_attn(cache, table, q, lens, window=500)
+
+
 @pytest.mark.parametrize("n", [1, 2, 64, 1000, 5000])
 def test_attn_one_row(n):
     for cdtype in (F16, E4M3):
@@ -452,7 +462,7 @@ def test_attn_row_counts(rows):
     run_attn(cache, table, q, lens)
 
 
-@pytest.mark.parametrize("heads,kv_heads,dim", [(16, 1, 256), (48, 1, 128), (32, 1, 64), (7, 7, 192)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(16, 1, 256), (32, 1, 256), (48, 1, 128), (32, 1, 64), (31, 1, 128), (7, 7, 192)])
 def test_attn_long_chains(heads, kv_heads, dim):
     """One row over most blocks of the grid: joined by slices of its heads."""
     n = 30011
