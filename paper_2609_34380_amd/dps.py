@@ -215,8 +215,9 @@ def _check(status):
 
 def _stream():
     """The raw handle of torch's current stream on the current device (an int;
-    building torch's Stream object costs a microsecond a call)."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    building torch's Stream object costs a microsecond a call).  Callers hold
+    device tensors, so the runtime is initialised."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ptr(t):
@@ -600,19 +601,14 @@ def _row_stride(name, t, rows, heads, dim, dtype):
     """The row stride in elements of a [rows][heads * dim] or [rows][heads][dim]
     device tensor whose rows are contiguous."""
     width = heads * dim
-    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == rows * width and \
-            (rows == 0 or t.shape[0] == rows):
+    if t.is_contiguous() and t.shape in ((rows, heads, dim), (rows, width)) and \
+            t.dtype is dtype and t.is_cuda:
         return width
-    inner = t.stride(-1) == 1 or t.shape[-1] <= 1
-    got = -1
-    if t.dim() == 3:
-        inner = inner and (t.shape[1] <= 1 or t.stride(1) == t.shape[2])
-        got = t.shape[1] * t.shape[2]
-    elif t.dim() == 2:
-        got = t.shape[1]
-    if not (t.is_cuda and t.dtype == dtype and inner and got == width and t.shape[0] == rows):
-        raise ValueError("%s must be %d device rows of %d contiguous %s" % (name, rows, width,
-                                                                            dtype))
+    inner = t.stride(-1) == 1 and (t.dim() == 2 or heads <= 1 or t.stride(1) == dim)
+    if not (t.shape in ((rows, heads, dim), (rows, width)) and inner and t.dtype == dtype and
+            t.is_cuda):
+        raise ValueError("%s must be %d device rows of %d x %d contiguous %s" %
+                         (name, rows, heads, dim, dtype))
     return t.stride(0) if rows > 1 else width
 
 

@@ -595,3 +595,39 @@ def test_empty_calls():
     got = dps.attn_decode(q.to(DEV), c, torch.empty(1, 0, dtype=torch.int32, device=DEV),
                           torch.tensor([5], dtype=torch.int32, device=DEV))
     assert bool((got == 0).all())
+
+
+def test_binding_refuses_other_shapes_and_types():
+    cache, table, q = build(F16, F16, 128, 1, 2, 16, [5, 9])
+    c, q, table = cache.up(), q.to(DEV), table.to(DEV)
+    n = torch.tensor([5, 9], dtype=torch.int32, device=DEV)
+    bad = [dict(kv_len=n.long()), dict(kv_len=n[:1]), dict(kv_len=n.cpu()), dict(table=table.long()),
+           dict(table=table.t()), dict(req=n[:1]), dict(out=q[:1]), dict(out=q.bfloat16()),
+           dict(out=q.transpose(0, 1)), dict(lse=torch.zeros(2, 3, device=DEV)),
+           dict(lse=torch.zeros(2, 2, device=DEV, dtype=F16)), dict(window=-1),
+           dict(q=q[..., :64]), dict(q=q.float()), dict(q=q.reshape(2, -1)),
+           dict(workspace=torch.zeros(1 << 24, dtype=torch.uint8))]
+    for kw in bad:
+        args = dict(dict(q=q, cache=c, table=table, kv_len=n), **kw)
+        with pytest.raises(ValueError):
+            dps.attn_decode(**args)
+    with pytest.raises(dps.DpsError):
+        dps.attn_decode(q, c, table, n, workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))
+    x = torch.zeros(3, 4 * 128, dtype=F16, device=DEV)
+    slot = torch.full((3,), -1, device=DEV)
+    rope = torch.zeros(8, 128, device=DEV)
+    w = torch.ones(128, dtype=F16, device=DEV)
+    for kw in [dict(heads=3), dict(slot=slot.int()), dict(slot=slot[:2]), dict(rope=rope),
+               dict(rope=rope, pos=slot), dict(rope=rope.half(), pos=slot.int()), dict(q_weight=w),
+               dict(q_weight=w, k_weight=w.bfloat16()), dict(q_weight=w[:64], k_weight=w),
+               dict(q_out=x), dict(k_out=x), dict(qkv=x.float())]:
+        args = dict(dict(qkv=x, cache=c, slot=slot, heads=2), **kw)
+        with pytest.raises(ValueError):
+            dps.kv_store(**args)
+    m = dps.make_kv_map(2, 4, DEV)
+    for kw in [dict(ctx_len=n.long()), dict(new_len=n[:1]), dict(table=table[:1]), dict(block_tokens=0),
+               dict(fresh=n.reshape(1, 2)), dict(out=dps.make_kv_map(3, 4, DEV)), dict(out=None),
+               dict(out=dps.KvMap(*m[:5], m.req[:2], m.kv_len))]:
+        args = dict(dict(ctx_len=n, new_len=n, fresh=n, table=table, block_tokens=16, out=m), **kw)
+        with pytest.raises(ValueError):
+            dps.kv_map(**args)
