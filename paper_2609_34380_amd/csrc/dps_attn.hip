@@ -474,9 +474,21 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     int state = 0;
     int row_n = row_tiles(RowSpan{lo, hi, req}), row_first = begin - skip;  // on the line
     const int head_row = row, head_n = row_n, head_first = row_first;
-    while (left > 0) {
+    const auto next_row = [&] {
+        if (++row >= rows)
+            return;
+        skip = 0;
+        row_first += row_n;
+        const RowSpan next = row_span(p, reqs, kv_len, row);
+        lo = next.lo;
+        hi = next.hi;
+        req = next.req;
+        row_n = row_tiles(next);
+    };
+    for (; left > 0 && row < rows; next_row()) {
         const int n_tiles = min(row_n - skip, left);
-        if (n_tiles > 0) {
+        if (n_tiles == 0)
+            continue;
         const int32_t *__restrict__ table = tables + (int64_t)req * p.table_cols;
 
         // ---- query fragments ------------------------------------------------
@@ -602,8 +614,8 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                     const bool live = t >= lo && t < hi && (j < 4 ? ok0 : ok1);
 #pragma unroll
                     for (int c = 0; c < HT; ++c) {
-                        float &x = reinterpret_cast<float *>(&scores[c][j >> 2])[j & 3];
-                        x = live ? x * to_log2 : -__builtin_inff();
+                        const float x = scores[c][j >> 2][j & 3] * to_log2;
+                        scores[c][j >> 2][j & 3] = live ? x : -__builtin_inff();
                     }
                     keep[j] = live ? ~0u : 0u;
                 }
@@ -704,17 +716,8 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                 finish(c, row);
             }
         }
-        }
-        if (left == 0 || row + 1 >= rows)
+        if (left == 0)
             break;
-        ++row;
-        skip = 0;
-        row_first += row_n;
-        const RowSpan next = row_span(p, reqs, kv_len, row);
-        lo = next.lo;
-        hi = next.hi;
-        req = next.req;
-        row_n = row_tiles(next);
     }
 
     // ---- what the block's waves share ------------------------------------------
@@ -816,45 +819,45 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
         const int each = (items + slices - 1) / slices;
         const int end = min((w - w0 + 1) * each, items);
         for (int i0 = (w - w0) * each; i0 < end; i0 += kJoinThreads) {
-        const int n = min(end - i0, kJoinThreads);
-        int groups = 1;  // threads an item
-        while (2 * groups * n <= kJoinThreads && groups < count)
-            groups *= 2;
-        const int g = tid / n, item = i0 + tid % n;
-        const int head = item / (dim / 4), d = item % (dim / 4) * 4;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        float ref = kNone, sum = 0.0f;
-        const auto add = [&](f32x4 part, float r, float l) {
-            const float to = fmaxf(ref, r);
-            const float a = __builtin_amdgcn_exp2f(ref - to), b = __builtin_amdgcn_exp2f(r - to);
-            o = o * a + part * b;
-            sum = sum * a + l * b;
-            ref = to;
-        };
-        if (g < groups) {
+            const int n = min(end - i0, kJoinThreads);
+            int groups = 1;  // threads an item
+            while (2 * groups * n <= kJoinThreads && groups < count)
+                groups *= 2;
+            const int g = tid / n, item = i0 + tid % n;
+            const int head = item / (dim / 4), d = item % (dim / 4) * 4;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+            float ref = kNone, sum = 0.0f;
+            const auto add = [&](f32x4 part, float r, float l) {
+                const float to = fmaxf(ref, r);
+                const float a = __builtin_amdgcn_exp2f(ref - to), b = __builtin_amdgcn_exp2f(r - to);
+                o = o * a + part * b;
+                sum = sum * a + l * b;
+                ref = to;
+            };
+            if (g < groups) {
 #pragma unroll 4
-            for (int k = g; k < count; k += groups) {
-                // the row's first partial is what its block began, the others what theirs continued
-                const int64_t slot =
-                    ((int64_t)((w0 + k) * 2 + (k == 0 ? 1 : 0)) * gridDim.y + hv) * p.group_step +
-                    head;
-                add(*reinterpret_cast<const f32x4 *>(p.part_out + slot * dim + d),
-                    p.part_stat[slot * 2], p.part_stat[slot * 2 + 1]);
+                for (int k = g; k < count; k += groups) {
+                    // the row's first partial is what its block began, the others what theirs continued
+                    const int64_t slot =
+                        ((int64_t)((w0 + k) * 2 + (k == 0 ? 1 : 0)) * gridDim.y + hv) * p.group_step +
+                        head;
+                    add(*reinterpret_cast<const f32x4 *>(p.part_out + slot * dim + d),
+                        p.part_stat[slot * 2], p.part_stat[slot * 2 + 1]);
+                }
             }
-        }
-        for (int half = groups / 2; half > 0; half /= 2) {
-            if (g >= half && g < 2 * half) {
-                s_out[tid] = o;
-                s_ref[tid] = ref;
-                s_sum[tid] = sum;
+            for (int half = groups / 2; half > 0; half /= 2) {
+                if (g >= half && g < 2 * half) {
+                    s_out[tid] = o;
+                    s_ref[tid] = ref;
+                    s_sum[tid] = sum;
+                }
+                __syncthreads();
+                if (g < half)
+                    add(s_out[tid + half * n], s_ref[tid + half * n], s_sum[tid + half * n]);
+                __syncthreads();
             }
-            __syncthreads();
-            if (g < half)
-                add(s_out[tid + half * n], s_ref[tid + half * n], s_sum[tid + half * n]);
-            __syncthreads();
-        }
-        if (g == 0)
-            attn_store<TYPE>(p, row, first_head + head, dim, d, o, ref, sum);
+            if (g == 0)
+                attn_store<TYPE>(p, row, first_head + head, dim, d, o, ref, sum);
         }
     }
 }
