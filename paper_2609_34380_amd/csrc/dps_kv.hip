@@ -236,7 +236,8 @@ template <int CONTROL>
 __device__ __forceinline__ float moved(float x)
 {
     return __builtin_bit_cast(
-        float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, false));
+        float,
+        __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, false));
 }
 
 // Sum over each group of 4, 8 or 16 lanes, in every lane of it.  Quads swap

@@ -44,7 +44,9 @@ class PagedBatch:
     def grow(self, new):
         """new[r] tokens join slot r in the coming step.  Takes the blocks they need
         (which may evict residuals: look at sums.mode afterwards) and brings the
-        lengths to the device.  False, with nothing changed, if no room is left."""
+        lengths to the device on the current stream: a step on another stream, or the
+        replay of a graph there, has to be ordered after it.  False, with nothing
+        changed, if no room is left."""
         if len(new) != len(self.lengths) or min(new) < 0 or sum(new) > self.rows:
             raise ValueError("one count of new tokens a slot, at most %d in all" % self.rows)
         need = []
@@ -117,7 +119,8 @@ class AttentionLayer:
 def rope_table(max_pos, rot, base=10000.0, device="cuda"):
     """float32 [max_pos][rot]: cosines then sines of pos * base^(-2i / rot)."""
     i = torch.arange(rot // 2, dtype=torch.float64, device=device)
-    angle = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * base ** (-2 * i / rot)
+    pos = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None]
+    angle = pos * base ** (-2 * i / rot)
     return torch.cat((angle.cos(), angle.sin()), 1).float()
 
 
