@@ -319,8 +319,8 @@ enum { DPS_KV_F16 = 0, DPS_KV_BF16 = 1, DPS_KV_E4M3 = 2 };
  *   kv_heads      1..4096.   head_dim  64, 96, 128, 192 or 256 (E4M3: not 96).
  *   block_tokens  a power of two, 16..256.
  *   type          DPS_KV_*.  E4M3 holds value / scale, k_scale for keys and
- *                 v_scale for values (positive; other types ignore their
- *                 value, which still has to be positive). */
+ *                 v_scale for values (positive, finite and not subnormal, for
+ *                 other types too, which ignore the value). */
 typedef struct {
     uint8_t *pool;
     int64_t pool_bytes;
@@ -412,7 +412,7 @@ typedef struct {
     const int32_t *kv_len;  /* [rows] tokens attended: positions 0 .. kv_len - 1          */
     int32_t window;         /* > 0: only the last `window` of them                        */
     int32_t type;           /* DPS_KV_F16 or DPS_KV_BF16: of q and out                    */
-    float scale;            /* of the products q . k                                      */
+    float scale;            /* of the products q . k; scale * k_scale is finite           */
     uint16_t *out;          /* [rows][heads][head_dim]                                    */
     int64_t out_stride;
     float *lse;             /* [rows][heads] log of the sum of exponentials, or NULL      */

@@ -740,7 +740,8 @@ dps_status check_cache(const dps_kv_cache *c, dps::KvCacheView *out)
     REQUIRE(aligned(c->pool, 16) && c->block_stride % 16 == 0, DPS_ERR_ALIGNMENT,
             "cache pool or block_stride is not 16-byte aligned");
     REQUIRE(c->pool_bytes >= bytes, DPS_ERR_INVALID_ARG, "pool_bytes is smaller than one block");
-    REQUIRE(c->k_scale > 0.0f && c->v_scale > 0.0f && c->k_scale <= 3.4e38f &&
+    // the store multiplies by 1 / scale: no infinity
+    REQUIRE(c->k_scale >= 1.2e-38f && c->v_scale >= 1.2e-38f && c->k_scale <= 3.4e38f &&
                 c->v_scale <= 3.4e38f,
             DPS_ERR_INVALID_ARG, "k_scale and v_scale must be positive and finite");
     out->pool = c->pool;
@@ -915,7 +916,8 @@ DPS_EXPORT dps_status dps_kv_store(const dps_kv_store_args *a, const dps_kv_cach
 DPS_EXPORT size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t kv_heads,
                                            int64_t head_dim)
 {
-    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || head_dim <= 0 || heads % kv_heads != 0)
+    if (rows <= 0 || heads <= 0 || heads > 65536 || kv_heads <= 0 || kv_heads > 4096 ||
+        head_dim <= 0 || head_dim > 256 || heads % kv_heads != 0)
         return 0;
     // the type of the cache is not known here: room for either
     const size_t wide = plan_attn(heads, kv_heads, head_dim, false).bytes();
@@ -941,8 +943,10 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
     REQUIRE(a->heads >= 1 && a->heads <= 65536 && a->heads % kv_heads == 0, DPS_ERR_INVALID_ARG,
             "heads must be a multiple of kv_heads, at most 65536");
     REQUIRE(a->window >= 0, DPS_ERR_INVALID_ARG, "window is negative");
-    REQUIRE(a->scale == a->scale && a->scale >= -3.4e38f && a->scale <= 3.4e38f,
-            DPS_ERR_INVALID_ARG, "scale must be finite");
+    // of the scores, with the factor that makes them powers of two
+    const double factor = 1.4426951 * a->scale * c.k_scale;
+    REQUIRE(factor >= -3.4e38 && factor <= 3.4e38, DPS_ERR_INVALID_ARG,
+            "scale, or scale * k_scale, must be finite");
     REQUIRE(a->rows <= 1 || (a->q_stride >= a->heads * dim && a->out_stride >= a->heads * dim),
             DPS_ERR_INVALID_ARG, "q_stride or out_stride is smaller than a row");
     if (a->rows == 0)

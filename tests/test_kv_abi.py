@@ -160,3 +160,23 @@ def test_binding_refuses_host_tensors():
         dps.KvCache(torch.zeros(1 << 16, dtype=torch.uint8), 16, 8, 128, torch.float16)
     with pytest.raises(ValueError):
         dps.KvCache(torch.zeros(1 << 16, dtype=torch.uint8), 16, 8, 128, torch.float32)
+
+
+@pytest.mark.parametrize("kw", [dict(k_scale=1e-39), dict(v_scale=1e-45)])
+def test_scales_without_a_reciprocal(lib, kw):
+    c = cache(type=dps.KV_E4M3, **kw)
+    assert lib.dps_kv_store(ctypes.byref(store()), ctypes.byref(c), None) == INVALID
+    assert lib.dps_attn_decode(ctypes.byref(attn()), ctypes.byref(c), 0x100, 1 << 30, None) == INVALID
+
+
+def test_score_factor_overflow(lib):
+    c = cache(type=dps.KV_E4M3, k_scale=1e10)
+    for scale in (1e30, -1e30):
+        args = attn(scale=scale)
+        got = lib.dps_attn_decode(ctypes.byref(args), ctypes.byref(c), 0x100, 1 << 30, None)
+        assert got == INVALID
+
+
+@pytest.mark.parametrize("sizes", [(4, 1 << 40, 1, 128), (4, 8192, 8192, 128), (4, 32, 8, 1 << 40)])
+def test_attn_workspace_of_sizes_that_no_call_has(lib, sizes):
+    assert lib.dps_attn_workspace_bytes(*sizes) == 0
