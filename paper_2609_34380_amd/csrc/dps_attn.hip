@@ -780,7 +780,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
 // began and handed on (row, blocks).  A row of up to kFew blocks is joined by its
 // first one, which loads the partials at once, before it knows whether there are
 // any: one memory latency less than in the general form (0.4-0.9 us of a call at
-// 34 to 300 rows, 0.9% over 29 cases).  For a longer row, the (head, 4 values)
+// 34 to 300 rows, 1.2 at 24 heads of 192).  For a longer row, the (head, 4 values)
 // items are dealt to as many of its blocks as gives a thread about four partials;
 // threads that share an item combine through LDS, in a fixed order.
 template <int TYPE, int D>
@@ -816,26 +816,33 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
         return ((int64_t)((w0 + k) * 2 + (k == 0 ? 1 : 0)) * gridDim.y + hv) * p.group_step;
     };
 
-    const bool narrow = items <= kJoinThreads;
-    {
-        // threads past the items, and partials past the last block, load another's
-        const int head = min(tid / (D / 4), n_heads - 1), d = tid % (D / 4) * 4;
-        f32x4 part[kFew];
-        float r[kFew], l[kFew];
+    f32x4 part[kFew];
+    float part_ref[kFew], part_sum[kFew];
+    const auto load = [&](int item) {
 #pragma unroll
-        for (int k = 0; k < kFew; ++k) {
-            const int64_t slot = slot_of(w, min(k, blocks - 1 - w)) + head;
-            part[k] = *reinterpret_cast<const f32x4 *>(p.part_out + slot * D + d);
-            r[k] = p.part_stat[slot * 2];
-            l[k] = p.part_stat[slot * 2 + 1];
+        for (int k = 0; k < kFew; ++k) {  // past the last block: its own partial again
+            const int64_t slot = slot_of(w, min(k, blocks - 1 - w)) + item / (D / 4);
+            part[k] = *reinterpret_cast<const f32x4 *>(p.part_out + slot * D + item % (D / 4) * 4);
+            part_ref[k] = p.part_stat[slot * 2];
+            part_sum[k] = p.part_stat[slot * 2 + 1];
         }
-        const int count = join[4];
-        if (narrow && count > 0 && count <= kFew && tid < items) {
+    };
+    load(min(tid, items - 1));
+    const int began = join[4];  // blocks of the row that block w began
+    if (began > 0 && began <= kFew) {
+        for (int item = tid; item < items;) {
+            o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            ref = kNone;
+            sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < kFew; ++k)
-                if (k < count)
-                    add(part[k], r[k], l[k]);
-            attn_store<TYPE>(p, join[3], first_head + head, D, d, o, ref, sum);
+                if (k < began)
+                    add(part[k], part_ref[k], part_sum[k]);
+            attn_store<TYPE>(p, join[3], first_head + item / (D / 4), D, item % (D / 4) * 4, o, ref,
+                             sum);
+            item += kJoinThreads;
+            if (item < items)
+                load(item);
         }
     }
 
@@ -851,11 +858,11 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
         }
     }
 
-    for (int began = 0; began < 2; ++began) {
-        const int row = join[began ? 3 : 0], count = join[began ? 4 : 2];
-        if (narrow && count <= kFew)
+    for (int mine = 0; mine < 2; ++mine) {
+        const int row = join[mine ? 3 : 0], count = join[mine ? 4 : 2];
+        if (count <= kFew)
             continue;
-        const int w0 = began ? w : join[1];
+        const int w0 = mine ? w : join[1];
         // the w - w0-th of the row's blocks takes that slice of the items
         const int slices = min(count, (count * items + 4 * kJoinThreads - 1) / (4 * kJoinThreads));
         if (w - w0 >= slices)
