@@ -361,7 +361,8 @@ typedef struct {
  *   requests          0..4096.
  *   fresh             device int32[n_fresh]: free block ids.
  *   table             device int32[requests][table_cols], fewer than 2^31 entries.
- *   step              host pointer; its arrays are written. */
+ *   step              host pointer; its arrays are written, and overlap no other
+ *                     argument (seq_len is not ctx_len). */
 dps_status dps_kv_map(const int32_t *ctx_len, const int32_t *new_len, int64_t requests,
                       int32_t block_tokens, const int32_t *fresh, int64_t n_fresh, int32_t *table,
                       int64_t table_cols, const dps_kv_step *step, void *stream);

@@ -817,6 +817,9 @@ DPS_EXPORT dps_status dps_kv_map(const int32_t *ctx_len, const int32_t *new_len,
     REQUIRE(step->q_start != nullptr && step->counts != nullptr &&
                 (requests == 0 || step->seq_len != nullptr),
             DPS_ERR_INVALID_ARG, "q_start, seq_len or counts is NULL");
+    // every block reads the lengths while one writes the results
+    REQUIRE(requests == 0 || (step->seq_len != ctx_len && step->seq_len != new_len),
+            DPS_ERR_INVALID_ARG, "seq_len is one of the lengths");
     REQUIRE(step->rows == 0 || (step->pos != nullptr && step->slot != nullptr &&
                                 step->req != nullptr && step->kv_len != nullptr),
             DPS_ERR_INVALID_ARG, "pos, slot, req or kv_len is NULL");

@@ -35,8 +35,8 @@
 //
 // Measured on MI355X, both launches replayed from a graph, 32 query and 8
 // key/value heads of 128: one row of 131000 tokens beside 16 short ones (598 MB)
-// 98.5 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 48.0; 256 BF16 rows of
-// up to 600, 64 query heads (305 MB) 57.4; 16 rows of 30000 in E4M3 (930 MB) 143,
+// 98.2 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 47.2; 256 BF16 rows of
+// up to 600, 64 query heads (305 MB) 56.7; 16 rows of 30000 in E4M3 (930 MB) 142,
 // 6.5 TB/s, where a nontemporal read of memory reaches 6.6-6.9.  Every byte is
 // fetched once (FETCH_SIZE).  With loads that caches retain the first three take
 // 112, 52 and 65 us (kernel alone) against 99, 46 and 57.  The second launch and

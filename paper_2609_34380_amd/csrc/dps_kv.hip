@@ -21,7 +21,7 @@ constexpr int kThreads = 256;
 // length arrays from L2, instead of a second launch that would wait for the
 // first; a thread then has one row.  Past 256 requests the blocks are of 1024
 // threads, so that a thread sums 4 requests at most.  MI355X, kernel time: 8
-// requests that decode 2.5 us, 256 3.4, 201 prompts of 92000 tokens (2.6 MB) 4.6,
+// requests that decode 2.5 us, 256 3.3, 201 prompts of 92000 tokens (2.6 MB) 4.5,
 // where an empty launch takes 1.5.
 
 struct Lengths {
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(THREADS) void kv_map_kernel(const KvMapProblem p)
 // Results are stored past the caches' retention, and the QKV rows, which the
 // product before has just written, loaded through them.  MI355X, from a graph:
 // 8192 rows of 32 + 16 heads of 128 40.0 us (206 MB, 5.1 TB/s, the rate of a plain
-// copy), 1531 rows into an E4M3 cache 10.6, one row 5.1.  With plain stores 8192
+// copy), 1531 rows into an E4M3 cache 10.6, one row 6.  With plain stores 8192
 // rows took 43.3 us against 40.5, with nontemporal loads too 41.0 (4038 rows of
 // 32 + 32 heads, partly in the Infinity Cache: 31.6 and 32.3 against 26.0).
 

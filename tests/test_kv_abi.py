@@ -180,3 +180,8 @@ def test_score_factor_overflow(lib):
 @pytest.mark.parametrize("sizes", [(4, 1 << 40, 1, 128), (4, 8192, 8192, 128), (4, 32, 8, 1 << 40)])
 def test_attn_workspace_of_sizes_that_no_call_has(lib, sizes):
     assert lib.dps_attn_workspace_bytes(*sizes) == 0
+
+
+@pytest.mark.parametrize("seq_len", [0x1000, 0x2000])
+def test_map_does_not_write_its_lengths(lib, seq_len):
+    assert _map(lib, seq_len=seq_len) == INVALID
