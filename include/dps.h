@@ -430,8 +430,10 @@ size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t kv_heads, i
  * the cache (a table entry of -1) are left out; a length past the table's
  * columns is cut there; a row that attends nothing (length 0, req outside the
  * table, no block) gives zeros and lse -inf.  Cache bytes outside the attended
- * tokens may hold anything.  Several rows may share a request (kv_len then says
- * what each sees).
+ * tokens may hold anything; an attended value that is infinite or not a number
+ * makes its component of the output infinite or not a number (an infinite one
+ * may give NaN: the weights are taken in two terms, of which one may be 0).
+ * Several rows may share a request (kv_len then says what each sees).
  *   ws  device scratch of ws_bytes >= dps_attn_workspace_bytes(...), 256-byte
  *       aligned. */
 dps_status dps_attn_decode(const dps_attn_args *args, const dps_kv_cache *cache, void *ws,
