@@ -470,6 +470,20 @@ def test_attn_long_chains(heads, kv_heads, dim):
     run_attn(cache, table, q, [n, 5])
 
 
+@pytest.mark.parametrize("tiles", [6, 11, 15, 18, 23])
+@pytest.mark.parametrize("cdtype,dim,heads", [(E4M3, 256, 32), (F16, 192, 13), (F16, 128, 4)])
+def test_attn_rows_over_a_few_blocks(tiles, cdtype, dim, heads):
+    """About a tile a wave, so that rows begin anywhere in a block and end one to six
+    blocks on: on both sides of the four that the first block joins, with one round
+    of its threads over the heads and with several."""
+    rows = 960 // tiles
+    lens = [32 * tiles + (37 * i) % 65 - 32 for i in range(rows)]
+    cache, table, q = build(F16, cdtype, dim, 1, heads, 32, lens, seed=tiles)
+    got, lse = run_attn(cache, table, q, lens)
+    again, _ = run_attn(cache, table, q, lens)
+    assert torch.equal(got, again)
+
+
 @pytest.mark.parametrize("case", ["rising", "falling", "large", "flat", "negative_scale"])
 def test_attn_score_ranges(case):
     """Scores that keep exceeding the running reference, that fall, that spread over
