@@ -150,13 +150,21 @@ struct RowSpan {
     int32_t req;
 };
 
+// UNIFORM: r is the wave's, and the result lies in scalar registers.
+template <bool UNIFORM>
 __device__ __forceinline__ RowSpan row_span(const AttnProblem &p, const int32_t *__restrict__ req,
                                             const int32_t *__restrict__ kv_len, int32_t r)
 {
     RowSpan s;
     s.req = req ? req[r] : r;
+    int32_t len = kv_len[r];
+    // both loads under way before either is looked at: one latency, not two (0.1-0.5 us)
+    if (UNIFORM)
+        asm("" : "+s"(s.req), "+s"(len));
+    else
+        asm("" : "+v"(s.req), "+v"(len));
     const int64_t room = min(p.table_cols << p.log2_tokens, kLongest);
-    int64_t n = kv_len[r];
+    int64_t n = len;
     if (s.req < 0 || s.req >= p.requests)
         n = 0;
     n = n < 0 ? 0 : (n > room ? room : n);
@@ -320,14 +328,14 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     if (rows <= 64) {
         span = RowSpan{0, 0, 0};
         if (lane < rows)
-            span = row_span(p, reqs, kv_len, lane);
+            span = row_span<false>(p, reqs, kv_len, lane);
         mine = row_tiles(span);
         incl = wave_scan(mine);
         tiles = __builtin_amdgcn_readlane(incl, 63);
     } else {
         const int32_t r1 = min((tid + 1) * per, rows);
         for (int32_t r = tid * per; r < r1; ++r)
-            mine += row_tiles(row_span(p, reqs, kv_len, r));
+            mine += row_tiles(row_span<false>(p, reqs, kv_len, r));
         incl = wave_scan(mine);
         if (lane == 63)
             s_sums[wave] = incl;
@@ -367,14 +375,14 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         if (per == 1) {
             row = chunk;
             skip = begin - chunk_first;
-            span = row_span(p, reqs, kv_len, row);
+            span = row_span<false>(p, reqs, kv_len, row);
         } else {
             const int32_t r1 = min((chunk + 1) * per, rows);
             for (int32_t r = chunk * per; r < r1; r += 64) {
                 if (rows > 64) {
                     span = RowSpan{0, 0, 0};
                     if (r + lane < r1)
-                        span = row_span(p, reqs, kv_len, r + lane);
+                        span = row_span<false>(p, reqs, kv_len, r + lane);
                     mine = row_tiles(span);
                     incl = wave_scan(mine);
                 }
@@ -479,7 +487,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
             return;
         skip = 0;
         row_first += row_n;
-        const RowSpan next = row_span(p, reqs, kv_len, row);
+        const RowSpan next = row_span<true>(p, reqs, kv_len, row);
         lo = next.lo;
         hi = next.hi;
         req = next.req;
@@ -849,7 +857,8 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
     for (int64_t r0 = w + (int64_t)wave * 64 * blocks; r0 < p.rows;
          r0 += (int64_t)kJoinThreads * blocks) {
         const int64_t r = r0 + (int64_t)lane * blocks;
-        uint64_t none = __ballot(r < p.rows && row_span(p, reqs, kv_len, (int32_t)r).hi == 0);
+        uint64_t none =
+            __ballot(r < p.rows && row_span<false>(p, reqs, kv_len, (int32_t)r).hi == 0);
         for (; none; none &= none - 1) {
             const int64_t row = r0 + (int64_t)__builtin_ctzll(none) * blocks;
             for (int i = lane; i < items; i += 64)

@@ -197,8 +197,11 @@ constexpr int attn_blocks_per_cu(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim
 // Query heads of a key/value head that share one pass over its tokens: two column
 // tiles of 16.  MI355X, 24 query heads a key/value head, against two passes: 13
 // rows of 13830 tokens, 8 heads of 64 in FP16 62.9 / 82.0 us, 21 rows of 20609 in
-// E4M3 82.0 / 108.8.  16-bit rows of 192 and 256 leave no registers for the
-// second tile (21 rows of 267 tokens, 16 heads of 192 32.7 / 28.1).
+// E4M3 82.0 / 108.8.  Short calls pay 1-5 us for it (3 rows of 300 tokens, 4 heads of
+// 128 in E4M3 13.7 / 10.8).  16-bit rows of 256 leave no registers for the second
+// tile; rows of 192 gain on long calls only and lose most on short ones (16 rows of
+// 3000, 8 heads 60.4 / 70.8; 30 mixed rows of up to 2000, 4 heads 33.9 / 29.8; 3 rows
+// of 300 18.7 / 13.7), and keep one.
 constexpr int attn_heads_a_pass(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim >= 384 ? 16 : 32; }
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream);
