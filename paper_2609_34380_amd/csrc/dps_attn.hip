@@ -35,8 +35,8 @@
 //
 // Measured on MI355X, both launches replayed from a graph, 32 query and 8
 // key/value heads of 128: one row of 131000 tokens beside 16 short ones (598 MB)
-// 98.2 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 47.2; 256 BF16 rows of
-// up to 600, 64 query heads (305 MB) 56.7; 16 rows of 30000 in E4M3 (930 MB) 142,
+// 97.5 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 46.8; 256 BF16 rows of
+// up to 600, 64 query heads (305 MB) 56.4; 16 rows of 30000 in E4M3 (930 MB) 142,
 // 6.5 TB/s, where a nontemporal read of memory reaches 6.6-6.9.  Every byte is
 // fetched once (FETCH_SIZE).  With loads that caches retain the first three take
 // 112, 52 and 65 us (kernel alone) against 99, 46 and 57.  The second launch and
@@ -65,6 +65,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLift = 6.0f, kRoom = 14.0f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 template <int TYPE>
 __device__ __forceinline__ f32x4 mfma32(u32x4 a, u32x4 b, f32x4 c)
@@ -451,13 +452,15 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                 f.sum == 0.0f ? -__builtin_inff() : (f.ref + __builtin_amdgcn_logf(f.sum)) * kLn2;
     };
     // a partial row for the join: slot 0 of the block began before it, slot 1 in it
-    const auto hand_on = [&](int c, int which) {
+    const auto slot_at = [&](int which) {
+        return ((int64_t)(block * 2 + which) * gridDim.y + hv) * p.group_step;
+    };
+    const auto hand_on = [&](int c) {
         const Partial<S::kAcc> &f = o[c];
         const int head = 16 * c + col;
         if (head >= n_heads)
             return;
-        const int64_t slot =
-            ((int64_t)(block * 2 + which) * gridDim.y + hv) * p.group_step + head;
+        const int64_t slot = slot_at(1) + head;
         float *at = p.part_out + slot * D;
         each_piece([&](auto width, int d0, int tile) {
             constexpr int W = width;
@@ -747,28 +750,61 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
             if (ends)
                 finish(c, row);
             else
-                hand_on(c, 1);
+                hand_on(c);
         }
         if (!ends && hv == 0) {
             s_join[3] = row;
             s_join[4] = (int)line.of(row_first + row_n - 1) / kWaves - block + 1;
         }
     }
-    if (wave == 0 && (state & kHead)) {  // a row that began in an earlier block
-        bool ends = false;
+    // A row that began in an earlier block: all of its parts lie in LDS, and the waves
+    // share their join.  Against wave 0 alone: one row of 777 tokens 11.1 / 11.6 us,
+    // 131000 tokens beside 16 short rows 97.3 / 97.9.
+    if (state_of(0) & kHead) {
+        int n = 1;  // waves that have parts of it
+        while (n < kWaves && !(state_of(n - 1) & kEnds) && (state_of(n) & kHead))
+            ++n;
 #pragma unroll
-        for (int c = 0; c < HT; ++c)
-            o[c].clear();
-        for (int i = 0; i < kWaves && !ends && (state_of(i) & kHead); ++i) {
+        for (int c = 0; c < HT; ++c) {
+            const int head = 16 * c + col;
+            float weight[kWaves], ref = kNone, sum = 0.0f;
 #pragma unroll
-            for (int c = 0; c < HT; ++c)
-                o[c].join(s_head[i][c], s_stat[i][c], lane);
-            ends = state_of(i) & kEnds;
+            for (int i = 0; i < kWaves; ++i) {
+                weight[i] = i < n ? s_stat[i][c][lane] : kNone;
+                ref = fmaxf(ref, weight[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                weight[i] = __builtin_amdgcn_exp2f(weight[i] - ref);
+                if (i < n)
+                    sum += s_stat[i][c][64 + lane] * weight[i];
+            }
+            const int64_t slot = slot_at(0) + head;
+            // a pair of output tiles at a time, dealt to the waves
+            for (int t = 2 * wave; t < S::kAcc; t += 2 * kWaves) {
+                f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) {
+                    if (i < n) {
+                        x += s_head[i][c][t * 64 + lane] * weight[i];
+                        y += s_head[i][c][(t + 1) * 64 + lane] * weight[i];
+                    }
+                }
+                const int width = t < 8 * S::kP8 ? 8 : (t < 8 * S::kP8 + 4 * S::kP4 ? 4 : 2);
+                float *at = p.part_out + slot * D + (t & -width) * 16 + (t & (width - 1)) +
+                            width * 4 * quarter;
+                if (head < n_heads) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x2 *>(at + width * i) = f32x2{x[i], y[i]};
+                }
+            }
+            if (wave == 0 && quarter == 0 && head < n_heads) {
+                p.part_stat[slot * 2] = ref;
+                p.part_stat[slot * 2 + 1] = sum;
+            }
         }
-#pragma unroll
-        for (int c = 0; c < HT; ++c)
-            hand_on(c, 0);
-        if (hv == 0) {
+        if (wave == 0 && hv == 0) {
             const int first_block = (int)line.of(head_first) / kWaves;
             s_join[0] = head_row;
             s_join[1] = first_block;
