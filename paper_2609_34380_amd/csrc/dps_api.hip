@@ -1,5 +1,6 @@
 // dps_api.hip -- the C ABI of libdps: argument validation, kernel planning and
 // launches.  Nothing here allocates device memory or synchronizes.
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -740,7 +741,7 @@ dps_status check_cache(const dps_kv_cache *c, dps::KvCacheView *out)
     REQUIRE(aligned(c->pool, 16) && c->block_stride % 16 == 0, DPS_ERR_ALIGNMENT,
             "cache pool or block_stride is not 16-byte aligned");
     REQUIRE(c->pool_bytes >= bytes, DPS_ERR_INVALID_ARG, "pool_bytes is smaller than one block");
-    // the store multiplies by 1 / scale: no infinity
+    // normal numbers: the store takes their exponent and fraction apart
     REQUIRE(c->k_scale >= 1.2e-38f && c->v_scale >= 1.2e-38f && c->k_scale <= 3.4e38f &&
                 c->v_scale <= 3.4e38f,
             DPS_ERR_INVALID_ARG, "k_scale and v_scale must be positive and finite");
@@ -753,6 +754,20 @@ dps_status check_cache(const dps_kv_cache *c, dps::KvCacheView *out)
     out->k_scale = c->type == DPS_KV_E4M3 ? c->k_scale : 1.0f;
     out->v_scale = c->type == DPS_KV_E4M3 ? c->v_scale : 1.0f;
     return DPS_OK;
+}
+
+dps::CodeScale code_scale(float scale)
+{
+    dps::CodeScale c;
+    int e;
+    c.unit = 2.0f * frexpf(scale, &e);
+    c.shift = 1 - e;
+    c.inv = 1.0f / c.unit;
+    const double most = 448.0 * c.unit;
+    c.most = (float)most;
+    if (c.most > most)
+        c.most = nextafterf(c.most, 0.0f);
+    return c;
 }
 
 // The 16-bit type of the activations beside a cache of `type`.
@@ -895,6 +910,8 @@ DPS_EXPORT dps_status dps_kv_store(const dps_kv_store_args *a, const dps_kv_cach
                               (a->k_out == nullptr || a->k_out_stride % 8 == 0))) &&
                 aligned(a->slot, 8) && aligned(a->pos, 4),
             DPS_ERR_ALIGNMENT, "a row is not 16-byte aligned, or slot or pos is off its alignment");
+    p.k_code = code_scale(p.cache.k_scale);
+    p.v_code = code_scale(p.cache.v_scale);
     p.qkv = a->qkv;
     p.qkv_stride = a->qkv_stride;
     p.rows = a->rows;

@@ -142,12 +142,20 @@ struct KvMapProblem {
 };
 hipError_t launch_kv_map(const KvMapProblem &p, hipStream_t stream);
 
+// A scale as the E4M3 store divides by it: unit * 2^-shift, 1 <= unit < 2.  inv is 1 / unit,
+// rounded; most the largest v with v / unit <= 448.
+struct CodeScale {
+    float unit, inv, most;
+    int32_t shift;
+};
+
 struct KvStoreProblem {
     const uint16_t *qkv;
     int64_t qkv_stride;
     int64_t rows;
     int32_t heads;
     KvCacheView cache;
+    CodeScale k_code, v_code;
     const int64_t *slot;
     const int32_t *pos;
     const float *rope;      // [max_pos][rot]: cos, then sin; nullptr: no rotation

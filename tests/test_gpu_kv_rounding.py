@@ -1,0 +1,51 @@
+"""Roundings of the paged KV cache's operators, against the exact results: E4M3 codes
+of the store at scales that are no powers of two."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import DEV
+from paper_2609_34380_amd import dps
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, E4M3 = torch.float16, torch.bfloat16, torch.float8_e4m3fn
+# the values of the codes 0 .. 126, from the format: 4 exponent bits of bias 7, 3 mantissa bits
+CODES = np.array([(c % 8) * 2.0 ** -9 if c < 8 else (1 + c % 8 / 8) * 2.0 ** (c // 8 - 7)
+                  for c in range(127)])
+
+
+def nearest(x):
+    """E4M3 values nearest to x (float64), ties to the even code, clamped; NaN stays."""
+    size = np.minimum(np.abs(x), 448.0)
+    at = np.clip(np.searchsorted(CODES, size, side="right") - 1, 0, 125)
+    mid = (CODES[at] + CODES[at + 1]) / 2       # exact, as the comparisons are
+    up = (size > mid) | ((size == mid) & (at % 2 == 1))
+    return np.where(np.isnan(x), np.nan, np.copysign(CODES[at + up], x))
+
+
+# 16 / 17 and the like put quotients of FP16 values within 2^-25 of the middle of two
+# codes: a quotient rounded to fp32 first would land on it
+@pytest.mark.parametrize("scale", [0.03, 41.0, 47 / 1024, 16 / 17, 16 / 19, 16 / 31, 1 / 3, 7e-5,
+                                   1.9, 3e38, 1.2e-38, 1e-30, 0.25])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_e4m3_codes_are_the_nearest_to_value_over_scale(dtype, scale):
+    """Every 16-bit value, as key and as value.  A quotient of 8 or 11 bits by 24 that is
+    not a code's middle is further from it than float64 resolves."""
+    words = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dtype)
+    rows, dim, tokens = 512, 128, 16
+    x = words.view(rows, dim).repeat(1, 3)
+    other = 2 * scale if scale < 1e38 else scale / 2
+    pool = torch.zeros(rows // tokens * 2 * tokens * dim, dtype=torch.uint8, device=DEV)
+    cache = dps.KvCache(pool, tokens, 1, dim, E4M3, k_scale=scale, v_scale=other)
+    dps.kv_store(x.to(DEV), cache, torch.arange(rows, device=DEV), 1)
+    got = pool.cpu().view(rows // tokens, 2, tokens * dim)
+    k = got[:, 0].reshape(-1, dim // 64, tokens, 64).transpose(1, 2).reshape(-1)
+    v = got[:, 1].reshape(-1)
+    for code, s in ((k, scale), (v, other)):
+        with np.errstate(over="ignore"):
+            want = nearest(words.double().numpy() / np.float64(np.float32(s)))
+        have = code.view(E4M3).double().numpy()
+        bad = ~((have == want) | (np.isnan(have) & np.isnan(want)))
+        assert not bad.any(), (s, int(bad.sum()), words.double().numpy()[bad][:4], have[bad][:4],
+                               want[bad][:4])
