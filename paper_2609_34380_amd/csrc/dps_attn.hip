@@ -27,11 +27,14 @@
 //   - Block ids come through scalar loads one tile ahead: a vector load of them
 //     would wait for every value load issued before it.
 //
-// Precision: products and softmax in fp32.  The weights P enter the matrix
-// cores as two 16-bit terms (value and remainder), which keeps them to about
-// 2^-16 or better; one term would add an error of the size of the output's own
-// rounding (relative error 2.1e-4 -> 2.9e-4 in FP16 over an E4M3 cache, 1.7e-3 ->
-// 2.1e-3 in BF16) and save 0-1% of the time.
+// Precision: products and softmax in fp32.  The weights P enter the matrix cores
+// as two 16-bit terms (value and remainder).  BF16 terms keep a weight to 2^-17 of
+// itself.  FP16 terms keep it to 2^-21 of itself or 2^-30 of the row's largest
+// weight, whichever is more: beside a token that outweighs it 2^24 times a token
+// loses up to 1.6% of its own share, under 2^-30 all of it (the sum counts it
+// whole).  One term would add an error of the size of the output's own rounding
+// (relative error 2.1e-4 -> 2.9e-4 in FP16 over an E4M3 cache, 1.7e-3 -> 2.1e-3 in
+// BF16) and save 0-1% of the time.
 //
 // Measured on MI355X, both launches replayed from a graph, 32 query and 8
 // key/value heads of 128: one row of 131000 tokens beside 16 short ones (598 MB)
@@ -86,18 +89,17 @@ __device__ __forceinline__ uint32_t wide2(uint32_t codes)
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.0f, HI));
 }
 
-// Two fp32 weights as two 16-bit terms each: hi (truncated) and the rest.
+// Two fp32 weights as two 16-bit terms each: hi and what it leaves.  BF16: both to
+// nearest, within 2^-17 of the weight to either side (truncated they lost 2^-17 on
+// average, and outputs came out that much nearer to zero).  FP16: both truncated,
+// within 2^-21 of the weight or 2^-24.
 template <int TYPE>
 __device__ __forceinline__ void split2(float p0, float p1, uint32_t &hi, uint32_t &lo)
 {
     if (TYPE == KV_BF16) {
-        const uint32_t b0 = __builtin_bit_cast(uint32_t, p0);
-        const uint32_t b1 = __builtin_bit_cast(uint32_t, p1);
-        hi = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-        const float r0 = p0 - __builtin_bit_cast(float, b0 & 0xffff0000u);
-        const float r1 = p1 - __builtin_bit_cast(float, b1 & 0xffff0000u);
-        lo = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, r1),
-                                   __builtin_bit_cast(uint32_t, r0), 0x07060302u);
+        hi = narrow2<TYPE>(p0, p1);
+        lo = narrow2<TYPE>(p0 - __builtin_bit_cast(float, hi << 16),
+                           p1 - __builtin_bit_cast(float, hi & 0xffff0000u));
     } else {
         const auto h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
         hi = __builtin_bit_cast(uint32_t, h);

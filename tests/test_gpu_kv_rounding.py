@@ -1,5 +1,5 @@
 """Roundings of the paged KV cache's operators, against the exact results: E4M3 codes
-of the store at scales that are no powers of two."""
+of the store at scales that are no powers of two, and the attention's weights."""
 import numpy as np
 import pytest
 import torch
@@ -49,3 +49,26 @@ def test_e4m3_codes_are_the_nearest_to_value_over_scale(dtype, scale):
         bad = ~((have == want) | (np.isnan(have) & np.isnan(want)))
         assert not bad.any(), (s, int(bad.sum()), words.double().numpy()[bad][:4], have[bad][:4],
                                want[bad][:4])
+
+
+@pytest.mark.parametrize("dtype,cdtype", [(BF16, BF16), (BF16, E4M3), (F16, F16)])
+def test_attention_leans_to_no_side(dtype, cdtype):
+    """Outputs of random weights over positive values: their errors, single roundings,
+    cancel.  2^23 outputs near 1.5 round with a deviation of 2^-7 / sqrt(12) (BF16), so
+    their mean relative error has one of 5e-7; a loss of weight shows as itself."""
+    rows, heads, tokens, dim = 4096, 16, 64, 128
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    rand = lambda *shape: torch.rand(*shape, generator=gen, device=DEV)
+    k = (4 * rand(rows, tokens, dim) - 2).to(cdtype)
+    v = (1 + rand(rows, tokens, dim)).to(cdtype)
+    seg = 64 // cdtype.itemsize
+    pool = torch.cat((k.view(rows, tokens, dim // seg, seg).transpose(1, 2).reshape(rows, -1)
+                      .view(torch.uint8), v.view(rows, -1).view(torch.uint8)), 1).contiguous()
+    cache = dps.KvCache(pool, tokens, 1, dim, cdtype)
+    q = (2 * rand(rows, heads, dim) - 1).to(dtype)
+    table = torch.arange(rows, dtype=torch.int32, device=DEV)[:, None].contiguous()
+    got = dps.attn_decode(q, cache, table, torch.full_like(table[:, 0], tokens)).double()
+    s = torch.matmul(q.double(), k.double().transpose(1, 2).contiguous()) * dim ** -0.5
+    want = torch.matmul(torch.softmax(s, -1), v.double())
+    lean = float(((got - want) / want).mean())
+    assert abs(lean) <= (2.0 ** -18 if dtype == BF16 else 2.0 ** -21), lean
