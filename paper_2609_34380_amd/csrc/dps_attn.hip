@@ -662,10 +662,10 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                     weigh(ref);
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 8; ++j)
                     x[j] = __builtin_amdgcn_exp2f(x[j]);
-                    o[c].sum += x[j];
-                }
+                // added up first: beside a large sum one small weight would round away
+                o[c].sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint32_t hi2, lo2;

@@ -72,3 +72,37 @@ def test_attention_leans_to_no_side(dtype, cdtype):
     want = torch.matmul(torch.softmax(s, -1), v.double())
     lean = float(((got - want) / want).mean())
     assert abs(lean) <= (2.0 ** -18 if dtype == BF16 else 2.0 ** -21), lean
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("gap", [8.0, 17.0, 20.0])
+@pytest.mark.parametrize("large", [0, 20002])
+def test_small_weights_beside_a_large_one(dtype, gap, large):
+    """One token e^gap above 20002 others, all of them in one wave's range of tiles (1100
+    rows of one request, about one a wave).  The sum meets a rounding of 2^-24 of itself
+    per tile of 32 tokens; FP16 terms lose up to 2^-30 of the largest weight a token,
+    BF16 terms 2^-17 of a token's own."""
+    n, dim, tokens, rows = 20003, 64, 16, 1100
+    blocks = -(-n // tokens)
+    k = torch.zeros(blocks * tokens, dim, dtype=dtype)
+    v = torch.ones(blocks * tokens, dim, dtype=dtype)
+    k[large, 0], v[large] = gap, 0.0
+    k, v = (x.view(blocks, tokens, dim) for x in (k, v))
+    pool = torch.cat((k.view(blocks, tokens, 2, 32).transpose(1, 2).reshape(blocks, -1),
+                      v.reshape(blocks, -1)), 1).contiguous().to(DEV)
+    q = torch.zeros(rows, 1, dim, dtype=dtype, device=DEV)
+    q[..., 0] = 1.0
+    i32 = lambda *shape, **kw: torch.zeros(*shape, dtype=torch.int32, device=DEV, **kw)
+    lse = torch.empty(rows, 1, device=DEV)
+    got = dps.attn_decode(q, dps.KvCache(pool, tokens, 1, dim, dtype),
+                          torch.arange(blocks, dtype=torch.int32, device=DEV)[None],
+                          i32(rows) + n, req=i32(rows), scale=1.0, lse=lse)
+    small = (n - 1) * np.exp(-gap)
+    drift = 2.0 ** -24 * (n // 32 + 2)
+    err = float((lse.double() - (gap + np.log1p(small))).abs().max())
+    assert err <= drift + 2.0 ** -18, err     # and lse's own rounding, at 16 to 32
+    want = small / (1 + small)
+    lost = (n - 1) * 2.0 ** -30 / (1 + small) if dtype == F16 else 2.0 ** -17 * want
+    half = 2.0 ** -11 if dtype == F16 else 2.0 ** -8
+    err = float((got.double() - want).abs().max())
+    assert err <= lost + (half + 2 * drift) * want + (2.0 ** -25 if dtype == F16 else 0), err
