@@ -25,7 +25,11 @@ class PagedBatch:
     block_tokens tokens) from `sums`.  A step takes at most `rows` new tokens.
 
     grow() does a step's host work (blocks, lengths to the device), map() enqueues
-    the GPU's; the results are in self.step (a dps.KvMap) and self.table."""
+    the GPU's; the results are in self.step (a dps.KvMap) and self.table.  Steps may
+    run on other streams than grow(): its copies wait for the work of every stream that
+    map() was called on, also to capture it, and are complete when it returns.  Before
+    the next grow() a caller waits for a graph replayed elsewhere than on the stream of
+    its capture."""
 
     def __init__(self, sums, batch, max_tokens, block_tokens, rows=None, device="cuda"):
         self.sums, self.block_tokens = sums, block_tokens
@@ -40,13 +44,15 @@ class PagedBatch:
         # a step never takes more than a block a slot and what its rows fill
         self.fresh = torch.full((batch + self.rows // block_tokens + 1,), -1, **i32)
         self.step = dps.make_kv_map(batch, self.rows, self.ctx_len.device)
+        # that the buffers were filled on, or map() was called on
+        self._streams = [torch.cuda.current_stream(self.table.device)]
 
     def grow(self, new):
         """new[r] tokens join slot r in the coming step.  Takes the blocks they need
         (which may evict residuals: look at sums.mode afterwards) and brings the
-        lengths to the device on the current stream: a step on another stream, or the
-        replay of a graph there, has to be ordered after it.  False, with nothing
-        changed, if no room is left."""
+        lengths to the device on the current stream, once the steps before have read
+        theirs (the host waits for that).  False, with nothing changed, if no room is
+        left."""
         if len(new) != len(self.lengths) or min(new) < 0 or sum(new) > self.rows:
             raise ValueError("one count of new tokens a slot, at most %d in all" % self.rows)
         need = []
@@ -57,6 +63,10 @@ class PagedBatch:
         taken = self.sums.alloc(sum(need))
         if taken is None:
             return False
+        here = torch.cuda.current_stream(self.table.device)
+        for stream in self._streams:   # earlier steps read what is replaced here
+            if stream != here:
+                here.wait_stream(stream)
         self.ctx_len.copy_(torch.tensor(self.lengths, dtype=torch.int32))
         self.new_len.copy_(torch.tensor(new, dtype=torch.int32))
         if taken:
@@ -70,6 +80,9 @@ class PagedBatch:
 
     def map(self):
         """Enqueue the step's block tables and slot maps."""
+        stream = torch.cuda.current_stream(self.table.device)
+        if stream not in self._streams:
+            self._streams.append(stream)
         return dps.kv_map(self.ctx_len, self.new_len, self.fresh, self.table, self.block_tokens,
                           out=self.step)
 
