@@ -25,11 +25,14 @@ class PagedBatch:
     block_tokens tokens) from `sums`.  A step takes at most `rows` new tokens.
 
     grow() does a step's host work (blocks, lengths to the device), map() enqueues
-    the GPU's; the results are in self.step (a dps.KvMap) and self.table.  Steps may
-    run on other streams than grow(): its copies wait for the work of every stream that
-    map() was called on, also to capture it, and are complete when it returns.  Before
-    the next grow() a caller waits for a graph replayed elsewhere than on the stream of
-    its capture."""
+    the GPU's; the results are in self.step (a dps.KvMap) and self.table.  Each grow()
+    is followed by its map(), or by one replay of a graph that holds it, before the
+    next: the blocks of a step that is not mapped reach no table.
+
+    Steps may run on other streams than grow(): its copies wait for the work of every
+    stream that map() was called on, also to capture it, and are complete when it
+    returns.  Before the next grow() a caller waits for a graph replayed elsewhere than
+    on the stream of its capture."""
 
     def __init__(self, sums, batch, max_tokens, block_tokens, rows=None, device="cuda"):
         self.sums, self.block_tokens = sums, block_tokens
@@ -46,6 +49,8 @@ class PagedBatch:
         self.step = dps.make_kv_map(batch, self.rows, self.ctx_len.device)
         # that the buffers were filled on, or map() was called on
         self._streams = [torch.cuda.current_stream(self.table.device)]
+        self._unmapped = set()               # slots that grew since the last map()
+        self._captured = False               # map() is in a graph: replays are not seen here
 
     def grow(self, new):
         """new[r] tokens join slot r in the coming step.  Takes the blocks they need
@@ -63,6 +68,9 @@ class PagedBatch:
         taken = self.sums.alloc(sum(need))
         if taken is None:
             return False
+        if self._unmapped and not self._captured:
+            self.sums.free(taken)
+            raise RuntimeError("the tokens of the last grow() are not mapped")
         here = torch.cuda.current_stream(self.table.device)
         for stream in self._streams:   # earlier steps read what is replaced here
             if stream != here:
@@ -76,6 +84,7 @@ class PagedBatch:
             self.blocks[r] += taken[at:at + n]
             at += n
             self.lengths[r] += new[r]
+        self._unmapped = {r for r, n in enumerate(new) if n}
         return True
 
     def map(self):
@@ -83,15 +92,19 @@ class PagedBatch:
         stream = torch.cuda.current_stream(self.table.device)
         if stream not in self._streams:
             self._streams.append(stream)
+        self._captured = self._captured or torch.cuda.is_current_stream_capturing()
+        self._unmapped.clear()
         return dps.kv_map(self.ctx_len, self.new_len, self.fresh, self.table, self.block_tokens,
                           out=self.step)
 
     def end(self, slot):
         """The request of a slot ends: its blocks go back.  True when residuals wait
-        for the units that became free.  The steps that read the blocks must have
-        completed: a restore worker copies on a stream of its own."""
+        for the units that became free.  The steps that use the blocks, the one that
+        grow() has just prepared among them, must have completed: a restore worker
+        copies on a stream of its own."""
         wake = self.sums.free(self.blocks[slot]) if self.blocks[slot] else False
         self.blocks[slot], self.lengths[slot] = [], 0
+        self._unmapped.discard(slot)
         return wake
 
 

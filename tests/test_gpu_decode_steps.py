@@ -59,3 +59,27 @@ def test_grow_waits_for_steps_on_another_stream(captured):
         torch.cuda.synchronize()
         slow.close()
         plain.close()
+
+
+def test_grow_again_before_map_is_refused():
+    """The blocks of a step that was never mapped would be in no table: the slot's next
+    rows would read what an earlier request left there."""
+    sums = dps.SumManager(1, 8, 0)
+    batch = decode.PagedBatch(sums, 2, 64, 16)
+    assert batch.grow([1, 0])
+    free = sums.counts()["free_blocks"]
+    for new in ([0, 1], [1, 1], [0, 0]):
+        with pytest.raises(RuntimeError):
+            batch.grow(new)
+    assert batch.lengths == [1, 0] and sums.counts()["free_blocks"] == free
+    batch.map()
+    assert batch.step.slot.tolist()[0] == batch.blocks[0][0] * 16
+    assert batch.grow([0, 0]) and batch.grow([0, 1])     # nothing to map between these
+    batch.map()
+    assert batch.step.slot.tolist()[0] == batch.blocks[1][0] * 16
+    assert batch.grow([1, 1])
+    batch.map()
+    assert batch.step.slot.tolist() == [b[0] * 16 + 1 for b in batch.blocks]
+    assert batch.grow([1, 0])
+    batch.end(0)                                         # the only slot that grew is gone
+    assert batch.grow([0, 1])
