@@ -21,8 +21,9 @@ from . import dps
 
 
 class PagedBatch:
-    """`batch` slots for requests of up to max_tokens tokens, their KV blocks (of
-    block_tokens tokens) from `sums`.  A step takes at most `rows` new tokens.
+    """`batch` slots for requests of up to max_tokens tokens (rounded up to whole
+    blocks: self.max_tokens), their KV blocks (of block_tokens tokens) from `sums`.  A
+    step takes at most `rows` new tokens.
 
     grow() does a step's host work (blocks, lengths to the device), map() enqueues
     the GPU's; the results are in self.step (a dps.KvMap) and self.table.  Each grow()
@@ -110,8 +111,9 @@ class PagedBatch:
 
 class AttentionLayer:
     """Attention of a decoder layer: qkv and o are dps.NestedWeight, cache the
-    layer's dps.KvCache (FP16 or E4M3), rope the rotation table; q_weight and
-    k_weight (FP16 [head_dim]) the head norms' weights, or None without norms."""
+    layer's dps.KvCache (FP16 or E4M3), rope the rotation table (of the batch's
+    max_tokens positions: past its end rows are NaN); q_weight and k_weight (FP16
+    [head_dim]) the head norms' weights, or None without norms."""
 
     def __init__(self, qkv, o, cache, heads, rope, q_weight=None, k_weight=None, rows=256,
                  window=0):
@@ -179,7 +181,7 @@ class SharedLayer:
         self.worker = dps.RestoreWorker(self.sums, targets, per_unit)
         self.batch = PagedBatch(self.sums, batch, max_tokens, self.TOKENS, device=device)
         self.q_weight = torch.ones(self.DIM, dtype=torch.float16, device=device)
-        self.rope = rope_table(max_tokens, self.DIM, device=device)
+        self.rope = rope_table(self.batch.max_tokens, self.DIM, device=device)
         cache = dps.KvCache(self.pool, self.TOKENS, self.KV_HEADS, self.DIM, torch.float16)
         self.layer = AttentionLayer(*self.nested, cache, self.HEADS, self.rope,
                                     self.q_weight, self.q_weight, rows=batch)

@@ -83,3 +83,20 @@ def test_grow_again_before_map_is_refused():
     assert batch.grow([1, 0])
     batch.end(0)                                         # the only slot that grew is gone
     assert batch.grow([0, 1])
+
+
+def test_shared_layer_to_its_batchs_last_token():
+    """max_tokens inside a block: the positions up to the block's end are rotated too."""
+    short, wide = (decode.SharedLayer(units=4, batch=1, max_tokens=n, seed=2) for n in (21, 4096))
+    try:
+        gen = torch.Generator().manual_seed(5)
+        for t in range(32):
+            x = torch.randn(1, short.HIDDEN, generator=gen).to(torch.float16).to(DEV)
+            got, want = short.decode(x, [1]), wide.decode(x, [1])
+            assert bool(torch.isfinite(want).all()) and torch.equal(got, want), t
+        with pytest.raises(ValueError):
+            short.decode(x, [1])
+    finally:
+        torch.cuda.synchronize()
+        short.close()
+        wide.close()
