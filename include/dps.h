@@ -396,8 +396,9 @@ typedef struct {
  * at the row's position; values are stored as they are.  fp32 arithmetic, one
  * rounding (nearest even; E4M3: of value / scale clamped to +-448).  A row whose
  * position is outside the rotation table gets NaN in what turns.  A 16-bit cache
- * has the type of the activations; an E4M3 cache goes with either.  Rows with
- * the same slot: one of them is stored. */
+ * has the type of the activations; an E4M3 cache goes with either.  The slots of
+ * a call are distinct, as dps_kv_map gives them; a slot that several rows name
+ * holds a mixture of theirs, heads and parts of heads from either. */
 dps_status dps_kv_store(const dps_kv_store_args *args, const dps_kv_cache *cache, void *stream);
 
 /* Arguments of dps_attn_decode.  Strides are in elements, multiples of 8. */

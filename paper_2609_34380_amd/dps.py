@@ -616,8 +616,8 @@ def kv_store(qkv, cache, slot, heads, pos=None, rope=None, q_weight=None, k_weig
              adjacent=False, q_out=None, k_out=None):
     """Head norms (with q_weight and k_weight, [head_dim]) and rotation of the query
     and key heads of qkv ([rows][(heads + 2 kv_heads) * head_dim], FP16 or BF16), keys
-    and values into `cache` at int64 `slot` [rows] (negative: not stored), in one pass
-    (dps_kv_store).  rope: float32 [max_pos][rot], rot / 2 cosines then sines, at the
+    and values into `cache` at int64 `slot` [rows] (distinct; negative: not stored), in
+    one pass (dps_kv_store).  rope: float32 [max_pos][rot], rot / 2 cosines then sines, at the
     int32 positions `pos`; adjacent: pairs (2i, 2i + 1) instead of (i, i + rot / 2).
     Returns the queries [rows][heads][head_dim] (q_out).  k_out: the finished keys
     [rows][kv_heads][head_dim] as well."""
