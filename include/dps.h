@@ -430,7 +430,8 @@ size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t kv_heads, i
  * a second launch; results do not depend on timing.  Tokens in a block outside
  * the cache (a table entry of -1) are left out; a length past the table's
  * columns is cut there; a row that attends nothing (length 0, req outside the
- * table, no block) gives zeros and lse -inf.  Cache bytes outside the attended
+ * table, no block, scores of -inf alone) gives zeros and lse -inf.  Scores count
+ * as far as log2(e) times them is finite in fp32, below that as -inf.  Cache bytes outside the attended
  * tokens may hold anything; an attended value that is infinite or not a number
  * makes its component of the output infinite or not a number (an infinite one
  * may give NaN: the weights are taken in two terms, of which one may be 0).

@@ -57,7 +57,7 @@ constexpr int kWaves = 4;
 constexpr int kTile = 32;               // tokens a wave takes at a time
 constexpr int kJoinThreads = 512;
 constexpr int64_t kLongest = 0x7fffff00;  // tokens of a row (a tile past it still fits 31 bits)
-constexpr float kNone = -3e38f;         // reference score before any token
+constexpr float kNone = -__FLT_MAX__;   // reference score before any token: no finite one is below
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // Weights are 2^(score - ref).  ref is set kLift below the largest score so far,

@@ -106,3 +106,34 @@ def test_small_weights_beside_a_large_one(dtype, gap, large):
     half = 2.0 ** -11 if dtype == F16 else 2.0 ** -8
     err = float((got.double() - want).abs().max())
     assert err <= lost + (half + 2 * drift) * want + (2.0 ** -25 if dtype == F16 else 0), err
+
+
+@pytest.mark.parametrize("score", [-2.2e38, -2.3e38, 2.3e38])
+def test_scores_near_the_ends_of_fp32(score):
+    """Equal scores whose powers of two (log2(e) times them) are still finite: the mean of
+    the values; one score far above them: its value alone."""
+    n, dim, tokens = 300, 64, 16
+    blocks = -(-n // tokens)
+    k = torch.zeros(blocks * tokens, dim, dtype=BF16)
+    k[:, 0] = score
+    v = torch.randn(blocks * tokens, dim, generator=torch.Generator().manual_seed(3)).to(BF16)
+    q = torch.zeros(2, 1, dim, dtype=BF16, device=DEV)
+    q[..., 0] = 1.0
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    for best in (None, 7):
+        if best is not None:
+            k[:, 0] = min(score, score / 2)
+            k[best, 0] = max(score, score / 2)
+        pool = torch.cat((k.view(blocks, tokens, 2, 32).transpose(1, 2).reshape(blocks, -1),
+                          v.view(blocks, -1)), 1).contiguous().to(DEV)
+        lse = torch.empty(2, 1, device=DEV)
+        got = dps.attn_decode(q, dps.KvCache(pool, tokens, 1, dim, BF16),
+                              i32([list(range(blocks))]), i32([n, 10]), req=i32([0, 0]),
+                              scale=1.0, lse=lse).cpu().double()
+        for row, m in enumerate((n, 10)):
+            want = v[:m].double().mean(0) if best is None else v[best].double()
+            spread = v[:m].double().abs().mean(0) if best is None else want.abs()
+            bound = 2.0 ** -8 * want.abs() + 2.0 ** -14 * spread
+            assert bool(((got[row, 0] - want).abs() <= bound).all())
+            top = float(k[:m, 0].double().max())
+            assert abs(float(lse[row, 0]) - top) <= 2.0 ** -20 * abs(top)
