@@ -16,11 +16,15 @@
 //     in registers (one byte permute per two values); the main loop has no LDS
 //     and no barrier.
 //   - Token 4 r + c of 16 sits in operand row 4 c + r.  With the cache's
-//     64-byte key segments every load of a wave is then contiguous (1 KiB at
-//     16 bytes a lane) for K and for V.
+//     64-byte key segments every key load of a wave is then 1 KiB of contiguous
+//     memory.  A value load takes 16 lanes' worth (up to 8 values each) of four
+//     neighbouring tokens: contiguous where that is the whole row (1 KiB for 16-bit
+//     heads of 128, 512 bytes for 16-bit heads of 64 and E4M3 heads of 128), else
+//     four runs of 64 to 256 bytes.
 //   - The tokens of all rows, in tiles of 32, form one line per key/value head,
 //     cut into equal ranges, one per wave: ragged lengths load every CU alike.
-//     A wave finishes the rows that lie inside its range by itself; what the
+//     A wave steps through the rows of its range one by one (an idle one costs a
+//     scalar load's latency, 0.2 us) and finishes those inside by itself; what the
 //     four waves of a block share is joined in LDS, what blocks share (at most
 //     two partial rows a block, however long a row is) in attn_join_kernel.
 //     Partials are joined in their order, so results do not depend on timing.
@@ -38,12 +42,13 @@
 //
 // Measured on MI355X, both launches replayed from a graph, 32 query and 8
 // key/value heads of 128: one row of 131000 tokens beside 16 short ones (598 MB)
-// 97.5 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 46.8; 256 BF16 rows of
-// up to 600, 64 query heads (305 MB) 56.4; 16 rows of 30000 in E4M3 (930 MB) 142,
-// 6.5 TB/s, where a nontemporal read of memory reaches 6.6-6.9.  Every byte is
-// fetched once (FETCH_SIZE).  With loads that caches retain the first three take
-// 112, 52 and 65 us (kernel alone) against 99, 46 and 57.  The second launch and
-// its join cost about 4 us, a block's start and end about 5.
+// 97.6 us, 6.1 TB/s; 34 FP16 rows of up to 4096 (272 MB) 46.8; 256 BF16 rows of
+// up to 600, 64 query heads (305 MB) 56.4; 16 rows of 30000 in E4M3 (930 MB) 142
+// (one call at a time 146), 6.5 TB/s, where a nontemporal read of memory reaches
+// 6.6-6.9.  A pass over a key/value head fetches every byte once (FETCH_SIZE).
+// With loads that caches retain the first three take 112, 52 and 65 us (kernel
+// alone) against 99, 46 and 57.  The second launch and its join cost about 4 us, a
+// block's start and end about 5.
 #include <type_traits>
 
 #include "dps_internal.h"

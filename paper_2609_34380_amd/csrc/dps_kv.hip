@@ -179,10 +179,11 @@ __global__ __launch_bounds__(THREADS) void kv_map_kernel(const KvMapProblem p)
 // every pair are its own and the only exchange is the sum of squares.
 // Results are stored past the caches' retention, and the QKV rows, which the
 // product before has just written, loaded through them.  MI355X, from a graph:
-// 8192 rows of 32 + 16 heads of 128 40.0 us (206 MB, 5.1 TB/s, the rate of a plain
-// copy), 1531 rows into an E4M3 cache 10.6, one row 6.  With plain stores 8192
-// rows took 43.3 us against 40.5, with nontemporal loads too 41.0 (4038 rows of
-// 32 + 32 heads, partly in the Infinity Cache: 31.6 and 32.3 against 26.0).
+// 8192 rows of 32 + 16 heads of 128 39.4 us (206 MB, 5.2 TB/s; a plain copy of 1 GiB
+// 5.15, but part of these rows is still in the Infinity Cache), 1531 rows into an
+// E4M3 cache 10.7, one row 6.3.  With plain stores 8192 rows took 43.3 us against
+// 40.5, with nontemporal loads too 41.0 (4038 rows of 32 + 32 heads, partly in the
+// Infinity Cache: 31.6 and 32.3 against 26.0).
 
 template <int TYPE>
 __device__ __forceinline__ float wide(uint16_t v)

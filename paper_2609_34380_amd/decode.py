@@ -28,7 +28,8 @@ class PagedBatch:
     grow() does a step's host work (blocks, lengths to the device), map() enqueues
     the GPU's; the results are in self.step (a dps.KvMap) and self.table.  Each grow()
     is followed by its map(), or by one replay of a graph that holds it, before the
-    next: the blocks of a step that is not mapped reach no table.
+    next: the blocks of a step that is not mapped reach no table.  Several new tokens of
+    a slot are rows that the attention serves one by one, each over all tokens before it.
 
     Steps may run on other streams than grow(): its copies wait for the work of every
     stream that map() was called on, also to capture it, and are complete when it
@@ -113,7 +114,10 @@ class AttentionLayer:
     """Attention of a decoder layer: qkv and o are dps.NestedWeight, cache the
     layer's dps.KvCache (FP16 or E4M3), rope the rotation table (of the batch's
     max_tokens positions: past its end rows are NaN); q_weight and k_weight (FP16
-    [head_dim]) the head norms' weights, or None without norms."""
+    [head_dim]) the head norms' weights, or None without norms.  Made for steps of
+    decode tokens: a prompt's rows are taken, at the cost of reading the cache anew for
+    each.  The buffers between the products are the layer's own, so one call runs at a
+    time: calls on several streams are ordered by the caller."""
 
     def __init__(self, qkv, o, cache, heads, rope, q_weight=None, k_weight=None, rows=256,
                  window=0):

@@ -673,7 +673,8 @@ def attn_decode(q, cache, table, kv_len, req=None, scale=None, window=0, out=Non
     """Attention of one new token a row over the paged cache (dps_attn_decode): row j
     of q ([rows][heads][head_dim]) attends positions 0 .. kv_len[j] - 1 (the last
     `window` of them if window > 0) of request req[j] (j without req), whose blocks
-    are table[req[j]].  scale: of the scores, 1 / sqrt(head_dim) by default.  lse:
+    are table[req[j]].  Rows of one request (a prompt's) share no loads: each reads its
+    tokens anew.  scale: of the scores, 1 / sqrt(head_dim) by default.  lse:
     float32 [rows][heads] for the log of the sums.  Returns out (q's shape)."""
     lib = _lib or load_library()
     if q.dim() != 3:
