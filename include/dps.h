@@ -444,6 +444,109 @@ dps_status dps_attn_decode(const dps_attn_args *args, const dps_kv_cache *cache,
                            size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Sequences that branch: several answers to one prompt, or beams, share the
+ * cache blocks of what they have in common.  Rows of a table share whole
+ * blocks only; each row's last block, while it has room, is its own.
+ * dps_kv_fork gives a step's rows the tables of the rows they go on from and
+ * lists the copies that needs, dps_kv_copy makes them (a call per layer whose
+ * blocks lie apart), dps_attn_shared attends rows that share a prefix, and
+ * dps_beam_select picks the rows to go on from.  dps_kv_copy and dps_kv_remap
+ * also compact a cache (dps_sum_compact says what to move).
+ * ------------------------------------------------------------------------ */
+
+/* What dps_kv_fork writes, device arrays that overlap no other argument.
+ * `rows` are the rows of the step to come. */
+typedef struct {
+    int64_t rows;       /* 0..4096                                                      */
+    int32_t *table;     /* [rows][table_cols] block ids, -1 past a row's last block     */
+    int32_t *seq_len;   /* [rows] tokens of each row                                    */
+    int32_t *src;       /* [rows] copies to make, in row order: from block src[i] ...   */
+    int32_t *dst;       /* [rows] ... to block dst[i] ...                               */
+    int32_t *tokens;    /* [rows] ... its first tokens[i] tokens; -1 in all three past
+                           the last copy                                                */
+    int32_t *freed;     /* [n_freed] blocks of the old tables that no new one holds,
+                           ascending; -1 past the last                                  */
+    int64_t n_freed;    /* room in freed; what does not fit is counted and left out     */
+    int32_t *counts;    /* [2] copies, which is also the blocks taken off `fresh`, and
+                           blocks freed, in all; the step fits if the first is at most
+                           n_fresh                                                      */
+} dps_kv_forked;
+
+/* Workspace bytes of dps_kv_fork.  Contents on entry do not matter. */
+size_t dps_kv_fork_workspace_bytes(int64_t rows, int64_t n_blocks);
+
+/* Block tables after rows have branched, ended or changed places: new row r goes
+ * on from old row parent[r] (outside 0 .. old_rows - 1: an empty row).  It has its
+ * parent's length and blocks, but for a last block with room in it: that stays with
+ * the first child (the lowest r), and every other child takes the next block off
+ * `fresh` and an entry in the list of copies (-1 as dst, and in the table, once
+ * `fresh` has run out).  Blocks past a row's length are not handed on.  Negative
+ * lengths count as 0; of a length past the table's columns only the blocks in the
+ * table are.  The same arguments give the same results.
+ *   parent      device int32[out->rows].
+ *   seq_len     device int32[old_rows], table device int32[old_rows][table_cols],
+ *               old_rows 0..4096.
+ *   fresh       device int32[n_fresh]: free block ids, in none of the tables.
+ *   n_blocks    blocks of the cache: ids from 0, fewer than 2^31 (an entry outside
+ *               is handed on, and never listed as freed).
+ *   ws          device scratch, 256-byte aligned, of ws_bytes >=
+ *               dps_kv_fork_workspace_bytes(out->rows, n_blocks). */
+dps_status dps_kv_fork(const int32_t *parent, const int32_t *seq_len, int64_t old_rows,
+                       int32_t block_tokens, const int32_t *table, int64_t table_cols,
+                       const int32_t *fresh, int64_t n_fresh, int64_t n_blocks,
+                       const dps_kv_forked *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Copies of cache blocks: for every i < n (and < *count, where count is not NULL: a
+ * device int32) the first tokens[i] tokens (all where tokens is NULL; cut to the
+ * block's) of every head's keys and values of block src[i] go to the same places of
+ * block dst[i].  A pair with an end outside the cache (-1), or with src = dst, is
+ * left out.  The dst of a call are distinct, and none is a src of it: a block
+ * that is both, or named twice as dst, holds a mixture.  n * block bytes < 2^44. */
+dps_status dps_kv_copy(const dps_kv_cache *cache, const int32_t *src, const int32_t *dst,
+                       const int32_t *tokens, int64_t n, const int32_t *count, void *stream);
+
+/* Entries of `table` (device int32[entries], fewer than 2^31) that name src[i]
+ * become dst[i], all at once.  src (device int32[n]) ascends, without repeats; of a
+ * list that does not, some ids may not be found.  Negative entries stay. */
+dps_status dps_kv_remap(int32_t *table, int64_t entries, const int32_t *src, const int32_t *dst,
+                        int64_t n, void *stream);
+
+/* Element types of the logits of dps_beam_select. */
+enum { DPS_BEAM_F16 = 0, DPS_BEAM_BF16 = 1, DPS_BEAM_F32 = 2 };
+
+typedef struct {
+    int64_t batch;          /* requests; batch * beams at most 2^20                     */
+    int64_t beams;          /* rows of each, 1..1024                                    */
+    int64_t vocab;          /* 1..2^24                                                  */
+    const void *logits;     /* [batch * beams][vocab], aligned to an element            */
+    int64_t logits_stride;  /* elements from row to row                                 */
+    int32_t type;           /* DPS_BEAM_*                                               */
+    int32_t end;            /* the token that ends a beam; -1: none                     */
+    const float *score;     /* [batch * beams] the beams' scores so far                 */
+    const uint8_t *done;    /* [batch * beams] != 0: the beam has ended; or NULL        */
+    int64_t keep;           /* beams to pick for each request, 1..256                   */
+    float *new_score;       /* [batch][keep], best first                                */
+    int32_t *parent;        /* [batch][keep] the row each goes on from                  */
+    int32_t *token;         /* [batch][keep] and with which token                       */
+    uint8_t *new_done;      /* [batch][keep] 1: it ends with that token, or had ended   */
+} dps_beam_args;
+
+/* Workspace bytes of dps_beam_select (0 for arguments it refuses). */
+size_t dps_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t vocab, int64_t keep);
+
+/* The next beams of each request: token t after beam w scores score_w + x_wt -
+ * log(sum_t exp(x_wt)); the `keep` highest of all beams and tokens of the request,
+ * of equal ones those of the lowest (w, t), go to the outputs in that order.  Scores
+ * are compared in 64 bits (sums of exponentials good to 2^-21 of themselves) and
+ * rounded once to fp32.  A beam that has ended counts as one candidate, its score
+ * with the token `end` (which has to be given with `done`).  A logit of -inf is never
+ * picked; a beam with a NaN or +inf among its logits, or whose score is not
+ * finite, has no candidates.  Where there are fewer than `keep`, the rest is score
+ * -inf, parent and token -1, done 0.  The outputs overlap no input.
+ *   ws  device scratch, 256-byte aligned, of ws_bytes >= dps_beam_workspace_bytes(). */
+dps_status dps_beam_select(const dps_beam_args *args, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * SUM manager (Sec. IV-B "SUM manager"; Sec. IV-D, Algorithm 1): host-side
  * bookkeeping of the shared region's physical units.  A unit holds either
  * one residual tensor (BACKED) or KV blocks (AVAIL: some free, FULL: none
@@ -480,6 +583,15 @@ dps_status dps_sum_alloc(dps_sum *s, int64_t n, int64_t *blocks);
  * that are not allocated, or listed twice, fail the whole call with
  * DPS_ERR_INVALID_ARG and change nothing. */
 dps_status dps_sum_free(dps_sum *s, const int64_t *blocks, int64_t n, int32_t *wake);
+
+/* Moves that empty whole units: for AVAIL units from the one with the fewest blocks on
+ * (the lowest id of equals), all of its blocks go to free places of the other AVAIL
+ * units, the fullest first, as long as they fit there and in max_moves in all.  The
+ * *n moves go to src[i] -> dst[i] (room for max_moves each), src ascending.  The dst
+ * blocks are allocated by this call and the src blocks stay so: the caller copies
+ * the blocks and changes its tables (dps_kv_copy, dps_kv_remap) and then frees src
+ * (dps_sum_free), which makes their units FREE. */
+dps_status dps_sum_compact(dps_sum *s, int64_t max_moves, int64_t *src, int64_t *dst, int64_t *n);
 
 /* Restore worker, first step: the lowest stale residual is bound to the
  * lowest FREE unit, which turns RESTORING.  *residual and *unit receive them,

@@ -1024,3 +1024,273 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
     return launched(dps::launch_attn(p, a->type, cache->type == DPS_KV_E4M3, (int)dim, plan.blocks,
                                      (hipStream_t)stream));
 }
+
+// ---- sequences that branch ---------------------------------------------------------
+
+namespace {
+
+// Whether [a, a + an) and [b, b + bn) have a byte in common.
+bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return an > 0 && bn > 0 && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+
+int64_t fork_words(int64_t n_blocks) { return cdiv(n_blocks, 32); }
+
+}  // namespace
+
+DPS_EXPORT size_t dps_kv_fork_workspace_bytes(int64_t rows, int64_t n_blocks)
+{
+    if (rows < 0 || rows > 4096 || n_blocks < 0 || n_blocks > 0x7fffffff)
+        return 0;
+    return align256(rows * 4) + align256(8 * fork_words(n_blocks));
+}
+
+DPS_EXPORT dps_status dps_kv_fork(const int32_t *parent, const int32_t *seq_len, int64_t old_rows,
+                                  int32_t block_tokens, const int32_t *table, int64_t table_cols,
+                                  const int32_t *fresh, int64_t n_fresh, int64_t n_blocks,
+                                  const dps_kv_forked *out, void *ws, size_t ws_bytes, void *stream)
+{
+    g_err[0] = 0;
+    REQUIRE(out != nullptr, DPS_ERR_INVALID_ARG, "output descriptor is NULL");
+    REQUIRE(out->rows >= 0 && old_rows >= 0 && table_cols >= 0 && n_fresh >= 0 &&
+                out->n_freed >= 0 && n_blocks >= 0,
+            DPS_ERR_INVALID_ARG, "rows, old_rows, table_cols, n_fresh, n_freed or n_blocks is negative");
+    REQUIRE(out->rows <= 4096 && old_rows <= 4096, DPS_ERR_UNSUPPORTED,
+            "more than 4096 rows in one call");
+    REQUIRE(block_tokens >= 16 && block_tokens <= 256 && (block_tokens & (block_tokens - 1)) == 0,
+            DPS_ERR_UNSUPPORTED, "block_tokens must be a power of two in 16..256");
+    REQUIRE(table_cols <= 0x7fffffff && old_rows * table_cols <= 0x7fffffff &&
+                out->rows * table_cols <= 0x7fffffff,
+            DPS_ERR_UNSUPPORTED, "table of 2^31 entries or more");
+    REQUIRE(n_blocks <= 0x7fffffff, DPS_ERR_UNSUPPORTED, "2^31 blocks or more");
+    const int64_t rows = out->rows;
+    REQUIRE(rows == 0 || (parent != nullptr && out->seq_len != nullptr && out->src != nullptr &&
+                          out->dst != nullptr && out->tokens != nullptr),
+            DPS_ERR_INVALID_ARG, "parent, or out's seq_len, src, dst or tokens is NULL");
+    REQUIRE(old_rows == 0 || seq_len != nullptr, DPS_ERR_INVALID_ARG, "seq_len is NULL");
+    REQUIRE(table_cols == 0 || ((old_rows == 0 || table != nullptr) &&
+                                (rows == 0 || out->table != nullptr)),
+            DPS_ERR_INVALID_ARG, "a table is NULL");
+    REQUIRE((n_fresh == 0 || fresh != nullptr) && (out->n_freed == 0 || out->freed != nullptr) &&
+                out->counts != nullptr,
+            DPS_ERR_INVALID_ARG, "fresh, freed or counts is NULL");
+    REQUIRE(aligned(parent, 4) && aligned(seq_len, 4) && aligned(table, 4) && aligned(fresh, 4) &&
+                aligned(out->table, 4) && aligned(out->seq_len, 4) && aligned(out->src, 4) &&
+                aligned(out->dst, 4) && aligned(out->tokens, 4) && aligned(out->freed, 4) &&
+                aligned(out->counts, 4),
+            DPS_ERR_ALIGNMENT, "an array is off the alignment of its entries");
+    // old tables and lengths are read while new ones are written
+    const struct {
+        const void *at;
+        int64_t bytes;
+    } in[] = {{parent, rows * 4}, {seq_len, old_rows * 4}, {table, old_rows * table_cols * 4},
+              {fresh, n_fresh * 4}},
+      to[] = {{out->table, rows * table_cols * 4}, {out->seq_len, rows * 4}, {out->src, rows * 4},
+              {out->dst, rows * 4}, {out->tokens, rows * 4}, {out->freed, out->n_freed * 4},
+              {out->counts, 8}};
+    for (const auto &a : to)
+        for (const auto &b : in)
+            REQUIRE(!overlap(a.at, a.bytes, b.at, b.bytes), DPS_ERR_INVALID_ARG,
+                    "an output overlaps an input");
+    const size_t need = dps_kv_fork_workspace_bytes(rows, n_blocks);
+    REQUIRE(ws_bytes >= need && (need == 0 || ws != nullptr), DPS_ERR_WORKSPACE,
+            "workspace is smaller than dps_kv_fork_workspace_bytes()");
+    REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");
+    dps::KvForkProblem p;
+    p.parent = parent;
+    p.seq_len = seq_len;
+    p.table = table;
+    p.fresh = fresh;
+    p.n_fresh = n_fresh;
+    p.rows = (int32_t)rows;
+    p.old_rows = (int32_t)old_rows;
+    p.cols = (int32_t)table_cols;
+    p.log2_tokens = __builtin_ctz((unsigned)block_tokens);
+    p.n_blocks = n_blocks;
+    p.words = fork_words(n_blocks);
+    p.new_table = out->table;
+    p.new_len = out->seq_len;
+    p.src = out->src;
+    p.dst = out->dst;
+    p.tokens = out->tokens;
+    p.freed = out->freed;
+    p.n_freed = out->n_freed;
+    p.counts = out->counts;
+    p.last = static_cast<int32_t *>(ws);
+    p.bits = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ws) + align256(rows * 4));
+    return launched(dps::launch_kv_fork(p, (hipStream_t)stream));
+}
+
+DPS_EXPORT dps_status dps_kv_copy(const dps_kv_cache *cache, const int32_t *src, const int32_t *dst,
+                                  const int32_t *tokens, int64_t n, const int32_t *count,
+                                  void *stream)
+{
+    g_err[0] = 0;
+    dps::KvCacheView c;
+    const dps_status s = check_cache(cache, &c);
+    if (s != DPS_OK)
+        return s;
+    REQUIRE(n >= 0 && n <= 0x7fffffff, DPS_ERR_INVALID_ARG, "n must be in 0..2^31-1");
+    if (n == 0)
+        return DPS_OK;
+    REQUIRE(src != nullptr && dst != nullptr, DPS_ERR_INVALID_ARG, "src or dst is NULL");
+    REQUIRE(aligned(src, 4) && aligned(dst, 4) && aligned(tokens, 4) && aligned(count, 4),
+            DPS_ERR_ALIGNMENT, "an array is off the alignment of its entries");
+    dps::KvCopyProblem p;
+    const int row_bytes = c.dim * (cache->type == DPS_KV_E4M3 ? 1 : 2);
+    p.pool = c.pool;
+    p.block_stride = c.block_stride;
+    p.n_blocks = c.n_blocks;
+    p.log2_tokens = c.log2_tokens;
+    p.key_units = (uint32_t)(((int64_t)c.kv_heads << c.log2_tokens) * (row_bytes / 16));
+    p.units = 2 * p.key_units;
+    const int row_units = row_bytes / 16;  // 4, 8, 16, 32 or 12, 24, and 48 of no type
+    p.thirds = row_units % 3 == 0;
+    p.row_shift = __builtin_ctz((unsigned)row_units);
+    p.pieces = (uint32_t)cdiv(p.units, dps::kv_copy_piece_units());
+    REQUIRE(n * p.pieces <= 0x7fffffff && n * p.pieces * dps::kv_copy_piece_units() < (1ll << 40),
+            DPS_ERR_UNSUPPORTED, "too many blocks for one call");
+    p.n = n;
+    p.src = src;
+    p.dst = dst;
+    p.tokens = tokens;
+    p.count = count;
+    return launched(dps::launch_kv_copy(p, (hipStream_t)stream));
+}
+
+DPS_EXPORT dps_status dps_kv_remap(int32_t *table, int64_t entries, const int32_t *src,
+                                   const int32_t *dst, int64_t n, void *stream)
+{
+    g_err[0] = 0;
+    REQUIRE(entries >= 0 && entries <= 0x7fffffff && n >= 0 && n <= 0x7fffffff,
+            DPS_ERR_INVALID_ARG, "entries or n is not in 0..2^31-1");
+    if (entries == 0 || n == 0)
+        return DPS_OK;
+    REQUIRE(table != nullptr && src != nullptr && dst != nullptr, DPS_ERR_INVALID_ARG,
+            "table, src or dst is NULL");
+    REQUIRE(aligned(table, 4) && aligned(src, 4) && aligned(dst, 4), DPS_ERR_ALIGNMENT,
+            "an array is off the alignment of its entries");
+    REQUIRE(!overlap(table, entries * 4, src, n * 4) && !overlap(table, entries * 4, dst, n * 4),
+            DPS_ERR_INVALID_ARG, "src or dst overlaps the table");
+    return launched(dps::launch_kv_remap(table, entries, src, dst, n, (hipStream_t)stream));
+}
+
+namespace {
+
+// 16-byte vectors a thread, pieces of a row, and the workspace's parts.
+struct BeamPlan {
+    int vecs;
+    int64_t pieces, lists;
+    size_t value_bytes, sum_bytes, listed_bytes;
+    size_t bytes() const { return 2 * value_bytes + sum_bytes + listed_bytes; }
+};
+
+BeamPlan plan_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t keep, int type)
+{
+    BeamPlan b;
+    const int64_t rows = batch * beams;
+    // a row may begin inside its first vector
+    const int64_t span = vocab + (type == DPS_BEAM_F32 ? 3 : 7);
+    b.vecs = dps::kBeamVecs;
+    if (rows * cdiv(span, dps::beam_piece(type, b.vecs)) < 2 * current_cu_count())
+        b.vecs = dps::kBeamFewVecs;
+    b.pieces = cdiv(span, dps::beam_piece(type, b.vecs));
+    b.lists = rows * b.pieces;
+    b.value_bytes = align256(b.lists * keep * 4);
+    b.sum_bytes = align256(b.lists * 16);
+    b.listed_bytes = align256(b.lists * 4);
+    return b;
+}
+
+bool beam_sizes(int64_t batch, int64_t beams, int64_t vocab, int64_t keep)
+{
+    return batch >= 0 && batch <= (1 << 20) && beams >= 1 && beams <= 1024 &&
+           batch * beams <= (1 << 20) && vocab >= 1 && vocab <= (1 << 24) && keep >= 1 &&
+           keep <= 256;
+}
+
+}  // namespace
+
+DPS_EXPORT size_t dps_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t vocab,
+                                           int64_t keep)
+{
+    if (!beam_sizes(batch, beams, vocab, keep) || batch == 0)
+        return 0;
+    // the type of the logits is not known here: room for either size
+    const size_t wide = plan_beam(batch, beams, vocab, keep, DPS_BEAM_F32).bytes();
+    const size_t half = plan_beam(batch, beams, vocab, keep, DPS_BEAM_F16).bytes();
+    return wide > half ? wide : half;
+}
+
+DPS_EXPORT dps_status dps_beam_select(const dps_beam_args *a, void *ws, size_t ws_bytes,
+                                      void *stream)
+{
+    g_err[0] = 0;
+    REQUIRE(a != nullptr, DPS_ERR_INVALID_ARG, "beam arguments are NULL");
+    REQUIRE(a->type == DPS_BEAM_F16 || a->type == DPS_BEAM_BF16 || a->type == DPS_BEAM_F32,
+            DPS_ERR_INVALID_ARG, "logits must be FP16, BF16 or FP32");
+    REQUIRE(beam_sizes(a->batch, a->beams, a->vocab, a->keep), DPS_ERR_UNSUPPORTED,
+            "batch, beams, vocab or keep is out of range");
+    REQUIRE(a->end >= -1 && a->end < a->vocab, DPS_ERR_INVALID_ARG,
+            "end must be a token, or -1");
+    REQUIRE(a->done == nullptr || a->end >= 0, DPS_ERR_INVALID_ARG,
+            "beams that have ended need the token that ends them");
+    const int64_t rows = a->batch * a->beams, outs = a->batch * a->keep;
+    if (a->batch == 0)
+        return DPS_OK;
+    REQUIRE(rows <= 1 || a->logits_stride >= a->vocab, DPS_ERR_INVALID_ARG,
+            "logits_stride is smaller than a row");
+    REQUIRE(a->logits_stride <= (int64_t(1) << 40), DPS_ERR_UNSUPPORTED,
+            "logits_stride of more than 2^40");
+    const int elt = a->type == DPS_BEAM_F32 ? 4 : 2;
+    REQUIRE(a->logits != nullptr && a->score != nullptr && a->new_score != nullptr &&
+                a->parent != nullptr && a->token != nullptr && a->new_done != nullptr,
+            DPS_ERR_INVALID_ARG, "logits, score or an output is NULL");
+    REQUIRE(aligned(a->logits, elt) && aligned(a->score, 4) && aligned(a->new_score, 4) &&
+                aligned(a->parent, 4) && aligned(a->token, 4),
+            DPS_ERR_ALIGNMENT, "an array is off the alignment of its entries");
+    // requests are picked at different times: one's outputs are not another's inputs
+    const int64_t logit_bytes = ((rows - 1) * a->logits_stride + a->vocab) * elt;
+    const struct {
+        const void *at;
+        int64_t bytes;
+    } in[] = {{a->logits, logit_bytes}, {a->score, rows * 4}, {a->done, a->done ? rows : 0}},
+      to[] = {{a->new_score, outs * 4}, {a->parent, outs * 4}, {a->token, outs * 4},
+              {a->new_done, outs}};
+    for (const auto &x : to)
+        for (const auto &y : in)
+            REQUIRE(!overlap(x.at, x.bytes, y.at, y.bytes), DPS_ERR_INVALID_ARG,
+                    "an output overlaps an input");
+    const BeamPlan plan = plan_beam(a->batch, a->beams, a->vocab, a->keep, a->type);
+    REQUIRE(plan.lists <= 0x7fffffff && plan.pieces * a->beams * a->keep <= 0x7fffffff,
+            DPS_ERR_UNSUPPORTED, "too many rows for one call");
+    REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
+            "workspace is smaller than dps_beam_workspace_bytes()");
+    REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");
+    dps::BeamProblem p;
+    p.logits = static_cast<const uint8_t *>(a->logits);
+    p.row_bytes = a->logits_stride * elt;
+    p.score = a->score;
+    p.done = a->done;
+    p.batch = a->batch;
+    p.beams = (int32_t)a->beams;
+    p.vocab = (int32_t)a->vocab;
+    p.keep = (int32_t)a->keep;
+    p.end = a->end;
+    p.pieces = (int32_t)plan.pieces;
+    p.new_score = a->new_score;
+    p.parent = a->parent;
+    p.token = a->token;
+    p.new_done = a->new_done;
+    uint8_t *at = static_cast<uint8_t *>(ws);
+    p.sums = reinterpret_cast<double *>(at);
+    at += plan.sum_bytes;
+    p.values = reinterpret_cast<float *>(at);
+    at += plan.value_bytes;
+    p.indexes = reinterpret_cast<int32_t *>(at);
+    at += plan.value_bytes;
+    p.listed = reinterpret_cast<int32_t *>(at);
+    return launched(dps::launch_beam(p, a->type, plan.vecs, (hipStream_t)stream));
+}

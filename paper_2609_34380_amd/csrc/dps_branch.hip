@@ -1,0 +1,333 @@
+// dps_branch.hip -- blocks of the paged KV cache when sequences branch (gfx950):
+// the block tables of a step whose rows go on from other rows (beams, several
+// answers to one prompt), copies of blocks, and tables after blocks have moved.
+#include "dps_internal.h"
+
+namespace dps {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPlanThreads = 1024;
+constexpr int kMostRows = 4096;  // rows of a table
+
+// ---- copies -----------------------------------------------------------------------
+// Pair i: the first n tokens of every head's keys and values of block src[i] into
+// block dst[i].  In a block the 16-byte units of a key segment lie token by token
+// (4 a token), those of a value row too (dim * element bytes / 16 a token), so a
+// unit's token follows from its index alone and a thread moves unit u to unit u.
+//
+// Bound: HBM, 2 bytes moved a byte of live tokens.  A block of threads takes kUnits
+// units a thread of one pair, all loads ahead of the first store.
+constexpr int kUnits = 4;
+
+template <bool PART>
+__global__ __launch_bounds__(kThreads) void kv_copy_kernel(
+    const KvCopyProblem p, const int32_t *__restrict__ srcs, const int32_t *__restrict__ dsts,
+    const int32_t *__restrict__ parts, const int32_t *__restrict__ count)
+{
+    const uint32_t pair = blockIdx.x / p.pieces, piece = blockIdx.x % p.pieces;
+    if (count && (int32_t)pair >= *count)
+        return;
+    const int32_t src = srcs[pair], dst = dsts[pair];
+    const int32_t most = 1 << p.log2_tokens;
+    const int32_t part = PART ? min(parts[pair], most) : most;
+    if (src < 0 || src >= p.n_blocks || dst < 0 || dst >= p.n_blocks || src == dst || part <= 0)
+        return;
+    const u32x4 *from = reinterpret_cast<const u32x4 *>(p.pool + src * p.block_stride);
+    u32x4 *to = reinterpret_cast<u32x4 *>(p.pool + dst * p.block_stride);
+    u32x4 x[kUnits];
+    bool live[kUnits];
+    const uint32_t u0 = piece * (kThreads * kUnits) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * kThreads;
+        live[i] = u < p.units;
+        if (PART && part < most) {
+            // units a token: 4 of keys; of values 2^row_shift, or three times that
+            uint32_t token = u >> 2;
+            if (u >= p.key_units) {
+                token = (u - p.key_units) >> p.row_shift;
+                if (p.thirds)
+                    token /= 3;
+            }
+            live[i] = live[i] && (int32_t)(token & (most - 1)) < part;
+        }
+        if (live[i])
+            x[i] = __builtin_nontemporal_load(from + u);
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+        if (live[i])
+            to[u0 + i * kThreads] = x[i];
+}
+
+// ---- tables after blocks have moved --------------------------------------------------
+// An entry that names src[i] becomes dst[i]; src ascends, so a thread finds its
+// entry by bisection in a copy of the list in LDS (log2 n steps of LDS latency each).
+// Lists too long for that are searched where they lie.
+//
+// Bound: latency.  kEntries entries a thread share the steps.
+constexpr int kEntries = 4;
+constexpr int kListed = 12288;  // 48 KiB
+
+template <bool LDS>
+__global__ __launch_bounds__(kThreads) void kv_remap_kernel(int32_t *__restrict__ table,
+                                                            int64_t entries,
+                                                            const int32_t *__restrict__ src,
+                                                            const int32_t *__restrict__ dst,
+                                                            int32_t n)
+{
+    extern __shared__ int32_t s_src[];
+    const int64_t e0 = (int64_t)blockIdx.x * (kThreads * kEntries) + threadIdx.x;
+    int32_t id[kEntries];
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i)
+        id[i] = e0 + i * kThreads < entries ? table[e0 + i * kThreads] : -1;
+    if (LDS) {
+        for (int i = threadIdx.x; i < n; i += kThreads)
+            s_src[i] = src[i];
+        __syncthreads();
+    }
+    const int32_t *list = LDS ? s_src : src;
+    // the last entry <= id, if any is: lo, by halving steps that all four share
+    int32_t lo[kEntries] = {0, 0, 0, 0};
+    for (int32_t step = n > 1 ? 1 << (31 - __builtin_clz(n - 1)) : 0; step > 0; step >>= 1) {
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) {
+            const int32_t at = lo[i] + step;
+            if (at < n && list[at] <= id[i])
+                lo[i] = at;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i)
+        if (id[i] >= 0 && list[lo[i]] == id[i])
+            table[e0 + i * kThreads] = dst[lo[i]];
+}
+
+// ---- forked tables -------------------------------------------------------------------
+// New row r goes on from old row p = parent[r].  Rows share whole blocks.  A last
+// block that is only partly filled stays with the first child (the lowest r) of its
+// row; the others get a block off `fresh` each, in row order, and an entry in the
+// list of copies.  Freed are the blocks of the old tables that no new one holds: one
+// bit a block for either side, set by the kernel that writes the tables.
+//
+// Bound: latency, and 4 bytes in and out a table entry.  Three launches, each of which
+// needs all of the one before: who copies (and cleared bits), tables and bits, the
+// list of freed blocks.
+
+__device__ __forceinline__ bool in_range(int32_t x, int32_t n) { return x >= 0 && x < n; }
+
+// Tokens of an old row, and the columns that hold them.
+__device__ __forceinline__ int32_t length_of(const KvForkProblem &p, int32_t row)
+{
+    return max(p.seq_len[row], 0);
+}
+__device__ __forceinline__ int32_t columns(const KvForkProblem &p, int32_t len)
+{
+    const uint32_t t = 1u << p.log2_tokens;
+    return min((int32_t)(((uint32_t)len + t - 1) >> p.log2_tokens), p.cols);
+}
+// Whether the row's last token lies in the table, in a block with room after it.
+__device__ __forceinline__ bool open_ended(const KvForkProblem &p, int32_t len)
+{
+    return (len & ((1 << p.log2_tokens) - 1)) != 0 && (len >> p.log2_tokens) < p.cols;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvForkProblem p)
+{
+    // bits of both sides, by every block
+    for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < 2 * p.words;
+         i += (int64_t)gridDim.x * kPlanThreads)
+        p.bits[i] = 0;
+    if (blockIdx.x != 0)
+        return;
+    constexpr int kPer = kMostRows / kPlanThreads;
+    __shared__ int32_t s_eldest[kMostRows];  // of each old row: its first child
+    __shared__ int32_t s_sums[kPlanThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < p.old_rows; i += kPlanThreads)
+        s_eldest[i] = 0x7fffffff;
+    __syncthreads();
+    const int r0 = tid * kPer;
+    int32_t from[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        from[i] = r0 + i < p.rows ? p.parent[r0 + i] : -1;
+        if (in_range(from[i], p.old_rows))
+            atomicMin(&s_eldest[from[i]], r0 + i);
+        else
+            from[i] = -1;
+    }
+    __syncthreads();
+    int32_t len[kPer], n = 0;
+    bool copies[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        len[i] = from[i] >= 0 ? length_of(p, from[i]) : 0;
+        copies[i] = from[i] >= 0 && open_ended(p, len[i]) && s_eldest[from[i]] != r0 + i;
+        n += copies[i];
+    }
+    const int32_t incl = wave_scan(n);
+    if (lane == 63)
+        s_sums[wave] = incl;
+    __syncthreads();
+    int32_t at = incl - n, all = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) {
+        at += i < wave ? s_sums[i] : 0;
+        all += s_sums[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i;
+        if (r >= p.rows)
+            break;
+        p.new_len[r] = len[i];
+        int32_t block = kKeep;
+        if (copies[i]) {
+            block = at < p.n_fresh ? p.fresh[at] : -1;
+            const int32_t col = len[i] >> p.log2_tokens;
+            p.src[at] = p.table[(int64_t)from[i] * p.cols + col];
+            p.dst[at] = block;
+            p.tokens[at] = len[i] & ((1 << p.log2_tokens) - 1);
+            ++at;
+        }
+        p.last[r] = block;
+    }
+    for (int i = all + tid; i < p.rows; i += kPlanThreads)
+        p.src[i] = p.dst[i] = p.tokens[i] = -1;
+    if (tid == 0)
+        p.counts[0] = all;
+}
+
+__device__ __forceinline__ void mark(uint32_t *bits, int32_t block, int64_t n_blocks)
+{
+    if (block < 0 || block >= n_blocks)
+        return;
+    uint32_t *word = bits + (block >> 5);
+    const uint32_t bit = 1u << (block & 31);
+    // rows that share a prefix set the same bits: most find theirs set
+    if (!(__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & bit))
+        atomicOr(word, bit);
+}
+
+__global__ __launch_bounds__(kThreads) void kv_fork_tables_kernel(const KvForkProblem p)
+{
+    const int32_t col = blockIdx.x * kThreads + threadIdx.x;
+    if (col >= p.cols)
+        return;
+    int32_t row = blockIdx.y;
+    if (row >= p.rows) {  // an old row
+        row -= p.rows;
+        mark(p.bits, p.table[(int64_t)row * p.cols + col], p.n_blocks);
+        return;
+    }
+    int32_t block = -1;
+    const int32_t from = p.parent[row];
+    if (in_range(from, p.old_rows)) {
+        const int32_t last = p.last[row];
+        const int32_t have = columns(p, length_of(p, from));
+        if (col < have)
+            block = col == have - 1 && last != kKeep ? last : p.table[(int64_t)from * p.cols + col];
+    }
+    p.new_table[(int64_t)row * p.cols + col] = block;
+    mark(p.bits + p.words, block, p.n_blocks);
+}
+
+// A block of threads lists the freed blocks of its words, after those of all words
+// before, which it counts itself.
+__global__ __launch_bounds__(kPlanThreads) void kv_fork_freed_kernel(const KvForkProblem p)
+{
+    __shared__ int32_t s_before[kPlanThreads / 64], s_after[kPlanThreads / 64],
+        s_sums[kPlanThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t w0 = (int64_t)blockIdx.x * kPlanThreads;
+    int32_t before = 0, after = 0;
+    uint32_t mine = 0;
+    for (int64_t w = tid; w < p.words; w += kPlanThreads) {
+        const uint32_t freed = p.bits[w] & ~p.bits[p.words + w];
+        if (w < w0)
+            before += __popc(freed);
+        else if (w >= w0 + kPlanThreads)
+            after += __popc(freed);
+        else
+            mine = freed;
+    }
+    const int32_t n = __popc(mine);
+    const int32_t incl = wave_scan(n), incl_before = wave_scan(before),
+                  incl_after = wave_scan(after);
+    if (lane == 63) {
+        s_sums[wave] = incl;
+        s_before[wave] = incl_before;
+        s_after[wave] = incl_after;
+    }
+    __syncthreads();
+    int32_t at = incl - n, all = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) {
+        at += s_before[i] + (i < wave ? s_sums[i] : 0);
+        all += s_before[i] + s_sums[i] + s_after[i];
+    }
+    for (uint32_t left = mine; left; left &= left - 1, ++at)
+        if (at < p.n_freed)
+            p.freed[at] = (int32_t)((w0 + tid) * 32) + __builtin_ctz(left);
+    for (int64_t i = all + w0 + tid; i < p.n_freed; i += (int64_t)gridDim.x * kPlanThreads)
+        p.freed[i] = -1;
+    if (blockIdx.x == 0 && tid == 0)
+        p.counts[1] = all;
+}
+
+}  // namespace
+
+hipError_t launch_kv_copy(const KvCopyProblem &p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(p.n * p.pieces));
+    if (p.tokens)
+        hipLaunchKernelGGL(kv_copy_kernel<true>, grid, dim3(kThreads), 0, stream, p, p.src, p.dst,
+                           p.tokens, p.count);
+    else
+        hipLaunchKernelGGL(kv_copy_kernel<false>, grid, dim3(kThreads), 0, stream, p, p.src, p.dst,
+                           p.tokens, p.count);
+    return hipGetLastError();
+}
+
+int kv_copy_piece_units() { return kThreads * kUnits; }
+
+hipError_t launch_kv_remap(int32_t *table, int64_t entries, const int32_t *src, const int32_t *dst,
+                           int64_t n, hipStream_t stream)
+{
+    const int64_t each = kThreads * kEntries;
+    const dim3 grid((unsigned)((entries + each - 1) / each));
+    if (n <= kListed)
+        hipLaunchKernelGGL(kv_remap_kernel<true>, grid, dim3(kThreads), (size_t)n * 4, stream,
+                           table, entries, src, dst, (int32_t)n);
+    else
+        hipLaunchKernelGGL(kv_remap_kernel<false>, grid, dim3(kThreads), 0, stream, table, entries,
+                           src, dst, (int32_t)n);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_fork(const KvForkProblem &p, hipStream_t stream)
+{
+    const int64_t clears = (2 * p.words + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
+    hipLaunchKernelGGL(kv_fork_plan_kernel, dim3((unsigned)(clears < 1 ? 1 : clears)),
+                       dim3(kPlanThreads), 0, stream, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return e;
+    if (p.cols > 0 && p.rows + p.old_rows > 0) {
+        hipLaunchKernelGGL(kv_fork_tables_kernel,
+                           dim3((unsigned)((p.cols + kThreads - 1) / kThreads),
+                                (unsigned)(p.rows + p.old_rows)),
+                           dim3(kThreads), 0, stream, p);
+        e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    const int64_t lists = (p.words + kPlanThreads - 1) / kPlanThreads;
+    hipLaunchKernelGGL(kv_fork_freed_kernel, dim3((unsigned)(lists < 1 ? 1 : lists)),
+                       dim3(kPlanThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace dps

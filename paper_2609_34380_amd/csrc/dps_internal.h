@@ -214,4 +214,66 @@ constexpr int attn_heads_a_pass(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim 
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream);
 
+// ---- sequences that branch ---------------------------------------------------------
+struct KvCopyProblem {
+    uint8_t *pool;
+    int64_t block_stride, n_blocks;
+    int32_t log2_tokens;
+    uint32_t units, key_units;  // 16-byte units of a block, and of its keys
+    int32_t row_shift;          // units of a value row: 1 << row_shift, or three times that
+    bool thirds;
+    uint32_t pieces;            // blocks of threads a pair
+    int64_t n;
+    const int32_t *src, *dst;
+    const int32_t *tokens;      // nullptr: whole blocks
+    const int32_t *count;       // device: the pairs in use; nullptr: n
+};
+int kv_copy_piece_units();
+hipError_t launch_kv_copy(const KvCopyProblem &p, hipStream_t stream);
+
+// Ids src[i] (ascending) of a table become dst[i]; n >= 1.
+hipError_t launch_kv_remap(int32_t *table, int64_t entries, const int32_t *src, const int32_t *dst,
+                           int64_t n, hipStream_t stream);
+
+constexpr int32_t kKeep = -2;  // KvForkProblem::last of a row that keeps its last block
+struct KvForkProblem {
+    const int32_t *parent;    // [rows]
+    const int32_t *seq_len;   // [old_rows]
+    const int32_t *table;     // [old_rows][cols]
+    const int32_t *fresh;
+    int64_t n_fresh;
+    int32_t rows, old_rows, cols;
+    int32_t log2_tokens;
+    int64_t n_blocks, words;  // words of 32 blocks
+    int32_t *new_table, *new_len, *src, *dst, *tokens, *freed, *counts;
+    int64_t n_freed;
+    // workspace
+    int32_t *last;            // [rows] the block that replaces the last one, or kKeep
+    uint32_t *bits;           // [2][words] blocks in the old tables, in the new ones
+};
+hipError_t launch_kv_fork(const KvForkProblem &p, hipStream_t stream);
+
+enum { BEAM_F16 = 0, BEAM_BF16 = 1, BEAM_F32 = 2 };
+struct BeamProblem {
+    const uint8_t *logits;
+    int64_t row_bytes;
+    const float *score;
+    const uint8_t *done;      // nullptr: no beam has ended
+    int64_t batch;
+    int32_t beams, vocab, keep, end;
+    int32_t pieces;           // of a row
+    float *new_score;
+    int32_t *parent, *token;
+    uint8_t *new_done;
+    // workspace, of every piece: [keep] values and indexes, the largest value and
+    // the sum of exponentials, and how many are listed
+    float *values;
+    int32_t *indexes;
+    double *sums;
+    int32_t *listed;
+};
+constexpr int kBeamVecs = 8, kBeamFewVecs = 2;  // 16-byte vectors a thread
+int64_t beam_piece(int type, int vecs);
+hipError_t launch_beam(const BeamProblem &p, int type, int vecs, hipStream_t stream);
+
 }  // namespace dps

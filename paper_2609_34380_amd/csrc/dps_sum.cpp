@@ -14,9 +14,11 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <new>
 #include <set>
+#include <utility>
 #include <vector>
 
 #include "dps.h"
@@ -184,6 +186,67 @@ DPS_EXPORT dps_status dps_sum_free(dps_sum *s, const int64_t *blocks, int64_t n,
             if (!s->evicted.empty() && wake)
                 *wake = 1;
         }
+    }
+    return DPS_OK;
+}
+
+// Compaction (the paper leaves it open): a residual returns only to a unit without
+// blocks, and blocks that outlive their neighbours keep units from getting there.
+// Units are emptied from the least used on, into the fullest ones, so that those
+// which take blocks in are never the next to be emptied while another is left.
+DPS_EXPORT dps_status dps_sum_compact(dps_sum *s, int64_t max_moves, int64_t *src, int64_t *dst,
+                                      int64_t *n)
+{
+    if (s == nullptr || n == nullptr || max_moves < 0 ||
+        (max_moves > 0 && (src == nullptr || dst == nullptr)))
+        return DPS_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lock(s->mu);
+    *n = 0;
+    try {
+        std::vector<int64_t> units(s->avail.begin(), s->avail.end());
+        std::stable_sort(units.begin(), units.end(),
+                         [&](int64_t a, int64_t b) { return s->used[a] < s->used[b]; });
+        int64_t room = 0, held = 0;
+        for (int64_t u : units) {
+            room += s->blocks_per_unit - s->used[u];
+            held += s->used[u];
+        }
+        std::vector<std::pair<int64_t, int64_t>> moves;
+        moves.reserve((size_t)std::min(max_moves, held));
+        size_t first = 0, last = units.size();  // to empty; behind the unit being filled
+        for (; first + 1 < last; ++first) {
+            const int64_t from = units[first], need = s->used[from];
+            room -= s->blocks_per_unit - need;  // its own places do not count
+            if (need > room || need > max_moves - (int64_t)moves.size())
+                break;
+            room -= need;
+            int64_t to_index = 0;
+            for (int64_t i = 0; i < s->blocks_per_unit; ++i) {
+                if (!s->taken[from][i])
+                    continue;
+                while (s->used[units[last - 1]] == s->blocks_per_unit) {
+                    --last;
+                    to_index = 0;
+                }
+                const int64_t to = units[last - 1];
+                while (s->taken[to][to_index])
+                    ++to_index;
+                s->taken[to][to_index] = 1;
+                ++s->used[to];
+                moves.emplace_back(from * s->blocks_per_unit + i,
+                                   to * s->blocks_per_unit + to_index);
+            }
+        }
+        for (int64_t u : units)
+            if (s->used[u] == s->blocks_per_unit)
+                move_unit(s, u, DPS_UNIT_FULL);
+        std::sort(moves.begin(), moves.end());
+        for (const auto &m : moves) {
+            src[*n] = m.first;
+            dst[(*n)++] = m.second;
+        }
+    } catch (...) {  // no memory for the lists, before the first change
+        return DPS_ERR_INVALID_ARG;
     }
     return DPS_OK;
 }

@@ -39,7 +39,9 @@ EXPORTED = ("dps_select_enc", "dps_split", "dps_merge", "dps_restore", "dps_back
             "dps_vmm_last_error", "dps_restore_worker_create", "dps_restore_worker_kick",
             "dps_restore_worker_wait_idle", "dps_restore_worker_restored",
             "dps_restore_worker_destroy", "dps_restore_worker_last_error",
-            "dps_kv_map", "dps_kv_store", "dps_attn_workspace_bytes", "dps_attn_decode")
+            "dps_kv_map", "dps_kv_store", "dps_attn_workspace_bytes", "dps_attn_decode",
+            "dps_kv_fork_workspace_bytes", "dps_kv_fork", "dps_kv_copy", "dps_kv_remap",
+            "dps_beam_workspace_bytes", "dps_beam_select", "dps_sum_compact")
 
 
 class DpsError(RuntimeError):
@@ -97,6 +99,22 @@ class CAttnArgs(ctypes.Structure):
                 ("req", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("window", ctypes.c_int32),
                 ("type", ctypes.c_int32), ("scale", ctypes.c_float), ("out", ctypes.c_void_p),
                 ("out_stride", ctypes.c_int64), ("lse", ctypes.c_void_p)]
+
+
+class CKvForked(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
+                ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+                ("freed", ctypes.c_void_p), ("n_freed", ctypes.c_int64),
+                ("counts", ctypes.c_void_p)]
+
+
+class CBeamArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("beams", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("end", ctypes.c_int32), ("score", ctypes.c_void_p),
+                ("done", ctypes.c_void_p), ("keep", ctypes.c_int64),
+                ("new_score", ctypes.c_void_p), ("parent", ctypes.c_void_p),
+                ("token", ctypes.c_void_p), ("new_done", ctypes.c_void_p)]
 
 
 _lib = None
@@ -199,6 +217,20 @@ def load_library(path=LIB_PATH):
     lib.dps_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.dps_attn_decode.argtypes = [P, ctypes.POINTER(CKvCache), P, ctypes.c_size_t, P]
     lib.dps_attn_decode.restype = ST
+    lib.dps_kv_fork_workspace_bytes.argtypes = [I64, I64]
+    lib.dps_kv_fork_workspace_bytes.restype = ctypes.c_size_t
+    lib.dps_kv_fork.argtypes = [P, P, I64, I32, P, I64, P, I64, I64, P, P, ctypes.c_size_t, P]
+    lib.dps_kv_fork.restype = ST
+    lib.dps_kv_copy.argtypes = [ctypes.POINTER(CKvCache), P, P, P, I64, P, P]
+    lib.dps_kv_copy.restype = ST
+    lib.dps_kv_remap.argtypes = [P, I64, P, P, I64, P]
+    lib.dps_kv_remap.restype = ST
+    lib.dps_beam_workspace_bytes.argtypes = [I64, I64, I64, I64]
+    lib.dps_beam_workspace_bytes.restype = ctypes.c_size_t
+    lib.dps_beam_select.argtypes = [P, P, ctypes.c_size_t, P]
+    lib.dps_beam_select.restype = ST
+    lib.dps_sum_compact.argtypes = [P, I64, P, P, PI64]
+    lib.dps_sum_compact.restype = ST
     lib.dps_status_str.argtypes = [ST]
     lib.dps_status_str.restype = ctypes.c_char_p
     lib.dps_last_error.argtypes = []
@@ -721,6 +753,216 @@ def attn_decode(q, cache, table, kv_len, req=None, scale=None, window=0, out=Non
     return out
 
 
+# ---- sequences that branch --------------------------------------------------------
+
+BEAM_F16, BEAM_BF16, BEAM_F32 = 0, 1, 2
+_BEAM_TYPES = {torch.float16: BEAM_F16, torch.bfloat16: BEAM_BF16, torch.float32: BEAM_F32}
+_pack_forked, _pack_beam = _packer(CKvForked), _packer(CBeamArgs)
+
+
+def _ints(name, t, dim=1):
+    """An int32 array of the current device, as the kernels take it."""
+    if not (t.dtype is _I32 and t.is_cuda and t.is_contiguous() and t.dim() == dim):
+        _require_int(name, t, _I32, dim)
+    _here(name, t)
+
+
+def _here(name, t):
+    """The calls go to the current device's stream."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s is not on the current device" % name)
+
+
+def _scratch(workspace, need, like):
+    """The workspace of a call: the caller's, or one of `need` bytes."""
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=like.device)
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    _here("workspace", workspace)
+    return workspace
+
+
+class KvFork(collections.namedtuple("KvFork", "table seq_len src dst tokens freed counts")):
+    """What kv_fork writes, int32: table [rows][columns] and seq_len [rows] of the new
+    rows; the copies to make, src, dst and tokens [rows]; freed blocks; counts [2]
+    (copies, blocks freed).  See dps_kv_forked in include/dps.h."""
+
+    def descriptor(self):
+        """The descriptor (bytes) of these buffers, checked and made once."""
+        made = self.__dict__.get("_made")
+        if made is None:
+            for name, t in zip(self._fields, self):
+                _ints(name, t, 2 if name == "table" else 1)
+            rows = self.table.shape[0]
+            for name in ("seq_len", "src", "dst", "tokens"):
+                _require(getattr(self, name).shape == (rows,), "%s differs in rows" % name)
+            _require(self.counts.shape == (2,), "counts must hold two values")
+            made = self._made = _pack_forked(
+                rows, *[t.data_ptr() for t in self[:6]], self.freed.shape[0],
+                self.counts.data_ptr())
+        return made
+
+
+def make_kv_fork(rows, columns, n_freed, device):
+    """Buffers for kv_fork: rows of the step to come, room for n_freed freed blocks."""
+    i32 = functools.partial(torch.empty, dtype=_I32, device=device)
+    return KvFork(i32((rows, columns)), i32(rows), i32(rows), i32(rows), i32(rows), i32(n_freed),
+                  i32(2))
+
+
+def kv_fork_workspace_bytes(rows, n_blocks):
+    """Workspace of kv_fork for `rows` new rows over a cache of n_blocks blocks."""
+    lib = _lib or load_library()
+    return lib.dps_kv_fork_workspace_bytes(rows, n_blocks)
+
+
+def kv_fork(parent, seq_len, table, fresh, block_tokens, n_blocks, out=None, workspace=None):
+    """Block tables after rows have branched, ended or changed places (dps_kv_fork):
+    new row r goes on from row parent[r] of `table` (int32 [old rows][columns], lengths
+    seq_len), an empty row where that is -1.  Whole blocks are shared; of a last block
+    with room in it every child but the first takes a copy, in a block off `fresh`,
+    which kv_copy makes (tokens=f.tokens, count=f.counts).  n_blocks: of the cache.
+    Returns a KvFork (out); its table is not `table`."""
+    lib = _lib or load_library()
+    for name, t, dim in (("parent", parent, 1), ("seq_len", seq_len, 1), ("fresh", fresh, 1),
+                         ("table", table, 2)):
+        _ints(name, t, dim)
+    rows, (old_rows, cols) = parent.shape[0], table.shape
+    if seq_len.shape[0] != old_rows:
+        raise ValueError("seq_len and table differ in rows")
+    if not 0 < block_tokens <= 256:
+        raise ValueError("block_tokens is out of range")
+    if out is None:
+        out = make_kv_fork(rows, cols, min(n_blocks, old_rows * cols), table.device)
+    elif out.table.shape != (rows, cols):
+        raise ValueError("out does not fit the rows, or the table's columns")
+    made = out.descriptor()
+    ws = _scratch(workspace, lib.dps_kv_fork_workspace_bytes(rows, n_blocks), table)
+    status = lib.dps_kv_fork(parent.data_ptr(), seq_len.data_ptr(), old_rows, block_tokens,
+                             table.data_ptr(), cols, fresh.data_ptr(), fresh.shape[0], n_blocks,
+                             made, ws.data_ptr(), ws.numel() * ws.element_size(), _stream())
+    if status:
+        _check(status)
+    return out
+
+
+def kv_copy(cache, src, dst, tokens=None, count=None):
+    """Copies of cache blocks (dps_kv_copy): the first tokens[i] tokens (all by default)
+    of block src[i] to block dst[i], int32 device tensors; count: an int32 device
+    tensor whose first value says how many of the pairs there are (KvFork.counts).
+    Every dst is named once, and is no src."""
+    lib = _lib or load_library()
+    _ints("src", src)
+    _ints("dst", dst)
+    n = src.shape[0]
+    if dst.shape[0] != n:
+        raise ValueError("src and dst differ in length")
+    tp = cp = None
+    if tokens is not None:
+        _ints("tokens", tokens)
+        if tokens.shape[0] != n:
+            raise ValueError("src and tokens differ in length")
+        tp = tokens.data_ptr()
+    if count is not None:
+        _ints("count", count)
+        if count.shape[0] < 1:
+            raise ValueError("count is empty")
+        cp = count.data_ptr()
+    status = lib.dps_kv_copy(cache.ref, src.data_ptr(), dst.data_ptr(), tp, n, cp, _stream())
+    if status:
+        _check(status)
+
+
+def kv_remap(table, src, dst):
+    """Block ids src[i] (ascending) of the table become dst[i], in place (dps_kv_remap):
+    the tables of a cache whose blocks kv_copy has moved."""
+    lib = _lib or load_library()
+    _ints("table", table, table.dim())
+    _ints("src", src)
+    _ints("dst", dst)
+    if src.shape != dst.shape:
+        raise ValueError("src and dst differ in length")
+    status = lib.dps_kv_remap(table.data_ptr(), table.numel(), src.data_ptr(), dst.data_ptr(),
+                              src.shape[0], _stream())
+    if status:
+        _check(status)
+    return table
+
+
+class BeamStep(collections.namedtuple("BeamStep", "score parent token done")):
+    """What beam_select writes, [batch][keep]: float32 score, int32 parent (a row of the
+    step) and token, uint8 done."""
+
+    def checked(self, shape):
+        if self.__dict__.get("_shape") != shape:
+            for name, t, dtype in zip(self._fields, self, (_F32, _I32, _I32, torch.uint8)):
+                _require(t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.shape == shape,
+                         "%s must be a contiguous %s device tensor of %s" % (name, dtype, shape))
+                _here(name, t)
+            self._shape = shape
+        return self
+
+
+def make_beam_step(batch, keep, device):
+    """Buffers for beam_select."""
+    new = functools.partial(torch.empty, (batch, keep), device=device)
+    return BeamStep(new(dtype=_F32), new(dtype=_I32), new(dtype=_I32), new(dtype=torch.uint8))
+
+
+def beam_workspace_bytes(batch, beams, vocab, keep):
+    """Workspace of beam_select."""
+    lib = _lib or load_library()
+    return lib.dps_beam_workspace_bytes(batch, beams, vocab, keep)
+
+
+def beam_select(logits, score, beams, keep=None, done=None, end=-1, out=None, workspace=None):
+    """The next beams (dps_beam_select) of logits [batch * beams][vocab] (FP16, BF16 or
+    FP32, rows contiguous): the `keep` (`beams` by default) best of score[row] +
+    log_softmax(logits[row])[token] for each request, best first, of equal ones those
+    of the lowest row and token.  score: float32, one a row; done: uint8, one a row:
+    the beam has ended and stands for itself with the token `end`.  Returns a BeamStep
+    (out); places without a candidate have score -inf, parent and token -1."""
+    lib = _lib or load_library()
+    kind = _BEAM_TYPES.get(logits.dtype)
+    if kind is None or logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be float16, bfloat16 or float32 device rows")
+    rows, vocab = logits.shape
+    keep = beams if keep is None else keep
+    if beams < 1 or rows % beams:
+        raise ValueError("rows must be a multiple of beams")
+    stride = vocab
+    if not logits.is_contiguous():
+        if logits.stride(1) != 1 and vocab > 1:
+            raise ValueError("the rows of logits must be contiguous")
+        stride = logits.stride(0) if rows > 1 else vocab
+    _here("logits", logits)
+    if not (score.dtype is _F32 and score.is_cuda and score.is_contiguous() and
+            score.shape == (rows,)):
+        raise ValueError("score must be a contiguous float32 device tensor, one entry a row")
+    _here("score", score)
+    dp = 0
+    if done is not None:
+        if not (done.dtype in (torch.uint8, torch.bool) and done.is_cuda and
+                done.is_contiguous() and done.shape == (rows,)):
+            raise ValueError("done must be a contiguous uint8 device tensor, one entry a row")
+        _here("done", done)
+        dp = done.data_ptr()
+    batch = rows // beams
+    if out is None:
+        _require(0 < keep <= 256, "keep must be in 1..256")
+        out = make_beam_step(batch, keep, logits.device)
+    out.checked((batch, keep))
+    ws = _scratch(workspace, lib.dps_beam_workspace_bytes(batch, beams, vocab, keep), logits)
+    args = _pack_beam(batch, beams, vocab, logits.data_ptr(), stride, kind, end, score.data_ptr(),
+                      dp, keep, out.score.data_ptr(), out.parent.data_ptr(), out.token.data_ptr(),
+                      out.done.data_ptr())
+    status = lib.dps_beam_select(args, ws.data_ptr(), ws.numel() * ws.element_size(), _stream())
+    if status:
+        _check(status)
+    return out
+
+
 class SumManager:
     """The SUM manager's unit bookkeeping (dps_sum_*): n_units units of
     blocks_per_unit KV blocks, residual r initially bound to unit r."""
@@ -761,6 +1003,16 @@ class SumManager:
         wake = ctypes.c_int32(0)
         _check(_lib.dps_sum_free(self._h, arr, len(blocks), ctypes.byref(wake)))
         return bool(wake.value)
+
+    def compact(self, max_moves):
+        """Moves that empty whole units (dps_sum_compact): two lists of block ids, src
+        (ascending) and dst.  dst is allocated from now on; src is freed by the caller,
+        with free(), once the blocks are copied (kv_copy) and no table names it
+        (kv_remap)."""
+        arr = ctypes.c_int64 * max(max_moves, 1)
+        src, dst, n = arr(), arr(), ctypes.c_int64(0)
+        _check(_lib.dps_sum_compact(self._h, max_moves, src, dst, ctypes.byref(n)))
+        return list(src[:n.value]), list(dst[:n.value])
 
     def restore_begin(self):
         """(residual, unit) now held for a restore, or None."""

@@ -1,0 +1,427 @@
+"""Sequences that branch, on the GPU: forked block tables, copies of blocks, tables
+after moves, and the selection of beams, against plain definitions on the CPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import DEV
+from paper_2609_34380_amd import dps
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32, E4M3 = torch.float16, torch.bfloat16, torch.float32, torch.float8_e4m3fn
+
+
+def i32(a):
+    return torch.tensor(np.array(a), dtype=torch.int32, device=DEV)
+
+
+# ---- forked tables ----------------------------------------------------------------
+
+
+def fork_oracle(parent, lens, table, fresh, tokens, n_blocks, n_freed):
+    cols = table.shape[1]
+    rows = len(parent)
+    new = np.full((rows, cols), -1)
+    out_len, copies, eldest = [], [], set()
+    for r, p in enumerate(parent):
+        if not 0 <= p < len(lens):
+            out_len.append(0)
+            continue
+        n = max(int(lens[p]), 0)
+        out_len.append(n)
+        have = min(-(-n // tokens), cols)
+        new[r, :have] = table[p, :have]
+        if n % tokens and n // tokens < cols and p in eldest:
+            block = fresh[len(copies)] if len(copies) < len(fresh) else -1
+            copies.append((table[p, n // tokens], block, n % tokens))
+            new[r, n // tokens] = block
+        eldest.add(p)
+    held = lambda t: {int(b) for b in t.reshape(-1) if 0 <= b < n_blocks}
+    freed = sorted(held(table) - held(new))
+    pad = lambda x, n: (list(x) + [-1] * n)[:n]
+    src, dst, part = (pad([c[i] for c in copies], rows) for i in range(3))
+    return [new, out_len, src, dst, part, pad(freed, n_freed), [len(copies), len(freed)]]
+
+
+def run_fork(parent, lens, table, fresh, tokens, n_blocks, n_freed=None):
+    table = np.array(table).reshape(len(lens), -1)
+    args = (i32(parent), i32(lens), i32(table).reshape(table.shape), i32(fresh), tokens, n_blocks)
+    n_freed = n_blocks if n_freed is None else n_freed
+    out = dps.make_kv_fork(len(parent), table.shape[1], n_freed, DEV)
+    need = dps.kv_fork_workspace_bytes(len(parent), n_blocks)
+    ws = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device=DEV)   # of any contents
+    want = fork_oracle(parent, lens, table, fresh, tokens, n_blocks, n_freed)
+    for _ in range(2):                                                    # and again
+        got = dps.kv_fork(*args, out=out, workspace=ws)
+        for name, a, b in zip(dps.KvFork._fields, got, want):
+            assert np.array_equal(a.cpu().numpy().reshape(-1), np.array(b).reshape(-1)), name
+    assert bool((ws[need:] == 0xA5).all())
+    assert torch.equal(args[2], i32(table).reshape(table.shape))          # the old table stays
+
+
+@pytest.mark.parametrize("old,new,tokens,longest", [
+    (1, 1, 16, 40), (1, 8, 16, 100), (8, 8, 16, 300), (65, 64, 32, 200), (33, 257, 16, 1000),
+    (256, 256, 64, 5000), (1000, 999, 16, 700), (4096, 4096, 256, 600), (1024, 4096, 16, 31),
+])
+def test_fork(old, new, tokens, longest):
+    rng = np.random.default_rng(old + new)
+    lens = rng.integers(0, longest + 1, old)
+    lens[::4] = lens[::4] // tokens * tokens        # full last blocks
+    cols = -(-longest // tokens) + 1
+    n_blocks = old * cols + new + 13
+    ids = rng.permutation(n_blocks)
+    table = ids[:old * cols].reshape(old, cols).copy()
+    for r in range(1, old):                          # neighbours share whole blocks
+        if rng.random() < 0.7:
+            n = int(min(lens[r], lens[r - 1]) // tokens)
+            table[r, :n] = table[r - 1, :n]
+    have = -(-lens // tokens)
+    table[(np.arange(cols) >= have[:, None]) & (rng.random(table.shape) < 0.8)] = -1
+    parent = rng.integers(-1, old, new)
+    parent[new // 2:] = np.sort(parent[new // 2:])
+    run_fork(parent, lens, table, ids[old * cols:], tokens, n_blocks)
+
+
+def test_fork_edges():
+    t = [[0, 1, 2], [3, 4, -1], [0, 5, -1]]
+    lens = [40, 20, 32]
+    run_fork([0, 1, 2], lens, t, [9], 16, 10)                 # every row as it was
+    run_fork([2, 1, 0], lens, t, [9], 16, 10)                 # changed places
+    run_fork([-1, 7, -5], lens, t, [9], 16, 10)               # nobody goes on
+    run_fork([0, 0, 0, 1, 1], lens, t, [9, 8], 16, 10)        # fresh runs out
+    run_fork([0, 0], lens, t, [], 16, 10)                     # no fresh block at all
+    run_fork([2, 2, 2], lens, t, [9], 16, 10)                 # full last blocks are shared
+    run_fork([0, 0], [0, 20, 32], t, [9], 16, 10)             # an empty row
+    run_fork([0, 0, 1], [48, -3, 0], t, [9], 16, 10)          # a full table row; negative
+    run_fork([0, 0, 1, 1], [49, 60, 0], t, [9], 16, 10)       # past the table's columns
+    run_fork([0, 0], [40, 20, 32], [[0, -1, -1], [3, 4, -1], [0, 5, -1]], [9], 16, 10)  # lost blocks
+    run_fork([1, 1], [40, 20, 32], [[0, 1, 2], [3, 70, -1], [0, 5, -1]], [9], 16, 10)   # outside
+    run_fork([], lens, t, [9], 16, 10)                        # no rows
+    run_fork([0, 0], lens, t, [9], 16, 10, n_freed=1)         # no room for all freed
+    run_fork([0, 0], lens, t, [9], 16, 10, n_freed=0)
+    run_fork([0, 0], lens, t, [9], 16, 0)                     # no blocks to list
+    run_fork([0, 1], [4, 5], np.zeros((2, 0)), [9], 16, 10)   # tables without columns
+    run_fork([0, 0, -1], [2 ** 31 - 1, 5, 0], t, [9], 16, 10)
+
+
+def test_fork_many_blocks():
+    """More words of bits than one block of threads lists: ids up to 200000."""
+    rng = np.random.default_rng(5)
+    ids = rng.permutation(200000)
+    table = ids[:40 * 1000].reshape(40, 1000)
+    run_fork(np.arange(40) // 2, np.full(40, 15990), table, ids[40000:40100], 16, 200000)
+
+
+# ---- copies and moves ---------------------------------------------------------------
+
+COPIES = [
+    # dtype, dim, kv_heads, tokens, offset, gap
+    (F16, 128, 8, 16, 0, 0), (F16, 64, 3, 32, 16, 48), (BF16, 96, 5, 16, 0, 0),
+    (F16, 192, 1, 64, 0, 16), (BF16, 256, 2, 256, 0, 0), (E4M3, 64, 1, 16, 32, 0),
+    (E4M3, 128, 8, 128, 0, 0), (E4M3, 192, 3, 16, 0, 0), (E4M3, 256, 1, 32, 0, 0),
+]
+
+
+def places(dtype, dim, kv_heads, tokens, n):
+    """Byte places in a block of its first n tokens' keys and values."""
+    row = dim * dtype.itemsize
+    h, t, byte = np.ix_(np.arange(kv_heads), np.arange(n), np.arange(row))
+    k = (h * (row // 64) + byte // 64) * tokens * 64 + t * 64 + byte % 64
+    v = ((kv_heads + h) * tokens + t) * row + byte
+    return np.concatenate((k.reshape(-1), v.reshape(-1)))
+
+
+@pytest.mark.parametrize("dtype,dim,kv_heads,tokens,offset,gap", COPIES)
+@pytest.mark.parametrize("part", [False, True])
+def test_copy(dtype, dim, kv_heads, tokens, offset, gap, part):
+    rng = np.random.default_rng(dim + tokens)
+    blocks, size = 23, 2 * kv_heads * tokens * dim * dtype.itemsize
+    stride = size + gap
+    host = rng.integers(0, 256, offset + (blocks - 1) * stride + size, dtype=np.uint8)
+    pool = torch.tensor(host, device=DEV)
+    cache = dps.KvCache(pool, tokens, kv_heads, dim, dtype, offset=offset, block_stride=stride)
+    assert cache.n_blocks == blocks
+    src = np.array([0, 22, 5, 0, 7, -1, 9, 23, 10, 6])
+    dst = np.array([1, 2, 21, 4, 7, 11, -1, 12, 30, 8])
+    n = np.array([tokens, 1, tokens - 1, tokens // 2 + 1, 3, 2, 2, 2, 2, 0])
+    want = host.copy()
+    for s, d, m in zip(src, dst, n if part else np.full(10, tokens)):
+        if 0 <= s < blocks and 0 <= d < blocks and s != d:
+            at = places(dtype, dim, kv_heads, tokens, m)
+            want[offset + d * stride + at] = host[offset + s * stride + at]
+    dps.kv_copy(cache, i32(src), i32(dst), tokens=i32(n) if part else None)
+    assert np.array_equal(pool.cpu().numpy(), want)
+
+
+def test_copy_counts():
+    """Only the first *count pairs; token counts past a block's and below 0."""
+    host = np.arange(6 * 4096, dtype=np.int64).astype(np.uint8) ^ np.repeat(np.arange(6), 4096).astype(np.uint8)
+    args = (16, 1, 64, F16)
+    for count, part in ((0, None), (1, None), (2, [99, -4]), (9, [16, 3])):
+        pool = torch.tensor(host, device=DEV)
+        cache = dps.KvCache(pool, *args)
+        dps.kv_copy(cache, i32([0, 1]), i32([4, 5]), tokens=None if part is None else i32(part),
+                    count=i32([count, 77]))
+        want = host.copy()
+        for i in range(min(count, 2)):
+            m = 16 if part is None else min(max(part[i], 0), 16)
+            at = places(F16, 64, 1, 16, m)
+            want[(4 + i) * 4096 + at] = host[i * 4096 + at]
+        assert np.array_equal(pool.cpu().numpy(), want), count
+    none = i32([])
+    dps.kv_copy(cache, none, none, tokens=none)
+
+
+@pytest.mark.parametrize("rows,cols,moves", [(1, 1, 1), (3, 7, 2), (17, 61, 40), (300, 513, 3000),
+                                             (64, 64, 12288), (50, 99, 12289), (9, 1000, 40000)])
+def test_remap(rows, cols, moves):
+    rng = np.random.default_rng(rows + moves)
+    ids = rng.permutation(3 * moves + 50)
+    src, dst = np.sort(ids[:moves]), ids[moves:2 * moves]
+    table = rng.integers(-2, 3 * moves + 60, (rows, cols))
+    to = np.arange(3 * moves + 60)
+    to[src] = dst
+    t = i32(table)
+    dps.kv_remap(t, i32(src), i32(dst))
+    assert np.array_equal(t.cpu().numpy(), np.where(table >= 0, to[table.clip(0)], table))
+
+
+def test_remap_swaps():
+    """All at once: an id that is both src and dst."""
+    t = i32([5, 1, 2, -1, 9, 0x7fffffff])
+    dps.kv_remap(t, i32([1, 5, 0x7fffffff]), i32([5, 1, 3]))
+    assert t.tolist() == [1, 5, 2, -1, 9, 3]
+    dps.kv_remap(t, i32([]), i32([]))
+
+
+def test_fork_and_copy_in_a_graph():
+    """A captured step replayed on other parents: every replay as the eager call."""
+    rng = np.random.default_rng(9)
+    rows, cols, tokens, n_blocks = 12, 9, 16, 200
+    ids = rng.permutation(n_blocks)
+    table = i32(ids[:rows * cols]).reshape(rows, cols)
+    lens = rng.integers(1, cols * tokens, rows)
+    seq, parent = i32(lens), i32(np.arange(rows))
+    fresh = i32(ids[rows * cols:])
+    host = rng.integers(0, 256, n_blocks * 4096, dtype=np.uint8)
+    pool = torch.tensor(host, device=DEV)
+    cache = dps.KvCache(pool, tokens, 1, 64, F16)
+    out = dps.make_kv_fork(rows, cols, n_blocks, DEV)
+    ws = torch.empty(dps.kv_fork_workspace_bytes(rows, n_blocks), dtype=torch.uint8, device=DEV)
+
+    def step():
+        f = dps.kv_fork(parent, seq, table, fresh, tokens, n_blocks, out=out, workspace=ws)
+        dps.kv_copy(cache, f.src, f.dst, tokens=f.tokens, count=f.counts)
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for _ in range(4):
+        p = rng.integers(-1, rows, rows)
+        parent.copy_(i32(p))
+        pool.copy_(torch.tensor(host))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = fork_oracle(p, lens, table.cpu().numpy(), fresh.cpu().numpy(), tokens, n_blocks,
+                           n_blocks)
+        for name, a, b in zip(dps.KvFork._fields, out, want):
+            assert np.array_equal(a.cpu().numpy().reshape(-1), np.array(b).reshape(-1)), name
+        moved = host.copy()
+        for s, d, m in zip(*want[2:5]):
+            if s >= 0:
+                at = places(F16, 64, 1, tokens, m)
+                moved[d * 4096 + at] = host[s * 4096 + at]
+        assert np.array_equal(pool.cpu().numpy(), moved)
+
+
+# ---- beams ------------------------------------------------------------------------
+
+
+def beam_oracle(x, score, beams, keep, done, end):
+    """In 64 bits; x [rows][vocab] float64."""
+    rows, vocab = x.shape
+    out = []
+    for b in range(rows // beams):
+        cand = []
+        for w in range(beams):
+            r = b * beams + w
+            s = np.float64(score[r])
+            if not np.isfinite(s):
+                continue
+            if done is not None and done[r]:
+                cand.append(np.array([[s], [w * vocab + end]]))
+                continue
+            row = x[r]
+            if np.isnan(row).any() or (row == np.inf).any() or (row == -np.inf).all():
+                continue
+            top = row.max()
+            lse = top + np.log(np.exp(row - top).sum())
+            t = np.flatnonzero(row > -np.inf)
+            cand.append(np.stack((s + (row[t] - lse), w * vocab + t)))
+        cand = np.concatenate(cand, 1) if cand else np.zeros((2, 0))
+        order = np.lexsort((cand[1], -cand[0]))[:keep]
+        s, at = cand[0][order], cand[1][order].astype(np.int64)
+        pad = keep - len(s)
+        parent, token = b * beams + at // vocab, at % vocab
+        ended = (token == end) | (False if done is None else np.array(done)[parent] != 0)
+        out.append((np.pad(s, (0, pad), constant_values=-np.inf),
+                    np.pad(parent, (0, pad), constant_values=-1),
+                    np.pad(token, (0, pad), constant_values=-1),
+                    np.pad(ended.astype(np.uint8), (0, pad))))
+    return [np.stack(o) for o in zip(*out)]
+
+
+def run_beam(x, score, beams, keep, done=None, end=-1, stride=None, offset=0):
+    """x: a CPU tensor of the logits' type."""
+    rows, vocab = x.shape
+    stride = vocab if stride is None else stride
+    room = torch.full((offset + rows * stride + 64,), float("nan"), dtype=x.dtype, device=DEV)
+    logits = room[offset:offset + rows * stride].view(rows, stride)[:, :vocab]
+    logits.copy_(x)
+    score = np.asarray(score, dtype=np.float32)
+    out = dps.make_beam_step(rows // beams, keep, DEV)
+    need = dps.beam_workspace_bytes(rows // beams, beams, vocab, keep)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    d = None if done is None else torch.tensor(done, dtype=torch.uint8, device=DEV)
+    got = [t.cpu().numpy() for t in dps.beam_select(logits, torch.tensor(score, device=DEV), beams,
+                                                    keep=keep, done=d, end=end, out=out,
+                                                    workspace=ws)]
+    want = beam_oracle(x.double().numpy(), score, beams, keep, done, end)
+    assert np.array_equal(got[1], want[1]) and np.array_equal(got[2], want[2])
+    assert np.array_equal(got[3], want[3])
+    fine = np.isfinite(want[0])
+    assert np.array_equal(got[0][~fine], want[0][~fine])
+    # the sum's 2^-21, and the rounding to fp32
+    bound = 2.0 ** -21 * (1 + 2.0 ** -8) + 2.0 ** -24 * np.abs(want[0][fine])
+    assert (np.abs(got[0][fine] - want[0][fine]) <= bound).all()
+    assert bool((ws[need:] == 0xFF).all())
+
+
+def rnd(*shape, seed=0, scale=3.0):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * scale
+
+
+BEAMS = [
+    # batch, beams, vocab, keep, dtype
+    (1, 1, 1, 1, F16), (1, 1, 1, 5, F32), (2, 3, 2, 6, BF16), (1, 4, 31, 4, F16),
+    (3, 2, 257, 2, F32), (1, 4, 4096, 4, F16), (1, 4, 4097, 8, BF16), (5, 1, 2049, 16, F32),
+    (2, 8, 16384, 8, F16), (1, 5, 16385, 10, F16), (7, 4, 32000, 8, BF16), (1, 40, 8191, 80, F16),
+    (40, 8, 10007, 16, BF16), (64, 8, 20001, 8, F16), (64, 16, 9000, 9, F32), (3, 33, 5000, 256, F16),
+    (1, 1, 70000, 256, F32), (300, 2, 515, 4, F16), (1, 1024, 90, 30, F32), (2, 6, 262144, 12, BF16),
+]
+
+
+@pytest.mark.parametrize("batch,beams,vocab,keep,dtype", BEAMS)
+def test_beams(batch, beams, vocab, keep, dtype):
+    """Types, sizes, both widths of a piece; values of 16 bits come with ties."""
+    rows = batch * beams
+    x = rnd(rows, vocab, seed=vocab + rows).to(dtype)
+    score = -10 * np.random.default_rng(rows).random(rows)
+    run_beam(x, score, beams, keep)
+
+
+@pytest.mark.parametrize("dtype,stride,offset", [(F16, 1003, 3), (BF16, 1001, 1), (F32, 1002, 1),
+                                                 (F32, 1005, 3), (F16, 1007, 7)])
+def test_beam_rows_anywhere(dtype, stride, offset):
+    x = rnd(12, 1001, seed=stride).to(dtype)
+    run_beam(x, -rnd(12, seed=1).abs().numpy(), 4, 8, stride=stride, offset=offset)
+
+
+def test_beam_ended():
+    x = rnd(24, 700, seed=3).to(F16)
+    score = -8 * np.random.default_rng(4).random(24)
+    done = np.random.default_rng(5).random(24) < 0.4
+    run_beam(x, score, 8, 8, done=done, end=2)
+    run_beam(x, score, 8, 16, done=np.ones(24), end=699)      # nothing else is left
+    run_beam(x, score, 6, 9, done=np.zeros(24), end=0)
+    run_beam(x, score, 6, 9, end=5)                           # ends without rows at their end
+
+
+def test_beam_first_step():
+    """All beams alike: one of them has a score."""
+    x = rnd(1, 5000, seed=8).to(F32).repeat(6, 1)
+    run_beam(x, [0.0] + [-math.inf] * 5, 6, 6)
+    run_beam(x, [math.nan, math.inf, -math.inf, -1.0, -math.inf, -2.0], 6, 6)
+    run_beam(x, [-math.inf] * 6, 3, 6)                        # no beam at all
+    run_beam(x, [-1.0] * 6, 3, 50)                            # equal beams: ties of rows
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_beam_masks(dtype):
+    """-inf, the lowest value, rows without a token, NaN and infinities."""
+    least = torch.finfo(dtype).min
+    x = rnd(16, 9001, seed=11).to(dtype)
+    few = torch.rand(16, 9001, generator=torch.Generator().manual_seed(2)) < 0.0005
+    x[0:4] = torch.where(few[0:4], x[0:4], float("-inf"))
+    x[4:8] = torch.where(few[4:8], x[4:8], least)
+    x[8] = float("-inf")
+    x[9] = least
+    x[10, 77] = float("nan")
+    x[11, 8000] = float("inf")
+    x[12, :] = 0.0
+    x[12, 100:] = -0.0
+    x[13, 5:] = float("-inf")
+    score = -np.random.default_rng(6).random(16)
+    for beams, keep in ((4, 4), (4, 9), (16, 256), (1, 7), (1, 200)):
+        run_beam(x, score, beams, keep)
+
+
+@pytest.mark.parametrize("vocab", [5000, 40000])
+def test_beam_many_ties(vocab):
+    """More of equal values than the list holds: the first ones are taken."""
+    rng = np.random.default_rng(vocab)
+    x = torch.tensor(rng.integers(0, 2, (600, vocab)), dtype=F16)      # wide pieces
+    run_beam(x, np.repeat(-rng.random(75), 8), 8, 16)
+    x = torch.tensor(rng.integers(0, 2, (8, vocab)), dtype=F32) * 3
+    run_beam(x, np.full(8, -2.0), 8, 256)
+    run_beam(torch.zeros(4, vocab, dtype=BF16), np.full(4, -1.5), 4, 33)
+    x = torch.arange(vocab, dtype=F32).repeat(3, 1) / 64                # in order, either way
+    run_beam(x, [-1.0, -1.25, -1.5], 3, 100)
+    run_beam(x.flip(1), [-1.0, -1.25, -1.5], 3, 100)
+
+
+def test_beam_far_scores():
+    """Scores of any size, and logits far apart."""
+    x = rnd(8, 3001, seed=21, scale=3000.0).to(F16)
+    run_beam(x, [-1e5, -1e5 - 1, -9e4, 0, 12, -7, -3e4, 1e4], 4, 8)
+    run_beam(rnd(8, 3001, seed=22, scale=1e6), [-1.0] * 8, 8, 40)
+
+
+def test_beam_in_a_graph():
+    x = rnd(16, 6000, seed=31).to(BF16).to(DEV)
+    score = torch.zeros(16, device=DEV)
+    done = torch.zeros(16, dtype=torch.uint8, device=DEV)
+    out = dps.make_beam_step(2, 8, DEV)
+    ws = torch.empty(dps.beam_workspace_bytes(2, 8, 6000, 8), dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    call = lambda: dps.beam_select(x, score, 8, done=done, end=3, out=out, workspace=ws)
+    with torch.cuda.stream(stream):
+        call()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call()
+    rng = np.random.default_rng(1)
+    for t in range(4):
+        s, d = -rng.random(16).astype(np.float32), (rng.random(16) < 0.3).astype(np.uint8)
+        x.copy_(rnd(16, 6000, seed=40 + t).to(BF16))
+        score.copy_(torch.tensor(s))
+        done.copy_(torch.tensor(d))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = beam_oracle(x.double().cpu().numpy(), s, 8, 8, d, 3)
+        for a, b in zip(out[1:], want[1:]):
+            assert np.array_equal(a.cpu().numpy(), b)
