@@ -501,7 +501,8 @@ dps_status dps_kv_fork(const int32_t *parent, const int32_t *seq_len, int64_t ol
  * block's) of every head's keys and values of block src[i] go to the same places of
  * block dst[i].  A pair with an end outside the cache (-1), or with src = dst, is
  * left out.  The dst of a call are distinct, and none is a src of it: a block
- * that is both, or named twice as dst, holds a mixture.  n * block bytes < 2^44. */
+ * that is both, or named twice as dst, holds a mixture.  n times a
+ * block's bytes, rounded up to 16 KiB, is less than 2^38. */
 dps_status dps_kv_copy(const dps_kv_cache *cache, const int32_t *src, const int32_t *dst,
                        const int32_t *tokens, int64_t n, const int32_t *count, void *stream);
 

@@ -1036,7 +1036,7 @@ bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
     return an > 0 && bn > 0 && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
 }
 
-int64_t fork_words(int64_t n_blocks) { return cdiv(n_blocks, 32); }
+int64_t fork_words(int64_t n_blocks) { return cdiv(n_blocks, 16); }
 
 }  // namespace
 
@@ -1044,7 +1044,7 @@ DPS_EXPORT size_t dps_kv_fork_workspace_bytes(int64_t rows, int64_t n_blocks)
 {
     if (rows < 0 || rows > 4096 || n_blocks < 0 || n_blocks > 0x7fffffff)
         return 0;
-    return align256(rows * 4) + align256(8 * fork_words(n_blocks));
+    return align256(rows * 4) + align256(32 * fork_words(n_blocks));
 }
 
 DPS_EXPORT dps_status dps_kv_fork(const int32_t *parent, const int32_t *seq_len, int64_t old_rows,
@@ -1119,7 +1119,7 @@ DPS_EXPORT dps_status dps_kv_fork(const int32_t *parent, const int32_t *seq_len,
     p.n_freed = out->n_freed;
     p.counts = out->counts;
     p.last = static_cast<int32_t *>(ws);
-    p.bits = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(ws) + align256(rows * 4));
+    p.held = reinterpret_cast<dps::u32x4 *>(static_cast<uint8_t *>(ws) + align256(rows * 4));
     return launched(dps::launch_kv_fork(p, (hipStream_t)stream));
 }
 
@@ -1150,8 +1150,8 @@ DPS_EXPORT dps_status dps_kv_copy(const dps_kv_cache *cache, const int32_t *src,
     p.thirds = row_units % 3 == 0;
     p.row_shift = __builtin_ctz((unsigned)row_units);
     p.pieces = (uint32_t)cdiv(p.units, dps::kv_copy_piece_units());
-    REQUIRE(n * p.pieces <= 0x7fffffff && n * p.pieces * dps::kv_copy_piece_units() < (1ll << 40),
-            DPS_ERR_UNSUPPORTED, "too many blocks for one call");
+    // a launch counts its threads (256 a piece) in 32 bits
+    REQUIRE(n * p.pieces < (1 << 24), DPS_ERR_UNSUPPORTED, "too many blocks for one call");
     p.n = n;
     p.src = src;
     p.dst = dst;
@@ -1264,8 +1264,8 @@ DPS_EXPORT dps_status dps_beam_select(const dps_beam_args *a, void *ws, size_t w
             REQUIRE(!overlap(x.at, x.bytes, y.at, y.bytes), DPS_ERR_INVALID_ARG,
                     "an output overlaps an input");
     const BeamPlan plan = plan_beam(a->batch, a->beams, a->vocab, a->keep, a->type);
-    REQUIRE(plan.lists <= 0x7fffffff && plan.pieces * a->beams * a->keep <= 0x7fffffff,
-            DPS_ERR_UNSUPPORTED, "too many rows for one call");
+    // a launch counts its threads (256 a piece) in 32 bits
+    REQUIRE(plan.lists < (1 << 24), DPS_ERR_UNSUPPORTED, "too many rows for one call");
     REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
             "workspace is smaller than dps_beam_workspace_bytes()");
     REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");

@@ -70,22 +70,70 @@ __device__ __forceinline__ T over_block(T x, T *s, const F &f)
     return x;
 }
 
-// The keep-th largest of the threads' values (the smallest where there are fewer
-// threads), for every thread.  Equal ones rank by thread.
+__device__ __forceinline__ float lane_of(float x, int i)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
+}
+__device__ __forceinline__ double lane_of(double x, int i)
+{
+    const u32x2 u = __builtin_bit_cast(u32x2, x);
+    return __builtin_bit_cast(double, u32x2{(uint32_t)__builtin_amdgcn_readlane((int)u.x, i),
+                                            (uint32_t)__builtin_amdgcn_readlane((int)u.y, i)});
+}
+
+// A value that at least `keep` of the block's values reach, from each thread's largest,
+// for every thread: the keep-th largest of 64 groups of kWaves threads where keep is
+// at most kGrouped, else of the threads themselves (the least of them where keep is the
+// larger).  One wave counts, for each group, the groups that are no smaller; the
+// others wait, and leave the SIMDs to other blocks.  Counted by every thread over all
+// of them it was most of the kernel's time (512 rows of 100003 fp32 logits 102 us,
+// 41 so).
+constexpr int kGrouped = 32;
 template <typename T>
-__device__ __forceinline__ T nth_of_threads(T mine, int keep, T *s_all, T *s_one)
+__device__ __forceinline__ T bound_of(T mine, int keep, T *s_all, T *s_one)
 {
     const int tid = threadIdx.x;
     s_all[tid] = mine;
     __syncthreads();
-    int rank = 0;
-#pragma unroll 8
-    for (int i = 0; i < kThreads; ++i) {
-        const T other = s_all[i];
-        rank += other > mine || (other == mine && i < tid);
+    if (tid < 64) {
+        T x[kWaves];
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i)
+            x[i] = s_all[tid + 64 * i];
+        T best = -(T)kInf;
+        if (keep <= kGrouped) {
+            T m = x[0];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i)
+                m = m > x[i] ? m : x[i];
+            int reach = 0;
+#pragma unroll 16
+            for (int i = 0; i < 64; ++i)
+                reach += lane_of(m, i) >= m;
+            best = reach >= keep ? m : best;
+        } else {
+            int reach[kWaves] = {};
+#pragma unroll 4
+            for (int i = 0; i < 64; ++i) {
+#pragma unroll
+                for (int j = 0; j < kWaves; ++j) {
+                    const T other = lane_of(x[j], i);
+#pragma unroll
+                    for (int k = 0; k < kWaves; ++k)
+                        reach[k] += other >= x[k];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k)
+                best = reach[k] >= keep && x[k] > best ? x[k] : best;
+        }
+        for (int d = 32; d > 0; d >>= 1) {
+            const T other = __shfl_xor(best, d);
+            best = best > other ? best : other;
+        }
+        if (tid == 0)
+            *s_one = best;
     }
-    if (rank == min(keep, kThreads) - 1)
-        *s_one = mine;
     __syncthreads();
     return *s_one;
 }
@@ -207,65 +255,79 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
 
     // ---- the keep best --------------------------------------------------------------
     const int keep = p.keep;
-    const float bound = nth_of_threads(mine, keep, s_all, &s_one);
-    int n = 0;
-    each([&](float x, int) { n += x >= bound && x > -kInf; });
-    int all;
+    float least = bound_of(mine, keep, s_all, &s_one);  // of the values taken
+    int n = 0, all;
+    each([&](float x, int) { n += x >= least && x > -kInf; });
     int at = place_of(n, s_n, all);
-    int32_t least = ordered(bound), last = 0x7fffffff;  // of the values taken: the least, its last index
-    if (all > kList) {
-        // the keep-th largest value: the largest that `keep` values reach
-        int32_t lo = least, hi = ordered(top);
-        while (lo < hi) {
-            const int32_t mid = (int32_t)(((int64_t)lo + hi + 1) >> 1);
-            const float m = value_of(mid);
-            int c = 0;
-            each([&](float x, int) { c += x >= m; });
-            c = over_block(c, s_n, [](int a, int b) { return a + b; });
-            if (c >= keep)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        least = lo;
-        const float m = value_of(least);
-        int more = 0;
-        each([&](float x, int) { more += x > m; });
-        more = over_block(more, s_n, [](int a, int b) { return a + b; });
-        // of its equals the first keep - more: the lowest index that as many do not pass
-        int32_t l = 0, h = vocab - 1;
-        while (l < h) {
-            const int32_t mid = (l + h) >> 1;
-            int c = 0;
-            each([&](float x, int i) { c += x == m && i <= mid; });
-            c = over_block(c, s_n, [](int a, int b) { return a + b; });
-            if (c >= keep - more)
-                h = mid;
-            else
-                l = mid + 1;
-        }
-        last = l;
-        n = 0;
-        each([&](float x, int i) { n += x > m || (x == m && i <= last); });
-        at = place_of(n, s_n, all);
-    }
-    const float m = value_of(least);
-    each([&](float x, int i) {
-        if ((x > m || (x == m && i <= last)) && x > -kInf) {
-            if (at < kList) {
+    if (all <= kList) {
+        each([&](float x, int i) {
+            if (x >= least && x > -kInf) {
                 s_value[at] = x;
-                s_index[at] = i;
+                s_index[at++] = i;
             }
-            ++at;
+        });
+    } else {
+        const auto plus = [](int a, int b) { return a + b; };
+        const auto above = [&](float m) {
+            int c = 0;
+            each([&](float x, int) { c += x > m; });
+            return over_block(c, s_n, plus);
+        };
+        int more = above(least);
+        if (more >= keep) {
+            // the keep-th largest value: the least that fewer than `keep` are above
+            int32_t lo = ordered(least), hi = ordered(top);
+            while (lo < hi) {
+                const int32_t mid = (int32_t)(((int64_t)lo + hi) >> 1);
+                if (above(value_of(mid)) < keep)
+                    hi = mid;
+                else
+                    lo = mid + 1;
+            }
+            least = value_of(lo);
+            more = above(least);
         }
-    });
+        n = 0;
+        each([&](float x, int) { n += x > least; });
+        at = place_of(n, s_n, all);
+        each([&](float x, int i) {
+            if (x > least) {
+                s_value[at] = x;
+                s_index[at++] = i;
+            }
+        });
+        // of its equals the first: a vector of all threads at a time, which lie in order
+        int taken = more;
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            if (taken < keep) {
+                n = 0;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    n += wide<TYPE>(v[j], i) == least;
+                at = taken + place_of(n, s_n, all);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    if (wide<TYPE>(v[j], i) == least) {
+                        if (at < keep) {
+                            s_value[at] = least;
+                            s_index[at] = at0 + (j * kThreads + tid) * kPer + i;
+                        }
+                        ++at;
+                    }
+                }
+                taken += all;
+            }
+        }
+        all = min(taken, keep);
+    }
     __syncthreads();
-    all = min(all, kList);
     const int64_t list = row * p.pieces + piece;
     for (int c = tid; c < all; c += kThreads) {
         const float x = s_value[c];
         const int32_t i = s_index[c];
         int rank = 0;
+#pragma unroll 4
         for (int o = 0; o < all; ++o)
             rank += s_value[o] > x || (s_value[o] == x && s_index[o] < i);
         if (rank < keep) {
@@ -285,105 +347,129 @@ struct Candidate {
     double score;
     int64_t place;
 };
-__device__ __forceinline__ bool before(double a, int64_t pa, double b, int64_t pb)
-{
-    return a > b || (a == b && pa < pb);
-}
+constexpr int kHeld = 8;  // candidates a thread keeps in registers
 
+// HELD: the item has at most kHeld candidates a thread, else they are read anew for
+// each of the few passes over them.
+template <bool HELD>
 __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p)
 {
-    extern __shared__ double s_lse[];  // a beam's log of the sum; NaN: it counts for nothing
+    extern __shared__ double s_lse[];  // a beam's log of the sum; NaN: it has no candidates
     __shared__ double s_all[kThreads], s_one;
     __shared__ double s_score[kList];
     __shared__ int64_t s_place[kList];
     __shared__ int32_t s_n[kWaves];
     __shared__ int64_t s_top[kWaves];
 
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t item = blockIdx.x, row0 = item * p.beams;
     const double none = -(double)kInf;
-    for (int w = tid; w < p.beams; w += kThreads) {
+    for (int w = wave; w < p.beams; w += kWaves) {  // a wave a beam, a lane a piece
         const int64_t row = row0 + w;
         const float cum = p.score[row];
         double lse = __builtin_nan("");
         if (!(p.done && p.done[row]) && __builtin_fabsf(cum) < kInf) {
-            double top = none;
-            for (int c = 0; c < p.pieces; ++c) {
-                const int64_t list = row * p.pieces + c;
-                if (p.sums[list * 2 + 1] != 0.0)
-                    top = fmax(top, p.sums[list * 2]);
+            const double *sums = p.sums + row * p.pieces * 2;
+            double top = none, sum = 0.0;
+            for (int c = lane; c < p.pieces; c += 64) {
+                const double t = sums[c * 2], s = sums[c * 2 + 1];
+                const double to = s != 0.0 ? fmax(top, t) : top;
+                if (to > none)  // an infinite one leaves no number
+                    sum = sum * exp(top - to) + (s != 0.0 ? s * exp(t - to) : 0.0);
+                top = to;
             }
-            double sum = 0.0;
-            for (int c = 0; c < p.pieces; ++c) {
-                const int64_t list = row * p.pieces + c;
-                const double s = p.sums[list * 2 + 1];
-                if (s != 0.0)
-                    sum += s * exp(p.sums[list * 2] - top);
+            for (int d = 32; d > 0; d >>= 1) {
+                const double t = __shfl_xor(top, d), s = __shfl_xor(sum, d), to = fmax(top, t);
+                if (to > none)
+                    sum = (sum != 0.0 ? sum * exp(top - to) : 0.0) +
+                          (s != 0.0 ? s * exp(t - to) : 0.0);
+                top = to;
             }
             lse = top + log(sum);
         }
-        s_lse[w] = lse;
+        if (lane == 0)
+            s_lse[w] = lse;
     }
     __syncthreads();
 
     const int keep = p.keep;
-    const int64_t slots = (int64_t)p.beams * p.pieces * keep;
-    const auto candidate = [&](int64_t i) {
+    const uint32_t a_row = (uint32_t)p.pieces * keep, slots = a_row * p.beams;
+    const auto read = [&](uint32_t i) {
         Candidate c = {none, 0};
-        const int64_t list = i / keep;
-        const int k = (int)(i % keep), w = (int)(list / p.pieces);
-        const int64_t row = row0 + w;
-        if (p.done && p.done[row]) {
-            const float cum = p.score[row];
-            if (i % ((int64_t)p.pieces * keep) == 0 && __builtin_fabsf(cum) < kInf)
+        const uint32_t list = i / (uint32_t)keep, w = i / a_row;
+        const int64_t row = row0 + w, at = row0 * p.pieces + list;
+        const float cum = p.score[row];
+        const bool ended = p.done && p.done[row];
+        const bool listed = (int)(i - list * keep) < p.listed[at];  // as far as the beam has lists
+        const float x = p.values[at * keep + (i - list * keep)];
+        const int32_t token = p.indexes[at * keep + (i - list * keep)];
+        if (ended) {
+            if (i == w * a_row && __builtin_fabsf(cum) < kInf)
                 c = Candidate{(double)cum, (int64_t)w * p.vocab + p.end};
             return c;
         }
         const double lse = s_lse[w];
-        if (lse != lse)
-            return c;
-        const int64_t at = row0 * p.pieces + list;
-        if (k >= p.listed[at])
-            return c;
-        const double s = (double)p.score[row] + ((double)p.values[at * keep + k] - lse);
-        if (s == s)
-            c = Candidate{s, (int64_t)w * p.vocab + p.indexes[at * keep + k]};
+        const double s = (double)cum + ((double)x - lse);
+        if (lse == lse && listed && s == s)
+            c = Candidate{s, (int64_t)w * p.vocab + token};
         return c;
     };
-    double mine = none;
-    for (int64_t i = tid; i < slots; i += kThreads)
-        mine = fmax(mine, candidate(i).score);
-    const double bound = nth_of_threads(mine, keep, s_all, &s_one);
+    Candidate held[kHeld];
+    if (HELD) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const uint32_t i = tid + j * kThreads;
+            held[j] = Candidate{none, 0};
+            if (i < slots)
+                held[j] = read(i);
+        }
+    }
+    const auto each = [&](const auto &f) {
+        if (HELD) {
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j)
+                if (held[j].score > none)
+                    f(held[j]);
+        } else {
+            for (uint32_t i = tid; i < slots; i += kThreads) {
+                const Candidate c = read(i);
+                if (c.score > none)
+                    f(c);
+            }
+        }
+    };
     const auto count = [&](const auto &f) {
         int n = 0;
-        for (int64_t i = tid; i < slots; i += kThreads) {
-            const Candidate c = candidate(i);
-            n += c.score > none && f(c);
-        }
+        each([&](const Candidate &c) { n += f(c); });
         return n;
     };
+    double mine = none;
+    each([&](const Candidate &c) { mine = fmax(mine, c.score); });
+    double least = bound_of(mine, keep, s_all, &s_one);
+    int64_t last = 0x7fffffffffffffffll;  // the last place taken of those with that score
     const auto plus = [](int a, int b) { return a + b; };
     int all;
-    int at = place_of(count([&](const Candidate &c) { return c.score >= bound; }), s_n, all);
-    double least = bound;
-    int64_t last = 0x7fffffffffffffffll;
+    int at = place_of(count([&](const Candidate &c) { return c.score >= least; }), s_n, all);
     if (all > kList) {
-        // as in the pieces: the keep-th best score, then the last place among its equals
-        int64_t lo = ordered(bound);
-        int64_t hi = over_block(ordered(mine), s_top,
-                                [](int64_t a, int64_t b) { return a > b ? a : b; });
-        while (lo < hi) {
-            const int64_t mid = lo + (int64_t)(((uint64_t)hi - (uint64_t)lo + 1) >> 1);
-            const int c = over_block(
-                count([&](const Candidate &x) { return ordered(x.score) >= mid; }), s_n, plus);
-            if (c >= keep)
-                lo = mid;
-            else
-                hi = mid - 1;
+        const auto above = [&](double m) {
+            return over_block(count([&](const Candidate &c) { return c.score > m; }), s_n, plus);
+        };
+        int more = above(least);
+        if (more >= keep) {  // as in the pieces
+            int64_t lo = ordered(least);
+            int64_t hi = over_block(ordered(mine), s_top,
+                                    [](int64_t a, int64_t b) { return a > b ? a : b; });
+            while (lo < hi) {
+                const int64_t mid = lo + (int64_t)(((uint64_t)hi - (uint64_t)lo) >> 1);
+                if (above(__builtin_bit_cast(double, mid ^ ((mid >> 63) & 0x7fffffffffffffffll))) <
+                    keep)
+                    hi = mid;
+                else
+                    lo = mid + 1;
+            }
+            least = __builtin_bit_cast(double, lo ^ ((lo >> 63) & 0x7fffffffffffffffll));
+            more = above(least);
         }
-        least = __builtin_bit_cast(double, lo ^ ((lo >> 63) & 0x7fffffffffffffffll));
-        const int more =
-            over_block(count([&](const Candidate &x) { return x.score > least; }), s_n, plus);
         int64_t l = 0, h = (int64_t)p.beams * p.vocab - 1;
         while (l < h) {
             const int64_t mid = (l + h) >> 1;
@@ -402,16 +488,15 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
                       }),
                       s_n, all);
     }
-    for (int64_t i = tid; i < slots; i += kThreads) {
-        const Candidate c = candidate(i);
-        if (c.score > none && (c.score > least || (c.score == least && c.place <= last))) {
+    each([&](const Candidate &c) {
+        if (c.score > least || (c.score == least && c.place <= last)) {
             if (at < kList) {
                 s_score[at] = c.score;
                 s_place[at] = c.place;
             }
             ++at;
         }
-    }
+    });
     __syncthreads();
     all = min(all, kList);
     const auto put = [&](int rank, float score, int32_t parent, int32_t token, bool ended) {
@@ -423,12 +508,13 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
     };
     for (int c = tid; c < all; c += kThreads) {
         const double s = s_score[c];
-        const int64_t at_ = s_place[c];
+        const int64_t place = s_place[c];
         int rank = 0;
+#pragma unroll 4
         for (int o = 0; o < all; ++o)
-            rank += before(s_score[o], s_place[o], s, at_);
+            rank += s_score[o] > s || (s_score[o] == s && s_place[o] < place);
         if (rank < keep) {
-            const int32_t w = (int32_t)(at_ / p.vocab), token = (int32_t)(at_ % p.vocab);
+            const int32_t w = (int32_t)(place / p.vocab), token = (int32_t)(place % p.vocab);
             put(rank, (float)s, (int32_t)row0 + w, token, token == p.end);
         }
     }
@@ -463,8 +549,13 @@ hipError_t launch_beam(const BeamProblem &p, int type, int vecs, hipStream_t str
                                              : launch_rows<BEAM_F16>(p, vecs, stream);
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(beam_pick_kernel, dim3((unsigned)p.batch), dim3(kThreads),
-                       (size_t)p.beams * 8, stream, p);
+    const bool held = (int64_t)p.beams * p.pieces * p.keep <= kThreads * kHeld;
+    const dim3 grid((unsigned)p.batch);
+    const size_t lds = (size_t)p.beams * 8;
+    if (held)
+        hipLaunchKernelGGL(beam_pick_kernel<true>, grid, dim3(kThreads), lds, stream, p);
+    else
+        hipLaunchKernelGGL(beam_pick_kernel<false>, grid, dim3(kThreads), lds, stream, p);
     return hipGetLastError();
 }
 

@@ -85,6 +85,7 @@ __global__ __launch_bounds__(kThreads) void kv_remap_kernel(int32_t *__restrict_
     for (int i = 0; i < kEntries; ++i)
         id[i] = e0 + i * kThreads < entries ? table[e0 + i * kThreads] : -1;
     if (LDS) {
+#pragma unroll 8
         for (int i = threadIdx.x; i < n; i += kThreads)
             s_src[i] = src[i];
         __syncthreads();
@@ -110,11 +111,13 @@ __global__ __launch_bounds__(kThreads) void kv_remap_kernel(int32_t *__restrict_
 // New row r goes on from old row p = parent[r].  Rows share whole blocks.  A last
 // block that is only partly filled stays with the first child (the lowest r) of its
 // row; the others get a block off `fresh` each, in row order, and an entry in the
-// list of copies.  Freed are the blocks of the old tables that no new one holds: one
-// bit a block for either side, set by the kernel that writes the tables.
+// list of copies.  Freed are the blocks of the old tables that no new one holds: a
+// byte a block for either side, set by the kernel that writes the tables (all writers
+// of a byte store the same, so plain stores do; bits set by atomics took 700 us of a
+// call with 2000 rows of 1300 columns).
 //
 // Bound: latency, and 4 bytes in and out a table entry.  Three launches, each of which
-// needs all of the one before: who copies (and cleared bits), tables and bits, the
+// needs all of the one before: who copies (and cleared bytes), tables and bytes, the
 // list of freed blocks.
 
 __device__ __forceinline__ bool in_range(int32_t x, int32_t n) { return x >= 0 && x < n; }
@@ -137,10 +140,10 @@ __device__ __forceinline__ bool open_ended(const KvForkProblem &p, int32_t len)
 
 __global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvForkProblem p)
 {
-    // bits of both sides, by every block
+    // bytes of both sides, by every block
     for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < 2 * p.words;
          i += (int64_t)gridDim.x * kPlanThreads)
-        p.bits[i] = 0;
+        p.held[i] = u32x4{0u, 0u, 0u, 0u};
     if (blockIdx.x != 0)
         return;
     constexpr int kPer = kMostRows / kPlanThreads;
@@ -201,60 +204,76 @@ __global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvFork
         p.counts[0] = all;
 }
 
-__device__ __forceinline__ void mark(uint32_t *bits, int32_t block, int64_t n_blocks)
-{
-    if (block < 0 || block >= n_blocks)
-        return;
-    uint32_t *word = bits + (block >> 5);
-    const uint32_t bit = 1u << (block & 31);
-    // rows that share a prefix set the same bits: most find theirs set
-    if (!(__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & bit))
-        atomicOr(word, bit);
-}
+// A thread has one column of kRows rows.  Rows that share a prefix lie side by side:
+// an entry that repeats the one above it is marked already.
+constexpr int kRows = 8;
 
 __global__ __launch_bounds__(kThreads) void kv_fork_tables_kernel(const KvForkProblem p)
 {
     const int32_t col = blockIdx.x * kThreads + threadIdx.x;
     if (col >= p.cols)
         return;
-    int32_t row = blockIdx.y;
-    if (row >= p.rows) {  // an old row
-        row -= p.rows;
-        mark(p.bits, p.table[(int64_t)row * p.cols + col], p.n_blocks);
-        return;
+    const int32_t groups = (p.rows + kRows - 1) / kRows;
+    const bool old = (int32_t)blockIdx.y >= groups;
+    const int32_t r0 = ((int32_t)blockIdx.y - (old ? groups : 0)) * kRows;
+    const int32_t rows = old ? p.old_rows : p.rows;
+    int32_t block[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int32_t row = r0 + i;
+        block[i] = -1;
+        if (row >= rows)
+            continue;
+        if (old) {
+            block[i] = p.table[(int64_t)row * p.cols + col];
+        } else {
+            const int32_t from = p.parent[row];
+            if (in_range(from, p.old_rows)) {
+                const int32_t last = p.last[row];
+                const int32_t have = columns(p, length_of(p, from));
+                if (col < have)
+                    block[i] = col == have - 1 && last != kKeep
+                                   ? last
+                                   : p.table[(int64_t)from * p.cols + col];
+            }
+            p.new_table[(int64_t)row * p.cols + col] = block[i];
+        }
     }
-    int32_t block = -1;
-    const int32_t from = p.parent[row];
-    if (in_range(from, p.old_rows)) {
-        const int32_t last = p.last[row];
-        const int32_t have = columns(p, length_of(p, from));
-        if (col < have)
-            block = col == have - 1 && last != kKeep ? last : p.table[(int64_t)from * p.cols + col];
-    }
-    p.new_table[(int64_t)row * p.cols + col] = block;
-    mark(p.bits + p.words, block, p.n_blocks);
+    uint8_t *held = reinterpret_cast<uint8_t *>(p.held + (old ? 0 : p.words));
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+        if (block[i] >= 0 && block[i] < p.n_blocks && (i == 0 || block[i] != block[i - 1]))
+            held[block[i]] = 1;
 }
 
-// A block of threads lists the freed blocks of its words, after those of all words
-// before, which it counts itself.
+// A block of threads lists the freed blocks of its 16-byte words, after those of all
+// words before, which it counts itself.
+__device__ __forceinline__ u32x4 freed_of(const KvForkProblem &p, int64_t w)
+{
+    return p.held[w] & ~p.held[p.words + w];
+}
+__device__ __forceinline__ int count(u32x4 x)
+{
+    return __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w);
+}
+
 __global__ __launch_bounds__(kPlanThreads) void kv_fork_freed_kernel(const KvForkProblem p)
 {
     __shared__ int32_t s_before[kPlanThreads / 64], s_after[kPlanThreads / 64],
         s_sums[kPlanThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t w0 = (int64_t)blockIdx.x * kPlanThreads;
+    const int64_t w0 = (int64_t)blockIdx.x * kPlanThreads, mine = w0 + tid;
     int32_t before = 0, after = 0;
-    uint32_t mine = 0;
-    for (int64_t w = tid; w < p.words; w += kPlanThreads) {
-        const uint32_t freed = p.bits[w] & ~p.bits[p.words + w];
-        if (w < w0)
-            before += __popc(freed);
-        else if (w >= w0 + kPlanThreads)
-            after += __popc(freed);
-        else
-            mine = freed;
-    }
-    const int32_t n = __popc(mine);
+#pragma unroll 4
+    for (int64_t w = tid; w < w0; w += kPlanThreads)
+        before += count(freed_of(p, w));
+    u32x4 freed = {0u, 0u, 0u, 0u};
+    if (mine < p.words)
+        freed = freed_of(p, mine);
+#pragma unroll 4
+    for (int64_t w = mine + kPlanThreads; w < p.words; w += kPlanThreads)
+        after += count(freed_of(p, w));
+    const int32_t n = count(freed);
     const int32_t incl = wave_scan(n), incl_before = wave_scan(before),
                   incl_after = wave_scan(after);
     if (lane == 63) {
@@ -268,10 +287,17 @@ __global__ __launch_bounds__(kPlanThreads) void kv_fork_freed_kernel(const KvFor
         at += s_before[i] + (i < wave ? s_sums[i] : 0);
         all += s_before[i] + s_sums[i] + s_after[i];
     }
-    for (uint32_t left = mine; left; left &= left - 1, ++at)
-        if (at < p.n_freed)
-            p.freed[at] = (int32_t)((w0 + tid) * 32) + __builtin_ctz(left);
-    for (int64_t i = all + w0 + tid; i < p.n_freed; i += (int64_t)gridDim.x * kPlanThreads)
+    if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if ((freed[i >> 2] >> (i & 3) * 8) & 1) {
+                if (at < p.n_freed)
+                    p.freed[at] = (int32_t)(mine * 16) + i;
+                ++at;
+            }
+        }
+    }
+    for (int64_t i = all + mine; i < p.n_freed; i += (int64_t)gridDim.x * kPlanThreads)
         p.freed[i] = -1;
     if (blockIdx.x == 0 && tid == 0)
         p.counts[1] = all;
@@ -318,7 +344,8 @@ hipError_t launch_kv_fork(const KvForkProblem &p, hipStream_t stream)
     if (p.cols > 0 && p.rows + p.old_rows > 0) {
         hipLaunchKernelGGL(kv_fork_tables_kernel,
                            dim3((unsigned)((p.cols + kThreads - 1) / kThreads),
-                                (unsigned)(p.rows + p.old_rows)),
+                                (unsigned)((p.rows + kRows - 1) / kRows +
+                                           (p.old_rows + kRows - 1) / kRows)),
                            dim3(kThreads), 0, stream, p);
         e = hipGetLastError();
         if (e != hipSuccess)

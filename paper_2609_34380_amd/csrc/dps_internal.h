@@ -244,12 +244,12 @@ struct KvForkProblem {
     int64_t n_fresh;
     int32_t rows, old_rows, cols;
     int32_t log2_tokens;
-    int64_t n_blocks, words;  // words of 32 blocks
+    int64_t n_blocks, words;  // words of 16 blocks
     int32_t *new_table, *new_len, *src, *dst, *tokens, *freed, *counts;
     int64_t n_freed;
     // workspace
     int32_t *last;            // [rows] the block that replaces the last one, or kKeep
-    uint32_t *bits;           // [2][words] blocks in the old tables, in the new ones
+    u32x4 *held;              // [2][words] a byte a block: in the old tables, in the new ones
 };
 hipError_t launch_kv_fork(const KvForkProblem &p, hipStream_t stream);
 

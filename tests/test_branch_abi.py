@@ -58,7 +58,7 @@ def fork(lib, **kw):
     (dict(out=dict(table=0x30000)), INVALID), (dict(out=dict(table=0x307fc)), INVALID),
     (dict(out=dict(table=0x30004 - 8 * 64 * 4)), INVALID), (dict(out=dict(seq_len=0x20000)), INVALID),
     (dict(out=dict(freed=0x40000)), INVALID), (dict(out=dict(counts=0x1001c)), INVALID),
-    (dict(ws=None), WORKSPACE), (dict(ws_bytes=511), WORKSPACE), (dict(ws=0x1080), ALIGNMENT),
+    (dict(ws=None), WORKSPACE), (dict(ws_bytes=2303), WORKSPACE), (dict(ws=0x1080), ALIGNMENT),
 ])
 def test_fork_refuses(lib, kw, status):
     assert fork(lib, **kw) == status
@@ -66,8 +66,8 @@ def test_fork_refuses(lib, kw, status):
 
 
 def test_fork_workspace(lib):
-    assert lib.dps_kv_fork_workspace_bytes(8, 1000) == 256 + 256
-    assert lib.dps_kv_fork_workspace_bytes(4096, 1 << 20) == 4 * 4096 + (1 << 18)
+    assert lib.dps_kv_fork_workspace_bytes(8, 1000) == 256 + 2048
+    assert lib.dps_kv_fork_workspace_bytes(4096, 1 << 20) == 4 * 4096 + (1 << 21)
     assert lib.dps_kv_fork_workspace_bytes(4097, 10) == 0
     assert lib.dps_kv_fork_workspace_bytes(-1, 10) == 0
 
