@@ -512,6 +512,28 @@ dps_status dps_kv_copy(const dps_kv_cache *cache, const int32_t *src, const int3
 dps_status dps_kv_remap(int32_t *table, int64_t entries, const int32_t *src, const int32_t *dst,
                         int64_t n, void *stream);
 
+/* Workspace bytes of dps_attn_shared on the current device (0 for sizes it refuses).
+ * Contents on entry do not matter. */
+size_t dps_attn_shared_workspace_bytes(int64_t rows, int64_t groups, int64_t heads,
+                                       int64_t kv_heads, int64_t head_dim);
+
+/* dps_attn_decode of rows that share prefixes: rows group_start[g] ..
+ * group_start[g + 1] - 1 have their first shared_len[g] tokens in common (in the same
+ * blocks, or in copies of them), which are read once for all of them, through the
+ * table row of the first that has them all.  A row that is shorter than that (an idle one), has no table
+ * row, or is in no group attends its tokens through its own table row alone, as do
+ * all rows where group_start does not ascend within 0 .. rows and those of a
+ * group whose shared_len is past the table's columns.  Each row's result is
+ * dps_attn_decode's but for the order of sums; args->window is 0.
+ *   group_start  device int32[groups + 1].
+ *   shared_len   device int32[groups], groups 0..1024; any length (a block and a tile
+ *                may end before or after it).
+ *   ws           device scratch, 256-byte aligned, of ws_bytes >=
+ *                dps_attn_shared_workspace_bytes(). */
+dps_status dps_attn_shared(const dps_attn_args *args, const dps_kv_cache *cache,
+                           const int32_t *group_start, const int32_t *shared_len, int64_t groups,
+                           void *ws, size_t ws_bytes, void *stream);
+
 /* Element types of the logits of dps_beam_select. */
 enum { DPS_BEAM_F16 = 0, DPS_BEAM_BF16 = 1, DPS_BEAM_F32 = 2 };
 

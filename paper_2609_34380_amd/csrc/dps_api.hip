@@ -945,10 +945,13 @@ DPS_EXPORT size_t dps_attn_workspace_bytes(int64_t rows, int64_t heads, int64_t 
     return wide > fp8 ? wide : fp8;
 }
 
-DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache *cache, void *ws,
-                                      size_t ws_bytes, void *stream)
+namespace {
+
+// Argument checks of the attention calls, and all of *p but the workspace.  No row: only
+// p->rows is set.
+dps_status check_attn(const dps_attn_args *a, const dps_kv_cache *cache, dps::AttnProblem *p,
+                      AttnPlan *plan)
 {
-    g_err[0] = 0;
     REQUIRE(a != nullptr, DPS_ERR_INVALID_ARG, "attention arguments are NULL");
     dps::KvCacheView c;
     dps_status s = check_cache(cache, &c);
@@ -969,6 +972,7 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
             "scale, or scale * k_scale, must be finite");
     REQUIRE(a->rows <= 1 || (a->q_stride >= a->heads * dim && a->out_stride >= a->heads * dim),
             DPS_ERR_INVALID_ARG, "q_stride or out_stride is smaller than a row");
+    p->rows = a->rows;
     if (a->rows == 0)
         return DPS_OK;
     REQUIRE(a->q != nullptr && a->out != nullptr && a->kv_len != nullptr, DPS_ERR_INVALID_ARG,
@@ -988,41 +992,62 @@ DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache
     const int64_t room = a->table_cols > (0x7fffffff >> c.log2_tokens)
                              ? 0x7fffffff
                              : a->table_cols << c.log2_tokens;
-    const AttnPlan plan = plan_attn(a->heads, kv_heads, dim, cache->type == DPS_KV_E4M3);
     REQUIRE(a->rows <= (1 << 20) && a->rows <= 0x7fffffff / (room / 32 + 2), DPS_ERR_UNSUPPORTED,
             "too many rows for one call");
+    *plan = plan_attn(a->heads, kv_heads, dim, cache->type == DPS_KV_E4M3);
+    p->q = a->q;
+    p->q_stride = a->q_stride;
+    p->out = a->out;
+    p->out_stride = a->out_stride;
+    p->lse = a->lse;
+    p->pool = c.pool;
+    p->block_stride = c.block_stride;
+    p->n_blocks = c.n_blocks;
+    p->log2_tokens = c.log2_tokens;
+    p->kv_heads = c.kv_heads;
+    p->group = (int32_t)(a->heads / kv_heads);
+    p->head_groups = plan->groups;
+    p->group_step = plan->step;
+    p->table = a->table;
+    p->table_cols = a->table_cols;
+    p->requests = a->requests;
+    p->req = a->req;
+    p->kv_len = a->kv_len;
+    p->rows = a->rows;
+    p->window = a->window;
+    p->score_scale = a->scale * c.k_scale;
+    p->value_scale = c.v_scale;
+    p->shared = nullptr;
+    p->own = p->own_stat = nullptr;
+    p->found = nullptr;
+    return DPS_OK;
+}
+
+// The attention's part of a workspace.
+void place_attn(const AttnPlan &plan, uint8_t *at, dps::AttnProblem *p)
+{
+    p->part_out = reinterpret_cast<float *>(at);
+    p->part_stat = reinterpret_cast<float *>(at + plan.out_bytes);
+    p->join = reinterpret_cast<int32_t *>(at + plan.out_bytes + plan.stat_bytes);
+}
+
+}  // namespace
+
+DPS_EXPORT dps_status dps_attn_decode(const dps_attn_args *a, const dps_kv_cache *cache, void *ws,
+                                      size_t ws_bytes, void *stream)
+{
+    g_err[0] = 0;
+    dps::AttnProblem p;
+    AttnPlan plan;
+    const dps_status s = check_attn(a, cache, &p, &plan);
+    if (s != DPS_OK || p.rows == 0)
+        return s;
     REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
             "workspace is smaller than dps_attn_workspace_bytes()");
     REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");
-    dps::AttnProblem p;
-    p.q = a->q;
-    p.q_stride = a->q_stride;
-    p.out = a->out;
-    p.out_stride = a->out_stride;
-    p.lse = a->lse;
-    p.pool = c.pool;
-    p.block_stride = c.block_stride;
-    p.n_blocks = c.n_blocks;
-    p.log2_tokens = c.log2_tokens;
-    p.kv_heads = c.kv_heads;
-    p.group = (int32_t)(a->heads / kv_heads);
-    p.head_groups = plan.groups;
-    p.group_step = plan.step;
-    p.table = a->table;
-    p.table_cols = a->table_cols;
-    p.requests = a->requests;
-    p.req = a->req;
-    p.kv_len = a->kv_len;
-    p.rows = a->rows;
-    p.window = a->window;
-    p.score_scale = a->scale * c.k_scale;
-    p.value_scale = c.v_scale;
-    uint8_t *at = static_cast<uint8_t *>(ws);
-    p.part_out = reinterpret_cast<float *>(at);
-    p.part_stat = reinterpret_cast<float *>(at + plan.out_bytes);
-    p.join = reinterpret_cast<int32_t *>(at + plan.out_bytes + plan.stat_bytes);
-    return launched(dps::launch_attn(p, a->type, cache->type == DPS_KV_E4M3, (int)dim, plan.blocks,
-                                     (hipStream_t)stream));
+    place_attn(plan, static_cast<uint8_t *>(ws), &p);
+    return launched(dps::launch_attn(p, a->type, cache->type == DPS_KV_E4M3, cache->head_dim,
+                                     plan.blocks, (hipStream_t)stream));
 }
 
 // ---- sequences that branch ---------------------------------------------------------
@@ -1293,4 +1318,115 @@ DPS_EXPORT dps_status dps_beam_select(const dps_beam_args *a, void *ws, size_t w
     at += plan.value_bytes;
     p.listed = reinterpret_cast<int32_t *>(at);
     return launched(dps::launch_beam(p, a->type, plan.vecs, (hipStream_t)stream));
+}
+
+namespace {
+
+// Launch shape and workspace of an attention call whose rows share prefixes.
+struct SharedPlan {
+    AttnPlan attn;
+    int columns, item_rows;
+    int64_t blocks, slots;
+    size_t row_bytes, found_bytes, own_bytes, own_stat_bytes, part_bytes, part_stat_bytes;
+    size_t bytes() const
+    {
+        return align256((int64_t)attn.bytes()) + row_bytes + found_bytes + own_bytes +
+               own_stat_bytes + part_bytes + part_stat_bytes;
+    }
+};
+
+SharedPlan plan_shared(int64_t rows, int64_t groups, int64_t heads, int64_t kv_heads, int64_t dim,
+                       bool fp8)
+{
+    SharedPlan s;
+    s.attn = plan_attn(heads, kv_heads, dim, fp8);
+    const int64_t lines = kv_heads * s.attn.groups;
+    s.columns = dps::shared_columns(rows, groups, s.attn.step, fp8, (int)dim);
+    s.item_rows = s.columns / s.attn.step;
+    s.blocks = cdiv((int64_t)dps::shared_blocks_per_cu(s.columns, fp8, (int)dim) *
+                        current_cu_count(), lines);
+    s.slots = s.blocks + rows / s.item_rows + groups;
+    const int64_t parts = lines * s.slots * s.columns;
+    s.row_bytes = align256(rows * 16);
+    s.found_bytes = align256(rows * 8);
+    s.own_bytes = align256(rows * heads * dim * 4);
+    s.own_stat_bytes = align256(rows * heads * 8);
+    s.part_bytes = align256(parts * dim * 4);
+    s.part_stat_bytes = align256(parts * 8);
+    return s;
+}
+
+bool shared_sizes(int64_t rows, int64_t groups, int64_t heads, int64_t kv_heads, int64_t dim)
+{
+    return rows > 0 && rows <= (1 << 20) && groups >= 0 && groups <= dps::kSharedGroups &&
+           heads > 0 && heads <= 65536 && kv_heads > 0 && kv_heads <= 4096 && dim > 0 &&
+           dim <= 256 && heads % kv_heads == 0;
+}
+
+}  // namespace
+
+DPS_EXPORT size_t dps_attn_shared_workspace_bytes(int64_t rows, int64_t groups, int64_t heads,
+                                                  int64_t kv_heads, int64_t head_dim)
+{
+    if (!shared_sizes(rows, groups, heads, kv_heads, head_dim))
+        return 0;
+    // the type of the cache is not known here: room for either
+    const size_t wide = plan_shared(rows, groups, heads, kv_heads, head_dim, false).bytes();
+    const size_t fp8 = plan_shared(rows, groups, heads, kv_heads, head_dim, true).bytes();
+    return wide > fp8 ? wide : fp8;
+}
+
+DPS_EXPORT dps_status dps_attn_shared(const dps_attn_args *a, const dps_kv_cache *cache,
+                                      const int32_t *group_start, const int32_t *shared_len,
+                                      int64_t groups, void *ws, size_t ws_bytes, void *stream)
+{
+    g_err[0] = 0;
+    dps::SharedProblem p;
+    AttnPlan attn;
+    const dps_status s = check_attn(a, cache, &p.attn, &attn);
+    if (s != DPS_OK)
+        return s;
+    REQUIRE(groups >= 0, DPS_ERR_INVALID_ARG, "groups is negative");
+    REQUIRE(groups <= dps::kSharedGroups, DPS_ERR_UNSUPPORTED, "more than 1024 groups in one call");
+    REQUIRE(a->window == 0, DPS_ERR_UNSUPPORTED, "rows that share a prefix have no window");
+    if (a->rows == 0)
+        return DPS_OK;
+    REQUIRE(groups == 0 || (group_start != nullptr && shared_len != nullptr), DPS_ERR_INVALID_ARG,
+            "group_start or shared_len is NULL");
+    REQUIRE(aligned(group_start, 4) && aligned(shared_len, 4), DPS_ERR_ALIGNMENT,
+            "group_start or shared_len is not 4-byte aligned");
+    const bool fp8 = cache->type == DPS_KV_E4M3;
+    const SharedPlan plan =
+        plan_shared(a->rows, groups, a->heads, cache->kv_heads, cache->head_dim, fp8);
+    const int64_t lines = (int64_t)cache->kv_heads * attn.groups;
+    // a launch counts its threads (256 a row and key/value head) in 32 bits, and a
+    // key/value head its partials
+    REQUIRE(a->rows * lines < (1 << 24) && plan.slots * plan.columns <= 0x7fffffff,
+            DPS_ERR_UNSUPPORTED, "too many rows for one call");
+    REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
+            "workspace is smaller than dps_attn_shared_workspace_bytes()");
+    REQUIRE(aligned(ws, 256), DPS_ERR_ALIGNMENT, "workspace is not 256-byte aligned");
+    uint8_t *at = static_cast<uint8_t *>(ws);
+    place_attn(plan.attn, at, &p.attn);
+    at += align256((int64_t)plan.attn.bytes());
+    p.rows = reinterpret_cast<dps::SharedRow *>(at);
+    p.attn.shared = p.rows;
+    at += plan.row_bytes;
+    p.attn.found = reinterpret_cast<int2 *>(at);
+    at += plan.found_bytes;
+    p.attn.own = reinterpret_cast<float *>(at);
+    at += plan.own_bytes;
+    p.attn.own_stat = reinterpret_cast<float *>(at);
+    at += plan.own_stat_bytes;
+    p.part_out = reinterpret_cast<float *>(at);
+    at += plan.part_bytes;
+    p.part_stat = reinterpret_cast<float *>(at);
+    p.group_start = group_start;
+    p.shared_len = shared_len;
+    p.groups = (int32_t)groups;
+    p.columns = plan.columns;
+    p.item_rows = plan.item_rows;
+    p.slots = (int32_t)plan.slots;
+    return launched(dps::launch_shared(p, a->type, fp8, cache->head_dim, (int)plan.blocks,
+                                       plan.attn.blocks, (hipStream_t)stream));
 }

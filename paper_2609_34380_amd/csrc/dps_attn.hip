@@ -51,6 +51,7 @@
 // block's start and end about 5.
 #include <type_traits>
 
+#include "dps_attn.h"
 #include "dps_internal.h"
 
 namespace dps {
@@ -59,98 +60,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
-constexpr int kTile = 32;               // tokens a wave takes at a time
 constexpr int kJoinThreads = 512;
-constexpr int64_t kLongest = 0x7fffff00;  // tokens of a row (a tile past it still fits 31 bits)
-constexpr float kNone = -__FLT_MAX__;   // reference score before any token: no finite one is below
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-// Weights are 2^(score - ref).  ref is set kLift below the largest score so far,
-// and follows a larger one only once that is kRoom above ref: weights stay
-// below 2^14, inside the FP16 range, the largest is at least 2^6, so that the
-// FP16 terms resolve weights down to 2^-30 of it, and most tiles rescale
-// nothing.
-constexpr float kLift = 6.0f, kRoom = 14.0f;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-template <int TYPE>
-__device__ __forceinline__ f32x4 mfma32(u32x4 a, u32x4 b, f32x4 c)
-{
-    if (TYPE == KV_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(a), as_half8(b), c, 0, 0, 0);
-}
-
-// Two E4M3 values (half `HI` of the dword) as two 16-bit values, exactly.
-template <int TYPE, bool HI>
-__device__ __forceinline__ uint32_t wide2(uint32_t codes)
-{
-    if (TYPE == KV_BF16)
-        return __builtin_bit_cast(uint32_t,
-                                  __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, HI));
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.0f, HI));
-}
-
-// Two fp32 weights as two 16-bit terms each: hi and what it leaves.  BF16: both to
-// nearest, within 2^-17 of the weight to either side (truncated they lost 2^-17 on
-// average, and outputs came out that much nearer to zero).  FP16: both truncated,
-// within 2^-21 of the weight or 2^-24.
-template <int TYPE>
-__device__ __forceinline__ void split2(float p0, float p1, uint32_t &hi, uint32_t &lo)
-{
-    if (TYPE == KV_BF16) {
-        hi = narrow2<TYPE>(p0, p1);
-        lo = narrow2<TYPE>(p0 - __builtin_bit_cast(float, hi << 16),
-                           p1 - __builtin_bit_cast(float, hi & 0xffff0000u));
-    } else {
-        const auto h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
-        hi = __builtin_bit_cast(uint32_t, h);
-        lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p0 - (float)h[0],
-                                                                     p1 - (float)h[1]));
-    }
-}
-
-// Over the four 16-lane quarters that share a head: each swap leaves a lane and
-// its partner's value in the two results.
-template <typename F>
-__device__ __forceinline__ float over_quarters(float x, const F &f)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const uint32_t a0 = a[0], a1 = a[1];
-    const uint32_t v = __builtin_bit_cast(
-        uint32_t, f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
-    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    const uint32_t b0 = b[0], b1 = b[1];
-    return f(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
-}
-__device__ __forceinline__ float quarters_max(float x)
-{
-    return over_quarters(x, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float quarters_sum(float x)
-{
-    return over_quarters(x, [](float a, float b) { return a + b; });
-}
-
-template <int BYTES>
-struct Piece;
-template <>
-struct Piece<16> { typedef u32x4 T; };
-template <>
-struct Piece<8> { typedef u32x2 T; };
-template <>
-struct Piece<4> { typedef uint32_t T; };
-
-// Bytes streamed once: loaded past the caches' retention.
-template <typename T>
-__device__ __forceinline__ T stream(const uint8_t *p)
-{
-    return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
-}
 
 // The live tokens [lo, hi) of a row and its table row; hi = 0: none.
 struct RowSpan {
@@ -158,14 +68,17 @@ struct RowSpan {
     int32_t req;
 };
 
-// UNIFORM: r is the wave's, and the result lies in scalar registers.
-template <bool UNIFORM>
+// UNIFORM: r is the wave's, and the result lies in scalar registers.  SHARED: the row
+// shares its first tokens with others, and this kernel has those after them.
+template <bool UNIFORM, bool SHARED>
 __device__ __forceinline__ RowSpan row_span(const AttnProblem &p, const int32_t *__restrict__ req,
-                                            const int32_t *__restrict__ kv_len, int32_t r)
+                                            const int32_t *__restrict__ kv_len,
+                                            const SharedRow *__restrict__ shared, int32_t r)
 {
     RowSpan s;
     s.req = req ? req[r] : r;
     int32_t len = kv_len[r];
+    const int32_t own = SHARED ? shared[r].start : 0;
     // both loads under way before either is looked at: one latency, not two (0.1-0.5 us)
     if (UNIFORM)
         asm("" : "+s"(s.req), "+s"(len));
@@ -177,11 +90,14 @@ __device__ __forceinline__ RowSpan row_span(const AttnProblem &p, const int32_t 
         n = 0;
     n = n < 0 ? 0 : (n > room ? room : n);
     s.hi = (int32_t)n;
-    s.lo = p.window > 0 && n > p.window ? (int32_t)(n - p.window) : 0;
+    if (SHARED)  // at most n: only a row that has all of them shares tokens
+        s.lo = own;
+    else
+        s.lo = p.window > 0 && n > p.window ? (int32_t)(n - p.window) : 0;
     return s;
 }
 
-// Tiles of a row (its live tokens on the grid of kTile tokens).
+// Tiles of a row (its live tokens on the grid of kTile tokens; none where lo = hi on it).
 __device__ __forceinline__ int32_t row_tiles(const RowSpan &s)
 {
     return s.hi == 0 ? 0 : (int32_t)(((uint32_t)s.hi + kTile - 1) / kTile) - s.lo / kTile;
@@ -233,21 +149,6 @@ __device__ __forceinline__ void attn_store(const AttnProblem &p, int64_t row, in
             sum == 0.0f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <int TYPE, bool FP8, int D, int HT>
-struct Shape {
-    static constexpr int kElt = FP8 ? 1 : 2;
-    static constexpr int kSteps = D / 32;              // matrix steps over head_dim
-    static constexpr int kKeyLoads = D * kElt / 64;    // 16-byte loads a lane per 16 tokens
-    static constexpr int kAcc = D / 16;                // output tiles
-    // head_dim of V in pieces of 16 lanes x W values: whole 128s, then 64, 32
-    static constexpr int kP8 = D / 128;
-    static constexpr int kP4 = (D % 128) / 64;
-    static constexpr int kP2 = (D % 64) / 32;
-    // Waves a SIMD is compiled for: 256 registers a lane, all 512 where two tiles'
-    // keys and a tile's values beside the output need them.
-    static constexpr int kWavesPerSimd = D * kElt >= (HT == 1 ? 512 : 192) ? 1 : 2;
-};
-
 // A wave's output of one row: acc (value d of a head in the lane and register
 // that the matrix instruction leaves it), reference score and sum per head.
 template <int KACC>
@@ -276,34 +177,12 @@ struct Partial {
     }
 };
 
-// One piece of V (16 lanes x W values of head_dim from d0 on) of a tile's 32
-// tokens, turned into W matrix operands.
-template <int TYPE, bool FP8, int W>
-struct VPiece {
-    typedef typename Piece<W * (FP8 ? 1 : 2)>::T Raw;
-    Raw raw[8];
-
-    // values 2i (even) and 2i + 1 (odd) of tokens 2j and 2j + 1, side by side
-    __device__ __forceinline__ void turn(int i, int j, uint32_t &even, uint32_t &odd) const
-    {
-        const uint32_t *a = reinterpret_cast<const uint32_t *>(&raw[2 * j]);
-        const uint32_t *b = reinterpret_cast<const uint32_t *>(&raw[2 * j + 1]);
-        if (FP8) {
-            const uint32_t t = __builtin_amdgcn_perm(b[i >> 1], a[i >> 1],
-                                                     i & 1 ? 0x07030602u : 0x05010400u);
-            even = wide2<TYPE, false>(t);
-            odd = wide2<TYPE, true>(t);
-        } else {
-            even = __builtin_amdgcn_perm(b[i], a[i], 0x05040100u);
-            odd = __builtin_amdgcn_perm(b[i], a[i], 0x07060302u);
-        }
-    }
-};
-
-template <int TYPE, bool FP8, int D, int HT>
+// SHARED: a row's output goes to p.own unfinished, for the join with its shared tokens,
+// and what it takes to find a row's partials to p.found.
+template <int TYPE, bool FP8, int D, int HT, bool SHARED>
 __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd)) void attn_kernel(
     const AttnProblem p, const int32_t *__restrict__ tables, const int32_t *__restrict__ reqs,
-    const int32_t *__restrict__ kv_len)
+    const int32_t *__restrict__ kv_len, const SharedRow *__restrict__ shared)
 {
     typedef Shape<TYPE, FP8, D, HT> S;
     __shared__ f32x4 s_head[kWaves][HT][S::kAcc * 64];  // rows that began before the wave
@@ -336,14 +215,14 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     if (rows <= 64) {
         span = RowSpan{0, 0, 0};
         if (lane < rows)
-            span = row_span<false>(p, reqs, kv_len, lane);
+            span = row_span<false, SHARED>(p, reqs, kv_len, shared, lane);
         mine = row_tiles(span);
         incl = wave_scan(mine);
         tiles = __builtin_amdgcn_readlane(incl, 63);
     } else {
         const int32_t r1 = min((tid + 1) * per, rows);
         for (int32_t r = tid * per; r < r1; ++r)
-            mine += row_tiles(row_span<false>(p, reqs, kv_len, r));
+            mine += row_tiles(row_span<false, SHARED>(p, reqs, kv_len, shared, r));
         incl = wave_scan(mine);
         if (lane == 63)
             s_sums[wave] = incl;
@@ -383,14 +262,14 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         if (per == 1) {
             row = chunk;
             skip = begin - chunk_first;
-            span = row_span<false>(p, reqs, kv_len, row);
+            span = row_span<false, SHARED>(p, reqs, kv_len, shared, row);
         } else {
             const int32_t r1 = min((chunk + 1) * per, rows);
             for (int32_t r = chunk * per; r < r1; r += 64) {
                 if (rows > 64) {
                     span = RowSpan{0, 0, 0};
                     if (r + lane < r1)
-                        span = row_span<false>(p, reqs, kv_len, r + lane);
+                        span = row_span<false, SHARED>(p, reqs, kv_len, shared, r + lane);
                     mine = row_tiles(span);
                     incl = wave_scan(mine);
                 }
@@ -431,11 +310,34 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                 8 * S::kP8 + 4 * S::kP4);
     };
     Partial<S::kAcc> o[HT];
+    // a partial row of one head, in fp32
+    const auto put_wide = [&](const Partial<S::kAcc> &f, float *at) {
+        each_piece([&](auto width, int d0, int tile) {
+            constexpr int W = width;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[W];
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+                    v[k] = f.acc[tile + k][i];
+                __builtin_memcpy(at + d0 + W * (4 * quarter + i), v, sizeof(v));
+            }
+        });
+    };
     const auto finish = [&](int c, int r) {
         const Partial<S::kAcc> &f = o[c];
         const int head = 16 * c + col;
+        if (SHARED && hv == 0 && lane == 0)
+            p.found[r] = int2{0, 0};
         if (head >= n_heads)
             return;
+        if (SHARED) {
+            const int64_t at = (int64_t)r * (p.kv_heads * p.group) + first_head + head;
+            put_wide(f, p.own + at * D);
+            if (quarter == 0)
+                *reinterpret_cast<f32x2 *>(p.own_stat + at * 2) = f32x2{f.ref, f.sum};
+            return;
+        }
         const float scale = f.sum == 0.0f ? 0.0f : p.value_scale / f.sum;
         uint16_t *at = static_cast<uint16_t *>(p.out) + r * p.out_stride +
                        (int64_t)(first_head + head) * D;
@@ -468,18 +370,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         if (head >= n_heads)
             return;
         const int64_t slot = slot_at(1) + head;
-        float *at = p.part_out + slot * D;
-        each_piece([&](auto width, int d0, int tile) {
-            constexpr int W = width;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[W];
-#pragma unroll
-                for (int k = 0; k < W; ++k)
-                    v[k] = f.acc[tile + k][i];
-                __builtin_memcpy(at + d0 + W * (4 * quarter + i), v, sizeof(v));
-            }
-        });
+        put_wide(f, p.part_out + slot * D);
         if (quarter == 0) {
             p.part_stat[slot * 2] = f.ref;
             p.part_stat[slot * 2 + 1] = f.sum;
@@ -497,7 +388,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
             return;
         skip = 0;
         row_first += row_n;
-        const RowSpan next = row_span<true>(p, reqs, kv_len, row);
+        const RowSpan next = row_span<true, SHARED>(p, reqs, kv_len, shared, row);
         lo = next.lo;
         hi = next.hi;
         req = next.req;
@@ -760,8 +651,11 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                 hand_on(c);
         }
         if (!ends && hv == 0) {
+            const int blocks = (int)line.of(row_first + row_n - 1) / kWaves - block + 1;
             s_join[3] = row;
-            s_join[4] = (int)line.of(row_first + row_n - 1) / kWaves - block + 1;
+            s_join[4] = blocks;
+            if (SHARED && lane == 0)
+                p.found[row] = int2{block, blocks};
         }
     }
     // A row that began in an earlier block: all of its parts lie in LDS, and the waves
@@ -825,6 +719,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     }
 }
 
+// (The join of rows that share tokens is dps_shared.hip's.)
 // Joins the rows that several blocks share, and gives rows without tokens their
 // zeros.  Block w of the attention left in join[w]: the row it continued from an
 // earlier block (row, first block of the row, blocks of the row), and the row it
@@ -901,7 +796,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
          r0 += (int64_t)kJoinThreads * blocks) {
         const int64_t r = r0 + (int64_t)lane * blocks;
         uint64_t none =
-            __ballot(r < p.rows && row_span<false>(p, reqs, kv_len, (int32_t)r).hi == 0);
+            __ballot(r < p.rows && row_span<false, false>(p, reqs, kv_len, nullptr, (int32_t)r).hi == 0);
         for (; none; none &= none - 1) {
             const int64_t row = r0 + (int64_t)__builtin_ctzll(none) * blocks;
             for (int i = lane; i < items; i += 64)
@@ -956,39 +851,39 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(
     }
 }
 
-template <int TYPE, bool FP8, int D>
+template <int TYPE, bool FP8, int D, bool SHARED>
 hipError_t launch(const AttnProblem &p, int blocks, hipStream_t stream)
 {
     const int heads = p.kv_heads * p.head_groups;
     const dim3 grid((unsigned)blocks, (unsigned)heads);
     constexpr int most = attn_heads_a_pass(FP8, D) / 16;
     if (p.group_step > 16)
-        hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D, most>), grid, dim3(kThreads), 0, stream, p,
-                           p.table, p.req, p.kv_len);
+        hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D, most, SHARED>), grid, dim3(kThreads), 0,
+                           stream, p, p.table, p.req, p.kv_len, p.shared);
     else
-        hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D, 1>), grid, dim3(kThreads), 0, stream, p,
-                           p.table, p.req, p.kv_len);
+        hipLaunchKernelGGL((attn_kernel<TYPE, FP8, D, 1, SHARED>), grid, dim3(kThreads), 0, stream,
+                           p, p.table, p.req, p.kv_len, p.shared);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
+    if (e != hipSuccess || SHARED)
         return e;
     hipLaunchKernelGGL((attn_join_kernel<TYPE, D>), dim3((unsigned)blocks, (unsigned)heads),
                        dim3(kJoinThreads), 0, stream, p, p.req, p.kv_len, p.join);
     return hipGetLastError();
 }
 
-template <int TYPE>
+template <int TYPE, bool SHARED>
 hipError_t launch_type(const AttnProblem &p, bool fp8, int dim, int blocks, hipStream_t stream)
 {
     switch (dim) {
-    case 64: return fp8 ? launch<TYPE, true, 64>(p, blocks, stream)
-                        : launch<TYPE, false, 64>(p, blocks, stream);
-    case 96: return fp8 ? hipErrorInvalidValue : launch<TYPE, false, 96>(p, blocks, stream);
-    case 128: return fp8 ? launch<TYPE, true, 128>(p, blocks, stream)
-                         : launch<TYPE, false, 128>(p, blocks, stream);
-    case 192: return fp8 ? launch<TYPE, true, 192>(p, blocks, stream)
-                         : launch<TYPE, false, 192>(p, blocks, stream);
-    case 256: return fp8 ? launch<TYPE, true, 256>(p, blocks, stream)
-                         : launch<TYPE, false, 256>(p, blocks, stream);
+    case 64: return fp8 ? launch<TYPE, true, 64, SHARED>(p, blocks, stream)
+                        : launch<TYPE, false, 64, SHARED>(p, blocks, stream);
+    case 96: return fp8 ? hipErrorInvalidValue : launch<TYPE, false, 96, SHARED>(p, blocks, stream);
+    case 128: return fp8 ? launch<TYPE, true, 128, SHARED>(p, blocks, stream)
+                         : launch<TYPE, false, 128, SHARED>(p, blocks, stream);
+    case 192: return fp8 ? launch<TYPE, true, 192, SHARED>(p, blocks, stream)
+                         : launch<TYPE, false, 192, SHARED>(p, blocks, stream);
+    case 256: return fp8 ? launch<TYPE, true, 256, SHARED>(p, blocks, stream)
+                         : launch<TYPE, false, 256, SHARED>(p, blocks, stream);
     }
     return hipErrorInvalidValue;
 }
@@ -998,8 +893,11 @@ hipError_t launch_type(const AttnProblem &p, bool fp8, int dim, int blocks, hipS
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream)
 {
-    return type == KV_BF16 ? launch_type<KV_BF16>(p, fp8, dim, blocks, stream)
-                           : launch_type<KV_F16>(p, fp8, dim, blocks, stream);
+    if (p.shared)
+        return type == KV_BF16 ? launch_type<KV_BF16, true>(p, fp8, dim, blocks, stream)
+                               : launch_type<KV_F16, true>(p, fp8, dim, blocks, stream);
+    return type == KV_BF16 ? launch_type<KV_BF16, false>(p, fp8, dim, blocks, stream)
+                           : launch_type<KV_F16, false>(p, fp8, dim, blocks, stream);
 }
 
 }  // namespace dps

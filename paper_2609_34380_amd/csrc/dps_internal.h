@@ -172,6 +172,12 @@ struct KvStoreProblem {
 // type: KV_F16 or KV_BF16 of qkv; fp8: the cache holds E4M3, else `type`.
 hipError_t launch_kv_store(const KvStoreProblem &p, int type, bool fp8, hipStream_t stream);
 
+// A row that shares its first `start` tokens: its column of its item (dps_shared.hip),
+// and the `count` partials of the item from slot `slot` on.
+struct SharedRow {
+    int32_t start, column, slot, count;
+};
+
 struct AttnProblem {
     const void *q;
     int64_t q_stride;       // elements
@@ -195,6 +201,12 @@ struct AttnProblem {
     // reference score and sum, and what the join finds of every block
     float *part_out, *part_stat;
     int32_t *join;
+    // rows that share their first tokens (nullptr: none do): [rows]; then, of the
+    // tokens after them, finished rows in fp32 with reference score and sum, and per row
+    // the first block and the number of blocks of its partial rows (0: finished)
+    const SharedRow *shared;
+    float *own, *own_stat;
+    int2 *found;
 };
 // Blocks of four waves a CU gets: one keeps enough bytes in flight (16 KiB a wave
 // at 128 16-bit values) and leaves the fewest partial rows; rows of 64 bytes take
@@ -213,6 +225,35 @@ constexpr int attn_blocks_per_cu(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim
 constexpr int attn_heads_a_pass(bool fp8, int dim) { return (fp8 ? 1 : 2) * dim >= 384 ? 16 : 32; }
 hipError_t launch_attn(const AttnProblem &p, int type, bool fp8, int dim, int blocks,
                        hipStream_t stream);
+
+// Rows [group_start[g], group_start[g + 1]) share their first shared_len[g] tokens.
+// An item is up to item_rows rows of a group on one key/value head (and pass over its
+// query heads): item_rows * attn.group_step of its `columns` columns.
+struct SharedProblem {
+    AttnProblem attn;       // .shared is what the first kernel writes (rows)
+    SharedRow *rows;
+    const int32_t *group_start, *shared_len;
+    int32_t groups;
+    int32_t columns, item_rows;
+    int32_t slots;          // partials of a key/value head and pass
+    // workspace: [heads and passes][slots][columns] rows, reference score and sum
+    float *part_out, *part_stat;
+};
+constexpr int kSharedGroups = 1024;
+// Columns of an item: a group of average size fills them where that is possible.
+constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, int dim)
+{
+    const int64_t mean = rows * step / (groups < 1 ? 1 : groups);
+    if (attn_heads_a_pass(fp8, dim) == 16)
+        return mean <= 16 ? 16 : 64;
+    return step <= 16 && mean <= 16 ? 16 : (mean <= 32 ? 32 : (step <= 16 && mean <= 64 ? 64 : 128));
+}
+constexpr int shared_blocks_per_cu(int columns, bool fp8, int dim)
+{
+    return (columns == 16 || columns == 64) && (fp8 ? 1 : 2) * dim < 512 ? 2 : 1;
+}
+hipError_t launch_shared(const SharedProblem &p, int type, bool fp8, int dim, int blocks,
+                         int attn_blocks, hipStream_t stream);
 
 // ---- sequences that branch ---------------------------------------------------------
 struct KvCopyProblem {

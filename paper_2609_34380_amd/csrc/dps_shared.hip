@@ -1,0 +1,690 @@
+// dps_shared.hip -- attention of one new token a row where rows share a prefix
+// (gfx950).
+//
+// Rows of a group attend the group's first L tokens, which lie in the same blocks for
+// all of them, and then tokens of their own.  With (o, m, l) the weighted values, the
+// reference score and the sum of weights of a part of a row's tokens, two parts join as
+//     m = max(m1, m2),  o = o1 2^(m1 - m) + o2 2^(m2 - m),  l alike,
+// so the shared part is computed for all rows of a group at once: their query heads
+// (of one key/value head) are the columns of the same matrix products, and a key or
+// value is read once for all of them.  Three launches: shared_kernel here, attn_kernel
+// (dps_attn.hip) over each row's own tokens, and shared_join_kernel.
+//
+// shared_kernel.  An item is up to `columns` columns of a group.  The tiles of all items
+// of a key/value head form one line, cut into equal ranges, one a block of threads; a
+// block has a contiguous part of an item at a time, and leaves one partial for it
+// (slot block + item: of two neighbours on the line that share an item, or of two
+// items that share a block, no two slots are the same).  WC waves of a block have
+// different columns of the same tokens, and its kWaves / WC teams different tokens,
+// which they join in LDS.
+//
+// The tile is attn_kernel's: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix
+// instructions, 32 tokens at a time, HT column tiles of 16 a wave; keys and values go
+// from memory to registers, values are turned there, and the weights enter the matrix
+// cores as two 16-bit terms (dps_attn.hip has the precision).
+#include <type_traits>
+
+#include "dps_attn.h"
+#include "dps_internal.h"
+
+namespace dps {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kPer = kSharedGroups / kThreads;
+
+// Where the groups lie: tiles and items of a key/value head before each group.
+struct Groups {
+    int32_t tiles[kSharedGroups + 1];
+    int32_t items[kSharedGroups + 1];
+    int32_t sums[2][kWaves];
+};
+
+// Tokens that a row has, as far as its table row holds them.
+__device__ __forceinline__ int32_t tokens_of(const SharedProblem &p, int32_t row, int32_t &req)
+{
+    const AttnProblem &a = p.attn;
+    req = a.req ? a.req[row] : row;
+    if (req < 0 || req >= a.requests)
+        return 0;
+    const int64_t room = min(a.table_cols << a.log2_tokens, kLongest);
+    return (int32_t)min((int64_t)max(a.kv_len[row], 0), room);
+}
+
+// Rows of group g and its length.  A length past the table's columns is no row's, and
+// the group shares nothing.  rows < 0: it does not lie within the rows.
+struct Group {
+    int32_t first, rows, length;
+};
+__device__ __forceinline__ Group group_of(const SharedProblem &p, int32_t g)
+{
+    Group x;
+    x.first = p.group_start[g];
+    const int32_t next = p.group_start[g + 1];
+    x.rows = x.first < 0 || next < x.first || next > p.attn.rows ? -1 : next - x.first;
+    const int64_t room = min(p.attn.table_cols << p.attn.log2_tokens, kLongest);
+    x.length = max(p.shared_len[g], 0);
+    if (x.length > room)
+        x.length = 0;
+    return x;
+}
+__device__ __forceinline__ int32_t tiles_of(const Group &x)
+{
+    return (int32_t)(((uint32_t)x.length + kTile - 1) / kTile);
+}
+__device__ __forceinline__ int32_t items_of(const SharedProblem &p, const Group &x)
+{
+    return x.length > 0 ? (x.rows + p.item_rows - 1) / p.item_rows : 0;
+}
+
+// Fills s for all groups; false: the groups do not ascend within the rows, and nothing
+// is shared.
+__device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int32_t tiles[kPer], items[kPer], n_tiles = 0, n_items = 0;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int32_t g = tid * kPer + i;
+        tiles[i] = items[i] = 0;
+        if (g < p.groups) {
+            const Group x = group_of(p, g);
+            bad = bad || x.rows < 0;
+            if (!bad) {
+                items[i] = items_of(p, x);
+                tiles[i] = items[i] * tiles_of(x);
+            }
+        }
+        n_tiles += tiles[i];
+        n_items += items[i];
+    }
+    const int32_t incl_tiles = wave_scan(n_tiles), incl_items = wave_scan(n_items);
+    if (lane == 63) {
+        s.sums[0][wave] = incl_tiles;
+        s.sums[1][wave] = incl_items;
+    }
+    bad = __syncthreads_or(bad);
+    int32_t at_tile = incl_tiles - n_tiles, at_item = incl_items - n_items;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        at_tile += i < wave ? s.sums[0][i] : 0;
+        at_item += i < wave ? s.sums[1][i] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int32_t g = tid * kPer + i;
+        if (g <= p.groups) {
+            s.tiles[g] = at_tile;
+            s.items[g] = at_item;
+        }
+        at_tile += tiles[i];
+        at_item += items[i];
+    }
+    if (tid == kThreads - 1 && p.groups == kSharedGroups) {
+        s.tiles[p.groups] = at_tile;
+        s.items[p.groups] = at_item;
+    }
+    __syncthreads();
+    return !bad;
+}
+
+// The last g in [0, n) with first[g] <= x; first[0] <= x.
+__device__ __forceinline__ int last_from(const int32_t *first, int n, int32_t x)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= x)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+// The line cut into `blocks` ranges of `each` tiles, the first `more` one longer.
+struct Line {
+    int32_t blocks, each, more;
+
+    __device__ __forceinline__ Line(int32_t tiles, int32_t most)
+        : blocks(min(tiles, most)), each(tiles / max(blocks, 1)), more(tiles - each * blocks)
+    {
+    }
+    __device__ __forceinline__ int32_t begin(int32_t b) const { return b * each + min(b, more); }
+    __device__ __forceinline__ int32_t of(int32_t t) const
+    {
+        const int32_t cut = more * (each + 1);
+        return t < cut ? t / (each + 1) : more + (t - cut) / each;
+    }
+};
+
+// What every row shares, and that no own token of it has been met.
+__device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s, bool good,
+                                         const Line &line, int32_t block, int32_t blocks)
+{
+    for (int64_t r = (int64_t)block * kThreads + threadIdx.x; r < p.attn.rows;
+         r += (int64_t)blocks * kThreads) {
+        SharedRow x = {0, 0, 0, 0};
+        if (good && p.groups > 0 && r >= p.group_start[0] && r < p.group_start[p.groups]) {
+            int lo = 0, hi = p.groups;  // the last group that begins at or before r
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (p.group_start[mid] <= r)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            const Group g = group_of(p, lo);
+            int32_t req;
+            if (g.length > 0 && tokens_of(p, (int32_t)r, req) >= g.length) {
+                const int32_t tiles = tiles_of(g), at = ((int32_t)r - g.first) / p.item_rows;
+                const int32_t item = s.items[lo] + at, tile = s.tiles[lo] + at * tiles;
+                const int32_t b0 = line.of(tile);
+                x.start = g.length;
+                x.column = (((int32_t)r - g.first) % p.item_rows) * p.attn.group_step;
+                x.slot = b0 + item;
+                x.count = line.of(tile + tiles - 1) - b0 + 1;
+            }
+        }
+        p.rows[r] = x;
+        p.attn.found[r] = int2{0, -1};
+    }
+}
+
+template <int TYPE, bool FP8, int D, int HT, int WC>
+__global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd)) void shared_kernel(
+    const SharedProblem p, const int32_t *__restrict__ tables)
+{
+    typedef Shape<TYPE, FP8, D, HT> S;
+    constexpr int kTeams = kWaves / WC;  // waves with the same columns and other tokens
+    __shared__ Groups s_groups;
+    __shared__ f32x4 s_part[kTeams > 1 ? kWaves : 1][S::kAcc * 64];  // a column tile at a time
+    __shared__ float s_stat[kTeams > 1 ? kWaves : 1][128];
+
+    const AttnProblem &a = p.attn;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    // the heads of one key/value head on one XCD, which deals blocks in turn: their items
+    // read the same tokens
+    const int heads = a.kv_heads * a.head_groups;
+    const int hv = blockIdx.x % heads, block = blockIdx.x / heads, blocks = gridDim.x / heads;
+    const int kvh = hv / a.head_groups, sub = hv % a.head_groups;
+    const int first_head = kvh * a.group + sub * a.group_step;
+    const int n_heads = min(a.group_step, a.group - sub * a.group_step);
+
+    const bool good = find_groups(p, s_groups);
+    const int32_t all = good ? s_groups.tiles[p.groups] : 0;
+    const Line line(all, blocks);
+    if (hv == 0)
+        put_rows(p, s_groups, good, line, block, blocks);
+    if (block >= line.blocks)
+        return;
+
+    const uint32_t tokens = 1u << a.log2_tokens;
+    const uint32_t key_lane = (4 * (col & 3) + (col >> 2)) * 64 + quarter * 16;
+    const uint32_t key_head = (uint32_t)kvh * S::kKeyLoads * tokens * 64;
+    const uint32_t val_head = (uint32_t)(a.kv_heads + kvh) * tokens * (D * S::kElt);
+    const float to_log2 = a.score_scale * kLog2e;
+    const int32_t last_col = (int32_t)a.table_cols - 1;
+    const int wc = wave % WC, team = wave / WC;
+
+    int32_t tile = line.begin(block);
+    const int32_t end = line.begin(block + 1);
+    int g = last_from(s_groups.tiles, p.groups, tile);
+    while (tile < end) {
+        while (s_groups.tiles[g + 1] <= tile)  // past groups without tiles
+            ++g;
+        const Group grp = group_of(p, g);
+        const int32_t n_tiles = tiles_of(grp);
+        const int32_t in_group = tile - s_groups.tiles[g];
+        const int32_t at = in_group / n_tiles, skip = in_group % n_tiles;
+        const int32_t part = min(n_tiles - skip, end - tile);  // tiles of the item in this block
+        const int32_t item = s_groups.items[g] + at;
+        const int32_t row0 = grp.first + at * p.item_rows;
+        const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
+        tile += part;
+
+        // the prefix as the group's first row that has all of it sees it
+        int32_t lead = -1;
+        for (int32_t r = grp.first; r < grp.first + grp.rows && lead < 0; r += 64) {
+            int32_t req = -1;
+            const bool has = r + lane < grp.first + grp.rows &&
+                             tokens_of(p, r + lane, req) >= grp.length;
+            const uint64_t any = __ballot(has);
+            if (any)
+                lead = __builtin_amdgcn_readlane(req, __builtin_ctzll(any));
+        }
+        if (lead < 0)
+            continue;  // no row reads the partials
+        const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
+
+        // ---- query fragments ------------------------------------------------------
+        int32_t column[HT];
+        bool used[HT];
+        u32x4 q[HT][S::kSteps];
+        f32x4 acc[HT][S::kAcc];
+        float ref[HT], sum[HT];
+#pragma unroll
+        for (int c = 0; c < HT; ++c) {
+            column[c] = (wc * HT + c) * 16 + col;
+            const int32_t r = column[c] / a.group_step, head = column[c] % a.group_step;
+            used[c] = r < n_rows && head < n_heads;
+            const uint8_t *qp = static_cast<const uint8_t *>(a.q) +
+                                ((int64_t)(row0 + r) * a.q_stride +
+                                 (int64_t)(first_head + head) * D) * 2;
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) {
+                const int d = FP8 ? 64 * (s >> 1) + 16 * quarter + 8 * (s & 1)
+                                  : 32 * s + 8 * quarter;
+                q[c][s] = u32x4{0u, 0u, 0u, 0u};
+                if (used[c])
+                    q[c][s] = load16(qp + d * 2);
+            }
+            ref[c] = kNone;
+            sum[c] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i)
+                acc[c][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+        // this wave's tiles of the part
+        const int32_t u0 = skip + (int32_t)((int64_t)part * team / kTeams);
+        const int32_t u1 = skip + (int32_t)((int64_t)part * (team + 1) / kTeams);
+        const int32_t hi = grp.length;
+
+        uint32_t place[2];
+        int32_t id[2];
+        const auto find = [&](int t0) {
+            const uint32_t second = (uint32_t)t0 + (t0 + 16 < hi ? 16 : 0);
+            place[0] = t0 & (tokens - 1);
+            place[1] = second & (tokens - 1);
+            id[0] = table[min(t0 >> a.log2_tokens, last_col)];
+            id[1] = table[min((int32_t)(second >> a.log2_tokens), last_col)];
+        };
+        u32x4 key[2][S::kKeyLoads];
+        VPiece<TYPE, FP8, 8> v8[S::kP8 ? S::kP8 : 1];
+        VPiece<TYPE, FP8, 4> v4[1];
+        VPiece<TYPE, FP8, (FP8 ? 4 : 2)> v2[1];
+        const uint8_t *base[2];
+        bool ok[2];  // a block outside the cache is never read: the first one stands in
+        uint32_t at_[2];
+        const auto load = [&](auto *to, const uint8_t *from) {
+            typedef typename std::remove_reference<decltype(*to)>::type T;
+            if (WC == 1)
+                *to = stream<T>(from);
+            else
+                *to = *reinterpret_cast<const T *>(from);
+        };
+        const auto load_keys = [&] {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                ok[h] = id[h] >= 0 && id[h] < a.n_blocks;
+                base[h] = a.pool + (int64_t)(ok[h] ? id[h] : 0) * a.block_stride;
+                at_[h] = place[h];
+#pragma unroll
+                for (int s = 0; s < S::kKeyLoads; ++s)
+                    load(&key[h][s],
+                         base[h] + (key_head + at_[h] * 64 + s * tokens * 64) + key_lane);
+            }
+        };
+        const auto load_piece = [&](auto &v, int d0, int width) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int h = j >> 2;
+                const uint32_t t = at_[h] + 4 * (j & 3);
+                load(&v.raw[j], base[h] + (val_head + (t * D + d0) * S::kElt) +
+                                    (quarter * D + col * width) * S::kElt);
+            }
+        };
+        const auto load_values = [&] {
+#pragma unroll
+            for (int i = 0; i < S::kP8; ++i)
+                load_piece(v8[i], 128 * i, 8);
+            if (S::kP4)
+                load_piece(v4[0], 128 * S::kP8, 4);
+            if (S::kP2)
+                load_piece(v2[0], 128 * S::kP8 + 64 * S::kP4, 2);
+        };
+        const auto take = [&](int t0, auto more) {
+            const bool ok0 = ok[0], ok1 = ok[1];
+            load_values();
+            f32x4 scores[HT][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int c = 0; c < HT; ++c)
+                    scores[c][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < S::kSteps; ++s) {
+                    u32x4 k;
+                    if (FP8) {
+                        const u32x4 k16 = key[h][s >> 1];
+                        const uint32_t c0 = s & 1 ? k16.z : k16.x, c1 = s & 1 ? k16.w : k16.y;
+                        k = u32x4{wide2<TYPE, false>(c0), wide2<TYPE, true>(c0),
+                                  wide2<TYPE, false>(c1), wide2<TYPE, true>(c1)};
+                    } else {
+                        k = key[h][s];
+                    }
+#pragma unroll
+                    for (int c = 0; c < HT; ++c)
+                        scores[c][h] = mfma32<TYPE>(k, q[c][s], scores[c][h]);
+                }
+            }
+            if (more) {
+                load_keys();
+                find(t0 + 2 * kTile);
+            }
+            float to_ref = to_log2;
+            uint32_t keep[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                keep[j] = ~0u;
+            if (t0 + kTile > hi || !ok0 || !ok1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int t = t0 + 16 * (j >> 2) + 4 * (j & 3) + quarter;
+                    const bool live = t < hi && (j < 4 ? ok0 : ok1);
+#pragma unroll
+                    for (int c = 0; c < HT; ++c) {
+                        const float x = scores[c][j >> 2][j & 3] * to_log2;
+                        scores[c][j >> 2][j & 3] = live ? x : -__builtin_inff();
+                    }
+                    keep[j] = live ? ~0u : 0u;
+                }
+                to_ref = 1.0f;
+            }
+            u32x4 p_hi[HT], p_lo[HT];
+#pragma unroll
+            for (int c = 0; c < HT; ++c) {
+                float x[8];
+                const auto weigh = [&](float r) {
+#pragma clang fp contract(off)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[j] = scores[c][j >> 2][j & 3] * to_ref - r;
+                    float m = x[0];
+#pragma unroll
+                    for (int j = 1; j < 8; ++j)
+                        m = fmaxf(m, x[j]);
+                    return m;
+                };
+                if (__any(weigh(ref[c]) > kRoom)) {
+                    const float r = fmaxf(quarters_max(weigh(0.0f)) - kLift, ref[c]);
+                    const float shrink = __builtin_amdgcn_exp2f(ref[c] - r);
+                    ref[c] = r;
+                    sum[c] *= shrink;
+#pragma unroll
+                    for (int i = 0; i < S::kAcc; ++i)
+                        acc[c][i] *= shrink;
+                    weigh(r);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = __builtin_amdgcn_exp2f(x[j]);
+                sum[c] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t hi2, lo2;
+                    split2<TYPE>(x[2 * j], x[2 * j + 1], hi2, lo2);
+                    p_hi[c][j] = hi2;
+                    p_lo[c][j] = lo2;
+                }
+            }
+            int out = 0;
+            const auto turn = [&](auto &v, int width) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    v.raw[j] &= keep[j];
+#pragma unroll
+                for (int i = 0; i < width / 2; ++i) {
+                    u32x4 even, odd;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t e, d;
+                        v.turn(i, j, e, d);
+                        even[j] = e;
+                        odd[j] = d;
+                    }
+#pragma unroll
+                    for (int c = 0; c < HT; ++c) {
+                        f32x4 &x = acc[c][out], &y = acc[c][out + 1];
+                        x = mfma32<TYPE>(even, p_hi[c], x);
+                        x = mfma32<TYPE>(even, p_lo[c], x);
+                        y = mfma32<TYPE>(odd, p_hi[c], y);
+                        y = mfma32<TYPE>(odd, p_lo[c], y);
+                    }
+                    out += 2;
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < S::kP8; ++i)
+                turn(v8[i], 8);
+            if (S::kP4)
+                turn(v4[0], 4);
+            if (S::kP2)
+                turn(v2[0], 2);
+        };
+        if (u0 < u1) {
+            find(u0 * kTile);
+            load_keys();
+            find(u0 * kTile + kTile);
+            for (int u = u0; u < u1 - 1; ++u)
+                take(u * kTile, std::true_type());
+            take((u1 - 1) * kTile, std::false_type());
+        }
+
+        // ---- the block's partial of the item -----------------------------------------
+        const int64_t slot = ((int64_t)hv * p.slots + block + item) * p.columns;
+        // the values of output tiles t and t + 1 of a column
+        const auto put2 = [&](int32_t column, int t, f32x4 x, f32x4 y) {
+            const int width = t < 8 * S::kP8 ? 8 : (t < 8 * S::kP8 + 4 * S::kP4 ? 4 : 2);
+            float *to = p.part_out + (slot + column) * D + (t & -width) * 16 +
+                        (t & (width - 1)) + width * 4 * quarter;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<f32x2 *>(to + width * k) = f32x2{x[k], y[k]};
+        };
+        const auto put_stat = [&](int32_t column, float r, float l) {
+            *reinterpret_cast<f32x2 *>(p.part_stat + (slot + column) * 2) = f32x2{r, l};
+        };
+#pragma unroll
+        for (int c = 0; c < HT; ++c) {
+            sum[c] = quarters_sum(sum[c]);
+            if (kTeams == 1) {
+                if (used[c]) {
+#pragma unroll
+                    for (int t = 0; t < S::kAcc; t += 2)
+                        put2(column[c], t, acc[c][t], acc[c][t + 1]);
+                    if (quarter == 0)
+                        put_stat(column[c], ref[c], sum[c]);
+                }
+                continue;
+            }
+            // the teams' parts, a pair of output tiles at a time, dealt to them
+            __syncthreads();  // the column tile before has been read
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i)
+                s_part[wave][i * 64 + lane] = acc[c][i];
+            s_stat[wave][lane] = ref[c];
+            s_stat[wave][64 + lane] = sum[c];
+            __syncthreads();
+            float weight[kTeams], top = kNone, total = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kTeams; ++i) {
+                weight[i] = s_stat[i * WC + wc][lane];
+                top = fmaxf(top, weight[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kTeams; ++i) {
+                weight[i] = __builtin_amdgcn_exp2f(weight[i] - top);
+                total += s_stat[i * WC + wc][64 + lane] * weight[i];
+            }
+            if (!used[c])
+                continue;
+            for (int t = 2 * team; t < S::kAcc; t += 2 * kTeams) {
+                f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+#pragma unroll
+                for (int k = 0; k < kTeams; ++k) {
+                    x += s_part[k * WC + wc][t * 64 + lane] * weight[k];
+                    y += s_part[k * WC + wc][(t + 1) * 64 + lane] * weight[k];
+                }
+                put2(column[c], t, x, y);
+            }
+            if (team == 0 && quarter == 0)
+                put_stat(column[c], top, total);
+        }
+    }
+}
+
+// Joins a row's partials: of its shared tokens, and of its own.  A block a row and
+// key/value head (and pass); the (head, 4 values) items are dealt to threads, several
+// threads an item where there are many partials, which combine through LDS in a fixed
+// order.
+template <int TYPE, int D>
+__global__ __launch_bounds__(kThreads) void shared_join_kernel(const SharedProblem p)
+{
+    __shared__ f32x4 s_out[kThreads];
+    __shared__ float s_ref[kThreads], s_sum[kThreads];
+    const AttnProblem &a = p.attn;
+    const int tid = threadIdx.x;
+    const int heads = a.kv_heads * a.head_groups;
+    const int hv = blockIdx.x % heads;
+    const int64_t row = blockIdx.x / heads;
+    const int kvh = hv / a.head_groups, sub = hv % a.head_groups;
+    const int first_head = kvh * a.group + sub * a.group_step;
+    const int n_heads = min(a.group_step, a.group - sub * a.group_step);
+    const int items = n_heads * (D / 4);
+    const SharedRow shared = p.rows[row];
+    const int2 found = a.found[row];
+    const int own = found.y < 0 ? 0 : max(found.y, 1), count = own + shared.count;
+
+    int groups = 1;  // threads an item
+    while (2 * groups * items <= kThreads && groups < count)
+        groups *= 2;
+    const int each = min(items, kThreads / groups);
+    for (int i0 = 0; i0 < items; i0 += each) {
+        const int g = tid / each, item = i0 + tid % each;
+        const bool live = g < groups && item < items;
+        const int head = item / (D / 4), d = item % (D / 4) * 4;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        float ref = kNone, sum = 0.0f;
+        const auto add = [&](f32x4 part, float r, float l) {
+            const float to = fmaxf(ref, r);
+            const float x = __builtin_amdgcn_exp2f(ref - to), y = __builtin_amdgcn_exp2f(r - to);
+            o = o * x + part * y;
+            sum = sum * x + l * y;
+            ref = to;
+        };
+        if (live) {
+#pragma unroll 4
+            for (int k = g; k < count; k += groups) {
+                const float *out, *stat;
+                if (k < shared.count) {
+                    const int64_t at = ((int64_t)hv * p.slots + shared.slot + k) * p.columns +
+                                       shared.column + head;
+                    out = p.part_out + at * D;
+                    stat = p.part_stat + at * 2;
+                } else if (found.y == 0) {
+                    const int64_t at = row * (a.kv_heads * a.group) + first_head + head;
+                    out = a.own + at * D;
+                    stat = a.own_stat + at * 2;
+                } else {
+                    const int b = k - shared.count;  // of the row's blocks
+                    const int64_t at = ((int64_t)((found.x + b) * 2 + (b == 0 ? 1 : 0)) * heads + hv) *
+                                           a.group_step + head;
+                    out = a.part_out + at * D;
+                    stat = a.part_stat + at * 2;
+                }
+                const f32x2 s = *reinterpret_cast<const f32x2 *>(stat);
+                add(*reinterpret_cast<const f32x4 *>(out + d), s[0], s[1]);
+            }
+        }
+        for (int half = groups / 2; half > 0; half /= 2) {
+            if (live && g >= half && g < 2 * half) {
+                s_out[tid] = o;
+                s_ref[tid] = ref;
+                s_sum[tid] = sum;
+            }
+            __syncthreads();
+            if (live && g < half)
+                add(s_out[tid + half * each], s_ref[tid + half * each], s_sum[tid + half * each]);
+            __syncthreads();
+        }
+        if (live && g == 0) {
+            const float scale = sum == 0.0f ? 0.0f : a.value_scale / sum;
+            uint16_t *at = static_cast<uint16_t *>(a.out) + row * a.out_stride +
+                           (int64_t)(first_head + head) * D + d;
+            *reinterpret_cast<u32x2 *>(at) = u32x2{narrow2<TYPE>(o[0] * scale, o[1] * scale),
+                                                   narrow2<TYPE>(o[2] * scale, o[3] * scale)};
+            if (d == 0 && a.lse)
+                a.lse[row * (a.kv_heads * a.group) + first_head + head] =
+                    sum == 0.0f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+    }
+}
+
+template <int TYPE, bool FP8, int D>
+hipError_t launch(const SharedProblem &p, int blocks, int attn_blocks, hipStream_t stream)
+{
+    const int heads = p.attn.kv_heads * p.attn.head_groups;
+    const dim3 grid((unsigned)(blocks * heads));
+    if (p.columns == 16)
+        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1, 1>), grid, dim3(kThreads), 0, stream, p,
+                           p.attn.table);
+    else if (p.columns == 64)
+        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1, 4>), grid, dim3(kThreads), 0, stream, p,
+                           p.attn.table);
+    else if constexpr (attn_heads_a_pass(FP8, D) == 32) {
+        if (p.columns == 32)
+            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 1>), grid, dim3(kThreads), 0, stream,
+                               p, p.attn.table);
+        else
+            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 4>), grid, dim3(kThreads), 0, stream,
+                               p, p.attn.table);
+    } else {
+        return hipErrorInvalidValue;
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return e;
+    e = launch_attn(p.attn, TYPE, FP8, D, attn_blocks, stream);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL((shared_join_kernel<TYPE, D>), dim3((unsigned)(p.attn.rows * heads)),
+                       dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t launch_type(const SharedProblem &p, bool fp8, int dim, int blocks, int attn_blocks,
+                       hipStream_t stream)
+{
+    switch (dim) {
+    case 64: return fp8 ? launch<TYPE, true, 64>(p, blocks, attn_blocks, stream)
+                        : launch<TYPE, false, 64>(p, blocks, attn_blocks, stream);
+    case 96: return fp8 ? hipErrorInvalidValue
+                        : launch<TYPE, false, 96>(p, blocks, attn_blocks, stream);
+    case 128: return fp8 ? launch<TYPE, true, 128>(p, blocks, attn_blocks, stream)
+                         : launch<TYPE, false, 128>(p, blocks, attn_blocks, stream);
+    case 192: return fp8 ? launch<TYPE, true, 192>(p, blocks, attn_blocks, stream)
+                         : launch<TYPE, false, 192>(p, blocks, attn_blocks, stream);
+    case 256: return fp8 ? launch<TYPE, true, 256>(p, blocks, attn_blocks, stream)
+                         : launch<TYPE, false, 256>(p, blocks, attn_blocks, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_shared(const SharedProblem &p, int type, bool fp8, int dim, int blocks,
+                         int attn_blocks, hipStream_t stream)
+{
+    return type == KV_BF16 ? launch_type<KV_BF16>(p, fp8, dim, blocks, attn_blocks, stream)
+                           : launch_type<KV_F16>(p, fp8, dim, blocks, attn_blocks, stream);
+}
+
+}  // namespace dps

@@ -41,6 +41,7 @@ EXPORTED = ("dps_select_enc", "dps_split", "dps_merge", "dps_restore", "dps_back
             "dps_restore_worker_destroy", "dps_restore_worker_last_error",
             "dps_kv_map", "dps_kv_store", "dps_attn_workspace_bytes", "dps_attn_decode",
             "dps_kv_fork_workspace_bytes", "dps_kv_fork", "dps_kv_copy", "dps_kv_remap",
+            "dps_attn_shared_workspace_bytes", "dps_attn_shared",
             "dps_beam_workspace_bytes", "dps_beam_select", "dps_sum_compact")
 
 
@@ -225,6 +226,10 @@ def load_library(path=LIB_PATH):
     lib.dps_kv_copy.restype = ST
     lib.dps_kv_remap.argtypes = [P, I64, P, P, I64, P]
     lib.dps_kv_remap.restype = ST
+    lib.dps_attn_shared_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+    lib.dps_attn_shared_workspace_bytes.restype = ctypes.c_size_t
+    lib.dps_attn_shared.argtypes = [P, ctypes.POINTER(CKvCache), P, P, I64, P, ctypes.c_size_t, P]
+    lib.dps_attn_shared.restype = ST
     lib.dps_beam_workspace_bytes.argtypes = [I64, I64, I64, I64]
     lib.dps_beam_workspace_bytes.restype = ctypes.c_size_t
     lib.dps_beam_select.argtypes = [P, P, ctypes.c_size_t, P]
@@ -888,6 +893,70 @@ def kv_remap(table, src, dst):
     if status:
         _check(status)
     return table
+
+
+def attn_shared_workspace_bytes(cache, rows, heads, groups):
+    """Workspace of attn_shared for up to `rows` rows of `heads` query heads in exactly
+    `groups` groups."""
+    lib = _lib or load_library()
+    return lib.dps_attn_shared_workspace_bytes(rows, groups, heads, cache.kv_heads, cache.head_dim)
+
+
+def attn_shared(q, cache, table, kv_len, group_start, shared_len, req=None, scale=None, out=None,
+                lse=None, workspace=None):
+    """attn_decode of rows that share prefixes (dps_attn_shared): rows group_start[g] ..
+    group_start[g + 1] - 1 (int32 [groups + 1], ascending) have their first shared_len[g]
+    tokens (int32 [groups]) in common (in the same blocks or in copies, as kv_fork leaves
+    them), which are read once for all of them.  Rows in no group, and rows shorter than their
+    group's prefix, attend their tokens by themselves.  Other arguments and the result
+    are attn_decode's."""
+    lib = _lib or load_library()
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][heads][head_dim]")
+    rows, heads, dim = q.shape
+    dtype = q.dtype
+    kind = _ACT_TYPES.get(dtype)
+    if kind is None or dim != cache.head_dim:
+        raise ValueError("q must be float16 or bfloat16, of the cache's head_dim")
+    q_stride = _row_stride("q", q, rows, heads, dim, dtype)
+    _here("q", q)
+    for name, t, n in (("table", table, 2), ("kv_len", kv_len, 1), ("group_start", group_start, 1),
+                       ("shared_len", shared_len, 1)):
+        _ints(name, t, n)
+    groups = shared_len.shape[0]
+    if kv_len.shape[0] != rows or group_start.shape[0] != groups + 1:
+        raise ValueError("kv_len has an entry a row, group_start one more than shared_len")
+    rp = lp = 0
+    if req is not None:
+        _ints("req", req)
+        if req.shape[0] != rows:
+            raise ValueError("req has an entry a row")
+        rp = req.data_ptr()
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=dtype, device=q.device)
+    out_stride = _row_stride("out", out, rows, heads, dim, dtype)
+    _here("out", out)
+    if lse is not None:
+        if not (lse.dtype is _F32 and lse.is_cuda and lse.is_contiguous() and
+                lse.shape == (rows, heads)):
+            raise ValueError("lse must be a contiguous float32 device tensor [rows][heads]")
+        _here("lse", lse)
+        lp = lse.data_ptr()
+    if workspace is None:
+        need = lib.dps_attn_shared_workspace_bytes(rows, groups, heads, cache.kv_heads, dim)
+        workspace = _scratch(None, need, q)
+    else:
+        _scratch(workspace, 0, q)
+    requests, cols = table.shape
+    args = _pack_attn(rows, heads, q.data_ptr(), q_stride, table.data_ptr(), requests, cols, rp,
+                      kv_len.data_ptr(), 0, kind, dim ** -0.5 if scale is None else scale,
+                      out.data_ptr(), out_stride, lp)
+    status = lib.dps_attn_shared(args, cache.ref, group_start.data_ptr(), shared_len.data_ptr(),
+                                 groups, workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream())
+    if status:
+        _check(status)
+    return out
 
 
 class BeamStep(collections.namedtuple("BeamStep", "score parent token done")):

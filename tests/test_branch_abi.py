@@ -232,3 +232,46 @@ def test_compact_refuses(lib):
     assert lib.dps_sum_compact(s._h, 3, None, None, ctypes.byref(n)) == INVALID
     assert lib.dps_sum_compact(s._h, 0, None, None, None) == INVALID
     assert s.compact(0) == ([], []) and s.compact(10) == ([], [])
+
+
+# ---- attention of rows that share prefixes ----------------------------------------------
+
+
+def shared(lib, kw=(), c=None, starts=0x60000, lens=0x70000, groups=2, ws=0x1000, ws_bytes=1 << 40):
+    from test_kv_abi import attn
+    a = attn(**dict(kw))
+    return lib.dps_attn_shared(ctypes.byref(a), ctypes.byref(c or cache()), starts, lens, groups, ws,
+                               ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,status", CACHES)
+def test_shared_cache(lib, kw, status):
+    assert shared(lib, c=cache(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(window=3), UNSUPPORTED), (dict(window=-1), INVALID), (dict(heads=12), INVALID),
+    (dict(rows=-1), INVALID), (dict(q=0), INVALID), (dict(kv_len=0), INVALID),
+    (dict(req=0, requests=3), INVALID), (dict(out=0x50008), ALIGNMENT),
+    (dict(rows=(1 << 20) + 1), UNSUPPORTED), (dict(rows=1 << 20, heads=512, q_stride=1 << 16, out_stride=1 << 16), UNSUPPORTED),
+    (dict(scale=float("inf")), INVALID), (dict(type=dps.KV_E4M3), INVALID),
+])
+def test_shared_refuses(lib, kw, status):
+    assert shared(lib, kw) == status
+    assert lib.dps_last_error()
+
+
+def test_shared_groups_and_workspace(lib):
+    assert shared(lib, groups=-1) == INVALID
+    assert shared(lib, groups=1025) == UNSUPPORTED
+    assert shared(lib, starts=None) == INVALID and shared(lib, lens=None) == INVALID
+    assert shared(lib, starts=0x60002) == ALIGNMENT and shared(lib, lens=0x70001) == ALIGNMENT
+    need = lib.dps_attn_shared_workspace_bytes(4, 2, 32, 8, 128)
+    assert need > lib.dps_attn_workspace_bytes(4, 32, 8, 128)
+    assert shared(lib, ws=None) == WORKSPACE and shared(lib, ws_bytes=256) == WORKSPACE
+    assert shared(lib, ws=0x1010) == ALIGNMENT
+    assert lib.dps_attn_shared(None, ctypes.byref(cache()), 0x1000, 0x2000, 1, 0x1000, need,
+                               None) == INVALID
+    for bad in ((0, 2, 32, 8, 128), (4, -1, 32, 8, 128), (4, 1025, 32, 8, 128), (4, 2, 30, 8, 128),
+                (4, 2, 32, 0, 128), (4, 2, 32, 8, 257), ((1 << 20) + 1, 2, 32, 8, 128)):
+        assert lib.dps_attn_shared_workspace_bytes(*bad) == 0
