@@ -240,17 +240,22 @@ struct SharedProblem {
     float *part_out, *part_stat;
 };
 constexpr int kSharedGroups = 1024;
-// Columns of an item: a group of average size fills them where that is possible.
+// Columns of an item: a group of average size fills them where that is possible.  16 and
+// 32: tokens from memory to registers, a block's waves on different ones; above, through
+// LDS for four or eight waves of 32 columns (16 for heads over 128).
 constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, int dim)
 {
     const int64_t mean = rows * step / (groups < 1 ? 1 : groups);
-    if (attn_heads_a_pass(fp8, dim) == 16)
-        return mean <= 16 ? 16 : 64;
-    return step <= 16 && mean <= 16 ? 16 : (mean <= 32 ? 32 : (step <= 16 && mean <= 64 ? 64 : 128));
+    const int wave = dim > 128 ? 16 : 32;
+    if (mean <= 16 && step <= 16)
+        return 16;
+    if (mean <= 32 && attn_heads_a_pass(fp8, dim) == 32)
+        return 32;
+    return mean <= 4 * wave ? 4 * wave : 8 * wave;
 }
 constexpr int shared_blocks_per_cu(int columns, bool fp8, int dim)
 {
-    return (columns == 16 || columns == 64) && (fp8 ? 1 : 2) * dim < 512 ? 2 : 1;
+    return columns == 16 && (fp8 ? 1 : 2) * dim < 512 ? 2 : 1;
 }
 hipError_t launch_shared(const SharedProblem &p, int type, bool fp8, int dim, int blocks,
                          int attn_blocks, hipStream_t stream);

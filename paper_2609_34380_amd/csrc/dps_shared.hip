@@ -33,13 +33,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
-constexpr int kPer = kSharedGroups / kThreads;
 
 // Where the groups lie: tiles and items of a key/value head before each group.
 struct Groups {
     int32_t tiles[kSharedGroups + 1];
     int32_t items[kSharedGroups + 1];
-    int32_t sums[2][kWaves];
+    int32_t sums[2][8];  // a wave
 };
 
 // Tokens that a row has, as far as its table row holds them.
@@ -81,8 +80,10 @@ __device__ __forceinline__ int32_t items_of(const SharedProblem &p, const Group 
 
 // Fills s for all groups; false: the groups do not ascend within the rows, and nothing
 // is shared.
+template <int WAVES>
 __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
 {
+    constexpr int kPer = kSharedGroups / (64 * WAVES);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int32_t tiles[kPer], items[kPer], n_tiles = 0, n_items = 0;
     bool bad = false;
@@ -109,7 +110,7 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
     bad = __syncthreads_or(bad);
     int32_t at_tile = incl_tiles - n_tiles, at_item = incl_items - n_items;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
         at_tile += i < wave ? s.sums[0][i] : 0;
         at_item += i < wave ? s.sums[1][i] : 0;
     }
@@ -123,7 +124,7 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
         at_tile += tiles[i];
         at_item += items[i];
     }
-    if (tid == kThreads - 1 && p.groups == kSharedGroups) {
+    if (tid == 64 * WAVES - 1 && p.groups == kSharedGroups) {
         s.tiles[p.groups] = at_tile;
         s.items[p.groups] = at_item;
     }
@@ -162,11 +163,12 @@ struct Line {
 };
 
 // What every row shares, and that no own token of it has been met.
+template <int WAVES>
 __device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s, bool good,
                                          const Line &line, int32_t block, int32_t blocks)
 {
-    for (int64_t r = (int64_t)block * kThreads + threadIdx.x; r < p.attn.rows;
-         r += (int64_t)blocks * kThreads) {
+    for (int64_t r = (int64_t)block * (64 * WAVES) + threadIdx.x; r < p.attn.rows;
+         r += (int64_t)blocks * (64 * WAVES)) {
         SharedRow x = {0, 0, 0, 0};
         if (good && p.groups > 0 && r >= p.group_start[0] && r < p.group_start[p.groups]) {
             int lo = 0, hi = p.groups;  // the last group that begins at or before r
@@ -194,6 +196,21 @@ __device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s
     }
 }
 
+// The table row through which a group's prefix is read: that of the first row that has
+// all of it; -1: none has.
+__device__ __forceinline__ int32_t lead_of(const SharedProblem &p, const Group &grp, int lane)
+{
+    for (int32_t r = grp.first; r < grp.first + grp.rows; r += 64) {
+        int32_t req = -1;
+        const bool has = r + lane < grp.first + grp.rows &&
+                         tokens_of(p, r + lane, req) >= grp.length;
+        const uint64_t any = __ballot(has);
+        if (any)
+            return __builtin_amdgcn_readlane(req, __builtin_ctzll(any));
+    }
+    return -1;
+}
+
 template <int TYPE, bool FP8, int D, int HT, int WC>
 __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd)) void shared_kernel(
     const SharedProblem p, const int32_t *__restrict__ tables)
@@ -216,11 +233,11 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     const int first_head = kvh * a.group + sub * a.group_step;
     const int n_heads = min(a.group_step, a.group - sub * a.group_step);
 
-    const bool good = find_groups(p, s_groups);
+    const bool good = find_groups<kWaves>(p, s_groups);
     const int32_t all = good ? s_groups.tiles[p.groups] : 0;
     const Line line(all, blocks);
     if (hv == 0)
-        put_rows(p, s_groups, good, line, block, blocks);
+        put_rows<kWaves>(p, s_groups, good, line, block, blocks);
     if (block >= line.blocks)
         return;
 
@@ -248,16 +265,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
         tile += part;
 
-        // the prefix as the group's first row that has all of it sees it
-        int32_t lead = -1;
-        for (int32_t r = grp.first; r < grp.first + grp.rows && lead < 0; r += 64) {
-            int32_t req = -1;
-            const bool has = r + lane < grp.first + grp.rows &&
-                             tokens_of(p, r + lane, req) >= grp.length;
-            const uint64_t any = __ballot(has);
-            if (any)
-                lead = __builtin_amdgcn_readlane(req, __builtin_ctzll(any));
-        }
+        const int32_t lead = lead_of(p, grp, lane);
         if (lead < 0)
             continue;  // no row reads the partials
         const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
@@ -540,6 +548,443 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     }
 }
 
+// The same for items of many columns.  A block of kWideWaves waves takes ST tiles of 32
+// tokens at a time.  Each wave brings a piece of them (keys or values) from memory to
+// registers one stage ahead, makes matrix operands of it (E4M3 widened, values turned,
+// tokens that are not there cleared) and puts them into LDS, lane by lane as the
+// matrix instructions take them, so that all reads and writes of LDS are 1 KiB in the
+// order of the lanes.  WC waves have HT column tiles each; the kWideWaves / WC teams
+// take a stage's tiles in turn and join at the item's end.
+constexpr int kWideWaves = 8;
+constexpr int kWideThreads = 64 * kWideWaves;
+
+template <bool FP8, int D>
+struct Wide {
+    static constexpr int kStage = D > 128 ? 2 : 4;    // tiles
+    static constexpr int kHT = D > 128 ? 1 : 2;
+    static constexpr int kFrags = D / 16;             // 1 KiB operands of a tile's keys, and values
+};
+
+template <int TYPE, bool FP8, int D, int WC>
+__global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
+    const SharedProblem p, const int32_t *__restrict__ tables)
+{
+    typedef Shape<TYPE, FP8, D, 1> S;
+    typedef Wide<FP8, D> W;
+    constexpr int HT = W::kHT, ST = W::kStage, kFrags = W::kFrags;
+    constexpr int kTeams = kWideWaves / WC;
+    // [2 stages][tiles][keys: half, step; values: output tile]
+    __shared__ u32x4 s_op[2][ST][2 * kFrags * 64];
+    __shared__ uint16_t s_live[2][ST][2];  // tokens of each half that are there
+    __shared__ float s_stat[kWideWaves][128];
+    __shared__ Groups s_groups;
+
+    const AttnProblem &a = p.attn;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const int heads = a.kv_heads * a.head_groups;
+    const int hv = blockIdx.x % heads, block = blockIdx.x / heads, blocks = gridDim.x / heads;
+    const int kvh = hv / a.head_groups, sub = hv % a.head_groups;
+    const int first_head = kvh * a.group + sub * a.group_step;
+    const int n_heads = min(a.group_step, a.group - sub * a.group_step);
+
+    const bool good = find_groups<kWideWaves>(p, s_groups);
+    const int32_t all = good ? s_groups.tiles[p.groups] : 0;
+    const Line line(all, blocks);
+    if (hv == 0)
+        put_rows<kWideWaves>(p, s_groups, good, line, block, blocks);
+    if (block >= line.blocks)
+        return;
+
+    const uint32_t tokens = 1u << a.log2_tokens;
+    const uint32_t key_lane = (4 * (col & 3) + (col >> 2)) * 64 + quarter * 16;
+    const uint32_t key_head = (uint32_t)kvh * S::kKeyLoads * tokens * 64;
+    const uint32_t val_head = (uint32_t)(a.kv_heads + kvh) * tokens * (D * S::kElt);
+    const float to_log2 = a.score_scale * kLog2e;
+    const int32_t last_col = (int32_t)a.table_cols - 1;
+    const int wc = wave % WC, team = wave / WC;
+    // this wave's piece of a stage: four waves keys, four values; a tile, or (two tiles a
+    // stage) a half of its tokens for keys, 128 values or the rest of them for values
+    const bool keys = wave < kWideWaves / 2;
+    const int my_tile = ST == 4 ? wave & 3 : (wave & 3) >> 1, my_part = ST == 4 ? 0 : wave & 1;
+
+    int32_t tile = line.begin(block);
+    const int32_t end = line.begin(block + 1);
+    int g = last_from(s_groups.tiles, p.groups, tile);
+    while (tile < end) {
+        while (s_groups.tiles[g + 1] <= tile)
+            ++g;
+        const Group grp = group_of(p, g);
+        const int32_t n_tiles = tiles_of(grp);
+        const int32_t in_group = tile - s_groups.tiles[g];
+        const int32_t at = in_group / n_tiles, skip = in_group % n_tiles;
+        const int32_t part = min(n_tiles - skip, end - tile);
+        const int32_t item = s_groups.items[g] + at;
+        const int32_t row0 = grp.first + at * p.item_rows;
+        const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
+        tile += part;
+        const int32_t lead = lead_of(p, grp, lane);
+        if (lead < 0)
+            continue;
+        const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
+        const int32_t hi = grp.length;
+
+        // ---- a piece of a stage: from memory, and into LDS as operands -----------------
+        // keys: a load a 64-byte segment and half; values: eight loads of four tokens
+        constexpr int kKeyHalves = ST == 4 ? 2 : 1;
+        constexpr int kRaw = kKeyHalves * S::kKeyLoads > 8 ? kKeyHalves * S::kKeyLoads : 8;
+        u32x4 raw[kRaw];
+        uint32_t live;     // bits of the tile's tokens
+        int32_t id[2];
+        const auto find = [&](int32_t stage) {  // block ids, one stage ahead of their use
+            const int32_t t0 = (skip + stage * ST + my_tile) * kTile;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                id[h] = table[min(min(t0 + 16 * h, hi - 1) >> a.log2_tokens, last_col)];
+        };
+        const auto fetch = [&](int32_t stage) {
+            const int32_t u = stage * ST + my_tile;
+            live = 0;
+            if (u >= part)
+                return;
+            const int32_t t0 = (skip + u) * kTile;
+            const uint8_t *base[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool ok = id[h] >= 0 && id[h] < a.n_blocks;
+                base[h] = a.pool + (int64_t)(ok ? id[h] : 0) * a.block_stride;
+                const int32_t left = max(0, min(hi - (t0 + 16 * h), 16));
+                if (ok)
+                    live |= ((1u << left) - 1u) << 16 * h;
+            }
+            if (keys) {
+#pragma unroll
+                for (int i = 0; i < kKeyHalves; ++i) {
+                    const int h = kKeyHalves == 2 ? i : my_part;
+                    const uint32_t place = (uint32_t)(t0 + 16 * h) & (tokens - 1);
+                    const uint8_t *from = (h ? base[1] : base[0]) + (key_head + place * 64) + key_lane;
+#pragma unroll
+                    for (int s = 0; s < S::kKeyLoads; ++s)
+                        raw[i * S::kKeyLoads + s] =
+                            *reinterpret_cast<const u32x4 *>(from + s * tokens * 64);
+                }
+            } else {
+                const int d0 = my_part * 128;
+                const auto values = [&](auto width, int from0, auto place_of_raw) {
+                    constexpr int N = width;
+                    typedef typename Piece<N * S::kElt>::T Raw;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int h = j >> 2;
+                        const uint32_t t = ((uint32_t)(t0 + 16 * h) & (tokens - 1)) + 4 * (j & 3);
+                        const Raw x = *reinterpret_cast<const Raw *>(
+                            base[h] + (val_head + (t * D + from0) * S::kElt) +
+                            (quarter * D + col * N) * S::kElt);
+                        place_of_raw(j, x);
+                    }
+                };
+                const auto keep = [&](int dword) {
+                    return [&, dword](int j, auto x) {
+                        uint32_t v[4] = {};
+                        __builtin_memcpy(v, &x, sizeof(x));
+#pragma unroll
+                        for (int k = 0; k < (int)sizeof(x) / 4; ++k)
+                            raw[j][(dword + k) & 3] = v[k];
+                    };
+                };
+                if (D >= 128 && (ST == 4 || my_part == 0))
+                    values(std::integral_constant<int, 8>(), 0, keep(0));
+                else if (D == 256)
+                    values(std::integral_constant<int, 8>(), d0, keep(0));
+                else if (D == 192 || D == 64)
+                    values(std::integral_constant<int, 4>(), D - 64, keep(0));
+                else if (!FP8) {  // 96: a piece of 64 and one of 32
+                    values(std::integral_constant<int, 4>(), 0, keep(0));
+                    values(std::integral_constant<int, (FP8 ? 4 : 2)>(), 64, keep(2));
+                }
+            }
+        };
+        const auto stash = [&](int32_t stage) {
+            const int32_t u = stage * ST + my_tile;
+            if (u >= part)
+                return;
+            u32x4 *to = s_op[stage & 1][my_tile] + lane;
+            if (keys) {
+#pragma unroll
+                for (int i = 0; i < kKeyHalves; ++i) {
+                    const int h = kKeyHalves == 2 ? i : my_part;
+#pragma unroll
+                    for (int s = 0; s < S::kSteps; ++s) {
+                        u32x4 k;
+                        if (FP8) {
+                            const u32x4 k16 = raw[i * S::kKeyLoads + (s >> 1)];
+                            const uint32_t c0 = s & 1 ? k16.z : k16.x, c1 = s & 1 ? k16.w : k16.y;
+                            k = u32x4{wide2<TYPE, false>(c0), wide2<TYPE, true>(c0),
+                                      wide2<TYPE, false>(c1), wide2<TYPE, true>(c1)};
+                        } else {
+                            k = raw[i * S::kKeyLoads + s];
+                        }
+                        to[(h * S::kSteps + s) * 64] = k;
+                    }
+                    if (lane == 0)
+                        s_live[stage & 1][my_tile][h] = (uint16_t)(live >> 16 * h);
+                }
+                return;
+            }
+            if (live != ~0u) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (!(live >> (16 * (j >> 2) + 4 * (j & 3) + quarter) & 1))
+                        raw[j] = u32x4{0u, 0u, 0u, 0u};
+            }
+            to += kFrags * 64;
+            // dword d of raw holds values 2d and 2d + 1 (E4M3: 4d ...) of a token
+            const auto turn = [&](int dword, int width, int out) {
+#pragma unroll
+                for (int i = 0; i < width / 2; ++i) {
+                    u32x4 even, odd;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (FP8) {
+                            const uint32_t t = __builtin_amdgcn_perm(
+                                raw[2 * j + 1][(dword + (i >> 1)) & 3],
+                                raw[2 * j][(dword + (i >> 1)) & 3],
+                                i & 1 ? 0x07030602u : 0x05010400u);
+                            even[j] = wide2<TYPE, false>(t);
+                            odd[j] = wide2<TYPE, true>(t);
+                        } else {
+                            const uint32_t x = raw[2 * j][(dword + i) & 3],
+                                           y = raw[2 * j + 1][(dword + i) & 3];
+                            even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                            odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                        }
+                    }
+                    to[(out + 2 * i) * 64] = even;
+                    to[(out + 2 * i + 1) * 64] = odd;
+                }
+            };
+            if (D >= 128 && (ST == 4 || my_part == 0)) {
+                turn(0, 8, 0);
+            } else if (D == 256) {
+                turn(0, 8, 8);
+            } else if (D == 192 || D == 64) {
+                turn(0, 4, (D - 64) / 16);
+            } else if (!FP8) {
+                turn(0, 4, 0);
+                turn(2, 2, 4);
+            }
+        };
+
+        // ---- query fragments ------------------------------------------------------
+        int32_t column[HT];
+        bool used[HT];
+        u32x4 q[HT][S::kSteps];
+        f32x4 acc[HT][S::kAcc];
+        float ref[HT], sum[HT];
+        find(0);
+        fetch(0);
+        find(1);
+#pragma unroll
+        for (int c = 0; c < HT; ++c) {
+            column[c] = (wc * HT + c) * 16 + col;
+            const int32_t r = column[c] / a.group_step, head = column[c] % a.group_step;
+            used[c] = r < n_rows && head < n_heads;
+            const uint8_t *qp = static_cast<const uint8_t *>(a.q) +
+                                ((int64_t)(row0 + r) * a.q_stride +
+                                 (int64_t)(first_head + head) * D) * 2;
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) {
+                const int d = FP8 ? 64 * (s >> 1) + 16 * quarter + 8 * (s & 1)
+                                  : 32 * s + 8 * quarter;
+                q[c][s] = u32x4{0u, 0u, 0u, 0u};
+                if (used[c])
+                    q[c][s] = load16(qp + d * 2);
+            }
+            ref[c] = kNone;
+            sum[c] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i)
+                acc[c][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+        const auto take = [&](const u32x4 *op, uint32_t there) {
+            f32x4 scores[HT][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int c = 0; c < HT; ++c)
+                    scores[c][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < S::kSteps; ++s) {
+                    const u32x4 k = op[(h * S::kSteps + s) * 64];
+#pragma unroll
+                    for (int c = 0; c < HT; ++c)
+                        scores[c][h] = mfma32<TYPE>(k, q[c][s], scores[c][h]);
+                }
+            }
+            float to_ref = to_log2;
+            if (there != ~0u) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool live = there >> (16 * (j >> 2) + 4 * (j & 3) + quarter) & 1;
+#pragma unroll
+                    for (int c = 0; c < HT; ++c) {
+                        const float x = scores[c][j >> 2][j & 3] * to_log2;
+                        scores[c][j >> 2][j & 3] = live ? x : -__builtin_inff();
+                    }
+                }
+                to_ref = 1.0f;
+            }
+            float x[HT][8];
+            const auto weigh = [&](int c, float r) {
+#pragma clang fp contract(off)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[c][j] = scores[c][j >> 2][j & 3] * to_ref - r;
+                float m = x[c][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j)
+                    m = fmaxf(m, x[c][j]);
+                return m;
+            };
+            float top = weigh(0, ref[0]);
+#pragma unroll
+            for (int c = 1; c < HT; ++c)
+                top = fmaxf(top, weigh(c, ref[c]));
+            if (__any(top > kRoom)) {
+#pragma unroll
+                for (int c = 0; c < HT; ++c) {
+                    const float most = quarters_max(weigh(c, 0.0f));
+                    const float r = most - ref[c] > kRoom ? most - kLift : ref[c];
+                    const float shrink = __builtin_amdgcn_exp2f(ref[c] - r);
+                    ref[c] = r;
+                    sum[c] *= shrink;
+#pragma unroll
+                    for (int i = 0; i < S::kAcc; ++i)
+                        acc[c][i] *= shrink;
+                    weigh(c, r);
+                }
+            }
+            u32x4 p_hi[HT], p_lo[HT];
+#pragma unroll
+            for (int c = 0; c < HT; ++c) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[c][j] = __builtin_amdgcn_exp2f(x[c][j]);
+                sum[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) +
+                          ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t hi2, lo2;
+                    split2<TYPE>(x[c][2 * j], x[c][2 * j + 1], hi2, lo2);
+                    p_hi[c][j] = hi2;
+                    p_lo[c][j] = lo2;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i) {
+                const u32x4 v = op[(kFrags + i) * 64];
+#pragma unroll
+                for (int c = 0; c < HT; ++c) {
+                    acc[c][i] = mfma32<TYPE>(v, p_hi[c], acc[c][i]);
+                    acc[c][i] = mfma32<TYPE>(v, p_lo[c], acc[c][i]);
+                }
+            }
+        };
+
+        const int32_t stages = (part + ST - 1) / ST;
+        __syncthreads();  // the item before has been joined
+        stash(0);
+        __syncthreads();
+        for (int32_t stage = 0; stage < stages; ++stage) {
+            fetch(stage + 1);  // past the part: nothing
+            find(stage + 2);
+            const auto op = s_op[stage & 1];
+            const auto each = [&](int i) {
+                if (stage * ST + i < part) {
+                    const uint32_t there = s_live[stage & 1][i][0] |
+                                           (uint32_t)s_live[stage & 1][i][1] << 16;
+                    take(op[i] + lane, __builtin_amdgcn_readfirstlane(there));
+                }
+            };
+            constexpr int kEach = ST / kTeams;  // tiles of a stage that a wave has
+#pragma unroll 1
+            for (int i = 0; i < (kEach + 1) / 2; ++i)
+                each(i * kTeams + team);
+            stash(stage + 1);
+#pragma unroll 1
+            for (int i = (kEach + 1) / 2; i < kEach; ++i)
+                each(i * kTeams + team);
+            __syncthreads();
+        }
+
+        // ---- the block's partial of the item -----------------------------------------
+        const int64_t slot = ((int64_t)hv * p.slots + block + item) * p.columns;
+        const auto put2 = [&](int32_t column, int t, f32x4 x, f32x4 y) {
+            const int width = t < 8 * S::kP8 ? 8 : (t < 8 * S::kP8 + 4 * S::kP4 ? 4 : 2);
+            float *to = p.part_out + (slot + column) * D + (t & -width) * 16 +
+                        (t & (width - 1)) + width * 4 * quarter;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<f32x2 *>(to + width * k) = f32x2{x[k], y[k]};
+        };
+        const auto put_stat = [&](int32_t column, float r, float l) {
+            *reinterpret_cast<f32x2 *>(p.part_stat + (slot + column) * 2) = f32x2{r, l};
+        };
+        f32x4 *parts = reinterpret_cast<f32x4 *>(&s_op[0][0][0]);  // [waves][kAcc][64]
+        static_assert(kTeams == 1 || sizeof(s_op) >= sizeof(f32x4) * kWideWaves * S::kAcc * 64,
+                      "a column tile of all waves fits the stages");
+#pragma unroll
+        for (int c = 0; c < HT; ++c) {
+            sum[c] = quarters_sum(sum[c]);
+            if (kTeams == 1) {
+                if (used[c]) {
+#pragma unroll
+                    for (int t = 0; t < S::kAcc; t += 2)
+                        put2(column[c], t, acc[c][t], acc[c][t + 1]);
+                    if (quarter == 0)
+                        put_stat(column[c], ref[c], sum[c]);
+                }
+                continue;
+            }
+            if (c > 0)
+                __syncthreads();
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i)
+                parts[(wave * S::kAcc + i) * 64 + lane] = acc[c][i];
+            s_stat[wave][lane] = ref[c];
+            s_stat[wave][64 + lane] = sum[c];
+            __syncthreads();
+            float weight[kTeams], top = kNone, total = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kTeams; ++i) {
+                weight[i] = s_stat[i * WC + wc][lane];
+                top = fmaxf(top, weight[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kTeams; ++i) {
+                weight[i] = __builtin_amdgcn_exp2f(weight[i] - top);
+                total += s_stat[i * WC + wc][64 + lane] * weight[i];
+            }
+            if (used[c]) {
+                for (int t = 2 * team; t < S::kAcc; t += 2 * kTeams) {
+                    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+#pragma unroll
+                    for (int k = 0; k < kTeams; ++k) {
+                        const f32x4 *at = parts + ((k * WC + wc) * S::kAcc + t) * 64 + lane;
+                        x += at[0] * weight[k];
+                        y += at[64] * weight[k];
+                    }
+                    put2(column[c], t, x, y);
+                }
+                if (team == 0 && quarter == 0)
+                    put_stat(column[c], top, total);
+            }
+        }
+    }
+}
+
 // Joins a row's partials: of its shared tokens, and of its own.  A block a row and
 // key/value head (and pass); the (head, 4 values) items are dealt to threads, several
 // threads an item where there are many partials, which combine through LDS in a fixed
@@ -632,22 +1077,21 @@ hipError_t launch(const SharedProblem &p, int blocks, int attn_blocks, hipStream
 {
     const int heads = p.attn.kv_heads * p.attn.head_groups;
     const dim3 grid((unsigned)(blocks * heads));
+    constexpr int a_wave = 16 * Wide<FP8, D>::kHT;
     if (p.columns == 16)
         hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1, 1>), grid, dim3(kThreads), 0, stream, p,
                            p.attn.table);
-    else if (p.columns == 64)
-        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1, 4>), grid, dim3(kThreads), 0, stream, p,
+    else if (p.columns == 8 * a_wave)
+        hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, 8>), grid, dim3(kWideThreads), 0,
+                           stream, p, p.attn.table);
+    else if (p.columns == 4 * a_wave)
+        hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, 4>), grid, dim3(kWideThreads), 0,
+                           stream, p, p.attn.table);
+    else if constexpr (attn_heads_a_pass(FP8, D) == 32)
+        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 1>), grid, dim3(kThreads), 0, stream, p,
                            p.attn.table);
-    else if constexpr (attn_heads_a_pass(FP8, D) == 32) {
-        if (p.columns == 32)
-            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 1>), grid, dim3(kThreads), 0, stream,
-                               p, p.attn.table);
-        else
-            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 4>), grid, dim3(kThreads), 0, stream,
-                               p, p.attn.table);
-    } else {
+    else
         return hipErrorInvalidValue;
-    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
