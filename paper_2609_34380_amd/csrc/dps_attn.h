@@ -57,8 +57,10 @@ __device__ __forceinline__ void split2(float p0, float p1, uint32_t &hi, uint32_
     } else {
         const auto h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
         hi = __builtin_bit_cast(uint32_t, h);
-        lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p0 - (float)h[0],
-                                                                     p1 - (float)h[1]));
+        // (a multiply-add takes the 16-bit value as it is)
+        lo = __builtin_bit_cast(uint32_t,
+                                __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf((float)h[0], -1.0f, p0),
+                                                           __builtin_fmaf((float)h[1], -1.0f, p1)));
     }
 }
 

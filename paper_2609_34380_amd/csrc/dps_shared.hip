@@ -557,6 +557,9 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
 // take a stage's tiles in turn and join at the item's end.
 constexpr int kWideWaves = 8;
 constexpr int kWideThreads = 64 * kWideWaves;
+// Up to here a score's product with its factor is off by less than 2^-8 when rounded, and
+// weights may come from the exact one.
+constexpr float kFar = 65536.0f;
 
 template <bool FP8, int D>
 struct Wide {
@@ -808,63 +811,74 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
                 acc[c][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 
+        bool far = false;  // a reference score so large that products are rounded first
         const auto take = [&](const u32x4 *op, uint32_t there) {
+            // all operands on their way before the first is waited for
+            u32x4 k[2 * S::kSteps], v[S::kAcc];
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    k[h * S::kSteps + s] = op[(h * S::kSteps + s) * 64];
+#pragma unroll
+            for (int i = 0; i < S::kAcc; ++i)
+                v[i] = op[(kFrags + i) * 64];
+            if (D <= 128)  // wider ones leave no registers for it
+                __builtin_amdgcn_sched_barrier(0);
             f32x4 scores[HT][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int c = 0; c < HT; ++c)
                     scores[c][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int s = 0; s < S::kSteps; ++s) {
-                    const u32x4 k = op[(h * S::kSteps + s) * 64];
+            for (int s = 0; s < S::kSteps; ++s) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
 #pragma unroll
                     for (int c = 0; c < HT; ++c)
-                        scores[c][h] = mfma32<TYPE>(k, q[c][s], scores[c][h]);
+                        scores[c][h] = mfma32<TYPE>(k[h * S::kSteps + s], q[c][s], scores[c][h]);
                 }
-            }
-            float to_ref = to_log2;
-            if (there != ~0u) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool live = there >> (16 * (j >> 2) + 4 * (j & 3) + quarter) & 1;
-#pragma unroll
-                    for (int c = 0; c < HT; ++c) {
-                        const float x = scores[c][j >> 2][j & 3] * to_log2;
-                        scores[c][j >> 2][j & 3] = live ? x : -__builtin_inff();
-                    }
-                }
-                to_ref = 1.0f;
             }
             float x[HT][8];
-            const auto weigh = [&](int c, float r) {
-#pragma clang fp contract(off)
+            const auto weigh = [&](int c, float factor, float r) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    x[c][j] = scores[c][j >> 2][j & 3] * to_ref - r;
+                    x[c][j] = __builtin_fmaf(scores[c][j >> 2][j & 3], factor, -r);
                 float m = x[c][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j)
                     m = fmaxf(m, x[c][j]);
                 return m;
             };
-            float top = weigh(0, ref[0]);
+            float top = weigh(0, to_log2, ref[0]);
 #pragma unroll
             for (int c = 1; c < HT; ++c)
-                top = fmaxf(top, weigh(c, ref[c]));
-            if (__any(top > kRoom)) {
+                top = fmaxf(top, weigh(c, to_log2, ref[c]));
+            if (__any(top > kRoom) || far || there != ~0u) {
+                // the products rounded before the differences: the largest score, which the
+                // reference came from, is then kLift above it whatever its size
+                bool large = false;
 #pragma unroll
                 for (int c = 0; c < HT; ++c) {
-                    const float most = quarters_max(weigh(c, 0.0f));
-                    const float r = most - ref[c] > kRoom ? most - kLift : ref[c];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool live = there >> (16 * (j >> 2) + 4 * (j & 3) + quarter) & 1;
+                        const float s = scores[c][j >> 2][j & 3] * to_log2;
+                        scores[c][j >> 2][j & 3] = live ? s : -__builtin_inff();
+                    }
+                    const float most = quarters_max(weigh(c, 1.0f, 0.0f));
+                    const float r = fmaxf(most - kLift, ref[c]);
                     const float shrink = __builtin_amdgcn_exp2f(ref[c] - r);
                     ref[c] = r;
                     sum[c] *= shrink;
 #pragma unroll
                     for (int i = 0; i < S::kAcc; ++i)
                         acc[c][i] *= shrink;
-                    weigh(c, r);
+                    weigh(c, 1.0f, r);
+                    large = large || __builtin_fabsf(r) > kFar;
                 }
+                far = __any(large);
             }
             u32x4 p_hi[HT], p_lo[HT];
 #pragma unroll
@@ -883,12 +897,16 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
                 }
             }
 #pragma unroll
-            for (int i = 0; i < S::kAcc; ++i) {
-                const u32x4 v = op[(kFrags + i) * 64];
+            for (int i = 0; i < S::kAcc; i += 2) {
 #pragma unroll
                 for (int c = 0; c < HT; ++c) {
-                    acc[c][i] = mfma32<TYPE>(v, p_hi[c], acc[c][i]);
-                    acc[c][i] = mfma32<TYPE>(v, p_lo[c], acc[c][i]);
+                    acc[c][i] = mfma32<TYPE>(v[i], p_hi[c], acc[c][i]);
+                    acc[c][i + 1] = mfma32<TYPE>(v[i + 1], p_hi[c], acc[c][i + 1]);
+                }
+#pragma unroll
+                for (int c = 0; c < HT; ++c) {
+                    acc[c][i] = mfma32<TYPE>(v[i], p_lo[c], acc[c][i]);
+                    acc[c][i + 1] = mfma32<TYPE>(v[i + 1], p_lo[c], acc[c][i + 1]);
                 }
             }
         };
