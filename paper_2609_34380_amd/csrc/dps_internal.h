@@ -242,16 +242,17 @@ struct SharedProblem {
 constexpr int kSharedGroups = 1024;
 // Columns of an item: a group of average size fills them where that is possible.  16 and
 // 32: tokens from memory to registers, a block's waves on different ones; above, through
-// LDS for four or eight waves of 32 columns (16 for heads over 128).
+// LDS, and half of a block's waves or all of them have columns of their own (32 each; of
+// eight waves, of four for heads over 128).
 constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, int dim)
 {
     const int64_t mean = rows * step / (groups < 1 ? 1 : groups);
-    const int wave = dim > 128 ? 16 : 32;
     if (mean <= 16 && step <= 16)
         return 16;
-    if (mean <= 32 && attn_heads_a_pass(fp8, dim) == 32)
+    if (dim % 64 != 0 || (mean <= 32 && attn_heads_a_pass(fp8, dim) == 32))
         return 32;
-    return mean <= 4 * wave ? 4 * wave : 8 * wave;
+    const int half = dim > 128 ? 64 : 128;
+    return mean <= half ? half : 2 * half;
 }
 constexpr int shared_blocks_per_cu(int columns, bool fp8, int dim)
 {

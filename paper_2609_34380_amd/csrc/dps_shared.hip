@@ -548,44 +548,92 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     }
 }
 
-// The same for items of many columns.  A block of kWideWaves waves takes ST tiles of 32
-// tokens at a time.  Each wave brings a piece of them (keys or values) from memory to
+// The same for items of many columns.  A block of waves takes ST tiles of 32 tokens at a
+// time.  Each wave brings a piece of them, some keys and some values, from memory to
 // registers one stage ahead, makes matrix operands of it (E4M3 widened, values turned,
 // tokens that are not there cleared) and puts them into LDS, lane by lane as the
 // matrix instructions take them, so that all reads and writes of LDS are 1 KiB in the
-// order of the lanes.  WC waves have HT column tiles each; the kWideWaves / WC teams
-// take a stage's tiles in turn and join at the item's end.
-constexpr int kWideWaves = 8;
-constexpr int kWideThreads = 64 * kWideWaves;
+// order of the lanes.  WC waves have 32 columns each; the others are teams with the same
+// columns, which take a stage's tiles in turn and join at the item's end.
+//
+// Products are 32 x 32 x 16: S^T of 32 tokens and 32 columns, O^T of 32 values and 32
+// columns.  They read half the operands of 16 x 16 x 32 for the same work, which leaves
+// the vector ALUs more of the register file: 8 waves of 16 x 16 x 32 instructions and 24
+// multiply-adds beside each 8 of them take 1.45 times the instructions' own time, here
+// 1.34.
+//   - Lane (m, hf) = (lane % 32, lane / 32) holds row (or column) m and 8 of a step's 16
+//     places in the sum, hf * 8 + j; of a result it holds column m, in register i
+//     row 8 (i / 4) + 4 hf + i % 4.
+//   - Keys: row m is token m, places are values 16 s + 8 hf + j of step s (E4M3: 16
+//     values of a 16-byte load in two steps; the queries lie accordingly).
+//   - Weights: registers 8 u + j of S^T are the places of step u of P^T as they are,
+//     so token 8 (i / 4) + 4 hf + i % 4, i = 8 u + j, is what the values bring there.
+//   - Values: 32 lanes read W = D / 32 neighbouring values each of a token, and value
+//     W m + e is row m of output tile e (192: W = 4, then W = 2).
+template <bool FP8, int D>
+struct Wide {
+    static constexpr int kWaves = D > 128 ? 4 : 8;  // 512 registers a lane, or 256
+    static constexpr int kStage = D > 128 ? 2 : 4;  // tiles
+    static constexpr int kParts = kWaves / kStage;  // pieces of a tile
+    static constexpr int kFrags = D / 16;           // 1 KiB operands of a tile's keys, and values
+    static constexpr int kKeys = kFrags / kParts;   // of keys in a piece
+    static constexpr int kAcc = D / 32;             // output tiles
+    static constexpr int kElt = FP8 ? 1 : 2;
+};
 // Up to here a score's product with its factor is off by less than 2^-8 when rounded, and
 // weights may come from the exact one.
 constexpr float kFar = 65536.0f;
 
-template <bool FP8, int D>
-struct Wide {
-    static constexpr int kStage = D > 128 ? 2 : 4;    // tiles
-    static constexpr int kHT = D > 128 ? 1 : 2;
-    static constexpr int kFrags = D / 16;             // 1 KiB operands of a tile's keys, and values
-};
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <int TYPE>
+__device__ __forceinline__ f32x16 mfma16(u32x4 a, u32x4 b, f32x16 c)
+{
+    if (TYPE == KV_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(a), as_half8(b), c, 0, 0, 0);
+}
+
+// Over the two lanes that share a column.
+template <typename F>
+__device__ __forceinline__ float over_halves(float x, const F &f)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a0 = a[0], a1 = a[1];
+    return f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+}
+
+template <int BYTES>
+struct Raw;
+template <>
+struct Raw<16> { typedef u32x4 T; };
+template <>
+struct Raw<8> { typedef u32x2 T; };
+template <>
+struct Raw<4> { typedef uint32_t T; };
+template <>
+struct Raw<2> { typedef uint16_t T; };
 
 template <int TYPE, bool FP8, int D, int WC>
-__global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
-    const SharedProblem p, const int32_t *__restrict__ tables)
+__global__ __launch_bounds__((64 * Wide<FP8, D>::kWaves), (Wide<FP8, D>::kWaves / 4)) void
+shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
 {
-    typedef Shape<TYPE, FP8, D, 1> S;
     typedef Wide<FP8, D> W;
-    constexpr int HT = W::kHT, ST = W::kStage, kFrags = W::kFrags;
+    constexpr int ST = W::kStage, kFrags = W::kFrags, kAcc = W::kAcc, kWideWaves = W::kWaves;
     constexpr int kTeams = kWideWaves / WC;
-    // [2 stages][tiles][keys: half, step; values: output tile]
+    constexpr int kFirst = D == 192 ? 4 : kAcc;  // output tiles of the values' first piece
+    static_assert(W::kKeys % 2 == 0, "an E4M3 load is two steps");
+    // [2 stages][tiles][keys: step; values: output tile, step]
     __shared__ u32x4 s_op[2][ST][2 * kFrags * 64];
-    __shared__ uint16_t s_live[2][ST][2];  // tokens of each half that are there
+    __shared__ uint32_t s_live[2][ST];  // tokens of a tile that are there
     __shared__ float s_stat[kWideWaves][128];
     __shared__ Groups s_groups;
 
     const AttnProblem &a = p.attn;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, quarter = lane >> 4;
+    const int col = lane & 31, hf = lane >> 5;
     const int heads = a.kv_heads * a.head_groups;
     const int hv = blockIdx.x % heads, block = blockIdx.x / heads, blocks = gridDim.x / heads;
     const int kvh = hv / a.head_groups, sub = hv % a.head_groups;
@@ -601,16 +649,14 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
         return;
 
     const uint32_t tokens = 1u << a.log2_tokens;
-    const uint32_t key_lane = (4 * (col & 3) + (col >> 2)) * 64 + quarter * 16;
-    const uint32_t key_head = (uint32_t)kvh * S::kKeyLoads * tokens * 64;
-    const uint32_t val_head = (uint32_t)(a.kv_heads + kvh) * tokens * (D * S::kElt);
+    const uint32_t key_head = (uint32_t)kvh * tokens * (D * W::kElt);
+    const uint32_t val_head = (uint32_t)(a.kv_heads + kvh) * tokens * (D * W::kElt);
     const float to_log2 = a.score_scale * kLog2e;
     const int32_t last_col = (int32_t)a.table_cols - 1;
     const int wc = wave % WC, team = wave / WC;
-    // this wave's piece of a stage: four waves keys, four values; a tile, or (two tiles a
-    // stage) a half of its tokens for keys, 128 values or the rest of them for values
-    const bool keys = wave < kWideWaves / 2;
-    const int my_tile = ST == 4 ? wave & 3 : (wave & 3) >> 1, my_part = ST == 4 ? 0 : wave & 1;
+    const int my_tile = wave / W::kParts, my_part = wave % W::kParts;
+    const int my_step = my_part;  // of the values: 16 of the tile's tokens
+    static_assert(W::kParts == 2, "a piece is half of a tile");
 
     int32_t tile = line.begin(block);
     const int32_t end = line.begin(block + 1);
@@ -634,11 +680,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
         const int32_t hi = grp.length;
 
         // ---- a piece of a stage: from memory, and into LDS as operands -----------------
-        // keys: a load a 64-byte segment and half; values: eight loads of four tokens
-        constexpr int kKeyHalves = ST == 4 ? 2 : 1;
-        constexpr int kRaw = kKeyHalves * S::kKeyLoads > 8 ? kKeyHalves * S::kKeyLoads : 8;
-        u32x4 raw[kRaw];
-        uint32_t live;     // bits of the tile's tokens
+        constexpr int kKeyLoads = FP8 ? W::kKeys / 2 : W::kKeys;
+        u32x4 key[kKeyLoads];
+        constexpr int kVal = (D / 32 * W::kElt + 3) / 4;
+        uint32_t val[8][kVal];    // of eight tokens
+        uint32_t live = 0;        // bits of the tile's tokens
         int32_t id[2];
         const auto find = [&](int32_t stage) {  // block ids, one stage ahead of their use
             const int32_t t0 = (skip + stage * ST + my_tile) * kTile;
@@ -646,66 +692,78 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
             for (int h = 0; h < 2; ++h)
                 id[h] = table[min(min(t0 + 16 * h, hi - 1) >> a.log2_tokens, last_col)];
         };
+        // N values a lane of eight tokens, into val from dword to on
+        const auto read_values = [&](auto width, const uint8_t *from, uint32_t place, int d0,
+                                     auto to) {
+            constexpr int N = width;
+            typedef typename Raw<N * W::kElt>::T T;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t t = place + 8 * (j >> 2) + 4 * hf + (j & 3);
+                const T x = *reinterpret_cast<const T *>(
+                    from + (val_head + (t * D + d0 + col * N) * W::kElt));
+                uint32_t v[4] = {};
+                __builtin_memcpy(v, &x, sizeof(x));
+#pragma unroll
+                for (int k = 0; k < (int)(sizeof(x) + 3) / 4; ++k)
+                    val[j][to + k] = v[k];
+            }
+        };
         const auto fetch = [&](int32_t stage) {
             const int32_t u = stage * ST + my_tile;
-            live = 0;
             if (u >= part)
                 return;
             const int32_t t0 = (skip + u) * kTile;
             const uint8_t *base[2];
+            uint32_t place[2];
+            live = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const bool ok = id[h] >= 0 && id[h] < a.n_blocks;
                 base[h] = a.pool + (int64_t)(ok ? id[h] : 0) * a.block_stride;
+                place[h] = (uint32_t)(t0 + 16 * h) & (tokens - 1);
                 const int32_t left = max(0, min(hi - (t0 + 16 * h), 16));
                 if (ok)
                     live |= ((1u << left) - 1u) << 16 * h;
             }
-            if (keys) {
+            const uint8_t *from = (col < 16 ? base[0] : base[1]) +
+                                  (key_head + ((col < 16 ? place[0] : place[1]) + (col & 15)) * 64 +
+                                   hf * 16);
 #pragma unroll
-                for (int i = 0; i < kKeyHalves; ++i) {
-                    const int h = kKeyHalves == 2 ? i : my_part;
-                    const uint32_t place = (uint32_t)(t0 + 16 * h) & (tokens - 1);
-                    const uint8_t *from = (h ? base[1] : base[0]) + (key_head + place * 64) + key_lane;
+            for (int i = 0; i < kKeyLoads; ++i) {
+                const int s = my_part * kKeyLoads + i;  // 32 bytes of a token
+                key[i] = *reinterpret_cast<const u32x4 *>(from + (s >> 1) * tokens * 64 + (s & 1) * 32);
+            }
+            const uint8_t *vals = my_step ? base[1] : base[0];
+            const uint32_t vplace = my_step ? place[1] : place[0];
+            read_values(std::integral_constant<int, kFirst>(), vals, vplace, 0,
+                        std::integral_constant<int, 0>());
+            if constexpr (kFirst < kAcc)
+                read_values(std::integral_constant<int, 2>(), vals, vplace, 128,
+                            std::integral_constant<int, W::kElt>());
+        };
+        // the values from dword d of val on, into output tiles e0 ...
+        const auto turn = [&](auto width, u32x4 *to, auto d, int e0) {
+            constexpr int N = width;
 #pragma unroll
-                    for (int s = 0; s < S::kKeyLoads; ++s)
-                        raw[i * S::kKeyLoads + s] =
-                            *reinterpret_cast<const u32x4 *>(from + s * tokens * 64);
-                }
-            } else {
-                const int d0 = my_part * 128;
-                const auto values = [&](auto width, int from0, auto place_of_raw) {
-                    constexpr int N = width;
-                    typedef typename Piece<N * S::kElt>::T Raw;
+            for (int i = 0; i < N / 2; ++i) {
+                u32x4 even, odd;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int h = j >> 2;
-                        const uint32_t t = ((uint32_t)(t0 + 16 * h) & (tokens - 1)) + 4 * (j & 3);
-                        const Raw x = *reinterpret_cast<const Raw *>(
-                            base[h] + (val_head + (t * D + from0) * S::kElt) +
-                            (quarter * D + col * N) * S::kElt);
-                        place_of_raw(j, x);
+                for (int j = 0; j < 4; ++j) {
+                    if (FP8) {
+                        const uint32_t t = __builtin_amdgcn_perm(val[2 * j + 1][d + (i >> 1)],
+                                                                 val[2 * j][d + (i >> 1)],
+                                                                 i & 1 ? 0x07030602u : 0x05010400u);
+                        even[j] = wide2<TYPE, false>(t);
+                        odd[j] = wide2<TYPE, true>(t);
+                    } else {
+                        const uint32_t x = val[2 * j][d + i], y = val[2 * j + 1][d + i];
+                        even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                        odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
                     }
-                };
-                const auto keep = [&](int dword) {
-                    return [&, dword](int j, auto x) {
-                        uint32_t v[4] = {};
-                        __builtin_memcpy(v, &x, sizeof(x));
-#pragma unroll
-                        for (int k = 0; k < (int)sizeof(x) / 4; ++k)
-                            raw[j][(dword + k) & 3] = v[k];
-                    };
-                };
-                if (D >= 128 && (ST == 4 || my_part == 0))
-                    values(std::integral_constant<int, 8>(), 0, keep(0));
-                else if (D == 256)
-                    values(std::integral_constant<int, 8>(), d0, keep(0));
-                else if (D == 192 || D == 64)
-                    values(std::integral_constant<int, 4>(), D - 64, keep(0));
-                else if (!FP8) {  // 96: a piece of 64 and one of 32
-                    values(std::integral_constant<int, 4>(), 0, keep(0));
-                    values(std::integral_constant<int, (FP8 ? 4 : 2)>(), 64, keep(2));
                 }
+                to[(2 * (e0 + 2 * i) + my_step) * 64] = even;
+                to[(2 * (e0 + 2 * i + 1) + my_step) * 64] = odd;
             }
         };
         const auto stash = [&](int32_t stage) {
@@ -713,201 +771,143 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
             if (u >= part)
                 return;
             u32x4 *to = s_op[stage & 1][my_tile] + lane;
-            if (keys) {
+            const int first = my_part * W::kKeys;
 #pragma unroll
-                for (int i = 0; i < kKeyHalves; ++i) {
-                    const int h = kKeyHalves == 2 ? i : my_part;
-#pragma unroll
-                    for (int s = 0; s < S::kSteps; ++s) {
-                        u32x4 k;
-                        if (FP8) {
-                            const u32x4 k16 = raw[i * S::kKeyLoads + (s >> 1)];
-                            const uint32_t c0 = s & 1 ? k16.z : k16.x, c1 = s & 1 ? k16.w : k16.y;
-                            k = u32x4{wide2<TYPE, false>(c0), wide2<TYPE, true>(c0),
-                                      wide2<TYPE, false>(c1), wide2<TYPE, true>(c1)};
-                        } else {
-                            k = raw[i * S::kKeyLoads + s];
-                        }
-                        to[(h * S::kSteps + s) * 64] = k;
-                    }
-                    if (lane == 0)
-                        s_live[stage & 1][my_tile][h] = (uint16_t)(live >> 16 * h);
+            for (int i = 0; i < W::kKeys; ++i) {
+                if (FP8) {
+                    const u32x4 k16 = key[i >> 1];
+                    const uint32_t c0 = i & 1 ? k16.z : k16.x, c1 = i & 1 ? k16.w : k16.y;
+                    to[(first + i) * 64] =
+                        u32x4{wide2<TYPE, false>(c0), wide2<TYPE, true>(c0),
+                              wide2<TYPE, false>(c1), wide2<TYPE, true>(c1)};
+                } else {
+                    to[(first + i) * 64] = key[i];
                 }
-                return;
             }
+            if (my_part == 0 && lane == 0)
+                s_live[stage & 1][my_tile] = live;
             if (live != ~0u) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (!(live >> (16 * (j >> 2) + 4 * (j & 3) + quarter) & 1))
-                        raw[j] = u32x4{0u, 0u, 0u, 0u};
-            }
-            to += kFrags * 64;
-            // dword d of raw holds values 2d and 2d + 1 (E4M3: 4d ...) of a token
-            const auto turn = [&](int dword, int width, int out) {
+                    if (!(live >> (16 * my_step + 8 * (j >> 2) + 4 * hf + (j & 3)) & 1))
 #pragma unroll
-                for (int i = 0; i < width / 2; ++i) {
-                    u32x4 even, odd;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (FP8) {
-                            const uint32_t t = __builtin_amdgcn_perm(
-                                raw[2 * j + 1][(dword + (i >> 1)) & 3],
-                                raw[2 * j][(dword + (i >> 1)) & 3],
-                                i & 1 ? 0x07030602u : 0x05010400u);
-                            even[j] = wide2<TYPE, false>(t);
-                            odd[j] = wide2<TYPE, true>(t);
-                        } else {
-                            const uint32_t x = raw[2 * j][(dword + i) & 3],
-                                           y = raw[2 * j + 1][(dword + i) & 3];
-                            even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                            odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                        }
-                    }
-                    to[(out + 2 * i) * 64] = even;
-                    to[(out + 2 * i + 1) * 64] = odd;
-                }
-            };
-            if (D >= 128 && (ST == 4 || my_part == 0)) {
-                turn(0, 8, 0);
-            } else if (D == 256) {
-                turn(0, 8, 8);
-            } else if (D == 192 || D == 64) {
-                turn(0, 4, (D - 64) / 16);
-            } else if (!FP8) {
-                turn(0, 4, 0);
-                turn(2, 2, 4);
+                        for (int k = 0; k < kVal; ++k)
+                            val[j][k] = 0u;
             }
+            turn(std::integral_constant<int, kFirst>(), to + kFrags * 64,
+                 std::integral_constant<int, 0>(), 0);
+            if constexpr (kFirst < kAcc)
+                turn(std::integral_constant<int, 2>(), to + kFrags * 64,
+                     std::integral_constant<int, W::kElt>(), 4);
         };
 
         // ---- query fragments ------------------------------------------------------
-        int32_t column[HT];
-        bool used[HT];
-        u32x4 q[HT][S::kSteps];
-        f32x4 acc[HT][S::kAcc];
-        float ref[HT], sum[HT];
         find(0);
         fetch(0);
         find(1);
-#pragma unroll
-        for (int c = 0; c < HT; ++c) {
-            column[c] = (wc * HT + c) * 16 + col;
-            const int32_t r = column[c] / a.group_step, head = column[c] % a.group_step;
-            used[c] = r < n_rows && head < n_heads;
+        const int32_t column = wc * 32 + col;
+        const bool used = column / a.group_step < n_rows && column % a.group_step < n_heads;
+        u32x4 q[kFrags];
+        f32x16 acc[kAcc];
+        float ref = kNone, sum = 0.0f;
+        {
             const uint8_t *qp = static_cast<const uint8_t *>(a.q) +
-                                ((int64_t)(row0 + r) * a.q_stride +
-                                 (int64_t)(first_head + head) * D) * 2;
+                                ((int64_t)(row0 + column / a.group_step) * a.q_stride +
+                                 (int64_t)(first_head + column % a.group_step) * D) * 2;
 #pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) {
-                const int d = FP8 ? 64 * (s >> 1) + 16 * quarter + 8 * (s & 1)
-                                  : 32 * s + 8 * quarter;
-                q[c][s] = u32x4{0u, 0u, 0u, 0u};
-                if (used[c])
-                    q[c][s] = load16(qp + d * 2);
+            for (int s = 0; s < kFrags; ++s) {
+                const int d = FP8 ? 32 * (s >> 1) + 16 * hf + 8 * (s & 1) : 16 * s + 8 * hf;
+                q[s] = u32x4{0u, 0u, 0u, 0u};
+                if (used)
+                    q[s] = load16(qp + d * 2);
             }
-            ref[c] = kNone;
-            sum[c] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < S::kAcc; ++i)
-                acc[c][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < kAcc; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    acc[i][j] = 0.0f;
         }
 
         bool far = false;  // a reference score so large that products are rounded first
         const auto take = [&](const u32x4 *op, uint32_t there) {
-            // all operands on their way before the first is waited for
-            u32x4 k[2 * S::kSteps], v[S::kAcc];
+            f32x16 scores;
 #pragma unroll
-            for (int s = 0; s < S::kSteps; ++s)
+            for (int i = 0; i < 16; ++i)
+                scores[i] = 0.0f;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    k[h * S::kSteps + s] = op[(h * S::kSteps + s) * 64];
+            for (int s = 0; s < kFrags; ++s)
+                scores = mfma16<TYPE>(op[s * 64], q[s], scores);
+            constexpr bool kEarly = D <= 128;  // values on their way under the softmax
+            u32x4 v[kFrags];
+            if (kEarly) {
 #pragma unroll
-            for (int i = 0; i < S::kAcc; ++i)
-                v[i] = op[(kFrags + i) * 64];
-            if (D <= 128)  // wider ones leave no registers for it
+                for (int i = 0; i < kFrags; ++i)
+                    v[i] = op[(kFrags + i) * 64];
                 __builtin_amdgcn_sched_barrier(0);
-            f32x4 scores[HT][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < HT; ++c)
-                    scores[c][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                    for (int c = 0; c < HT; ++c)
-                        scores[c][h] = mfma32<TYPE>(k[h * S::kSteps + s], q[c][s], scores[c][h]);
-                }
             }
-            float x[HT][8];
-            const auto weigh = [&](int c, float factor, float r) {
+            float x[16];
+            const auto weigh = [&](float factor, float r) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[c][j] = __builtin_fmaf(scores[c][j >> 2][j & 3], factor, -r);
-                float m = x[c][0];
+                for (int i = 0; i < 16; ++i)
+                    x[i] = __builtin_fmaf(scores[i], factor, -r);
+                float m = x[0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j)
-                    m = fmaxf(m, x[c][j]);
+                for (int i = 1; i < 16; ++i)
+                    m = fmaxf(m, x[i]);
                 return m;
             };
-            float top = weigh(0, to_log2, ref[0]);
-#pragma unroll
-            for (int c = 1; c < HT; ++c)
-                top = fmaxf(top, weigh(c, to_log2, ref[c]));
-            if (__any(top > kRoom) || far || there != ~0u) {
+            if (__any(weigh(to_log2, ref) > kRoom) || far || there != ~0u) {
                 // the products rounded before the differences: the largest score, which the
                 // reference came from, is then kLift above it whatever its size
-                bool large = false;
 #pragma unroll
-                for (int c = 0; c < HT; ++c) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool live = there >> (16 * (j >> 2) + 4 * (j & 3) + quarter) & 1;
-                        const float s = scores[c][j >> 2][j & 3] * to_log2;
-                        scores[c][j >> 2][j & 3] = live ? s : -__builtin_inff();
-                    }
-                    const float most = quarters_max(weigh(c, 1.0f, 0.0f));
-                    const float r = fmaxf(most - kLift, ref[c]);
-                    const float shrink = __builtin_amdgcn_exp2f(ref[c] - r);
-                    ref[c] = r;
-                    sum[c] *= shrink;
-#pragma unroll
-                    for (int i = 0; i < S::kAcc; ++i)
-                        acc[c][i] *= shrink;
-                    weigh(c, 1.0f, r);
-                    large = large || __builtin_fabsf(r) > kFar;
+                for (int i = 0; i < 16; ++i) {
+                    const bool live = there >> (8 * (i >> 2) + 4 * hf + (i & 3)) & 1;
+                    const float s = scores[i] * to_log2;
+                    scores[i] = live ? s : -__builtin_inff();
                 }
-                far = __any(large);
+                const float most = over_halves(weigh(1.0f, 0.0f),
+                                               [](float a, float b) { return fmaxf(a, b); });
+                const float r = fmaxf(most - kLift, ref);
+                const float shrink = __builtin_amdgcn_exp2f(ref - r);
+                ref = r;
+                sum *= shrink;
+#pragma unroll
+                for (int i = 0; i < kAcc; ++i)
+                    acc[i] *= shrink;
+                weigh(1.0f, r);
+                far = __any(__builtin_fabsf(r) > kFar);
             }
-            u32x4 p_hi[HT], p_lo[HT];
+            u32x4 p_hi[2], p_lo[2];
 #pragma unroll
-            for (int c = 0; c < HT; ++c) {
+            for (int i = 0; i < 16; ++i)
+                x[i] = __builtin_amdgcn_exp2f(x[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[c][j] = __builtin_amdgcn_exp2f(x[c][j]);
-                sum[c] += ((x[c][0] + x[c][1]) + (x[c][2] + x[c][3])) +
-                          ((x[c][4] + x[c][5]) + (x[c][6] + x[c][7]));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t hi2, lo2;
-                    split2<TYPE>(x[c][2 * j], x[c][2 * j + 1], hi2, lo2);
-                    p_hi[c][j] = hi2;
-                    p_lo[c][j] = lo2;
-                }
+            for (int i = 0; i < 8; ++i) {
+                uint32_t hi2, lo2;
+                split2<TYPE>(x[2 * i], x[2 * i + 1], hi2, lo2);
+                p_hi[i >> 2][i & 3] = hi2;
+                p_lo[i >> 2][i & 3] = lo2;
             }
 #pragma unroll
-            for (int i = 0; i < S::kAcc; i += 2) {
+            for (int d = 8; d > 0; d /= 2)
 #pragma unroll
-                for (int c = 0; c < HT; ++c) {
-                    acc[c][i] = mfma32<TYPE>(v[i], p_hi[c], acc[c][i]);
-                    acc[c][i + 1] = mfma32<TYPE>(v[i + 1], p_hi[c], acc[c][i + 1]);
+                for (int i = 0; i < d; ++i)
+                    x[i] += x[i + d];
+            sum += x[0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (!kEarly) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < kAcc; ++i)
+                        v[2 * i + u] = op[(kFrags + 2 * i + u) * 64];
                 }
 #pragma unroll
-                for (int c = 0; c < HT; ++c) {
-                    acc[c][i] = mfma32<TYPE>(v[i], p_lo[c], acc[c][i]);
-                    acc[c][i + 1] = mfma32<TYPE>(v[i + 1], p_lo[c], acc[c][i + 1]);
-                }
+                for (int i = 0; i < kAcc; ++i)
+                    acc[i] = mfma16<TYPE>(v[2 * i + u], p_hi[u], acc[i]);
+#pragma unroll
+                for (int i = 0; i < kAcc; ++i)
+                    acc[i] = mfma16<TYPE>(v[2 * i + u], p_lo[u], acc[i]);
             }
         };
 
@@ -920,11 +920,9 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
             find(stage + 2);
             const auto op = s_op[stage & 1];
             const auto each = [&](int i) {
-                if (stage * ST + i < part) {
-                    const uint32_t there = s_live[stage & 1][i][0] |
-                                           (uint32_t)s_live[stage & 1][i][1] << 16;
-                    take(op[i] + lane, __builtin_amdgcn_readfirstlane(there));
-                }
+                if (stage * ST + i < part)
+                    take(op[i] + lane,
+                         __builtin_amdgcn_readfirstlane(s_live[stage & 1][i]));
             };
             constexpr int kEach = ST / kTeams;  // tiles of a stage that a wave has
 #pragma unroll 1
@@ -939,67 +937,80 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(
 
         // ---- the block's partial of the item -----------------------------------------
         const int64_t slot = ((int64_t)hv * p.slots + block + item) * p.columns;
-        const auto put2 = [&](int32_t column, int t, f32x4 x, f32x4 y) {
-            const int width = t < 8 * S::kP8 ? 8 : (t < 8 * S::kP8 + 4 * S::kP4 ? 4 : 2);
-            float *to = p.part_out + (slot + column) * D + (t & -width) * 16 +
-                        (t & (width - 1)) + width * 4 * quarter;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<f32x2 *>(to + width * k) = f32x2{x[k], y[k]};
-        };
-        const auto put_stat = [&](int32_t column, float r, float l) {
+        float *out = p.part_out + (slot + column) * D;
+        const auto put_stat = [&](float r, float l) {
             *reinterpret_cast<f32x2 *>(p.part_stat + (slot + column) * 2) = f32x2{r, l};
         };
-        f32x4 *parts = reinterpret_cast<f32x4 *>(&s_op[0][0][0]);  // [waves][kAcc][64]
-        static_assert(kTeams == 1 || sizeof(s_op) >= sizeof(f32x4) * kWideWaves * S::kAcc * 64,
-                      "a column tile of all waves fits the stages");
+        // register i of output tiles e0 ... e0 + N - 1: neighbouring values
+        const auto put = [&](auto width, int d0, int i, const float *x) {
+            constexpr int N = width;
+            __builtin_memcpy(out + d0 + N * (8 * (i >> 2) + 4 * hf + (i & 3)), x, 4 * N);
+        };
+        sum = over_halves(sum, [](float a, float b) { return a + b; });
+        if (kTeams == 1) {
+            if (used) {
 #pragma unroll
-        for (int c = 0; c < HT; ++c) {
-            sum[c] = quarters_sum(sum[c]);
-            if (kTeams == 1) {
-                if (used[c]) {
+                for (int i = 0; i < 16; ++i) {
+                    float x[kAcc];
 #pragma unroll
-                    for (int t = 0; t < S::kAcc; t += 2)
-                        put2(column[c], t, acc[c][t], acc[c][t + 1]);
-                    if (quarter == 0)
-                        put_stat(column[c], ref[c], sum[c]);
+                    for (int e = 0; e < kAcc; ++e)
+                        x[e] = acc[e][i];
+                    put(std::integral_constant<int, kFirst>(), 0, i, x);
+                    if constexpr (kFirst < kAcc)
+                        put(std::integral_constant<int, 2>(), 128, i, x + kFirst);
                 }
-                continue;
+                if (hf == 0)
+                    put_stat(ref, sum);
             }
-            if (c > 0)
+            continue;
+        }
+        // teams: through LDS, kJoin registers of every output tile at a time, dealt to them
+        constexpr int kJoin = sizeof(s_op) >= 4096ull * kWideWaves * kAcc ? 16 : 4;
+        float *parts = reinterpret_cast<float *>(&s_op[0][0][0]);  // [waves][kJoin][kAcc][64]
+        static_assert(sizeof(s_op) >= 256ull * kWideWaves * kAcc * kJoin, "they fit the stages");
+        s_stat[wave][lane] = ref;
+        s_stat[wave][64 + lane] = sum;
+        float weight[kTeams], top = kNone, total = 0.0f;
+#pragma unroll
+        for (int i0 = 0; i0 < 16; i0 += kJoin) {
+            if (i0 > 0)
                 __syncthreads();
 #pragma unroll
-            for (int i = 0; i < S::kAcc; ++i)
-                parts[(wave * S::kAcc + i) * 64 + lane] = acc[c][i];
-            s_stat[wave][lane] = ref[c];
-            s_stat[wave][64 + lane] = sum[c];
+            for (int i = 0; i < kJoin; ++i)
+#pragma unroll
+                for (int e = 0; e < kAcc; ++e)
+                    parts[((wave * kJoin + i) * kAcc + e) * 64 + lane] = acc[e][i0 + i];
             __syncthreads();
-            float weight[kTeams], top = kNone, total = 0.0f;
+            if (i0 == 0) {
 #pragma unroll
-            for (int i = 0; i < kTeams; ++i) {
-                weight[i] = s_stat[i * WC + wc][lane];
-                top = fmaxf(top, weight[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < kTeams; ++i) {
-                weight[i] = __builtin_amdgcn_exp2f(weight[i] - top);
-                total += s_stat[i * WC + wc][64 + lane] * weight[i];
-            }
-            if (used[c]) {
-                for (int t = 2 * team; t < S::kAcc; t += 2 * kTeams) {
-                    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
-#pragma unroll
-                    for (int k = 0; k < kTeams; ++k) {
-                        const f32x4 *at = parts + ((k * WC + wc) * S::kAcc + t) * 64 + lane;
-                        x += at[0] * weight[k];
-                        y += at[64] * weight[k];
-                    }
-                    put2(column[c], t, x, y);
+                for (int k = 0; k < kTeams; ++k) {
+                    weight[k] = s_stat[k * WC + wc][lane];
+                    top = fmaxf(top, weight[k]);
                 }
-                if (team == 0 && quarter == 0)
-                    put_stat(column[c], top, total);
+#pragma unroll
+                for (int k = 0; k < kTeams; ++k) {
+                    weight[k] = __builtin_amdgcn_exp2f(weight[k] - top);
+                    total += s_stat[k * WC + wc][64 + lane] * weight[k];
+                }
+            }
+            if (!used)
+                continue;
+            for (int i = team; i < kJoin; i += kTeams) {
+                float x[kAcc];
+#pragma unroll
+                for (int e = 0; e < kAcc; ++e) {
+                    x[e] = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kTeams; ++k)
+                        x[e] += parts[(((k * WC + wc) * kJoin + i) * kAcc + e) * 64 + lane] * weight[k];
+                }
+                put(std::integral_constant<int, kFirst>(), 0, i0 + i, x);
+                if constexpr (kFirst < kAcc)
+                    put(std::integral_constant<int, 2>(), 128, i0 + i, x + kFirst);
             }
         }
+        if (used && team == 0 && hf == 0)
+            put_stat(top, total);
     }
 }
 
@@ -1095,21 +1106,31 @@ hipError_t launch(const SharedProblem &p, int blocks, int attn_blocks, hipStream
 {
     const int heads = p.attn.kv_heads * p.attn.head_groups;
     const dim3 grid((unsigned)(blocks * heads));
-    constexpr int a_wave = 16 * Wide<FP8, D>::kHT;
-    if (p.columns == 16)
+    if (p.columns == 16) {
         hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1, 1>), grid, dim3(kThreads), 0, stream, p,
                            p.attn.table);
-    else if (p.columns == 8 * a_wave)
-        hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, 8>), grid, dim3(kWideThreads), 0,
-                           stream, p, p.attn.table);
-    else if (p.columns == 4 * a_wave)
-        hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, 4>), grid, dim3(kWideThreads), 0,
-                           stream, p, p.attn.table);
-    else if constexpr (attn_heads_a_pass(FP8, D) == 32)
-        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 1>), grid, dim3(kThreads), 0, stream, p,
-                           p.attn.table);
-    else
-        return hipErrorInvalidValue;
+    } else if (p.columns == 32) {
+        if constexpr (attn_heads_a_pass(FP8, D) == 32)
+            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 1>), grid, dim3(kThreads), 0, stream,
+                               p, p.attn.table);
+        else
+            return hipErrorInvalidValue;
+    } else {
+        if constexpr (D % 64 == 0) {
+            constexpr int waves = Wide<FP8, D>::kWaves;
+            const dim3 threads(64 * waves);
+            if (p.columns == 32 * waves)
+                hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, waves>), grid, threads, 0,
+                                   stream, p, p.attn.table);
+            else if (p.columns == 16 * waves)
+                hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, waves / 2>), grid, threads, 0,
+                                   stream, p, p.attn.table);
+            else
+                return hipErrorInvalidValue;
+        } else {
+            return hipErrorInvalidValue;
+        }
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
