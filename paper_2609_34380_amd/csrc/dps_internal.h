@@ -256,7 +256,7 @@ constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, i
 }
 constexpr int shared_blocks_per_cu(int columns, bool fp8, int dim)
 {
-    return columns == 16 && (fp8 ? 1 : 2) * dim < 512 ? 2 : 1;
+    return columns <= 32 && (fp8 ? 1 : 2) * dim < (columns == 16 ? 512 : 192) ? 2 : 1;
 }
 hipError_t launch_shared(const SharedProblem &p, int type, bool fp8, int dim, int blocks,
                          int attn_blocks, hipStream_t stream);

@@ -34,10 +34,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 
-// Where the groups lie: tiles and items of a key/value head before each group.
+// Where the groups lie: tiles and items of a key/value head before each group, and the
+// table row of its first row where that has the whole prefix (-1: another may).
 struct Groups {
     int32_t tiles[kSharedGroups + 1];
     int32_t items[kSharedGroups + 1];
+    int32_t lead[kSharedGroups];
+    int32_t first[kSharedGroups], rows[kSharedGroups], length[kSharedGroups];
     int32_t sums[2][8];  // a wave
 };
 
@@ -86,18 +89,31 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
     constexpr int kPer = kSharedGroups / (64 * WAVES);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int32_t tiles[kPer], items[kPer], n_tiles = 0, n_items = 0;
+    int32_t req[kPer], has[kPer];  // of the groups' first rows; they arrive under the scan
     bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int32_t g = i * (64 * WAVES) + tid;
+        if (g < p.groups) {
+            const Group x = group_of(p, g);
+            bad = bad || x.rows < 0;
+            s.first[g] = x.first;
+            s.rows[g] = x.rows;
+            s.length[g] = x.length;
+            has[i] = -1;
+            if (x.rows > 0)
+                has[i] = tokens_of(p, x.first, req[i]) - x.length;
+        }
+    }
+    bad = __syncthreads_or(bad);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int32_t g = tid * kPer + i;
         tiles[i] = items[i] = 0;
-        if (g < p.groups) {
-            const Group x = group_of(p, g);
-            bad = bad || x.rows < 0;
-            if (!bad) {
-                items[i] = items_of(p, x);
-                tiles[i] = items[i] * tiles_of(x);
-            }
+        if (g < p.groups && !bad) {
+            const Group x = {s.first[g], s.rows[g], s.length[g]};
+            items[i] = items_of(p, x);
+            tiles[i] = items[i] * tiles_of(x);
         }
         n_tiles += tiles[i];
         n_items += items[i];
@@ -107,7 +123,7 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
         s.sums[0][wave] = incl_tiles;
         s.sums[1][wave] = incl_items;
     }
-    bad = __syncthreads_or(bad);
+    __syncthreads();
     int32_t at_tile = incl_tiles - n_tiles, at_item = incl_items - n_items;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
@@ -128,11 +144,17 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
         s.tiles[p.groups] = at_tile;
         s.items[p.groups] = at_item;
     }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int32_t g = i * (64 * WAVES) + tid;
+        if (g < p.groups)
+            s.lead[g] = has[i] >= 0 ? req[i] : -1;
+    }
     __syncthreads();
     return !bad;
 }
 
-// The last g in [0, n) with first[g] <= x; first[0] <= x.
+// The last g in [0, n) with first[g] <= x, or 0.
 __device__ __forceinline__ int last_from(const int32_t *first, int n, int32_t x)
 {
     int lo = 0, hi = n;
@@ -170,16 +192,10 @@ __device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s
     for (int64_t r = (int64_t)block * (64 * WAVES) + threadIdx.x; r < p.attn.rows;
          r += (int64_t)blocks * (64 * WAVES)) {
         SharedRow x = {0, 0, 0, 0};
-        if (good && p.groups > 0 && r >= p.group_start[0] && r < p.group_start[p.groups]) {
-            int lo = 0, hi = p.groups;  // the last group that begins at or before r
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (p.group_start[mid] <= r)
-                    lo = mid;
-                else
-                    hi = mid;
-            }
-            const Group g = group_of(p, lo);
+        // the last group that begins at or before r
+        const int lo = good && p.groups > 0 ? last_from(s.first, p.groups, (int32_t)r) : 0;
+        if (good && p.groups > 0 && r >= s.first[lo] && r < s.first[lo] + s.rows[lo]) {
+            const Group g = {s.first[lo], s.rows[lo], s.length[lo]};
             int32_t req;
             if (g.length > 0 && tokens_of(p, (int32_t)r, req) >= g.length) {
                 const int32_t tiles = tiles_of(g), at = ((int32_t)r - g.first) / p.item_rows;
@@ -198,8 +214,11 @@ __device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s
 
 // The table row through which a group's prefix is read: that of the first row that has
 // all of it; -1: none has.
-__device__ __forceinline__ int32_t lead_of(const SharedProblem &p, const Group &grp, int lane)
+__device__ __forceinline__ int32_t lead_of(const SharedProblem &p, const Group &grp, int32_t first,
+                                           int lane)
 {
+    if (first >= 0)
+        return first;
     for (int32_t r = grp.first; r < grp.first + grp.rows; r += 64) {
         int32_t req = -1;
         const bool has = r + lane < grp.first + grp.rows &&
@@ -255,7 +274,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     while (tile < end) {
         while (s_groups.tiles[g + 1] <= tile)  // past groups without tiles
             ++g;
-        const Group grp = group_of(p, g);
+        const Group grp = {s_groups.first[g], s_groups.rows[g], s_groups.length[g]};
         const int32_t n_tiles = tiles_of(grp);
         const int32_t in_group = tile - s_groups.tiles[g];
         const int32_t at = in_group / n_tiles, skip = in_group % n_tiles;
@@ -265,7 +284,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
         tile += part;
 
-        const int32_t lead = lead_of(p, grp, lane);
+        const int32_t lead = lead_of(p, grp, __builtin_amdgcn_readfirstlane(s_groups.lead[g]), lane);
         if (lead < 0)
             continue;  // no row reads the partials
         const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
@@ -664,7 +683,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
     while (tile < end) {
         while (s_groups.tiles[g + 1] <= tile)
             ++g;
-        const Group grp = group_of(p, g);
+        const Group grp = {s_groups.first[g], s_groups.rows[g], s_groups.length[g]};
         const int32_t n_tiles = tiles_of(grp);
         const int32_t in_group = tile - s_groups.tiles[g];
         const int32_t at = in_group / n_tiles, skip = in_group % n_tiles;
@@ -673,7 +692,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         const int32_t row0 = grp.first + at * p.item_rows;
         const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
         tile += part;
-        const int32_t lead = lead_of(p, grp, lane);
+        const int32_t lead = lead_of(p, grp, __builtin_amdgcn_readfirstlane(s_groups.lead[g]), lane);
         if (lead < 0)
             continue;
         const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
