@@ -240,10 +240,11 @@ struct SharedProblem {
     float *part_out, *part_stat;
 };
 constexpr int kSharedGroups = 1024;
-// Columns of an item: a group of average size fills them where that is possible.  16 and
-// 32: tokens from memory to registers, a block's waves on different ones; above, through
-// LDS, and half of a block's waves or all of them have columns of their own (32 each; of
-// eight waves, of four for heads over 128).
+// Columns of an item.  Up to 32 for a group of average size: tokens from memory to
+// registers, a block's waves on different ones, which keeps the most loads in flight
+// (8 FP8 prefixes of 9000 tokens and 32 columns 42 us, through LDS 58; 5 BF16 ones of 2000
+// and 28 columns 17 / 25).  More: through LDS, for up to eight waves of 32 columns (four
+// for heads over 128), since each pass of 32 would read the tokens again.
 constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, int dim)
 {
     const int64_t mean = rows * step / (groups < 1 ? 1 : groups);
@@ -251,8 +252,7 @@ constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, i
         return 16;
     if (dim % 64 != 0 || (mean <= 32 && attn_heads_a_pass(fp8, dim) == 32))
         return 32;
-    const int half = dim > 128 ? 64 : 128;
-    return mean <= half ? half : 2 * half;
+    return dim > 128 ? 128 : 256;
 }
 constexpr int shared_blocks_per_cu(int columns, bool fp8, int dim)
 {

@@ -572,8 +572,9 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
 // registers one stage ahead, makes matrix operands of it (E4M3 widened, values turned,
 // tokens that are not there cleared) and puts them into LDS, lane by lane as the
 // matrix instructions take them, so that all reads and writes of LDS are 1 KiB in the
-// order of the lanes.  WC waves have 32 columns each; the others are teams with the same
-// columns, which take a stage's tiles in turn and join at the item's end.
+// order of the lanes.  As many waves as the item has 32 columns have columns of their own;
+// as often as they go into the block's, teams of them take a stage's tiles in turn and
+// join at the item's end.
 //
 // Products are 32 x 32 x 16: S^T of 32 tokens and 32 columns, O^T of 32 values and 32
 // columns.  They read half the operands of 16 x 16 x 32 for the same work, which leaves
@@ -634,13 +635,12 @@ struct Raw<4> { typedef uint32_t T; };
 template <>
 struct Raw<2> { typedef uint16_t T; };
 
-template <int TYPE, bool FP8, int D, int WC>
+template <int TYPE, bool FP8, int D>
 __global__ __launch_bounds__((64 * Wide<FP8, D>::kWaves), (Wide<FP8, D>::kWaves / 4)) void
 shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
 {
     typedef Wide<FP8, D> W;
     constexpr int ST = W::kStage, kFrags = W::kFrags, kAcc = W::kAcc, kWideWaves = W::kWaves;
-    constexpr int kTeams = kWideWaves / WC;
     constexpr int kFirst = D == 192 ? 4 : kAcc;  // output tiles of the values' first piece
     static_assert(W::kKeys % 2 == 0, "an E4M3 load is two steps");
     // [2 stages][tiles][keys: step; values: output tile, step]
@@ -672,7 +672,6 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
     const uint32_t val_head = (uint32_t)(a.kv_heads + kvh) * tokens * (D * W::kElt);
     const float to_log2 = a.score_scale * kLog2e;
     const int32_t last_col = (int32_t)a.table_cols - 1;
-    const int wc = wave % WC, team = wave / WC;
     const int my_tile = wave / W::kParts, my_part = wave % W::kParts;
     const int my_step = my_part;  // of the values: 16 of the tile's tokens
     static_assert(W::kParts == 2, "a piece is half of a tile");
@@ -824,8 +823,12 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         find(0);
         fetch(0);
         find(1);
+        const int n_waves = (min(n_rows, p.item_rows) * a.group_step + 31) / 32;  // with columns
+        const int teams = kWideWaves / n_waves;
+        const int team = wave / n_waves, wc = wave - team * n_waves;
         const int32_t column = wc * 32 + col;
-        const bool used = column / a.group_step < n_rows && column % a.group_step < n_heads;
+        const bool active = team < teams;
+        const bool used = active && column / a.group_step < n_rows && column % a.group_step < n_heads;
         u32x4 q[kFrags];
         f32x16 acc[kAcc];
         float ref = kNone, sum = 0.0f;
@@ -938,19 +941,18 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
             fetch(stage + 1);  // past the part: nothing
             find(stage + 2);
             const auto op = s_op[stage & 1];
-            const auto each = [&](int i) {
-                if (stage * ST + i < part)
-                    take(op[i] + lane,
-                         __builtin_amdgcn_readfirstlane(s_live[stage & 1][i]));
-            };
-            constexpr int kEach = ST / kTeams;  // tiles of a stage that a wave has
+            const int here = active ? min(ST, part - stage * ST) : 0;  // tiles of the stage
+            bool stashed = false;
 #pragma unroll 1
-            for (int i = 0; i < (kEach + 1) / 2; ++i)
-                each(i * kTeams + team);
-            stash(stage + 1);
-#pragma unroll 1
-            for (int i = (kEach + 1) / 2; i < kEach; ++i)
-                each(i * kTeams + team);
+            for (int i = team; i < here; i += teams) {
+                if (i >= ST / 2 && !stashed) {  // the loads have had half of the stage
+                    stash(stage + 1);
+                    stashed = true;
+                }
+                take(op[i] + lane, __builtin_amdgcn_readfirstlane(s_live[stage & 1][i]));
+            }
+            if (!stashed)
+                stash(stage + 1);
             __syncthreads();
         }
 
@@ -966,7 +968,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
             __builtin_memcpy(out + d0 + N * (8 * (i >> 2) + 4 * hf + (i & 3)), x, 4 * N);
         };
         sum = over_halves(sum, [](float a, float b) { return a + b; });
-        if (kTeams == 1) {
+        if (teams == 1) {
             if (used) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -989,7 +991,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         static_assert(sizeof(s_op) >= 256ull * kWideWaves * kAcc * kJoin, "they fit the stages");
         s_stat[wave][lane] = ref;
         s_stat[wave][64 + lane] = sum;
-        float weight[kTeams], top = kNone, total = 0.0f;
+        float weight[kWideWaves], top = kNone, total = 0.0f;
 #pragma unroll
         for (int i0 = 0; i0 < 16; i0 += kJoin) {
             if (i0 > 0)
@@ -1002,26 +1004,34 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
             __syncthreads();
             if (i0 == 0) {
 #pragma unroll
-                for (int k = 0; k < kTeams; ++k) {
-                    weight[k] = s_stat[k * WC + wc][lane];
+                for (int k = 0; k < kWideWaves; ++k) {
+                    weight[k] = kNone;
+                    if (k < teams)
+                        weight[k] = s_stat[k * n_waves + wc][lane];
                     top = fmaxf(top, weight[k]);
                 }
 #pragma unroll
-                for (int k = 0; k < kTeams; ++k) {
+                for (int k = 0; k < kWideWaves; ++k) {
                     weight[k] = __builtin_amdgcn_exp2f(weight[k] - top);
-                    total += s_stat[k * WC + wc][64 + lane] * weight[k];
+                    if (k < teams)
+                        total += s_stat[k * n_waves + wc][64 + lane] * weight[k];
                 }
             }
             if (!used)
                 continue;
-            for (int i = team; i < kJoin; i += kTeams) {
+            for (int i = team; i < kJoin; i += teams) {
                 float x[kAcc];
 #pragma unroll
-                for (int e = 0; e < kAcc; ++e) {
+                for (int e = 0; e < kAcc; ++e)
                     x[e] = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < kTeams; ++k)
-                        x[e] += parts[(((k * WC + wc) * kJoin + i) * kAcc + e) * 64 + lane] * weight[k];
+                for (int k = 0; k < kWideWaves; ++k) {
+                    if (k >= teams)
+                        break;
+#pragma unroll
+                    for (int e = 0; e < kAcc; ++e)
+                        x[e] += parts[(((k * n_waves + wc) * kJoin + i) * kAcc + e) * 64 + lane] *
+                                weight[k];
                 }
                 put(std::integral_constant<int, kFirst>(), 0, i0 + i, x);
                 if constexpr (kFirst < kAcc)
@@ -1138,14 +1148,10 @@ hipError_t launch(const SharedProblem &p, int blocks, int attn_blocks, hipStream
         if constexpr (D % 64 == 0) {
             constexpr int waves = Wide<FP8, D>::kWaves;
             const dim3 threads(64 * waves);
-            if (p.columns == 32 * waves)
-                hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, waves>), grid, threads, 0,
-                                   stream, p, p.attn.table);
-            else if (p.columns == 16 * waves)
-                hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D, waves / 2>), grid, threads, 0,
-                                   stream, p, p.attn.table);
-            else
+            if (p.columns != 32 * waves)
                 return hipErrorInvalidValue;
+            hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D>), grid, threads, 0, stream, p,
+                               p.attn.table);
         } else {
             return hipErrorInvalidValue;
         }
