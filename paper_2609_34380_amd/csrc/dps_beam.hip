@@ -34,6 +34,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kList = 1024;
+constexpr int kFew = 128;  // threads whose values are looked through one by one
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_inff();
 
@@ -167,6 +168,17 @@ __device__ __forceinline__ float wide(const u32x4 &v, int i)
     return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w >> 16 : w));
 }
 
+template <int TYPE>
+__device__ __forceinline__ float read(const uint8_t *row, int32_t at)
+{
+    if (TYPE == BEAM_F32)
+        return reinterpret_cast<const float *>(row)[at];
+    const uint16_t x = reinterpret_cast<const uint16_t *>(row)[at];
+    if (TYPE == BEAM_BF16)
+        return __builtin_bit_cast(float, (uint32_t)x << 16);
+    return (float)__builtin_bit_cast(_Float16, x);
+}
+
 // VECS 16-byte vectors a thread.  Rows may begin anywhere an element may: vectors lie
 // on the 16-byte grid of memory, the one before a row's first element included.
 template <int TYPE, int VECS>
@@ -182,6 +194,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
     __shared__ double s_d[kWaves];
     __shared__ int32_t s_n[kWaves];
     __shared__ float s_one;
+    __shared__ int32_t s_thread[kFew], s_threads, s_found;
 
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / p.pieces;
@@ -256,10 +269,47 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
     // ---- the keep best --------------------------------------------------------------
     const int keep = p.keep;
     float least = bound_of(mine, keep, s_all, &s_one);  // of the values taken
-    int n = 0, all;
-    each([&](float x, int) { n += x >= least && x > -kInf; });
-    int at = place_of(n, s_n, all);
-    if (all <= kList) {
+    // the threads whose largest reaches it: seldom more than keep
+    if (tid == 0)
+        s_threads = s_found = 0;
+    __syncthreads();
+    if (mine >= least && mine > -kInf) {
+        const int i = atomicAdd(&s_threads, 1);
+        if (i < kFew)
+            s_thread[i] = tid;
+    }
+    __syncthreads();
+    int n = 0, all = s_threads;
+    bool listed = all <= kFew;
+    if (listed) {
+        // their values again, from the caches, a wave a thread's and a lane a value
+        constexpr int kEach = VECS * kPer;
+        for (int c = tid >> 6; c < all; c += kWaves) {
+            const int t = s_thread[c], i = tid & 63;
+            const int32_t at = at0 + ((i / kPer) * kThreads + t) * kPer + i % kPer;
+            if (i < kEach && at >= 0 && at < vocab) {
+                const float x = read<TYPE>(first, at);
+                if (x >= least && x > -kInf) {
+                    const int o = atomicAdd(&s_found, 1);  // they are ranked below
+                    if (o < kList) {
+                        s_value[o] = x;
+                        s_index[o] = at;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        all = s_found;
+        listed = all <= kList;
+        __syncthreads();
+    }
+    int at = 0;
+    if (!listed) {
+        each([&](float x, int) { n += x >= least && x > -kInf; });
+        at = place_of(n, s_n, all);
+    }
+    if (listed) {
+    } else if (all <= kList) {
         each([&](float x, int i) {
             if (x >= least && x > -kInf) {
                 s_value[at] = x;
@@ -371,20 +421,18 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
         if (!(p.done && p.done[row]) && __builtin_fabsf(cum) < kInf) {
             const double *sums = p.sums + row * p.pieces * 2;
             double top = none, sum = 0.0;
+            for (int c = lane; c < p.pieces; c += 64)
+                if (sums[c * 2 + 1] != 0.0)
+                    top = fmax(top, sums[c * 2]);
+            for (int d = 32; d > 0; d >>= 1)
+                top = fmax(top, __shfl_xor(top, d));
             for (int c = lane; c < p.pieces; c += 64) {
-                const double t = sums[c * 2], s = sums[c * 2 + 1];
-                const double to = s != 0.0 ? fmax(top, t) : top;
-                if (to > none)  // an infinite one leaves no number
-                    sum = sum * exp(top - to) + (s != 0.0 ? s * exp(t - to) : 0.0);
-                top = to;
+                const double s = sums[c * 2 + 1];
+                if (s != 0.0)  // an infinite top leaves no number
+                    sum += s * exp(sums[c * 2] - top);
             }
-            for (int d = 32; d > 0; d >>= 1) {
-                const double t = __shfl_xor(top, d), s = __shfl_xor(sum, d), to = fmax(top, t);
-                if (to > none)
-                    sum = (sum != 0.0 ? sum * exp(top - to) : 0.0) +
-                          (s != 0.0 ? s * exp(t - to) : 0.0);
-                top = to;
-            }
+            for (int d = 32; d > 0; d >>= 1)
+                sum += __shfl_xor(sum, d);
             lse = top + log(sum);
         }
         if (lane == 0)

@@ -6,6 +6,8 @@ paged KV blocks take turns in).
                     manager, block tables and slot maps built on the GPU
     AttentionLayer  QKV product, head norms with rotation into the cache,
                     attention, O product, in the precision mode of the pass
+    Beams           beam search over the slots of a PagedBatch: several answers
+                    to one prompt share its blocks, which are read once for all
 
 Everything an AttentionLayer and PagedBatch.map() enqueue reads lengths, tables
 and slots on the device, so a step can be captured (graphs.ModeGraphs) and
@@ -13,8 +15,12 @@ replayed while requests grow.
 
 Run as a program (python -m paper_2609_34380_amd.decode), it decodes with a small
 layer until KV blocks push the residuals out, goes on in fast mode, and returns
-to full mode once the requests end and the residuals are restored.
+to full mode once the requests end and the residuals are restored; with the argument
+"beams" the requests are beams of one prompt, and blocks that end up scattered over the
+units are moved together so that the residuals can return.
 """
+import sys
+
 import torch
 
 from . import dps
@@ -34,10 +40,15 @@ class PagedBatch:
     Steps may run on other streams than grow(): its copies wait for the work of every
     stream that map() was called on, also to capture it, and are complete when it
     returns.  Before the next grow() a caller waits for a graph replayed elsewhere than
-    on the stream of its capture."""
+    on the stream of its capture.
 
-    def __init__(self, sums, batch, max_tokens, block_tokens, rows=None, device="cuda"):
-        self.sums, self.block_tokens = sums, block_tokens
+    fork() lets slots go on from other slots, sharing their whole blocks.  With groups > 0
+    (the most groups of rows that one step's attention treats as one) grow() also finds
+    which neighbouring rows share their first blocks: self.group_start and
+    self.shared_len, for dps.attn_shared."""
+
+    def __init__(self, sums, batch, max_tokens, block_tokens, rows=None, device="cuda", groups=0):
+        self.sums, self.block_tokens, self.groups = sums, block_tokens, groups
         self.lengths = [0] * batch           # tokens in the cache, after the last step
         self.blocks = [[] for _ in range(batch)]
         columns = -(-max_tokens // block_tokens)
@@ -53,6 +64,10 @@ class PagedBatch:
         self._streams = [torch.cuda.current_stream(self.table.device)]
         self._unmapped = set()               # slots that grew since the last map()
         self._captured = False               # map() is in a graph: replays are not seen here
+        self._forks = 0                      # > 0: slots may have blocks in common
+        self._group_key = None               # of the groups that are on the device
+        self.wake = False                    # what fork() freed lets residuals return
+        self.group_start, self.shared_len = (torch.zeros(n, **i32) for n in (groups + 1, groups))
 
     def grow(self, new):
         """new[r] tokens join slot r in the coming step.  Takes the blocks they need
@@ -70,13 +85,14 @@ class PagedBatch:
         taken = self.sums.alloc(sum(need))
         if taken is None:
             return False
-        if self._unmapped and not self._captured:
+        try:
+            self._mapped()
+        except RuntimeError:
             self.sums.free(taken)
-            raise RuntimeError("the tokens of the last grow() are not mapped")
-        here = torch.cuda.current_stream(self.table.device)
-        for stream in self._streams:   # earlier steps read what is replaced here
-            if stream != here:
-                here.wait_stream(stream)
+            raise
+        self._after_steps()
+        if self.groups:
+            self._group([r for r, n in enumerate(new) for _ in range(n)])
         self.ctx_len.copy_(torch.tensor(self.lengths, dtype=torch.int32))
         self.new_len.copy_(torch.tensor(new, dtype=torch.int32))
         if taken:
@@ -89,6 +105,45 @@ class PagedBatch:
         self._unmapped = {r for r, n in enumerate(new) if n}
         return True
 
+    def _after_steps(self):
+        """Work enqueued from here on comes after every step: it replaces what they read."""
+        here = torch.cuda.current_stream(self.table.device)
+        for stream in self._streams:
+            if stream != here:
+                here.wait_stream(stream)
+        return here
+
+    def _group(self, slots):
+        """The groups of a step whose rows are those slots': neighbours with the same first
+        block, and the blocks, full before the step, that all of them have in common."""
+        key = (slots, self._forks)
+        if key == self._group_key:
+            return
+        # rows of one slot share what it holds, which grows from step to step
+        self._group_key = key if len(set(slots)) == len(slots) else None
+        starts, lengths = [], []
+        row = 0
+        while self._forks and row < len(slots) and len(starts) < self.groups:
+            first = self.blocks[slots[row]]
+            end, common = row + 1, self.lengths[slots[row]] // self.block_tokens
+            while end < len(slots) and common and self.blocks[slots[end]][:1] == first[:1]:
+                other = self.blocks[slots[end]][:self.lengths[slots[end]] // self.block_tokens]
+                common = next((i for i, (a, b) in enumerate(zip(first[:common], other)) if a != b),
+                              min(common, len(other)))
+                end += 1
+            if end > row + 1 or starts:     # (between groups a row by itself is one, too)
+                starts.append(row)
+                lengths.append(common * self.block_tokens if end > row + 1 else 0)
+            row = end
+        pad = self.groups - len(starts)
+        starts += [row if starts else 0] * (pad + 1)
+        self.group_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        self.shared_len.copy_(torch.tensor(lengths + [0] * pad, dtype=torch.int32))
+
+    def _mapped(self):
+        if self._unmapped and not self._captured:
+            raise RuntimeError("the tokens of the last grow() are not mapped")
+
     def map(self):
         """Enqueue the step's block tables and slot maps."""
         stream = torch.cuda.current_stream(self.table.device)
@@ -99,15 +154,80 @@ class PagedBatch:
         return dps.kv_map(self.ctx_len, self.new_len, self.fresh, self.table, self.block_tokens,
                           out=self.step)
 
+    def fork(self, parents, caches):
+        """Slot r goes on from slot parents[r] (an int32 device tensor, or a list; -1: the
+        slot is empty from now on), for all slots at once: shared whole blocks, and a copy
+        of a last block that has room, in each of `caches` (every layer's).  Takes the
+        blocks of the copies (False, with nothing changed, if no room is left) and gives
+        back those that no slot holds any more; self.wake says then whether residuals wait
+        for the units that became free.  Waits for the steps before, as grow() does, and
+        for the copies."""
+        self._mapped()
+        host = parents.tolist() if torch.is_tensor(parents) else list(parents)
+        if len(host) != len(self.lengths) or max(host) >= len(host):
+            raise ValueError("one parent a slot, a slot or -1")
+        copied, seen = [], set()
+        for r, p in enumerate(host):
+            if p >= 0 and p in seen and self.lengths[p] % self.block_tokens:
+                copied.append(r)
+            seen.add(p)
+        taken = self.sums.alloc(len(copied))
+        if taken is None:
+            return False
+        if not torch.is_tensor(parents):
+            parents = torch.tensor(host, dtype=torch.int32, device=self.table.device)
+        here = self._after_steps()
+        i32 = dict(dtype=torch.int32, device=self.table.device)
+        held = sorted({b for blocks in self.blocks for b in blocks})
+        out = dps.make_kv_fork(len(host), self.table.shape[1], len(held), self.table.device)
+        out = out._replace(table=self.table)    # where captured steps look for it
+        f = dps.kv_fork(parents, torch.tensor(self.lengths, **i32), self.table.clone(),
+                        torch.tensor(taken, **i32), self.block_tokens,
+                        max(held + taken, default=-1) + 1, out=out)
+        for cache in caches:
+            dps.kv_copy(cache, f.src, f.dst, tokens=f.tokens, count=f.counts)
+        fresh = dict(zip(copied, taken))
+        blocks = [list(self.blocks[p]) if p >= 0 else [] for p in host]
+        for r, block in fresh.items():
+            blocks[r][-1] = block
+        self.lengths = [self.lengths[p] if p >= 0 else 0 for p in host]
+        self.blocks, self._forks = blocks, self._forks + 1
+        here.synchronize()
+        freed = f.freed[:int(f.counts[1])].tolist()
+        self.wake = self.sums.free(freed) if freed else False
+        return True
+
+    def compact(self, caches, max_moves=1 << 16):
+        """Moves blocks of nearly empty units together (dps.SumManager.compact), in each of
+        `caches`, so that units become free: True when residuals wait for them.  Waits for
+        the steps before and for the moves."""
+        self._mapped()
+        src, dst = self.sums.compact(max_moves)
+        if not src:
+            return False
+        here = self._after_steps()
+        i32 = dict(dtype=torch.int32, device=self.table.device)
+        s, d = torch.tensor(src, **i32), torch.tensor(dst, **i32)
+        for cache in caches:
+            dps.kv_copy(cache, s, d)
+        dps.kv_remap(self.table, s, d)
+        to = dict(zip(src, dst))
+        self.blocks = [[to.get(b, b) for b in blocks] for blocks in self.blocks]
+        here.synchronize()
+        return self.sums.free(src)
+
     def end(self, slot):
-        """The request of a slot ends: its blocks go back.  True when residuals wait
-        for the units that became free.  The steps that use the blocks, the one that
-        grow() has just prepared among them, must have completed: a restore worker
-        copies on a stream of its own."""
-        wake = self.sums.free(self.blocks[slot]) if self.blocks[slot] else False
+        """The request of a slot ends: its blocks go back, but for those it shares.  True
+        when residuals wait for the units that became free.  The steps that use the blocks,
+        the one that grow() has just prepared among them, must have completed: a restore
+        worker copies on a stream of its own."""
+        mine = self.blocks[slot]
         self.blocks[slot], self.lengths[slot] = [], 0
+        if self._forks:
+            others = {b for blocks in self.blocks for b in blocks}
+            mine = [b for b in mine if b not in others]
         self._unmapped.discard(slot)
-        return wake
+        return self.sums.free(mine) if mine else False
 
 
 class AttentionLayer:
@@ -116,11 +236,12 @@ class AttentionLayer:
     max_tokens positions: past its end rows are NaN); q_weight and k_weight (FP16
     [head_dim]) the head norms' weights, or None without norms.  Made for steps of
     decode tokens: a prompt's rows are taken, at the cost of reading the cache anew for
-    each.  The buffers between the products are the layer's own, so one call runs at a
-    time: calls on several streams are ordered by the caller."""
+    each.  groups: those of the batch (PagedBatch), whose shared blocks are then read once
+    (without a window).  The buffers between the products are the layer's own, so one call
+    runs at a time: calls on several streams are ordered by the caller."""
 
     def __init__(self, qkv, o, cache, heads, rope, q_weight=None, k_weight=None, rows=256,
-                 window=0):
+                 window=0, groups=0):
         self.qkv, self.o, self.cache, self.heads, self.rope = qkv, o, cache, heads, rope
         self.q_weight, self.k_weight, self.window = q_weight, k_weight, window
         dim, device = cache.head_dim, qkv.hi.device
@@ -128,7 +249,12 @@ class AttentionLayer:
         self._qkv = torch.empty((rows, qkv.n), **f16)
         self._q = torch.empty((rows, heads, dim), **f16)
         self._a = torch.empty((rows, heads, dim), **f16)
+        if groups and window:
+            raise ValueError("rows that share blocks have no window")
+        self.groups = groups
         need = max([256, dps.attn_workspace_bytes(cache, rows, heads)] +
+                   [dps.attn_shared_workspace_bytes(cache, m, heads, groups)
+                    for m in range(1, rows + 1) if groups] +
                    [dps.workspace_bytes(mode, dps.ACT_FP16, m, w.n, w.k)
                     for mode in (dps.MODE_FULL, dps.MODE_FAST) for w in (qkv, o)
                     for m in range(1, rows + 1)])
@@ -143,9 +269,55 @@ class AttentionLayer:
         dps.linear(x, self.qkv, mode, out=qkv, workspace=self._ws)
         dps.kv_store(qkv, self.cache, step.slot, self.heads, pos=step.pos, rope=self.rope,
                      q_weight=self.q_weight, k_weight=self.k_weight, q_out=q)
-        dps.attn_decode(q, self.cache, batch.table, step.kv_len, req=step.req, out=a,
-                        window=self.window, workspace=self._ws)
+        if self.groups != batch.groups:
+            raise ValueError("the layer is for %d groups, the batch has %d" %
+                             (self.groups, batch.groups))
+        if self.groups:
+            dps.attn_shared(q, self.cache, batch.table, step.kv_len, batch.group_start,
+                            batch.shared_len, req=step.req, out=a, workspace=self._ws)
+        else:
+            dps.attn_decode(q, self.cache, batch.table, step.kv_len, req=step.req, out=a,
+                            window=self.window, workspace=self._ws)
         return dps.linear(a.view(rows, -1), self.o, mode, out=out, workspace=self._ws)
+
+
+class Beams:
+    """Beam search over the slots of a PagedBatch, `beams` slots a request: pick() takes
+    the logits of a step's rows (a new token in every slot), gives every slot the beam it
+    goes on with, and returns the tokens of the next step.  caches: every layer's.  end:
+    the token that ends a beam (-1: none).  Ended beams keep their slots, and slots for
+    which there is no beam are empty and have no score; both take tokens like the others,
+    whose logits do not count."""
+
+    def __init__(self, batch, caches, beams, vocab, end=-1):
+        slots = len(batch.lengths)
+        if slots % beams:
+            raise ValueError("the batch's slots must be a multiple of beams")
+        device = batch.table.device
+        self.batch, self.caches, self.beams, self.end = batch, caches, beams, end
+        # at first the beams of a request are alike, and one of them counts
+        self.score = torch.full((slots // beams, beams), float("-inf"), device=device)
+        self.score[:, 0] = 0.0
+        self.done = torch.zeros(slots, dtype=torch.uint8, device=device)
+        self.tokens = [[] for _ in range(slots)]
+        self._step = dps.make_beam_step(slots // beams, beams, device)
+        self._ws = torch.empty(max(1, dps.beam_workspace_bytes(slots // beams, beams, vocab, beams)),
+                               dtype=torch.uint8, device=device)
+
+    def pick(self, logits):
+        """int32 [slots] tokens (-1: no beam), or None if no room is left for the copies of
+        blocks that the beams need."""
+        step = dps.beam_select(logits, self.score.view(-1), self.beams,
+                               done=self.done if self.end >= 0 else None, end=self.end,
+                               out=self._step, workspace=self._ws)
+        if not self.batch.fork(step.parent.view(-1), self.caches):
+            return None
+        self.score.copy_(step.score)
+        self.done.copy_(step.done.view(-1))
+        parents, tokens = step.parent.view(-1).tolist(), step.token.view(-1)
+        self.tokens = [self.tokens[p] + [t] if p >= 0 else []
+                       for p, t in zip(parents, tokens.tolist())]
+        return tokens
 
 
 def rope_table(max_pos, rot, base=10000.0, device="cuda"):
@@ -163,7 +335,7 @@ class SharedLayer:
     HIDDEN, HEADS, KV_HEADS, DIM, TOKENS = 1024, 16, 4, 64, 16
     UNIT, LOG2_CHUNK = 2 << 20, 16
 
-    def __init__(self, units=4, batch=4, max_tokens=4096, seed=0, device="cuda"):
+    def __init__(self, units=4, batch=4, max_tokens=4096, seed=0, device="cuda", groups=0):
         from . import workloads
 
         block = 2 * self.KV_HEADS * self.TOKENS * self.DIM * 2
@@ -183,12 +355,14 @@ class SharedLayer:
             targets.append((dps.backup(nw.residual, n * k), n * k, nw.residual))
         torch.cuda.synchronize()   # the backups are complete
         self.worker = dps.RestoreWorker(self.sums, targets, per_unit)
-        self.batch = PagedBatch(self.sums, batch, max_tokens, self.TOKENS, device=device)
+        self.batch = PagedBatch(self.sums, batch, max_tokens, self.TOKENS, device=device,
+                                groups=groups)
         self.q_weight = torch.ones(self.DIM, dtype=torch.float16, device=device)
         self.rope = rope_table(self.batch.max_tokens, self.DIM, device=device)
         cache = dps.KvCache(self.pool, self.TOKENS, self.KV_HEADS, self.DIM, torch.float16)
         self.layer = AttentionLayer(*self.nested, cache, self.HEADS, self.rope,
-                                    self.q_weight, self.q_weight, rows=batch)
+                                    self.q_weight, self.q_weight, rows=batch, groups=groups)
+        self.cache = cache
 
     def decode(self, x, new):
         """One token (new[r] = 1) of each active slot; x holds their rows first.  The
@@ -225,5 +399,44 @@ def main(steps=1600):
     shared.close()
 
 
+def main_beams(steps=900, beams=8, vocab=32000, prompt=400):
+    """One prompt of `prompt` tokens, then beams over a vocabulary."""
+    shared = SharedLayer(batch=beams, groups=1)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    head = torch.randn((vocab, SharedLayer.HIDDEN), device="cuda", generator=gen).to(torch.float16)
+    embed = torch.randn((vocab, SharedLayer.HIDDEN), device="cuda", generator=gen).to(torch.float16)
+    names = {dps.MODE_FULL: "full", dps.MODE_FAST: "fast"}
+    search, batch, mode = Beams(shared.batch, [shared.cache], beams, vocab), shared.batch, None
+    x = torch.zeros((beams, SharedLayer.HIDDEN), dtype=torch.float16, device="cuda")
+    for t in range(prompt):   # in the first slot
+        x[0] = embed[t % vocab]
+        y = shared.decode(x, [1] + [0] * (beams - 1))
+    batch.fork([0] * beams, [shared.cache])
+    y = y[:1].repeat(beams, 1)
+    for t in range(steps):
+        token = search.pick(y @ head.t())
+        if token is None:
+            print("step %d: no room for more KV blocks" % t)
+            break
+        y = shared.decode(embed[token.long().clamp(min=0)], [1] * beams)
+        if y is None:
+            print("step %d: no room for more KV blocks" % t)
+            break
+        if shared.sums.mode != mode:
+            mode = shared.sums.mode
+            print("step %d: %s mode, %s" % (t, names[mode], shared.sums.counts()))
+    torch.cuda.synchronize()
+    print("%d beams of %d tokens in %d blocks, %d of them shared" %
+          (beams, batch.lengths[0], len({b for x in batch.blocks for b in x}),
+           int(batch.shared_len[0]) // batch.block_tokens))
+    wake = any([batch.end(r) for r in range(1, beams)])
+    if batch.compact([shared.cache]) or wake:
+        shared.worker.kick()
+    shared.worker.wait_idle()
+    print("one beam is left, its blocks together: %s mode, %s" %
+          (names[shared.sums.mode], shared.sums.counts()))
+    shared.close()
+
+
 if __name__ == "__main__":
-    main()
+    main_beams() if sys.argv[1:] == ["beams"] else main()
