@@ -1208,8 +1208,8 @@ namespace {
 struct BeamPlan {
     int vecs;
     int64_t pieces, lists;
-    size_t value_bytes, sum_bytes, listed_bytes;
-    size_t bytes() const { return 2 * value_bytes + sum_bytes + listed_bytes; }
+    size_t value_bytes, sum_bytes;
+    size_t bytes() const { return 2 * value_bytes + sum_bytes; }
 };
 
 BeamPlan plan_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t keep, int type)
@@ -1225,7 +1225,6 @@ BeamPlan plan_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t keep, in
     b.lists = rows * b.pieces;
     b.value_bytes = align256(b.lists * keep * 4);
     b.sum_bytes = align256(b.lists * 16);
-    b.listed_bytes = align256(b.lists * 4);
     return b;
 }
 
@@ -1315,8 +1314,6 @@ DPS_EXPORT dps_status dps_beam_select(const dps_beam_args *a, void *ws, size_t w
     p.values = reinterpret_cast<float *>(at);
     at += plan.value_bytes;
     p.indexes = reinterpret_cast<int32_t *>(at);
-    at += plan.value_bytes;
-    p.listed = reinterpret_cast<int32_t *>(at);
     return launched(dps::launch_beam(p, a->type, plan.vecs, (hipStream_t)stream));
 }
 

@@ -218,8 +218,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
         const int32_t at = at0 + (j * kThreads + tid) * kPer;
         v[j] = u32x4{kNone, kNone, kNone, kNone};
         if (at >= 0 && at + kPer <= vocab) {
-            v[j] = __builtin_nontemporal_load(
-                reinterpret_cast<const u32x4 *>(base + (int64_t)(at + skew) * kElt));
+            v[j] = *reinterpret_cast<const u32x4 *>(base + (int64_t)(at + skew) * kElt);
         } else if (at + kPer > 0 && at < vocab) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -385,132 +384,137 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
             p.indexes[list * keep + rank] = i;
         }
     }
+    for (int r = all + tid; r < keep; r += kThreads)
+        p.values[list * keep + r] = -kInf;  // its index is not read
     if (tid == 0) {
         p.sums[list * 2] = (double)ref;
         p.sums[list * 2 + 1] = total;
-        p.listed[list] = min(all, keep);
     }
 }
 
-// A candidate: its place among all of its batch item is beam * vocab + token.
-struct Candidate {
-    double score;
-    int64_t place;
-};
-constexpr int kHeld = 8;  // candidates a thread keeps in registers
+// Candidates of a batch item are numbered as they lie in the lists: beam, piece, rank.
+// Their place among equals is the beam, then the token.
+constexpr int kHeld = 8;  // scores of candidates that a thread keeps in registers
 
-// HELD: the item has at most kHeld candidates a thread, else they are read anew for
-// each of the few passes over them.
+// What LDS holds of a beam.
+struct Beam {
+    double lse;   // log of its sum of exponentials; NaN: it has no candidates
+    float score;  // of a beam that has ended: the score of its one candidate, and lse 0
+    int32_t ended;
+};
+
+// HELD: the item has at most kHeld candidates a thread, else their scores are made anew
+// for each of the few passes over them.
 template <bool HELD>
 __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p)
 {
-    extern __shared__ double s_lse[];  // a beam's log of the sum; NaN: it has no candidates
+    extern __shared__ Beam s_beam[];
     __shared__ double s_all[kThreads], s_one;
     __shared__ double s_score[kList];
     __shared__ int64_t s_place[kList];
     __shared__ int32_t s_n[kWaves];
     __shared__ int64_t s_top[kWaves];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x;
     const int64_t item = blockIdx.x, row0 = item * p.beams;
     const double none = -(double)kInf;
-    for (int w = wave; w < p.beams; w += kWaves) {  // a wave a beam, a lane a piece
+    const uint32_t keep = p.keep, a_row = (uint32_t)p.pieces * keep, slots = a_row * p.beams;
+    const float *values = p.values + row0 * a_row;
+    float value[kHeld];
+    if (HELD) {  // on their way while the sums are joined
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            value[j] = values[min(tid + j * kThreads, (int)slots - 1)];
+    }
+    // `per` lanes a beam (a power of two, at most a wave), a lane a piece
+    int per = 64;
+    while (per > 1 && per * p.beams > kThreads)
+        per >>= 1;
+    for (int w = tid / per; w < p.beams; w += kThreads / per) {
         const int64_t row = row0 + w;
+        const double *sums = p.sums + row * p.pieces * 2;
         const float cum = p.score[row];
-        double lse = __builtin_nan("");
-        if (!(p.done && p.done[row]) && __builtin_fabsf(cum) < kInf) {
-            const double *sums = p.sums + row * p.pieces * 2;
-            double top = none, sum = 0.0;
-            for (int c = lane; c < p.pieces; c += 64)
-                if (sums[c * 2 + 1] != 0.0)
-                    top = fmax(top, sums[c * 2]);
-            for (int d = 32; d > 0; d >>= 1)
-                top = fmax(top, __shfl_xor(top, d));
-            for (int c = lane; c < p.pieces; c += 64) {
-                const double s = sums[c * 2 + 1];
-                if (s != 0.0)  // an infinite top leaves no number
-                    sum += s * exp(sums[c * 2] - top);
-            }
-            for (int d = 32; d > 0; d >>= 1)
-                sum += __shfl_xor(sum, d);
-            lse = top + log(sum);
+        const bool ended = p.done && p.done[row], finite = __builtin_fabsf(cum) < kInf;
+        const bool counts = !ended && finite;
+        double top = none, sum = 0.0;
+        for (int c = tid % per; c < p.pieces; c += per)
+            if (counts && sums[c * 2 + 1] != 0.0)
+                top = fmax(top, sums[c * 2]);
+        for (int d = per / 2; d > 0; d >>= 1)
+            top = fmax(top, __shfl_xor(top, d));
+        for (int c = tid % per; c < p.pieces; c += per) {
+            const double s = sums[c * 2 + 1];
+            if (counts && s != 0.0)  // an infinite top leaves no number
+                sum += s * exp(sums[c * 2] - top);
         }
-        if (lane == 0)
-            s_lse[w] = lse;
+        for (int d = per / 2; d > 0; d >>= 1)
+            sum += __shfl_xor(sum, d);
+        if (tid % per == 0)
+            s_beam[w] = Beam{counts ? top + log(sum) : finite ? 0.0 : __builtin_nan(""), cum, ended};
     }
     __syncthreads();
 
-    const int keep = p.keep;
-    const uint32_t a_row = (uint32_t)p.pieces * keep, slots = a_row * p.beams;
-    const auto read = [&](uint32_t i) {
-        Candidate c = {none, 0};
-        const uint32_t list = i / (uint32_t)keep, w = i / a_row;
-        const int64_t row = row0 + w, at = row0 * p.pieces + list;
-        const float cum = p.score[row];
-        const bool ended = p.done && p.done[row];
-        const bool listed = (int)(i - list * keep) < p.listed[at];  // as far as the beam has lists
-        const float x = p.values[at * keep + (i - list * keep)];
-        const int32_t token = p.indexes[at * keep + (i - list * keep)];
-        if (ended) {
-            if (i == w * a_row && __builtin_fabsf(cum) < kInf)
-                c = Candidate{(double)cum, (int64_t)w * p.vocab + p.end};
-            return c;
-        }
-        const double lse = s_lse[w];
-        const double s = (double)cum + ((double)x - lse);
-        if (lse == lse && listed && s == s)
-            c = Candidate{s, (int64_t)w * p.vocab + token};
-        return c;
+    const auto score_of = [&](uint32_t i, float x) {
+        const Beam b = s_beam[i / a_row];
+        double s = (double)b.score + ((double)x - b.lse);
+        if (b.ended)
+            s = i % a_row == 0 ? (double)b.score - b.lse : none;
+        return s == s ? s : none;
     };
-    Candidate held[kHeld];
+    const auto place_at = [&](uint32_t i) {
+        const uint32_t w = i / a_row;
+        const int32_t token = s_beam[w].ended ? p.end : p.indexes[row0 * a_row + i];
+        return (int64_t)w << 32 | (uint32_t)token;
+    };
+    double held[kHeld];
     if (HELD) {
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) {
-            const uint32_t i = tid + j * kThreads;
-            held[j] = Candidate{none, 0};
-            if (i < slots)
-                held[j] = read(i);
+            held[j] = none;
+            if (tid + j * kThreads < slots)
+                held[j] = score_of(tid + j * kThreads, value[j]);
         }
     }
+    // f(score, number) for the thread's candidates
     const auto each = [&](const auto &f) {
         if (HELD) {
 #pragma unroll
             for (int j = 0; j < kHeld; ++j)
-                if (held[j].score > none)
-                    f(held[j]);
+                if (held[j] > none)
+                    f(held[j], (uint32_t)(tid + j * kThreads));
         } else {
             for (uint32_t i = tid; i < slots; i += kThreads) {
-                const Candidate c = read(i);
-                if (c.score > none)
-                    f(c);
+                const double s = score_of(i, values[i]);
+                if (s > none)
+                    f(s, i);
             }
         }
     };
     const auto count = [&](const auto &f) {
         int n = 0;
-        each([&](const Candidate &c) { n += f(c); });
+        each([&](double s, uint32_t i) { n += f(s, i); });
         return n;
     };
     double mine = none;
-    each([&](const Candidate &c) { mine = fmax(mine, c.score); });
-    double least = bound_of(mine, keep, s_all, &s_one);
+    each([&](double s, uint32_t) { mine = fmax(mine, s); });
+    double least = bound_of(mine, (int)keep, s_all, &s_one);
     int64_t last = 0x7fffffffffffffffll;  // the last place taken of those with that score
     const auto plus = [](int a, int b) { return a + b; };
     int all;
-    int at = place_of(count([&](const Candidate &c) { return c.score >= least; }), s_n, all);
+    int at = place_of(count([&](double s, uint32_t) { return s >= least; }), s_n, all);
     if (all > kList) {
         const auto above = [&](double m) {
-            return over_block(count([&](const Candidate &c) { return c.score > m; }), s_n, plus);
+            return over_block(count([&](double s, uint32_t) { return s > m; }), s_n, plus);
         };
         int more = above(least);
-        if (more >= keep) {  // as in the pieces
+        if (more >= (int)keep) {  // as in the pieces
             int64_t lo = ordered(least);
             int64_t hi = over_block(ordered(mine), s_top,
                                     [](int64_t a, int64_t b) { return a > b ? a : b; });
             while (lo < hi) {
                 const int64_t mid = lo + (int64_t)(((uint64_t)hi - (uint64_t)lo) >> 1);
                 if (above(__builtin_bit_cast(double, mid ^ ((mid >> 63) & 0x7fffffffffffffffll))) <
-                    keep)
+                    (int)keep)
                     hi = mid;
                 else
                     lo = mid + 1;
@@ -518,35 +522,38 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
             least = __builtin_bit_cast(double, lo ^ ((lo >> 63) & 0x7fffffffffffffffll));
             more = above(least);
         }
-        int64_t l = 0, h = (int64_t)p.beams * p.vocab - 1;
+        int64_t l = 0, h = ((int64_t)p.beams << 32) - 1;
         while (l < h) {
             const int64_t mid = (l + h) >> 1;
-            const int c = over_block(count([&](const Candidate &x) {
-                                         return x.score == least && x.place <= mid;
-                                     }),
-                                     s_n, plus);
-            if (c >= keep - more)
+            const int c = over_block(
+                count([&](double s, uint32_t i) { return s == least && place_at(i) <= mid; }), s_n,
+                plus);
+            if (c >= (int)keep - more)
                 h = mid;
             else
                 l = mid + 1;
         }
         last = l;
-        at = place_of(count([&](const Candidate &c) {
-                          return c.score > least || (c.score == least && c.place <= last);
+        at = place_of(count([&](double s, uint32_t i) {
+                          return s > least || (s == least && place_at(i) <= last);
                       }),
                       s_n, all);
     }
-    each([&](const Candidate &c) {
-        if (c.score > least || (c.score == least && c.place <= last)) {
+    const bool ties = last != 0x7fffffffffffffffll;  // beyond the list
+    each([&](double s, uint32_t i) {
+        if (s > least || (s == least && (!ties || place_at(i) <= last))) {
             if (at < kList) {
-                s_score[at] = c.score;
-                s_place[at] = c.place;
+                s_score[at] = s;
+                s_place[at] = i;
             }
             ++at;
         }
     });
     __syncthreads();
     all = min(all, kList);
+    for (int c = tid; c < all; c += kThreads)  // one latency for all of them
+        s_place[c] = place_at((uint32_t)s_place[c]);
+    __syncthreads();
     const auto put = [&](int rank, float score, int32_t parent, int32_t token, bool ended) {
         const int64_t o = item * keep + rank;
         p.new_score[o] = score;
@@ -561,12 +568,12 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
 #pragma unroll 4
         for (int o = 0; o < all; ++o)
             rank += s_score[o] > s || (s_score[o] == s && s_place[o] < place);
-        if (rank < keep) {
-            const int32_t w = (int32_t)(place / p.vocab), token = (int32_t)(place % p.vocab);
+        if (rank < (int)keep) {
+            const int32_t w = (int32_t)(place >> 32), token = (int32_t)place;
             put(rank, (float)s, (int32_t)row0 + w, token, token == p.end);
         }
     }
-    for (int r = all + tid; r < keep; r += kThreads)
+    for (int r = all + tid; r < (int)keep; r += kThreads)
         put(r, -kInf, -1, -1, false);
 }
 
@@ -599,7 +606,7 @@ hipError_t launch_beam(const BeamProblem &p, int type, int vecs, hipStream_t str
         return e;
     const bool held = (int64_t)p.beams * p.pieces * p.keep <= kThreads * kHeld;
     const dim3 grid((unsigned)p.batch);
-    const size_t lds = (size_t)p.beams * 8;
+    const size_t lds = (size_t)p.beams * sizeof(Beam);
     if (held)
         hipLaunchKernelGGL(beam_pick_kernel<true>, grid, dim3(kThreads), lds, stream, p);
     else

@@ -312,12 +312,11 @@ struct BeamProblem {
     float *new_score;
     int32_t *parent, *token;
     uint8_t *new_done;
-    // workspace, of every piece: [keep] values and indexes, the largest value and
-    // the sum of exponentials, and how many are listed
+    // workspace, of every piece: [keep] values and indexes (-inf past the last), the largest
+    // value and the sum of exponentials
     float *values;
     int32_t *indexes;
     double *sums;
-    int32_t *listed;
 };
 constexpr int kBeamVecs = 8, kBeamFewVecs = 2;  // 16-byte vectors a thread
 int64_t beam_piece(int type, int vecs);
