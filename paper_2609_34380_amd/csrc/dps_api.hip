@@ -1224,7 +1224,7 @@ BeamPlan plan_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t keep, in
     b.pieces = cdiv(span, dps::beam_piece(type, b.vecs));
     b.lists = rows * b.pieces;
     b.value_bytes = align256(b.lists * keep * 4);
-    b.sum_bytes = align256(b.lists * 16);
+    b.sum_bytes = align256(b.lists * 16 * dps::kBeamWaves);
     return b;
 }
 

@@ -6,7 +6,7 @@
 // row can give up all but its `keep` best before the row's sum is known.
 //
 // Two launches.  The first reads every logit once: a block of threads holds a piece
-// of a row in registers, sums its exponentials and lists its best.  The second, a
+// of a row in registers, sums its exponentials (a wave each) and lists its best.  The second, a
 // block a batch item, joins the sums and picks from the lists.
 //
 // Bound: HBM for the first where rows are many (2 or 4 bytes a logit), else latency.
@@ -17,7 +17,7 @@
 // more than the list holds, the keep-th best value, and the last index among its
 // equals, are found by bisection over the register values: exact whatever the data.
 //
-// Precision: exponentials in fp32 of differences from the piece's largest (of which
+// Precision: exponentials in fp32 of differences from the wave's largest (of which
 // none is above 0), the values of a 16-byte vector added in fp32, in pairs; their
 // sums, log and scores in 64 bits, since candidates of different beams may lie closer
 // than fp32 tells apart.  A sum is good to 2^-21 of itself: 3 roundings of 2^-24 in
@@ -32,9 +32,10 @@ namespace dps {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kWaves = kBeamWaves;
+static_assert(kThreads == 64 * kWaves, "a sum a wave");
 constexpr int kList = 1024;
-constexpr int kFew = 128;  // threads whose values are looked through one by one
+constexpr int kFew = 64;  // threads whose values are looked through one by one
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_inff();
 
@@ -195,6 +196,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
     __shared__ int32_t s_n[kWaves];
     __shared__ float s_one;
     __shared__ int32_t s_thread[kFew], s_threads, s_found;
+    __shared__ u32x4 s_raw[kFew * VECS];
 
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / p.pieces;
@@ -243,10 +245,12 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
                 f(wide<TYPE>(v[j], i), at0 + (j * kThreads + tid) * kPer + i);
     };
 
-    // ---- the sum of exponentials -------------------------------------------------
+    // ---- the sum of exponentials, a wave's beside its largest value ---------------
     float mine = -kInf;
     each([&](float x, int) { mine = fmaxf(mine, x); });
-    const float top = over_block(mine, s_f, [](float a, float b) { return fmaxf(a, b); });
+    float top = mine;
+    for (int d = 32; d > 0; d >>= 1)
+        top = fmaxf(top, __shfl_xor(top, d));
     const float ref = top == -kInf ? 0.0f : top;
     // a NaN, or an infinity less itself, makes the sum no number, and the row count for nothing
     double sum = 0.0;
@@ -263,37 +267,46 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
                 e[i] += e[i + d];
         sum += e[0];
     }
-    const double total = over_block(sum, s_d, [](double a, double b) { return a + b; });
+    for (int d = 32; d > 0; d >>= 1)
+        sum += __shfl_xor(sum, d);
+    if ((tid & 63) == 0) {
+        s_f[tid >> 6] = ref;
+        s_d[tid >> 6] = sum;
+    }
 
     // ---- the keep best --------------------------------------------------------------
     const int keep = p.keep;
     float least = bound_of(mine, keep, s_all, &s_one);  // of the values taken
+    const float wave_ref = s_f[tid & (kWaves - 1)];
+    const double wave_sum = s_d[tid & (kWaves - 1)];
     // the threads whose largest reaches it: seldom more than keep
     if (tid == 0)
         s_threads = s_found = 0;
     __syncthreads();
     if (mine >= least && mine > -kInf) {
         const int i = atomicAdd(&s_threads, 1);
-        if (i < kFew)
+        if (i < kFew) {
             s_thread[i] = tid;
+#pragma unroll
+            for (int j = 0; j < VECS; ++j)
+                s_raw[i * VECS + j] = v[j];
+        }
     }
     __syncthreads();
     int n = 0, all = s_threads;
     bool listed = all <= kFew;
     if (listed) {
-        // their values again, from the caches, a wave a thread's and a lane a value
+        // a wave a thread's values, a lane a value
         constexpr int kEach = VECS * kPer;
+        const uint8_t *raw = reinterpret_cast<const uint8_t *>(s_raw);
         for (int c = tid >> 6; c < all; c += kWaves) {
-            const int t = s_thread[c], i = tid & 63;
-            const int32_t at = at0 + ((i / kPer) * kThreads + t) * kPer + i % kPer;
-            if (i < kEach && at >= 0 && at < vocab) {
-                const float x = read<TYPE>(first, at);
-                if (x >= least && x > -kInf) {
-                    const int o = atomicAdd(&s_found, 1);  // they are ranked below
-                    if (o < kList) {
-                        s_value[o] = x;
-                        s_index[o] = at;
-                    }
+            const int i = tid & 63;
+            const float x = i < kEach ? read<TYPE>(raw, c * kEach + i) : -kInf;
+            if (x >= least && x > -kInf) {
+                const int o = atomicAdd(&s_found, 1);  // they are ranked below
+                if (o < kList) {
+                    s_value[o] = x;
+                    s_index[o] = at0 + ((i / kPer) * kThreads + s_thread[c]) * kPer + i % kPer;
                 }
             }
         }
@@ -302,54 +315,43 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
         listed = all <= kList;
         __syncthreads();
     }
-    int at = 0;
     if (!listed) {
-        each([&](float x, int) { n += x >= least && x > -kInf; });
-        at = place_of(n, s_n, all);
-    }
-    if (listed) {
-    } else if (all <= kList) {
-        each([&](float x, int i) {
-            if (x >= least && x > -kInf) {
-                s_value[at] = x;
-                s_index[at++] = i;
-            }
-        });
-    } else {
-        const auto plus = [](int a, int b) { return a + b; };
+        // the keep-th largest value is the least that fewer than `keep` are above
         const auto above = [&](float m) {
-            int c = 0;
-            each([&](float x, int) { c += x > m; });
-            return over_block(c, s_n, plus);
+            n = 0;
+            each([&](float x, int) { n += x > m; });
         };
-        int more = above(least);
-        if (more >= keep) {
-            // the keep-th largest value: the least that fewer than `keep` are above
+        above(least);
+        int at = place_of(n, s_n, all);
+        if (all >= keep) {
+            top = over_block(top, s_f, [](float a, float b) { return fmaxf(a, b); });
             int32_t lo = ordered(least), hi = ordered(top);
             while (lo < hi) {
                 const int32_t mid = (int32_t)(((int64_t)lo + hi) >> 1);
-                if (above(value_of(mid)) < keep)
+                above(value_of(mid));
+                if (over_block(n, s_n, [](int a, int b) { return a + b; }) < keep)
                     hi = mid;
                 else
                     lo = mid + 1;
             }
             least = value_of(lo);
-            more = above(least);
+            above(least);
+            at = place_of(n, s_n, all);
         }
-        n = 0;
-        each([&](float x, int) { n += x > least; });
-        at = place_of(n, s_n, all);
-        each([&](float x, int i) {
-            if (x > least) {
-                s_value[at] = x;
-                s_index[at++] = i;
-            }
-        });
+        const int more = all;
+        if (n > 0) {
+            each([&](float x, int i) {
+                if (x > least) {
+                    s_value[at] = x;
+                    s_index[at++] = i;
+                }
+            });
+        }
         // of its equals the first: a vector of all threads at a time, which lie in order
         int taken = more;
 #pragma unroll
         for (int j = 0; j < VECS; ++j) {
-            if (taken < keep) {
+            if (taken < keep && least > -kInf) {
                 n = 0;
 #pragma unroll
                 for (int i = 0; i < kPer; ++i)
@@ -386,14 +388,16 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
     }
     for (int r = all + tid; r < keep; r += kThreads)
         p.values[list * keep + r] = -kInf;  // its index is not read
-    if (tid == 0) {
-        p.sums[list * 2] = (double)ref;
-        p.sums[list * 2 + 1] = total;
+    if (tid < kWaves) {  // a pair a wave; the second kernel joins them
+        p.sums[(list * kWaves + tid) * 2] = (double)wave_ref;
+        p.sums[(list * kWaves + tid) * 2 + 1] = wave_sum;
     }
 }
 
-// Candidates of a batch item are numbered as they lie in the lists: beam, piece, rank.
-// Their place among equals is the beam, then the token.
+// Candidates of a batch item are numbered by rank in their lists, then by list (beam,
+// piece), so that the best of all lists are dealt to different threads: numbered as they
+// lie they fell to one thread in `keep`, whose largest made a low bound (16 items of 8
+// beams, 16 kept: 14.4 us, 10.0 so).  Their place among equals is the beam, then the token.
 constexpr int kHeld = 8;  // scores of candidates that a thread keeps in registers
 
 // What LDS holds of a beam.
@@ -418,31 +422,33 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
     const int tid = threadIdx.x;
     const int64_t item = blockIdx.x, row0 = item * p.beams;
     const double none = -(double)kInf;
-    const uint32_t keep = p.keep, a_row = (uint32_t)p.pieces * keep, slots = a_row * p.beams;
-    const float *values = p.values + row0 * a_row;
+    const uint32_t keep = p.keep, lists = (uint32_t)p.pieces * p.beams, slots = lists * keep;
+    const float *values = p.values + item * slots;
+    const auto where = [&](uint32_t i) { return i % lists * keep + i / lists; };
     float value[kHeld];
     if (HELD) {  // on their way while the sums are joined
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
-            value[j] = values[min(tid + j * kThreads, (int)slots - 1)];
+            value[j] = values[where(min(tid + j * kThreads, (int)slots - 1))];
     }
-    // `per` lanes a beam (a power of two, at most a wave), a lane a piece
+    // `per` lanes a beam (a power of two, at most a wave), a lane the sum of a wave's values
     int per = 64;
     while (per > 1 && per * p.beams > kThreads)
         per >>= 1;
     for (int w = tid / per; w < p.beams; w += kThreads / per) {
         const int64_t row = row0 + w;
-        const double *sums = p.sums + row * p.pieces * 2;
+        const int pairs = p.pieces * kWaves;
+        const double *sums = p.sums + row * pairs * 2;
         const float cum = p.score[row];
         const bool ended = p.done && p.done[row], finite = __builtin_fabsf(cum) < kInf;
         const bool counts = !ended && finite;
         double top = none, sum = 0.0;
-        for (int c = tid % per; c < p.pieces; c += per)
+        for (int c = tid % per; c < pairs; c += per)
             if (counts && sums[c * 2 + 1] != 0.0)
                 top = fmax(top, sums[c * 2]);
         for (int d = per / 2; d > 0; d >>= 1)
             top = fmax(top, __shfl_xor(top, d));
-        for (int c = tid % per; c < p.pieces; c += per) {
+        for (int c = tid % per; c < pairs; c += per) {
             const double s = sums[c * 2 + 1];
             if (counts && s != 0.0)  // an infinite top leaves no number
                 sum += s * exp(sums[c * 2] - top);
@@ -455,15 +461,16 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
     __syncthreads();
 
     const auto score_of = [&](uint32_t i, float x) {
-        const Beam b = s_beam[i / a_row];
+        const uint32_t list = i % lists, w = list / p.pieces;
+        const Beam b = s_beam[w];
         double s = (double)b.score + ((double)x - b.lse);
-        if (b.ended)
-            s = i % a_row == 0 ? (double)b.score - b.lse : none;
+        if (b.ended)  // the first of its first list
+            s = i == list && list == w * p.pieces ? (double)b.score - b.lse : none;
         return s == s ? s : none;
     };
     const auto place_at = [&](uint32_t i) {
-        const uint32_t w = i / a_row;
-        const int32_t token = s_beam[w].ended ? p.end : p.indexes[row0 * a_row + i];
+        const uint32_t w = i % lists / p.pieces;
+        const int32_t token = s_beam[w].ended ? p.end : p.indexes[item * slots + where(i)];
         return (int64_t)w << 32 | (uint32_t)token;
     };
     double held[kHeld];
@@ -484,7 +491,7 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
                     f(held[j], (uint32_t)(tid + j * kThreads));
         } else {
             for (uint32_t i = tid; i < slots; i += kThreads) {
-                const double s = score_of(i, values[i]);
+                const double s = score_of(i, values[where(i)]);
                 if (s > none)
                     f(s, i);
             }

@@ -312,12 +312,13 @@ struct BeamProblem {
     float *new_score;
     int32_t *parent, *token;
     uint8_t *new_done;
-    // workspace, of every piece: [keep] values and indexes (-inf past the last), the largest
-    // value and the sum of exponentials
+    // workspace, of every piece: [keep] values and indexes (-inf past the last), and of its
+    // kBeamWaves waves the largest value and the sum of exponentials
     float *values;
     int32_t *indexes;
     double *sums;
 };
+constexpr int kBeamWaves = 4;
 constexpr int kBeamVecs = 8, kBeamFewVecs = 2;  // 16-byte vectors a thread
 int64_t beam_piece(int type, int vecs);
 hipError_t launch_beam(const BeamProblem &p, int type, int vecs, hipStream_t stream);
