@@ -116,8 +116,8 @@ __global__ __launch_bounds__(kThreads) void kv_remap_kernel(int32_t *__restrict_
 // of a byte store the same, so plain stores do; bits set by atomics took 700 us of a
 // call with 2000 rows of 1300 columns).
 //
-// Bound: latency, and 4 bytes in and out a table entry.  Three launches, each of which
-// needs all of the one before: who copies (and cleared bytes), tables and bytes, the
+// Bound: latency, and 4 bytes in and out a table entry.  Three launches (one for small
+// tables), each of which needs all of the one before: who copies (and cleared bytes), tables and bytes, the
 // list of freed blocks.
 
 __device__ __forceinline__ bool in_range(int32_t x, int32_t n) { return x >= 0 && x < n; }
@@ -138,20 +138,15 @@ __device__ __forceinline__ bool open_ended(const KvForkProblem &p, int32_t len)
     return (len & ((1 << p.log2_tokens) - 1)) != 0 && (len >> p.log2_tokens) < p.cols;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvForkProblem p)
+// Who copies: lengths, the list of copies, and what replaces each new row's last block.
+// By kPlanThreads threads; s_eldest holds old_rows entries.
+__device__ __forceinline__ void plan_copies(const KvForkProblem &p, int32_t *s_eldest,
+                                            int32_t *s_sums)
 {
-    // bytes of both sides, by every block
-    for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < 2 * p.words;
-         i += (int64_t)gridDim.x * kPlanThreads)
-        p.held[i] = u32x4{0u, 0u, 0u, 0u};
-    if (blockIdx.x != 0)
-        return;
     constexpr int kPer = kMostRows / kPlanThreads;
-    __shared__ int32_t s_eldest[kMostRows];  // of each old row: its first child
-    __shared__ int32_t s_sums[kPlanThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int i = tid; i < p.old_rows; i += kPlanThreads)
-        s_eldest[i] = 0x7fffffff;
+        s_eldest[i] = 0x7fffffff;  // its first child
     __syncthreads();
     const int r0 = tid * kPer;
     int32_t from[kPer];
@@ -163,12 +158,14 @@ __global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvFork
         else
             from[i] = -1;
     }
-    __syncthreads();
     int32_t len[kPer], n = 0;
     bool copies[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < kPer; ++i)
         len[i] = from[i] >= 0 ? length_of(p, from[i]) : 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
         copies[i] = from[i] >= 0 && open_ended(p, len[i]) && s_eldest[from[i]] != r0 + i;
         n += copies[i];
     }
@@ -204,6 +201,93 @@ __global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvFork
         p.counts[0] = all;
 }
 
+// The block of a new row's column.
+__device__ __forceinline__ int32_t block_of(const KvForkProblem &p, int32_t row, int32_t col)
+{
+    const int32_t from = p.parent[row];
+    if (!in_range(from, p.old_rows))
+        return -1;
+    const int32_t last = p.last[row], have = columns(p, length_of(p, from));
+    if (col >= have)
+        return -1;
+    return col == have - 1 && last != kKeep ? last : p.table[(int64_t)from * p.cols + col];
+}
+
+__global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(const KvForkProblem p)
+{
+    __shared__ int32_t s_eldest[kMostRows];
+    __shared__ int32_t s_sums[kPlanThreads / 64];
+    // bytes of both sides, by every block
+    for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < 2 * p.words;
+         i += (int64_t)gridDim.x * kPlanThreads)
+        p.held[i] = u32x4{0u, 0u, 0u, 0u};
+    if (blockIdx.x == 0)
+        plan_copies(p, s_eldest, s_sums);
+}
+
+// All of it in one block of threads, a bit a block in LDS: for tables so small that the
+// time is that of the launches (8 rows of 256 columns: one of 6 us for three of 3-5 each).
+constexpr int64_t kSmallEntries = 16384;  // of both tables, 16 a thread
+constexpr int64_t kSmallBlocks = 131072;
+constexpr int kSmallWords = kSmallBlocks / 32;
+constexpr int kSmallRows = 1024;
+
+__global__ __launch_bounds__(kPlanThreads) void kv_fork_small_kernel(const KvForkProblem p)
+{
+    __shared__ int32_t s_eldest[kSmallRows];
+    __shared__ int32_t s_sums[kPlanThreads / 64];
+    __shared__ uint32_t s_old[kSmallWords], s_new[kSmallWords];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int32_t words = (int32_t)((p.n_blocks + 31) / 32);
+    for (int i = tid; i < words; i += kPlanThreads)
+        s_old[i] = s_new[i] = 0;
+    plan_copies(p, s_eldest, s_sums);  // meets at its barriers
+    __threadfence_block();
+    __syncthreads();
+    const auto mark = [&](uint32_t *bits, int32_t block) {
+        if (block >= 0 && block < p.n_blocks)
+            atomicOr(&bits[block >> 5], 1u << (block & 31));
+    };
+    const int32_t olds = p.old_rows * p.cols, news = p.rows * p.cols;
+#pragma unroll 4
+    for (int i = tid; i < olds; i += kPlanThreads)
+        mark(s_old, p.table[i]);
+#pragma unroll 4
+    for (int i = tid; i < news; i += kPlanThreads) {
+        const int32_t row = i / p.cols, block = block_of(p, row, i - row * p.cols);
+        p.new_table[i] = block;
+        mark(s_new, block);
+    }
+    __syncthreads();
+    constexpr int kPer = kSmallWords / kPlanThreads;
+    uint32_t freed[kPer];
+    int32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int w = tid * kPer + i;
+        freed[i] = w < words ? s_old[w] & ~s_new[w] : 0;
+        n += __popc(freed[i]);
+    }
+    const int32_t incl = wave_scan(n);
+    if (lane == 63)
+        s_sums[wave] = incl;
+    __syncthreads();
+    int32_t at = incl - n, all = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) {
+        at += i < wave ? s_sums[i] : 0;
+        all += s_sums[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        for (uint32_t left = freed[i]; left; left &= left - 1, ++at)
+            if (at < p.n_freed)
+                p.freed[at] = (tid * kPer + i) * 32 + __builtin_ctz(left);
+    for (int64_t i = all + tid; i < p.n_freed; i += kPlanThreads)
+        p.freed[i] = -1;
+    if (tid == 0)
+        p.counts[1] = all;
+}
+
 // A thread has one column of kRows rows.  Rows that share a prefix lie side by side:
 // an entry that repeats the one above it is marked already.
 constexpr int kRows = 8;
@@ -227,15 +311,7 @@ __global__ __launch_bounds__(kThreads) void kv_fork_tables_kernel(const KvForkPr
         if (old) {
             block[i] = p.table[(int64_t)row * p.cols + col];
         } else {
-            const int32_t from = p.parent[row];
-            if (in_range(from, p.old_rows)) {
-                const int32_t last = p.last[row];
-                const int32_t have = columns(p, length_of(p, from));
-                if (col < have)
-                    block[i] = col == have - 1 && last != kKeep
-                                   ? last
-                                   : p.table[(int64_t)from * p.cols + col];
-            }
+            block[i] = block_of(p, row, col);
             p.new_table[(int64_t)row * p.cols + col] = block[i];
         }
     }
@@ -335,6 +411,11 @@ hipError_t launch_kv_remap(int32_t *table, int64_t entries, const int32_t *src, 
 
 hipError_t launch_kv_fork(const KvForkProblem &p, hipStream_t stream)
 {
+    if (p.rows <= kSmallRows && p.old_rows <= kSmallRows && p.n_blocks <= kSmallBlocks &&
+        ((int64_t)p.rows + p.old_rows) * p.cols <= kSmallEntries) {
+        hipLaunchKernelGGL(kv_fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
+        return hipGetLastError();
+    }
     const int64_t clears = (2 * p.words + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
     hipLaunchKernelGGL(kv_fork_plan_kernel, dim3((unsigned)(clears < 1 ? 1 : clears)),
                        dim3(kPlanThreads), 0, stream, p);
