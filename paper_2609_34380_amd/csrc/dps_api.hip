@@ -1322,7 +1322,7 @@ namespace {
 // Launch shape and workspace of an attention call whose rows share prefixes.
 struct SharedPlan {
     AttnPlan attn;
-    int columns, item_rows;
+    int kind, columns, item_rows;
     int64_t blocks, slots;
     size_t row_bytes, found_bytes, own_bytes, own_stat_bytes, part_bytes, part_stat_bytes;
     size_t bytes() const
@@ -1338,9 +1338,10 @@ SharedPlan plan_shared(int64_t rows, int64_t groups, int64_t heads, int64_t kv_h
     SharedPlan s;
     s.attn = plan_attn(heads, kv_heads, dim, fp8);
     const int64_t lines = kv_heads * s.attn.groups;
-    s.columns = dps::shared_columns(rows, groups, s.attn.step, fp8, (int)dim);
+    s.kind = dps::shared_kind(rows, groups, s.attn.step, fp8, (int)dim);
+    s.columns = dps::shared_columns(s.kind, (int)dim);
     s.item_rows = s.columns / s.attn.step;
-    s.blocks = cdiv((int64_t)dps::shared_blocks_per_cu(s.columns, fp8, (int)dim) *
+    s.blocks = cdiv((int64_t)dps::shared_blocks_per_cu(s.kind, fp8, (int)dim) *
                         current_cu_count(), lines);
     s.slots = s.blocks + rows / s.item_rows + groups;
     const int64_t parts = lines * s.slots * s.columns;
@@ -1398,7 +1399,11 @@ DPS_EXPORT dps_status dps_attn_shared(const dps_attn_args *a, const dps_kv_cache
     const int64_t lines = (int64_t)cache->kv_heads * attn.groups;
     // a launch counts its threads (256 a row and key/value head) in 32 bits, and a
     // key/value head its partials
-    REQUIRE(a->rows * lines < (1 << 24) && plan.slots * plan.columns <= 0x7fffffff,
+    // (a tile counts up to eight times on the line)
+    const int64_t room = a->table_cols > 0x7fffffff / cache->block_tokens
+                             ? 0x7fffffff
+                             : a->table_cols * cache->block_tokens;
+    REQUIRE(a->rows <= 0x7fffffff / 8 / (room / 32 + 2) && a->rows * lines < (1 << 24) && plan.slots * plan.columns <= 0x7fffffff,
             DPS_ERR_UNSUPPORTED, "too many rows for one call");
     REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
             "workspace is smaller than dps_attn_shared_workspace_bytes()");
@@ -1421,6 +1426,7 @@ DPS_EXPORT dps_status dps_attn_shared(const dps_attn_args *a, const dps_kv_cache
     p.group_start = group_start;
     p.shared_len = shared_len;
     p.groups = (int32_t)groups;
+    p.kind = plan.kind;
     p.columns = plan.columns;
     p.item_rows = plan.item_rows;
     p.slots = (int32_t)plan.slots;

@@ -234,29 +234,34 @@ struct SharedProblem {
     SharedRow *rows;
     const int32_t *group_start, *shared_len;
     int32_t groups;
+    int32_t kind;           // SHARED_*: the kernel
     int32_t columns, item_rows;
     int32_t slots;          // partials of a key/value head and pass
     // workspace: [heads and passes][slots][columns] rows, reference score and sum
     float *part_out, *part_stat;
 };
 constexpr int kSharedGroups = 1024;
-// Columns of an item.  Up to 32 for a group of average size: tokens from memory to
-// registers, a block's waves on different ones, which keeps the most loads in flight
-// (8 FP8 prefixes of 9000 tokens and 32 columns 42 us, through LDS 58; 5 BF16 ones of 2000
-// and 28 columns 17 / 25).  More: through LDS, for up to eight waves of 32 columns (four
-// for heads over 128), since each pass of 32 would read the tokens again.
-constexpr int shared_columns(int64_t rows, int64_t groups, int step, bool fp8, int dim)
+// The kernel, by the columns of a group of average size.  16 and 32: tokens from memory to
+// registers, a block's waves on different ones, which keeps the most loads in flight (8
+// FP8 prefixes of 9000 tokens 42 us, through LDS 58; 5 BF16 ones of 2000 17 / 25).  Wide:
+// through LDS, 32 columns a wave, eight waves (four for heads over 128), where passes of
+// 32 columns would each read the tokens.
+enum { SHARED_16 = 0, SHARED_32 = 1, SHARED_WIDE = 2 };
+constexpr int shared_kind(int64_t rows, int64_t groups, int step, bool fp8, int dim)
 {
     const int64_t mean = rows * step / (groups < 1 ? 1 : groups);
-    if (mean <= 16 && step <= 16)
-        return 16;
-    if (dim % 64 != 0 || (mean <= 32 && attn_heads_a_pass(fp8, dim) == 32))
-        return 32;
-    return dim > 128 ? 128 : 256;
+    const bool two = attn_heads_a_pass(fp8, dim) == 32;
+    if (dim % 64 == 0 && mean > (two ? 32 : 16))
+        return SHARED_WIDE;
+    return two && (step > 16 || mean > 16) ? SHARED_32 : SHARED_16;
 }
-constexpr int shared_blocks_per_cu(int columns, bool fp8, int dim)
+constexpr int shared_columns(int kind, int dim)
 {
-    return columns <= 32 && (fp8 ? 1 : 2) * dim < (columns == 16 ? 512 : 192) ? 2 : 1;
+    return kind == SHARED_WIDE ? (dim > 128 ? 128 : 256) : kind == SHARED_32 ? 32 : 16;
+}
+constexpr int shared_blocks_per_cu(int kind, bool fp8, int dim)
+{
+    return kind == SHARED_WIDE || (fp8 ? 1 : 2) * dim >= (kind == SHARED_16 ? 512 : 192) ? 1 : 2;
 }
 hipError_t launch_shared(const SharedProblem &p, int type, bool fp8, int dim, int blocks,
                          int attn_blocks, hipStream_t stream);

@@ -11,12 +11,15 @@
 // (dps_attn.hip) over each row's own tokens, and shared_join_kernel.
 //
 // shared_kernel.  An item is up to `columns` columns of a group.  The tiles of all items
-// of a key/value head form one line, cut into equal ranges, one a block of threads; a
-// block has a contiguous part of an item at a time, and leaves one partial for it
-// (slot block + item: of two neighbours on the line that share an item, or of two
-// items that share a block, no two slots are the same).  WC waves of a block have
-// different columns of the same tokens, and its kWaves / WC teams different tokens,
-// which they join in LDS.
+// of a key/value head, each as long as it takes a block, form one line, cut into equal
+// ranges, one a block of threads; a block has a contiguous part of an item at a time, and
+// leaves one partial for it (slot block + item: of two neighbours on the line that share
+// an item, or of two items that share a block, no two slots are the same).  A block's
+// waves have different tokens, and join in LDS.  shared_wide_kernel takes more columns at a
+// time: as many of its waves as the item needs have columns of their own, and teams of them
+// different tokens.  Where groups are few, there every item gets whole blocks of its own instead, as many as make the longest
+// range shortest: a block that begins and ends an item twice loses 6 to 10 us (240 rows of
+// 64 heads under 16384 tokens 250 us on the line, 230 so).
 //
 // The tile is attn_kernel's: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix
 // instructions, 32 tokens at a time, HT column tiles of 16 a wave; keys and values go
@@ -33,15 +36,43 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
+constexpr int kFewGroups = 16;  // whose items get whole blocks where they can
 
-// Where the groups lie: tiles and items of a key/value head before each group, and the
-// table row of its first row where that has the whole prefix (-1: another may).
+// What every lane of the wave holds, in a scalar register.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// How a kernel deals columns to a block's waves, MOST of them with columns of their own,
+// and how long a tile takes it, of at most MOST: what is its own of memory and LDS (BASE),
+// and team turns for the rest.
+template <int WAVES, int COLUMNS, int MOST, int BASE>
+struct Deal {
+    static constexpr int kWaves = WAVES;
+    static constexpr int kMost = MOST;
+
+    static __device__ __forceinline__ int32_t waves(const SharedProblem &p, int32_t rows)
+    {
+        return (rows * p.attn.group_step + COLUMNS - 1) / COLUMNS;
+    }
+    static __device__ __forceinline__ int32_t weight(const SharedProblem &p, int32_t rows)
+    {
+        if (MOST == 1)
+            return 1;
+        const int32_t turns = MOST / (MOST / waves(p, rows));
+        return (BASE * MOST + (MOST - BASE) * turns + MOST / 2) / MOST;
+    }
+};
+
+// Where the groups lie: the length of the line of a key/value head before each group, the
+// items, and the table row of its first row where that has the whole prefix (-1: another
+// may).
 struct Groups {
-    int32_t tiles[kSharedGroups + 1];
+    int32_t line[kSharedGroups + 1];
     int32_t items[kSharedGroups + 1];
     int32_t lead[kSharedGroups];
     int32_t first[kSharedGroups], rows[kSharedGroups], length[kSharedGroups];
     int32_t sums[2][8];  // a wave
+    int32_t share;       // > 0: items have whole blocks, of at most so much of the line; and
+                         // `line` counts blocks
 };
 
 // Tokens that a row has, as far as its table row holds them.
@@ -81,14 +112,49 @@ __device__ __forceinline__ int32_t items_of(const SharedProblem &p, const Group 
     return x.length > 0 ? (x.rows + p.item_rows - 1) / p.item_rows : 0;
 }
 
+// The items of a group on the line: full ones, and a last one that may have fewer rows.
+template <typename DEAL>
+struct Items {
+    int32_t tiles, count, full, last;  // tiles and weights
+
+    __device__ __forceinline__ Items(const SharedProblem &p, const Group &x)
+        : tiles(tiles_of(x)), count(items_of(p, x)), full(0), last(0)
+    {
+        if (count > 0) {
+            full = DEAL::weight(p, p.item_rows);
+            last = DEAL::weight(p, x.rows - (count - 1) * p.item_rows);
+        }
+    }
+    // whole blocks of an item, at `share` each, and of all
+    __device__ __forceinline__ int32_t blocks(int32_t weight, int32_t share) const
+    {
+        const int32_t length = weight * tiles;
+        int32_t n = (int32_t)((float)length * __builtin_amdgcn_rcpf((float)share));
+        while ((int64_t)n * share < length)  // at most a few: the quotient was rounded
+            ++n;
+        return n;
+    }
+    __device__ __forceinline__ int32_t blocks(int32_t share) const
+    {
+        return count > 0 ? (count - 1) * blocks(full, share) + blocks(last, share) : 0;
+    }
+    __device__ __forceinline__ int32_t begin(int32_t i) const { return i * full * tiles; }
+    __device__ __forceinline__ int32_t weight(int32_t i) const { return i < count - 1 ? full : last; }
+    __device__ __forceinline__ int32_t length() const
+    {
+        return count > 0 ? begin(count - 1) + last * tiles : 0;
+    }
+};
+
 // Fills s for all groups; false: the groups do not ascend within the rows, and nothing
 // is shared.
-template <int WAVES>
-__device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
+template <typename DEAL>
+__device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s, int32_t blocks)
 {
+    constexpr int WAVES = DEAL::kWaves;
     constexpr int kPer = kSharedGroups / (64 * WAVES);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int32_t tiles[kPer], items[kPer], n_tiles = 0, n_items = 0;
+    int32_t lengths[kPer], items[kPer], length = 0, n_items = 0;
     int32_t req[kPer], has[kPer];  // of the groups' first rows; they arrive under the scan
     bool bad = false;
 #pragma unroll
@@ -109,39 +175,39 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int32_t g = tid * kPer + i;
-        tiles[i] = items[i] = 0;
+        lengths[i] = items[i] = 0;
         if (g < p.groups && !bad) {
-            const Group x = {s.first[g], s.rows[g], s.length[g]};
-            items[i] = items_of(p, x);
-            tiles[i] = items[i] * tiles_of(x);
+            const Items<DEAL> x(p, Group{s.first[g], s.rows[g], s.length[g]});
+            items[i] = x.count;
+            lengths[i] = x.length();
         }
-        n_tiles += tiles[i];
+        length += lengths[i];
         n_items += items[i];
     }
-    const int32_t incl_tiles = wave_scan(n_tiles), incl_items = wave_scan(n_items);
+    const int32_t incl_length = wave_scan(length), incl_items = wave_scan(n_items);
     if (lane == 63) {
-        s.sums[0][wave] = incl_tiles;
+        s.sums[0][wave] = incl_length;
         s.sums[1][wave] = incl_items;
     }
     __syncthreads();
-    int32_t at_tile = incl_tiles - n_tiles, at_item = incl_items - n_items;
+    int32_t at = incl_length - length, at_item = incl_items - n_items;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-        at_tile += i < wave ? s.sums[0][i] : 0;
+        at += i < wave ? s.sums[0][i] : 0;
         at_item += i < wave ? s.sums[1][i] : 0;
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int32_t g = tid * kPer + i;
         if (g <= p.groups) {
-            s.tiles[g] = at_tile;
+            s.line[g] = at;
             s.items[g] = at_item;
         }
-        at_tile += tiles[i];
+        at += lengths[i];
         at_item += items[i];
     }
     if (tid == 64 * WAVES - 1 && p.groups == kSharedGroups) {
-        s.tiles[p.groups] = at_tile;
+        s.line[p.groups] = at;
         s.items[p.groups] = at_item;
     }
 #pragma unroll
@@ -149,6 +215,39 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s)
         const int32_t g = i * (64 * WAVES) + tid;
         if (g < p.groups)
             s.lead[g] = has[i] >= 0 ? req[i] : -1;
+    }
+    if (tid == 0)
+        s.share = DEAL::kMost > 1 ? 0x7fffffff : 0;
+    __syncthreads();
+    if (DEAL::kMost == 1)
+        return !bad;
+    const int32_t all = s.line[p.groups];
+    const bool few = !bad && p.groups <= kFewGroups && s.items[p.groups] <= blocks;
+    if (few && all > DEAL::kMost * blocks) {
+        // thread i tries 1 + i / 128 times the mean
+        const int32_t mean = (all + blocks - 1) / blocks;
+        const int32_t share = mean + (int32_t)((int64_t)mean * tid / 128);
+        int32_t n = 0;
+        for (int g = 0; g < p.groups; ++g)
+            n += Items<DEAL>(p, Group{s.first[g], s.rows[g], s.length[g]}).blocks(share);
+        if (n <= blocks)
+            atomicMin(&s.share, share);
+    }
+    __syncthreads();
+    const int32_t share = s.share;
+    __syncthreads();
+    if (share != 0x7fffffff) {
+        if (tid == 0) {
+            int32_t at_block = 0;
+            for (int g = 0; g <= p.groups; ++g) {
+                s.line[g] = at_block;
+                if (g < p.groups)
+                    at_block +=
+                        Items<DEAL>(p, Group{s.first[g], s.rows[g], s.length[g]}).blocks(share);
+            }
+        }
+    } else if (tid == 0) {
+        s.share = 0;
     }
     __syncthreads();
     return !bad;
@@ -168,12 +267,15 @@ __device__ __forceinline__ int last_from(const int32_t *first, int n, int32_t x)
     return lo;
 }
 
-// The line cut into `blocks` ranges of `each` tiles, the first `more` one longer.
+// The line cut into `blocks` ranges of `each`, the first `more` one longer.  A range has
+// the tiles that begin in it, and is as long as the longest tile: a block between two
+// that have tiles of an item has one, too.
 struct Line {
     int32_t blocks, each, more;
 
-    __device__ __forceinline__ Line(int32_t tiles, int32_t most)
-        : blocks(min(tiles, most)), each(tiles / max(blocks, 1)), more(tiles - each * blocks)
+    __device__ __forceinline__ Line(int32_t length, int32_t most, int32_t tile)
+        : blocks(length > 0 ? max(1, min(length / tile, most)) : 0), each(length / max(blocks, 1)),
+          more(length - each * blocks)
     {
     }
     __device__ __forceinline__ int32_t begin(int32_t b) const { return b * each + min(b, more); }
@@ -185,10 +287,11 @@ struct Line {
 };
 
 // What every row shares, and that no own token of it has been met.
-template <int WAVES>
+template <typename DEAL>
 __device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s, bool good,
                                          const Line &line, int32_t block, int32_t blocks)
 {
+    constexpr int WAVES = DEAL::kWaves;
     for (int64_t r = (int64_t)block * (64 * WAVES) + threadIdx.x; r < p.attn.rows;
          r += (int64_t)blocks * (64 * WAVES)) {
         SharedRow x = {0, 0, 0, 0};
@@ -198,18 +301,54 @@ __device__ __forceinline__ void put_rows(const SharedProblem &p, const Groups &s
             const Group g = {s.first[lo], s.rows[lo], s.length[lo]};
             int32_t req;
             if (g.length > 0 && tokens_of(p, (int32_t)r, req) >= g.length) {
-                const int32_t tiles = tiles_of(g), at = ((int32_t)r - g.first) / p.item_rows;
-                const int32_t item = s.items[lo] + at, tile = s.tiles[lo] + at * tiles;
-                const int32_t b0 = line.of(tile);
+                const Items<DEAL> items(p, g);
+                const int32_t at = ((int32_t)r - g.first) / p.item_rows;
                 x.start = g.length;
                 x.column = (((int32_t)r - g.first) % p.item_rows) * p.attn.group_step;
-                x.slot = b0 + item;
-                x.count = line.of(tile + tiles - 1) - b0 + 1;
+                if (s.share > 0) {
+                    x.slot = s.line[lo] + at * items.blocks(items.full, s.share);
+                    x.count = items.blocks(items.weight(at), s.share);
+                } else {
+                    const int32_t begin = s.line[lo] + items.begin(at);
+                    const int32_t b0 = line.of(begin);
+                    x.slot = b0 + s.items[lo] + at;
+                    x.count = line.of(begin + (items.tiles - 1) * items.weight(at)) - b0 + 1;
+                }
             }
         }
         p.rows[r] = x;
         p.attn.found[r] = int2{0, -1};
     }
+}
+
+// A block's next part of an item: tiles skip ... skip + part - 1 (none: part <= 0) of item
+// `at` of its group, and where it goes on.
+struct Part {
+    int32_t at, skip, part, next;
+};
+template <typename DEAL>
+__device__ __forceinline__ Part next_part(const SharedProblem &p, const Group &grp, int32_t line,
+                                          int32_t share, int32_t from, int32_t end)
+{
+    const Items<DEAL> items(p, grp);
+    const int32_t x = from - line;
+    Part r;
+    if (share > 0) {
+        const int32_t each = items.blocks(items.full, share);
+        r.at = min(x / each, items.count - 1);
+        const int32_t n = items.blocks(items.weight(r.at), share), k = x - r.at * each;
+        r.skip = (int32_t)((int64_t)items.tiles * k / n);
+        r.part = (int32_t)((int64_t)items.tiles * (k + 1) / n) - r.skip;
+        r.next = end;
+        return r;
+    }
+    r.at = min(x / (items.full * items.tiles), items.count - 1);
+    const int32_t begin = items.begin(r.at), w = items.weight(r.at);
+    const int32_t stop = min(end - line, begin + w * items.tiles);
+    r.skip = (x - begin + w - 1) / w;
+    r.part = (stop - begin + w - 1) / w - r.skip;
+    r.next = line + stop;
+    return r;
 }
 
 // The table row through which a group's prefix is read: that of the first row that has
@@ -230,15 +369,14 @@ __device__ __forceinline__ int32_t lead_of(const SharedProblem &p, const Group &
     return -1;
 }
 
-template <int TYPE, bool FP8, int D, int HT, int WC>
+template <int TYPE, bool FP8, int D, int HT>
 __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd)) void shared_kernel(
     const SharedProblem p, const int32_t *__restrict__ tables)
 {
     typedef Shape<TYPE, FP8, D, HT> S;
-    constexpr int kTeams = kWaves / WC;  // waves with the same columns and other tokens
     __shared__ Groups s_groups;
-    __shared__ f32x4 s_part[kTeams > 1 ? kWaves : 1][S::kAcc * 64];  // a column tile at a time
-    __shared__ float s_stat[kTeams > 1 ? kWaves : 1][128];
+    __shared__ f32x4 s_part[kWaves][S::kAcc * 64];  // a column tile at a time
+    __shared__ float s_stat[kWaves][128];
 
     const AttnProblem &a = p.attn;
     const int lane = threadIdx.x & 63;
@@ -252,12 +390,13 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     const int first_head = kvh * a.group + sub * a.group_step;
     const int n_heads = min(a.group_step, a.group - sub * a.group_step);
 
-    const bool good = find_groups<kWaves>(p, s_groups);
-    const int32_t all = good ? s_groups.tiles[p.groups] : 0;
-    const Line line(all, blocks);
+    typedef Deal<kWaves, 16 * HT, 1, 0> DealT;
+    const bool good = find_groups<DealT>(p, s_groups, blocks);
+    const int32_t share = uniform(s_groups.share);
+    const Line line(good ? s_groups.line[p.groups] : 0, blocks, DealT::kMost);
     if (hv == 0)
-        put_rows<kWaves>(p, s_groups, good, line, block, blocks);
-    if (block >= line.blocks)
+        put_rows<DealT>(p, s_groups, good, line, block, blocks);
+    if (block >= (share > 0 ? uniform(s_groups.line[p.groups]) : line.blocks))
         return;
 
     const uint32_t tokens = 1u << a.log2_tokens;
@@ -266,25 +405,24 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
     const uint32_t val_head = (uint32_t)(a.kv_heads + kvh) * tokens * (D * S::kElt);
     const float to_log2 = a.score_scale * kLog2e;
     const int32_t last_col = (int32_t)a.table_cols - 1;
-    const int wc = wave % WC, team = wave / WC;
 
-    int32_t tile = line.begin(block);
-    const int32_t end = line.begin(block + 1);
-    int g = last_from(s_groups.tiles, p.groups, tile);
-    while (tile < end) {
-        while (s_groups.tiles[g + 1] <= tile)  // past groups without tiles
+    int32_t at = share > 0 ? block : uniform(line.begin(block));
+    const int32_t end = share > 0 ? block + 1 : uniform(line.begin(block + 1));
+    int g = uniform(last_from(s_groups.line, p.groups, at));
+    while (at < end) {
+        while (uniform(s_groups.line[g + 1]) <= at)  // past groups without tiles
             ++g;
-        const Group grp = {s_groups.first[g], s_groups.rows[g], s_groups.length[g]};
-        const int32_t n_tiles = tiles_of(grp);
-        const int32_t in_group = tile - s_groups.tiles[g];
-        const int32_t at = in_group / n_tiles, skip = in_group % n_tiles;
-        const int32_t part = min(n_tiles - skip, end - tile);  // tiles of the item in this block
-        const int32_t item = s_groups.items[g] + at;
-        const int32_t row0 = grp.first + at * p.item_rows;
+        const Group grp = {uniform(s_groups.first[g]), uniform(s_groups.rows[g]),
+                           uniform(s_groups.length[g])};
+        const Part now = next_part<DealT>(p, grp, uniform(s_groups.line[g]), share, at, end);
+        at = now.next;
+        const int32_t skip = now.skip, part = now.part;
+        const int32_t item = share > 0 ? 0 : uniform(s_groups.items[g]) + now.at;
+        const int32_t row0 = grp.first + now.at * p.item_rows;
         const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
-        tile += part;
-
-        const int32_t lead = lead_of(p, grp, __builtin_amdgcn_readfirstlane(s_groups.lead[g]), lane);
+        if (part <= 0)
+            continue;
+        const int32_t lead = lead_of(p, grp, uniform(s_groups.lead[g]), lane);
         if (lead < 0)
             continue;  // no row reads the partials
         const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
@@ -297,7 +435,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         float ref[HT], sum[HT];
 #pragma unroll
         for (int c = 0; c < HT; ++c) {
-            column[c] = (wc * HT + c) * 16 + col;
+            column[c] = c * 16 + col;
             const int32_t r = column[c] / a.group_step, head = column[c] % a.group_step;
             used[c] = r < n_rows && head < n_heads;
             const uint8_t *qp = static_cast<const uint8_t *>(a.q) +
@@ -319,8 +457,8 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         }
 
         // this wave's tiles of the part
-        const int32_t u0 = skip + (int32_t)((int64_t)part * team / kTeams);
-        const int32_t u1 = skip + (int32_t)((int64_t)part * (team + 1) / kTeams);
+        const int32_t u0 = skip + (int32_t)((int64_t)part * wave / kWaves);
+        const int32_t u1 = skip + (int32_t)((int64_t)part * (wave + 1) / kWaves);
         const int32_t hi = grp.length;
 
         uint32_t place[2];
@@ -341,10 +479,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         uint32_t at_[2];
         const auto load = [&](auto *to, const uint8_t *from) {
             typedef typename std::remove_reference<decltype(*to)>::type T;
-            if (WC == 1)
-                *to = stream<T>(from);
-            else
-                *to = *reinterpret_cast<const T *>(from);
+            *to = stream<T>(from);
         };
         const auto load_keys = [&] {
 #pragma unroll
@@ -521,17 +656,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
 #pragma unroll
         for (int c = 0; c < HT; ++c) {
             sum[c] = quarters_sum(sum[c]);
-            if (kTeams == 1) {
-                if (used[c]) {
-#pragma unroll
-                    for (int t = 0; t < S::kAcc; t += 2)
-                        put2(column[c], t, acc[c][t], acc[c][t + 1]);
-                    if (quarter == 0)
-                        put_stat(column[c], ref[c], sum[c]);
-                }
-                continue;
-            }
-            // the teams' parts, a pair of output tiles at a time, dealt to them
+            // the waves' parts, a pair of output tiles at a time, dealt to them
             __syncthreads();  // the column tile before has been read
 #pragma unroll
             for (int i = 0; i < S::kAcc; ++i)
@@ -539,29 +664,29 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
             s_stat[wave][lane] = ref[c];
             s_stat[wave][64 + lane] = sum[c];
             __syncthreads();
-            float weight[kTeams], top = kNone, total = 0.0f;
+            float weight[kWaves], top = kNone, total = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kTeams; ++i) {
-                weight[i] = s_stat[i * WC + wc][lane];
+            for (int i = 0; i < kWaves; ++i) {
+                weight[i] = s_stat[i][lane];
                 top = fmaxf(top, weight[i]);
             }
 #pragma unroll
-            for (int i = 0; i < kTeams; ++i) {
+            for (int i = 0; i < kWaves; ++i) {
                 weight[i] = __builtin_amdgcn_exp2f(weight[i] - top);
-                total += s_stat[i * WC + wc][64 + lane] * weight[i];
+                total += s_stat[i][64 + lane] * weight[i];
             }
             if (!used[c])
                 continue;
-            for (int t = 2 * team; t < S::kAcc; t += 2 * kTeams) {
+            for (int t = 2 * wave; t < S::kAcc; t += 2 * kWaves) {
                 f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
 #pragma unroll
-                for (int k = 0; k < kTeams; ++k) {
-                    x += s_part[k * WC + wc][t * 64 + lane] * weight[k];
-                    y += s_part[k * WC + wc][(t + 1) * 64 + lane] * weight[k];
+                for (int k = 0; k < kWaves; ++k) {
+                    x += s_part[k][t * 64 + lane] * weight[k];
+                    y += s_part[k][(t + 1) * 64 + lane] * weight[k];
                 }
                 put2(column[c], t, x, y);
             }
-            if (team == 0 && quarter == 0)
+            if (wave == 0 && quarter == 0)
                 put_stat(column[c], top, total);
         }
     }
@@ -659,12 +784,13 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
     const int first_head = kvh * a.group + sub * a.group_step;
     const int n_heads = min(a.group_step, a.group - sub * a.group_step);
 
-    const bool good = find_groups<kWideWaves>(p, s_groups);
-    const int32_t all = good ? s_groups.tiles[p.groups] : 0;
-    const Line line(all, blocks);
+    typedef Deal<kWideWaves, 32, kWideWaves, kWideWaves * 3 / 8> DealT;
+    const bool good = find_groups<DealT>(p, s_groups, blocks);
+    const int32_t share = uniform(s_groups.share);
+    const Line line(good ? s_groups.line[p.groups] : 0, blocks, DealT::kMost);
     if (hv == 0)
-        put_rows<kWideWaves>(p, s_groups, good, line, block, blocks);
-    if (block >= line.blocks)
+        put_rows<DealT>(p, s_groups, good, line, block, blocks);
+    if (block >= (share > 0 ? uniform(s_groups.line[p.groups]) : line.blocks))
         return;
 
     const uint32_t tokens = 1u << a.log2_tokens;
@@ -676,22 +802,23 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
     const int my_step = my_part;  // of the values: 16 of the tile's tokens
     static_assert(W::kParts == 2, "a piece is half of a tile");
 
-    int32_t tile = line.begin(block);
-    const int32_t end = line.begin(block + 1);
-    int g = last_from(s_groups.tiles, p.groups, tile);
-    while (tile < end) {
-        while (s_groups.tiles[g + 1] <= tile)
+    int32_t at = share > 0 ? block : uniform(line.begin(block));
+    const int32_t end = share > 0 ? block + 1 : uniform(line.begin(block + 1));
+    int g = uniform(last_from(s_groups.line, p.groups, at));
+    while (at < end) {
+        while (uniform(s_groups.line[g + 1]) <= at)  // past groups without tiles
             ++g;
-        const Group grp = {s_groups.first[g], s_groups.rows[g], s_groups.length[g]};
-        const int32_t n_tiles = tiles_of(grp);
-        const int32_t in_group = tile - s_groups.tiles[g];
-        const int32_t at = in_group / n_tiles, skip = in_group % n_tiles;
-        const int32_t part = min(n_tiles - skip, end - tile);
-        const int32_t item = s_groups.items[g] + at;
-        const int32_t row0 = grp.first + at * p.item_rows;
+        const Group grp = {uniform(s_groups.first[g]), uniform(s_groups.rows[g]),
+                           uniform(s_groups.length[g])};
+        const Part now = next_part<DealT>(p, grp, uniform(s_groups.line[g]), share, at, end);
+        at = now.next;
+        const int32_t skip = now.skip, part = now.part;
+        const int32_t item = share > 0 ? 0 : uniform(s_groups.items[g]) + now.at;
+        const int32_t row0 = grp.first + now.at * p.item_rows;
         const int32_t n_rows = min(p.item_rows, grp.first + grp.rows - row0);
-        tile += part;
-        const int32_t lead = lead_of(p, grp, __builtin_amdgcn_readfirstlane(s_groups.lead[g]), lane);
+        if (part <= 0)
+            continue;
+        const int32_t lead = lead_of(p, grp, uniform(s_groups.lead[g]), lane);
         if (lead < 0)
             continue;
         const int32_t *__restrict__ table = tables + (int64_t)lead * a.table_cols;
@@ -823,7 +950,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         find(0);
         fetch(0);
         find(1);
-        const int n_waves = (min(n_rows, p.item_rows) * a.group_step + 31) / 32;  // with columns
+        const int n_waves = DealT::waves(p, n_rows);  // with columns
         const int teams = kWideWaves / n_waves;
         const int team = wave / n_waves, wc = wave - team * n_waves;
         const int32_t column = wc * 32 + col;
@@ -1135,26 +1262,24 @@ hipError_t launch(const SharedProblem &p, int blocks, int attn_blocks, hipStream
 {
     const int heads = p.attn.kv_heads * p.attn.head_groups;
     const dim3 grid((unsigned)(blocks * heads));
-    if (p.columns == 16) {
-        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1, 1>), grid, dim3(kThreads), 0, stream, p,
+    switch (p.kind) {
+    case SHARED_16:
+        hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 1>), grid, dim3(kThreads), 0, stream, p,
                            p.attn.table);
-    } else if (p.columns == 32) {
+        break;
+    case SHARED_32:
         if constexpr (attn_heads_a_pass(FP8, D) == 32)
-            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2, 1>), grid, dim3(kThreads), 0, stream,
+            hipLaunchKernelGGL((shared_kernel<TYPE, FP8, D, 2>), grid, dim3(kThreads), 0, stream,
                                p, p.attn.table);
         else
             return hipErrorInvalidValue;
-    } else {
-        if constexpr (D % 64 == 0) {
-            constexpr int waves = Wide<FP8, D>::kWaves;
-            const dim3 threads(64 * waves);
-            if (p.columns != 32 * waves)
-                return hipErrorInvalidValue;
-            hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D>), grid, threads, 0, stream, p,
-                               p.attn.table);
-        } else {
+        break;
+    default:
+        if constexpr (D % 64 == 0)
+            hipLaunchKernelGGL((shared_wide_kernel<TYPE, FP8, D>), grid,
+                               dim3(64 * Wide<FP8, D>::kWaves), 0, stream, p, p.attn.table);
+        else
             return hipErrorInvalidValue;
-        }
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
