@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "dps_attn.h"
+#include "dps_gemm_common.h"
 #include "dps_internal.h"
 
 namespace dps {
@@ -826,7 +827,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
 
         // ---- a piece of a stage: from memory, and into LDS as operands -----------------
         constexpr int kKeyLoads = FP8 ? W::kKeys / 2 : W::kKeys;
-        u32x4 key[kKeyLoads];
+        u32x4 key[FP8 ? kKeyLoads : 1];
         constexpr int kVal = (D / 32 * W::kElt + 3) / 4;
         uint32_t val[8][kVal];    // of eight tokens
         uint32_t live = 0;        // bits of the tile's tokens
@@ -838,7 +839,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
                 id[h] = table[min(min(t0 + 16 * h, hi - 1) >> a.log2_tokens, last_col)];
         };
         // N values a lane of eight tokens, into val from dword to on
-        const auto read_values = [&](auto width, const uint8_t *from, uint32_t place, int d0,
+        const auto fetch_values = [&](auto width, const uint8_t *from, uint32_t place, int d0,
                                      auto to) {
             constexpr int N = width;
             typedef typename Raw<N * W::kElt>::T T;
@@ -877,14 +878,18 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
 #pragma unroll
             for (int i = 0; i < kKeyLoads; ++i) {
                 const int s = my_part * kKeyLoads + i;  // 32 bytes of a token
-                key[i] = *reinterpret_cast<const u32x4 *>(from + (s >> 1) * tokens * 64 + (s & 1) * 32);
+                const uint8_t *at = from + (s >> 1) * tokens * 64 + (s & 1) * 32;
+                if (FP8)
+                    key[i] = *reinterpret_cast<const u32x4 *>(at);
+                else  // operands as they are
+                    dma16_at<AUX_CACHED>(at, (lds_u8 *)(s_op[stage & 1][my_tile] + s * 64));
             }
             const uint8_t *vals = my_step ? base[1] : base[0];
             const uint32_t vplace = my_step ? place[1] : place[0];
-            read_values(std::integral_constant<int, kFirst>(), vals, vplace, 0,
+            fetch_values(std::integral_constant<int, kFirst>(), vals, vplace, 0,
                         std::integral_constant<int, 0>());
             if constexpr (kFirst < kAcc)
-                read_values(std::integral_constant<int, 2>(), vals, vplace, 128,
+                fetch_values(std::integral_constant<int, 2>(), vals, vplace, 128,
                             std::integral_constant<int, W::kElt>());
         };
         // the values from dword d of val on, into output tiles e0 ...
@@ -918,16 +923,11 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
             u32x4 *to = s_op[stage & 1][my_tile] + lane;
             const int first = my_part * W::kKeys;
 #pragma unroll
-            for (int i = 0; i < W::kKeys; ++i) {
-                if (FP8) {
-                    const u32x4 k16 = key[i >> 1];
-                    const uint32_t c0 = i & 1 ? k16.z : k16.x, c1 = i & 1 ? k16.w : k16.y;
-                    to[(first + i) * 64] =
-                        u32x4{wide2<TYPE, false>(c0), wide2<TYPE, true>(c0),
-                              wide2<TYPE, false>(c1), wide2<TYPE, true>(c1)};
-                } else {
-                    to[(first + i) * 64] = key[i];
-                }
+            for (int i = 0; FP8 && i < W::kKeys; ++i) {
+                const u32x4 k16 = key[i >> 1];
+                const uint32_t c0 = i & 1 ? k16.z : k16.x, c1 = i & 1 ? k16.w : k16.y;
+                to[(first + i) * 64] = u32x4{wide2<TYPE, false>(c0), wide2<TYPE, true>(c0),
+                                             wide2<TYPE, false>(c1), wide2<TYPE, true>(c1)};
             }
             if (my_part == 0 && lane == 0)
                 s_live[stage & 1][my_tile] = live;
@@ -948,6 +948,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
 
         // ---- query fragments ------------------------------------------------------
         find(0);
+        __syncthreads();  // the item before has been joined, in the memory of the stages
         fetch(0);
         find(1);
         const int n_waves = DealT::waves(p, n_rows);  // with columns
@@ -978,20 +979,34 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         }
 
         bool far = false;  // a reference score so large that products are rounded first
-        const auto take = [&](const u32x4 *op, uint32_t there) {
+        // operands on their way under the softmax: values, and the next tile's keys, as far
+        // as registers go; the others wait for LDS where they are due
+        constexpr bool kEarly = D <= 128, kEarlyKeys = D * (FP8 ? 2 : 1) <= 128;
+        u32x4 k[kFrags];
+        const auto read_keys = [&](const u32x4 *op) {
+#pragma unroll
+            for (int s = 0; s < kFrags; ++s)
+                k[s] = op[s * 64];
+        };
+        // a tile; `next`: the one after it
+        const auto take = [&](const u32x4 *op, uint32_t there, const u32x4 *next) {
             f32x16 scores;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 scores[i] = 0.0f;
 #pragma unroll
             for (int s = 0; s < kFrags; ++s)
-                scores = mfma16<TYPE>(op[s * 64], q[s], scores);
-            constexpr bool kEarly = D <= 128;  // values on their way under the softmax
-            u32x4 v[kFrags];
-            if (kEarly) {
+                scores = mfma16<TYPE>(kEarlyKeys ? k[s] : op[s * 64], q[s], scores);
+            u32x4 v[kAcc];
+            const auto read_values = [&](int u) {
 #pragma unroll
-                for (int i = 0; i < kFrags; ++i)
-                    v[i] = op[(kFrags + i) * 64];
+                for (int i = 0; i < kAcc; ++i)
+                    v[i] = op[(kFrags + 2 * i + u) * 64];
+            };
+            if (kEarly) {
+                read_values(0);
+                if (kEarlyKeys)
+                    read_keys(next);
                 __builtin_amdgcn_sched_barrier(0);
             }
             float x[16];
@@ -1045,42 +1060,47 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
             sum += x[0];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                if (!kEarly) {
+                if (!kEarly || u > 0) {
                     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int i = 0; i < kAcc; ++i)
-                        v[2 * i + u] = op[(kFrags + 2 * i + u) * 64];
+                    read_values(u);
                 }
 #pragma unroll
                 for (int i = 0; i < kAcc; ++i)
-                    acc[i] = mfma16<TYPE>(v[2 * i + u], p_hi[u], acc[i]);
+                    acc[i] = mfma16<TYPE>(v[i], p_hi[u], acc[i]);
 #pragma unroll
                 for (int i = 0; i < kAcc; ++i)
-                    acc[i] = mfma16<TYPE>(v[2 * i + u], p_lo[u], acc[i]);
+                    acc[i] = mfma16<TYPE>(v[i], p_lo[u], acc[i]);
             }
+        };
+        // what this wave has put into LDS, its direct loads among it, is there
+        const auto meet = [&] {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
         };
 
         const int32_t stages = (part + ST - 1) / ST;
-        __syncthreads();  // the item before has been joined
         stash(0);
-        __syncthreads();
+        meet();
         for (int32_t stage = 0; stage < stages; ++stage) {
             fetch(stage + 1);  // past the part: nothing
             find(stage + 2);
             const auto op = s_op[stage & 1];
             const int here = active ? min(ST, part - stage * ST) : 0;  // tiles of the stage
             bool stashed = false;
+            if (kEarlyKeys && team < here)
+                read_keys(op[team] + lane);
 #pragma unroll 1
             for (int i = team; i < here; i += teams) {
                 if (i >= ST / 2 && !stashed) {  // the loads have had half of the stage
                     stash(stage + 1);
                     stashed = true;
                 }
-                take(op[i] + lane, __builtin_amdgcn_readfirstlane(s_live[stage & 1][i]));
+                take(op[i] + lane, uniform((int32_t)s_live[stage & 1][i]),
+                     op[i + teams < here ? i + teams : i] + lane);
             }
             if (!stashed)
                 stash(stage + 1);
-            __syncthreads();
+            meet();
         }
 
         // ---- the block's partial of the item -----------------------------------------
