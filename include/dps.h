@@ -512,8 +512,8 @@ dps_status dps_kv_copy(const dps_kv_cache *cache, const int32_t *src, const int3
 dps_status dps_kv_remap(int32_t *table, int64_t entries, const int32_t *src, const int32_t *dst,
                         int64_t n, void *stream);
 
-/* Workspace bytes of dps_attn_shared on the current device (0 for sizes it refuses).
- * Contents on entry do not matter. */
+/* Workspace bytes of a dps_attn_shared call of these sizes on the current device (0 for
+ * sizes it refuses; not always more for more rows).  Contents on entry do not matter. */
 size_t dps_attn_shared_workspace_bytes(int64_t rows, int64_t groups, int64_t heads,
                                        int64_t kv_heads, int64_t head_dim);
 
@@ -554,7 +554,8 @@ typedef struct {
     uint8_t *new_done;      /* [batch][keep] 1: it ends with that token, or had ended   */
 } dps_beam_args;
 
-/* Workspace bytes of dps_beam_select (0 for arguments it refuses). */
+/* Workspace bytes of a dps_beam_select call of these sizes on the current device (0 for
+ * sizes it refuses; not always more for larger ones).  Contents on entry do not matter. */
 size_t dps_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t vocab, int64_t keep);
 
 /* The next beams of each request: token t after beam w scores score_w + x_wt -

@@ -163,7 +163,11 @@ class PagedBatch:
         for the units that became free.  Waits for the steps before, as grow() does, and
         for the copies."""
         self._mapped()
-        host = parents.tolist() if torch.is_tensor(parents) else list(parents)
+        given = torch.is_tensor(parents)
+        if given and not (parents.dtype == torch.int32 and parents.device == self.table.device and
+                          parents.is_contiguous() and parents.dim() == 1):
+            raise ValueError("parents must be a list, or a contiguous int32 tensor beside the table")
+        host = parents.tolist() if given else list(parents)
         if len(host) != len(self.lengths) or max(host) >= len(host):
             raise ValueError("one parent a slot, a slot or -1")
         copied, seen = [], set()
@@ -174,7 +178,7 @@ class PagedBatch:
         taken = self.sums.alloc(len(copied))
         if taken is None:
             return False
-        if not torch.is_tensor(parents):
+        if not given:
             parents = torch.tensor(host, dtype=torch.int32, device=self.table.device)
         here = self._after_steps()
         i32 = dict(dtype=torch.int32, device=self.table.device)

@@ -896,8 +896,8 @@ def kv_remap(table, src, dst):
 
 
 def attn_shared_workspace_bytes(cache, rows, heads, groups):
-    """Workspace of attn_shared for up to `rows` rows of `heads` query heads in exactly
-    `groups` groups."""
+    """Workspace of attn_shared for `rows` rows of `heads` query heads in `groups` groups
+    (whoever calls with several sizes takes the largest of theirs)."""
     lib = _lib or load_library()
     return lib.dps_attn_shared_workspace_bytes(rows, groups, heads, cache.kv_heads, cache.head_dim)
 

@@ -165,6 +165,12 @@ def test_refusals():
             batch.fork([0, 0], [shared.cache])
         with pytest.raises(ValueError):
             batch.fork([0, 3, 1], [shared.cache])
+        for bad in (torch.int64, torch.float32):
+            with pytest.raises(ValueError):
+                batch.fork(torch.zeros(3, dtype=bad, device=DEV), [shared.cache])
+        with pytest.raises(ValueError):
+            batch.fork(torch.zeros(3, dtype=torch.int32), [shared.cache])
+        assert sum(shared.sums.counts()[n] for n in ("avail", "full")) == 0   # nothing taken
         assert batch.grow([1, 0, 0])
         with pytest.raises(RuntimeError):
             batch.fork([0, 0, 0], [shared.cache])
