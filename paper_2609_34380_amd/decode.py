@@ -227,6 +227,7 @@ class PagedBatch:
         worker copies on a stream of its own."""
         mine = self.blocks[slot]
         self.blocks[slot], self.lengths[slot] = [], 0
+        self._group_key = None              # the slot's next request shares nothing
         if self._forks:
             others = {b for blocks in self.blocks for b in blocks}
             mine = [b for b in mine if b not in others]

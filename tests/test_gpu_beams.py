@@ -124,6 +124,38 @@ def test_random_life(seed):
         shared.close()
 
 
+def test_another_request_in_a_slot_of_a_group():
+    """A slot that shared a prefix ends; the request that comes after it grows past that
+    prefix's length with the same slots in every step."""
+    shared = decode.SharedLayer(units=4, batch=3, groups=2)
+    try:
+        batch, ref = shared.batch, Layer64(shared, 3)
+        gen = torch.Generator().manual_seed(11)
+
+        def step(active):
+            x = torch.zeros(3, 1024, dtype=torch.float16)
+            x[:len(active)] = torch.randn(len(active), 1024, generator=gen).to(torch.float16)
+            y = shared.decode(x.to(DEV), [1 if r in active else 0 for r in range(3)])
+            close(y[:len(active)], ref.step(x[:len(active)], active, shared.sums.mode))
+
+        for _ in range(35):
+            step([0])
+        assert batch.fork([0, 0, 0], [shared.cache])
+        fork_ref(ref, [0, 0, 0])
+        step([0, 1, 2])
+        assert batch.shared_len.tolist() == [32, 0]
+        for slot in (1, 0):
+            torch.cuda.synchronize()
+            batch.end(slot)
+            ref.k[slot], ref.v[slot] = [], []
+            for _ in range(40):
+                step([0, 1, 2])
+            assert batch.shared_len.tolist() == [0, 0]
+            check_blocks(batch)
+    finally:
+        shared.close()
+
+
 def test_compaction_brings_full_mode_back():
     """Blocks of slots that live on are scattered over the units that evicted residuals
     wait for; together they leave one free, and the outputs stay what they were."""
