@@ -520,10 +520,10 @@ size_t dps_attn_shared_workspace_bytes(int64_t rows, int64_t groups, int64_t hea
 /* dps_attn_decode of rows that share prefixes: rows group_start[g] ..
  * group_start[g + 1] - 1 have their first shared_len[g] tokens in common (in the same
  * blocks, or in copies of them), which are read once for all of them, through the
- * table row of the first that has them all.  A row that is shorter than that (an idle one), has no table
- * row, or is in no group attends its tokens through its own table row alone, as do
- * all rows where group_start does not ascend within 0 .. rows and those of a
- * group whose shared_len is past the table's columns.  Each row's result is
+ * table row of the first that has them all.  A row that is shorter than that (an idle
+ * one), has no table row, or is in no group attends its tokens through its own table
+ * row alone, as do all rows where group_start does not ascend within 0 .. rows and
+ * those of a group whose shared_len is past the table's columns.  Each row's result is
  * dps_attn_decode's but for the order of sums; args->window is 0.
  *   group_start  device int32[groups + 1].
  *   shared_len   device int32[groups], groups 0..1024; any length (a block and a tile

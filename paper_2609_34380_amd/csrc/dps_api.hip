@@ -1081,7 +1081,8 @@ DPS_EXPORT dps_status dps_kv_fork(const int32_t *parent, const int32_t *seq_len,
     REQUIRE(out != nullptr, DPS_ERR_INVALID_ARG, "output descriptor is NULL");
     REQUIRE(out->rows >= 0 && old_rows >= 0 && table_cols >= 0 && n_fresh >= 0 &&
                 out->n_freed >= 0 && n_blocks >= 0,
-            DPS_ERR_INVALID_ARG, "rows, old_rows, table_cols, n_fresh, n_freed or n_blocks is negative");
+            DPS_ERR_INVALID_ARG,
+            "rows, old_rows, table_cols, n_fresh, n_freed or n_blocks is negative");
     REQUIRE(out->rows <= 4096 && old_rows <= 4096, DPS_ERR_UNSUPPORTED,
             "more than 4096 rows in one call");
     REQUIRE(block_tokens >= 16 && block_tokens <= 256 && (block_tokens & (block_tokens - 1)) == 0,
@@ -1397,13 +1398,13 @@ DPS_EXPORT dps_status dps_attn_shared(const dps_attn_args *a, const dps_kv_cache
     const SharedPlan plan =
         plan_shared(a->rows, groups, a->heads, cache->kv_heads, cache->head_dim, fp8);
     const int64_t lines = (int64_t)cache->kv_heads * attn.groups;
-    // a launch counts its threads (256 a row and key/value head) in 32 bits, and a
-    // key/value head its partials
-    // (a tile counts up to eight times on the line)
+    // a launch counts its threads (256 a row and key/value head) in 32 bits, a key/value
+    // head its partials, and its line the tiles, each up to eight times
     const int64_t room = a->table_cols > 0x7fffffff / cache->block_tokens
                              ? 0x7fffffff
                              : a->table_cols * cache->block_tokens;
-    REQUIRE(a->rows <= 0x7fffffff / 8 / (room / 32 + 2) && a->rows * lines < (1 << 24) && plan.slots * plan.columns <= 0x7fffffff,
+    REQUIRE(a->rows <= 0x7fffffff / 8 / (room / 32 + 2) && a->rows * lines < (1 << 24) &&
+                plan.slots * plan.columns <= 0x7fffffff,
             DPS_ERR_UNSUPPORTED, "too many rows for one call");
     REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,
             "workspace is smaller than dps_attn_shared_workspace_bytes()");

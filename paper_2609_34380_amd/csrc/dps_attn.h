@@ -95,6 +95,8 @@ template <>
 struct Piece<8> { typedef u32x2 T; };
 template <>
 struct Piece<4> { typedef uint32_t T; };
+template <>
+struct Piece<2> { typedef uint16_t T; };
 
 // Bytes streamed once: loaded past the caches' retention.
 template <typename T>

@@ -206,7 +206,8 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const BeamProblem p
     if ((p.done && p.done[row]) || !(__builtin_fabsf(cum) < kInf))
         return;
     const uint8_t *first = p.logits + row * p.row_bytes;
-    const int skew = (int)((uintptr_t)first & 15) / kElt;  // elements before the row in its first vector
+    // elements before the row in its first vector
+    const int skew = (int)((uintptr_t)first & 15) / kElt;
     const uint8_t *base = first - skew * kElt;
     const int32_t vocab = p.vocab;
     const int32_t at0 = piece * kPiece - skew;  // index of the piece's first element
@@ -456,7 +457,8 @@ __global__ __launch_bounds__(kThreads) void beam_pick_kernel(const BeamProblem p
         for (int d = per / 2; d > 0; d >>= 1)
             sum += __shfl_xor(sum, d);
         if (tid % per == 0)
-            s_beam[w] = Beam{counts ? top + log(sum) : finite ? 0.0 : __builtin_nan(""), cum, ended};
+            s_beam[w] = Beam{counts ? top + log(sum) : finite ? 0.0 : __builtin_nan(""), cum,
+                             ended};
     }
     __syncthreads();
 

@@ -117,8 +117,8 @@ __global__ __launch_bounds__(kThreads) void kv_remap_kernel(int32_t *__restrict_
 // call with 2000 rows of 1300 columns).
 //
 // Bound: latency, and 4 bytes in and out a table entry.  Three launches (one for small
-// tables), each of which needs all of the one before: who copies (and cleared bytes), tables and bytes, the
-// list of freed blocks.
+// tables), each of which needs all of the one before: who copies (and cleared bytes),
+// tables and bytes, the list of freed blocks.
 
 __device__ __forceinline__ bool in_range(int32_t x, int32_t n) { return x >= 0 && x < n; }
 
@@ -322,8 +322,11 @@ __global__ __launch_bounds__(kThreads) void kv_fork_tables_kernel(const KvForkPr
             held[block[i]] = 1;
 }
 
-// A block of threads lists the freed blocks of its 16-byte words, after those of all
-// words before, which it counts itself.
+// A block of threads lists the freed blocks of its share of the 16-byte words, kPlanThreads
+// at a time, after those of all words before, which it counts itself: 16 bytes a block of
+// either side, read by at most kListers blocks.
+constexpr int64_t kListers = 256;
+
 __device__ __forceinline__ u32x4 freed_of(const KvForkProblem &p, int64_t w)
 {
     return p.held[w] & ~p.held[p.words + w];
@@ -333,47 +336,61 @@ __device__ __forceinline__ int count(u32x4 x)
     return __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w);
 }
 
-__global__ __launch_bounds__(kPlanThreads) void kv_fork_freed_kernel(const KvForkProblem p)
+__global__ __launch_bounds__(kPlanThreads) void kv_fork_freed_kernel(const KvForkProblem p,
+                                                                     int64_t share)
 {
     __shared__ int32_t s_before[kPlanThreads / 64], s_after[kPlanThreads / 64],
         s_sums[kPlanThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t w0 = (int64_t)blockIdx.x * kPlanThreads, mine = w0 + tid;
-    int32_t before = 0, after = 0;
+    const int64_t w0 = (int64_t)blockIdx.x * share, w1 = min(w0 + share, p.words);
+    int32_t before = 0, after = 0;  // of the words before its share, and of the others
 #pragma unroll 4
     for (int64_t w = tid; w < w0; w += kPlanThreads)
         before += count(freed_of(p, w));
     u32x4 freed = {0u, 0u, 0u, 0u};
-    if (mine < p.words)
-        freed = freed_of(p, mine);
+    if (w0 + tid < w1)
+        freed = freed_of(p, w0 + tid);
 #pragma unroll 4
-    for (int64_t w = mine + kPlanThreads; w < p.words; w += kPlanThreads)
+    for (int64_t w = w0 + tid + kPlanThreads; w < p.words; w += kPlanThreads)
         after += count(freed_of(p, w));
-    const int32_t n = count(freed);
-    const int32_t incl = wave_scan(n), incl_before = wave_scan(before),
-                  incl_after = wave_scan(after);
+    const int32_t incl_before = wave_scan(before), incl_after = wave_scan(after + count(freed));
     if (lane == 63) {
-        s_sums[wave] = incl;
         s_before[wave] = incl_before;
         s_after[wave] = incl_after;
     }
     __syncthreads();
-    int32_t at = incl - n, all = 0;
+    int32_t base = 0, all = 0;
     for (int i = 0; i < kPlanThreads / 64; ++i) {
-        at += s_before[i] + (i < wave ? s_sums[i] : 0);
-        all += s_before[i] + s_sums[i] + s_after[i];
+        base += s_before[i];
+        all += s_before[i] + s_after[i];
     }
-    if (n > 0) {
+    for (int64_t w = w0; w < w1; w += kPlanThreads) {
+        const int64_t mine = w + tid;
+        if (w > w0)
+            freed = mine < w1 ? freed_of(p, mine) : u32x4{0u, 0u, 0u, 0u};
+        const int32_t n = count(freed), incl = wave_scan(n);
+        __syncthreads();  // the sums before have been read
+        if (lane == 63)
+            s_sums[wave] = incl;
+        __syncthreads();
+        int32_t at = base + incl - n;
+        for (int i = 0; i < kPlanThreads / 64; ++i) {
+            at += i < wave ? s_sums[i] : 0;
+            base += s_sums[i];
+        }
+        if (n > 0) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if ((freed[i >> 2] >> (i & 3) * 8) & 1) {
-                if (at < p.n_freed)
-                    p.freed[at] = (int32_t)(mine * 16) + i;
-                ++at;
+            for (int i = 0; i < 16; ++i) {
+                if ((freed[i >> 2] >> (i & 3) * 8) & 1) {
+                    if (at < p.n_freed)
+                        p.freed[at] = (int32_t)(mine * 16) + i;
+                    ++at;
+                }
             }
         }
     }
-    for (int64_t i = all + mine; i < p.n_freed; i += (int64_t)gridDim.x * kPlanThreads)
+    for (int64_t i = all + (int64_t)blockIdx.x * kPlanThreads + tid; i < p.n_freed;
+         i += (int64_t)gridDim.x * kPlanThreads)
         p.freed[i] = -1;
     if (blockIdx.x == 0 && tid == 0)
         p.counts[1] = all;
@@ -432,9 +449,11 @@ hipError_t launch_kv_fork(const KvForkProblem &p, hipStream_t stream)
         if (e != hipSuccess)
             return e;
     }
-    const int64_t lists = (p.words + kPlanThreads - 1) / kPlanThreads;
-    hipLaunchKernelGGL(kv_fork_freed_kernel, dim3((unsigned)(lists < 1 ? 1 : lists)),
-                       dim3(kPlanThreads), 0, stream, p);
+    int64_t share = (p.words + kListers - 1) / kListers;
+    share = (share + kPlanThreads - 1) / kPlanThreads * kPlanThreads;
+    const int64_t lists = share > 0 ? (p.words + share - 1) / share : 1;
+    hipLaunchKernelGGL(kv_fork_freed_kernel, dim3((unsigned)lists), dim3(kPlanThreads), 0, stream,
+                       p, share);
     return hipGetLastError();
 }
 

@@ -17,9 +17,10 @@
 // an item, or of two items that share a block, no two slots are the same).  A block's
 // waves have different tokens, and join in LDS.  shared_wide_kernel takes more columns at a
 // time: as many of its waves as the item needs have columns of their own, and teams of them
-// different tokens.  Where groups are few, there every item gets whole blocks of its own instead, as many as make the longest
-// range shortest: a block that begins and ends an item twice loses 6 to 10 us (240 rows of
-// 64 heads under 16384 tokens 250 us on the line, 230 so).
+// different tokens.  Where groups are few, there every item gets whole blocks of its own
+// instead, as many as make the longest range shortest: a block that begins and ends an item
+// twice loses 6 to 10 us (240 rows of 64 heads under 16384 tokens: 250 us on the line, 230
+// so).
 //
 // The tile is attn_kernel's: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix
 // instructions, 32 tokens at a time, HT column tiles of 16 a wave; keys and values go
@@ -140,7 +141,10 @@ struct Items {
         return count > 0 ? (count - 1) * blocks(full, share) + blocks(last, share) : 0;
     }
     __device__ __forceinline__ int32_t begin(int32_t i) const { return i * full * tiles; }
-    __device__ __forceinline__ int32_t weight(int32_t i) const { return i < count - 1 ? full : last; }
+    __device__ __forceinline__ int32_t weight(int32_t i) const
+    {
+        return i < count - 1 ? full : last;
+    }
     __device__ __forceinline__ int32_t length() const
     {
         return count > 0 ? begin(count - 1) + last * tiles : 0;
@@ -750,17 +754,6 @@ __device__ __forceinline__ float over_halves(float x, const F &f)
     return f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
 }
 
-template <int BYTES>
-struct Raw;
-template <>
-struct Raw<16> { typedef u32x4 T; };
-template <>
-struct Raw<8> { typedef u32x2 T; };
-template <>
-struct Raw<4> { typedef uint32_t T; };
-template <>
-struct Raw<2> { typedef uint16_t T; };
-
 template <int TYPE, bool FP8, int D>
 __global__ __launch_bounds__((64 * Wide<FP8, D>::kWaves), (Wide<FP8, D>::kWaves / 4)) void
 shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
@@ -842,7 +835,7 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         const auto fetch_values = [&](auto width, const uint8_t *from, uint32_t place, int d0,
                                      auto to) {
             constexpr int N = width;
-            typedef typename Raw<N * W::kElt>::T T;
+            typedef typename Piece<N * W::kElt>::T T;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t t = place + 8 * (j >> 2) + 4 * hf + (j & 3);
@@ -956,7 +949,8 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         const int team = wave / n_waves, wc = wave - team * n_waves;
         const int32_t column = wc * 32 + col;
         const bool active = team < teams;
-        const bool used = active && column / a.group_step < n_rows && column % a.group_step < n_heads;
+        const bool used =
+            active && column / a.group_step < n_rows && column % a.group_step < n_heads;
         u32x4 q[kFrags];
         f32x16 acc[kAcc];
         float ref = kNone, sum = 0.0f;

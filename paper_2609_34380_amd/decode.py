@@ -154,6 +154,13 @@ class PagedBatch:
         return dps.kv_map(self.ctx_len, self.new_len, self.fresh, self.table, self.block_tokens,
                           out=self.step)
 
+    def _ours(self, caches):
+        """Every block that the manager hands out has to be one of each cache's."""
+        blocks = self.sums.n_units * self.sums.blocks_per_unit
+        for cache in caches:
+            if cache.block_tokens != self.block_tokens or cache.n_blocks < blocks:
+                raise ValueError("a cache has other blocks than the batch")
+
     def fork(self, parents, caches):
         """Slot r goes on from slot parents[r] (an int32 device tensor, or a list; -1: the
         slot is empty from now on), for all slots at once: shared whole blocks, and a copy
@@ -163,6 +170,7 @@ class PagedBatch:
         for the units that became free.  Waits for the steps before, as grow() does, and
         for the copies."""
         self._mapped()
+        self._ours(caches)
         given = torch.is_tensor(parents)
         if given and not (parents.dtype == torch.int32 and parents.device == self.table.device and
                           parents.is_contiguous() and parents.dim() == 1):
@@ -206,6 +214,7 @@ class PagedBatch:
         `caches`, so that units become free: True when residuals wait for them.  Waits for
         the steps before and for the moves."""
         self._mapped()
+        self._ours(caches)
         src, dst = self.sums.compact(max_moves)
         if not src:
             return False

@@ -806,6 +806,7 @@ class KvFork(collections.namedtuple("KvFork", "table seq_len src dst tokens free
             made = self._made = _pack_forked(
                 rows, *[t.data_ptr() for t in self[:6]], self.freed.shape[0],
                 self.counts.data_ptr())
+        _here("out", self.table)
         return made
 
 
@@ -970,6 +971,7 @@ class BeamStep(collections.namedtuple("BeamStep", "score parent token done")):
                          "%s must be a contiguous %s device tensor of %s" % (name, dtype, shape))
                 _here(name, t)
             self._shape = shape
+        _here("out", self.score)
         return self
 
 

@@ -202,6 +202,12 @@ def test_refusals():
                 batch.fork(torch.zeros(3, dtype=bad, device=DEV), [shared.cache])
         with pytest.raises(ValueError):
             batch.fork(torch.zeros(3, dtype=torch.int32), [shared.cache])
+        pool = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+        for tokens in (shared.TOKENS, 2 * shared.TOKENS):    # too few blocks, others
+            cache = dps.KvCache(pool, tokens, 8, 128, torch.float16)
+            for call in (lambda: batch.fork([0, 0, 0], [cache]), lambda: batch.compact([cache])):
+                with pytest.raises(ValueError):
+                    call()
         assert sum(shared.sums.counts()[n] for n in ("avail", "full")) == 0   # nothing taken
         assert batch.grow([1, 0, 0])
         with pytest.raises(RuntimeError):

@@ -115,6 +115,17 @@ def test_fork_many_blocks():
     run_fork(np.arange(40) // 2, np.full(40, 15990), table, ids[40000:40100], 16, 200000)
 
 
+def test_fork_more_blocks_than_one_turn():
+    """Ids of 5 million blocks, beyond what the listing kernel's blocks take at once; freed
+    ones in every part of them, and no room for the last."""
+    rng = np.random.default_rng(6)
+    ids = rng.choice(5000000, 40100, replace=False)
+    ids[:3] = 0, 4999999, 4999984
+    table = ids[:40000].reshape(40, 1000)
+    run_fork(np.arange(40) // 2, np.full(40, 15990), table, ids[40000:], 16, 5000000, 30000)
+    run_fork(np.arange(40) // 2, np.full(40, 15990), table, ids[40000:], 16, 5000000, 19000)
+
+
 # ---- copies and moves ---------------------------------------------------------------
 
 COPIES = [
