@@ -826,10 +826,12 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
         uint32_t live = 0;        // bits of the tile's tokens
         int32_t id[2];
         const auto find = [&](int32_t stage) {  // block ids, one stage ahead of their use
-            const int32_t t0 = (skip + stage * ST + my_tile) * kTile;
+            // past the longest prefix no signed number holds it
+            const uint32_t t0 = (uint32_t)(skip + stage * ST + my_tile) * kTile;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                id[h] = table[min(min(t0 + 16 * h, hi - 1) >> a.log2_tokens, last_col)];
+                id[h] = table[min((int32_t)(min(t0 + 16 * h, (uint32_t)hi - 1) >> a.log2_tokens),
+                                  last_col)];
         };
         // N values a lane of eight tokens, into val from dword to on
         const auto fetch_values = [&](auto width, const uint8_t *from, uint32_t place, int d0,

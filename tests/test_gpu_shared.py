@@ -347,3 +347,26 @@ def test_empty_and_refused_calls():
     with pytest.raises(dps.DpsError):
         dps.attn_shared(q, cache, table, lens, starts, shared,
                         workspace=torch.empty(64, dtype=torch.uint8, device=DEV))
+
+
+def test_longest_prefix():
+    """Two rows of 32 heads under 2^31 - 256 tokens, all of them in one block: a token counts
+    as often as the block is named.  Sums grow over up to 2^16 tiles, each of which rounds
+    them (and what the matrix cores hold, 4 times) to 2^-24 of themselves."""
+    tokens, dim, cols = 256, 64, 2 ** 23 - 1
+    c = Cache(1, tokens, 1, dim, E4M3, 0.05, 0.02)
+    k, v = rnd(tokens, 1, dim, seed=1), 1 + 0.5 * rnd(tokens, 1, dim, seed=2)
+    c.place(torch.arange(tokens), k / 0.05, v / 0.02)
+    q = rnd(2, 32, dim, seed=3).to(F16)
+    one = torch.zeros(1, dtype=torch.int32)
+    want, lse64 = attn_oracle(q, c, one[:, None], torch.tensor([tokens] * 2), torch.zeros(2).int(),
+                              dim ** -0.5, 0)[:2]
+    table = torch.zeros((1, cols), dtype=torch.int32, device=DEV)
+    n = i32([cols * tokens]).to(DEV)
+    lse = torch.empty((2, 32), device=DEV)
+    got = dps.attn_shared(q.to(DEV), c.up(), table, n.repeat(2), i32([0, 2]).to(DEV), n,
+                          req=torch.zeros(2, dtype=torch.int32, device=DEV), lse=lse)
+    step = 2.0 ** 16 * 2.0 ** -24
+    err = (got.cpu().double() - want.double().reshape(got.shape)).abs().max()
+    assert err <= 5 * step * float(v.abs().max()) + 2.0 ** -10, err
+    assert float((lse.cpu().double() - lse64.reshape(2, 32) - math.log(cols)).abs().max()) <= 2 * step
