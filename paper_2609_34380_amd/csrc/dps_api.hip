@@ -1213,12 +1213,14 @@ struct BeamPlan {
     size_t bytes() const { return 2 * value_bytes + sum_bytes; }
 };
 
-BeamPlan plan_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t keep, int type)
+// skewed: some rows begin inside a 16-byte vector.
+BeamPlan plan_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t keep, int type,
+                   bool skewed)
 {
     BeamPlan b;
     const int64_t rows = batch * beams;
-    // a row may begin inside its first vector
-    const int64_t span = vocab + (type == DPS_BEAM_F32 ? 3 : 7);
+    // a whole number of pieces is one more where a row begins inside its first vector
+    const int64_t span = vocab + (!skewed ? 0 : type == DPS_BEAM_F32 ? 3 : 7);
     b.vecs = dps::kBeamVecs;
     if (rows * cdiv(span, dps::beam_piece(type, b.vecs)) < 2 * current_cu_count())
         b.vecs = dps::kBeamFewVecs;
@@ -1243,10 +1245,15 @@ DPS_EXPORT size_t dps_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t
 {
     if (!beam_sizes(batch, beams, vocab, keep) || batch == 0)
         return 0;
-    // the type of the logits is not known here: room for either size
-    const size_t wide = plan_beam(batch, beams, vocab, keep, DPS_BEAM_F32).bytes();
-    const size_t half = plan_beam(batch, beams, vocab, keep, DPS_BEAM_F16).bytes();
-    return wide > half ? wide : half;
+    // the type of the logits, and where they lie, are not known here: room for all
+    size_t most = 0;
+    for (const int type : {DPS_BEAM_F32, DPS_BEAM_F16}) {
+        for (const bool skewed : {false, true}) {
+            const size_t need = plan_beam(batch, beams, vocab, keep, type, skewed).bytes();
+            most = need > most ? need : most;
+        }
+    }
+    return most;
 }
 
 DPS_EXPORT dps_status dps_beam_select(const dps_beam_args *a, void *ws, size_t ws_bytes,
@@ -1288,7 +1295,8 @@ DPS_EXPORT dps_status dps_beam_select(const dps_beam_args *a, void *ws, size_t w
         for (const auto &y : in)
             REQUIRE(!overlap(x.at, x.bytes, y.at, y.bytes), DPS_ERR_INVALID_ARG,
                     "an output overlaps an input");
-    const BeamPlan plan = plan_beam(a->batch, a->beams, a->vocab, a->keep, a->type);
+    const bool skewed = !aligned(a->logits, 16) || (rows > 1 && a->logits_stride * elt % 16 != 0);
+    const BeamPlan plan = plan_beam(a->batch, a->beams, a->vocab, a->keep, a->type, skewed);
     // a launch counts its threads (256 a piece) in 32 bits
     REQUIRE(plan.lists < (1 << 24), DPS_ERR_UNSUPPORTED, "too many rows for one call");
     REQUIRE(ws != nullptr && ws_bytes >= plan.bytes(), DPS_ERR_WORKSPACE,

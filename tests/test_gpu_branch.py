@@ -329,6 +329,7 @@ BEAMS = [
     (2, 8, 16384, 8, F16), (1, 5, 16385, 10, F16), (7, 4, 32000, 8, BF16), (1, 40, 8191, 80, F16),
     (40, 8, 10007, 16, BF16), (64, 8, 20001, 8, F16), (64, 16, 9000, 9, F32), (3, 33, 5000, 256, F16),
     (1, 1, 70000, 256, F32), (300, 2, 515, 4, F16), (1, 1024, 90, 30, F32), (2, 6, 262144, 12, BF16),
+    (2, 8, 32768, 16, F16), (1, 16, 32768, 200, BF16), (3, 64, 4096, 40, F16),
 ]
 
 
