@@ -242,16 +242,25 @@ struct SharedProblem {
 };
 constexpr int kSharedGroups = 1024;
 // The kernel, by the columns of a group of average size.  16 and 32: tokens from memory to
-// registers, a block's waves on different ones, which keeps the most loads in flight (8
-// FP8 prefixes of 9000 tokens 42 us, through LDS 58; 5 BF16 ones of 2000 17 / 25).  Wide:
-// through LDS, 32 columns a wave, eight waves (four for heads over 128), where passes of
-// 32 columns would each read the tokens.
+// registers, a block's waves on different ones, which keeps the most loads in flight; a
+// group of more columns is read once an item, mostly from the caches.  Wide: through LDS, 32
+// columns a wave, eight waves (four for heads over 128): one read, at 20 us for its start
+// and end.  Whole calls, registers / wide: 45 columns of 5 BF16 prefixes of 3000 tokens 32 /
+// 41 us, 64 of 16 FP16 ones of 16384 266 / 296 and of 3000 84 / 103, 128 of 4 119 / 100 and
+// (of 4000) 59 / 68; 64 of 16 E4M3 ones of 12000 116 / 190, 128 of 8 93 / 115, 256 of 4 99 /
+// 104.
+// With at most kSharedAligned groups the items' blocks have the same ranges of tokens at the
+// same time: 192 columns of one FP16 prefix of 16384 tokens 58 / 66 us, of 3000 33 / 46, of
+// 60000 133 / 120; 256 of one E4M3 prefix of 12000 46 / 56.  Heads of 192 and 256 values in 16
+// bits, 16 columns an item: 48 columns 64 / 64 and 36 / 41, 96 91 / 89.
 enum { SHARED_16 = 0, SHARED_32 = 1, SHARED_WIDE = 2 };
+constexpr int kSharedAligned = 2;
 constexpr int shared_kind(int64_t rows, int64_t groups, int step, bool fp8, int dim)
 {
     const int64_t mean = rows * step / (groups < 1 ? 1 : groups);
     const bool two = attn_heads_a_pass(fp8, dim) == 32;
-    if (dim % 64 == 0 && mean > (two ? 32 : 16))
+    const int most = groups <= kSharedAligned ? (fp8 ? 8 : two ? 6 : 3) : fp8 ? 4 : 2;  // items
+    if (dim % 64 == 0 && mean > most * (two ? 32 : 16))
         return SHARED_WIDE;
     return two && (step > 16 || mean > 16) ? SHARED_32 : SHARED_16;
 }

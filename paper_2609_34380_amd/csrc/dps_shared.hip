@@ -20,7 +20,9 @@
 // different tokens.  Where groups are few, there every item gets whole blocks of its own
 // instead, as many as make the longest range shortest: a block that begins and ends an item
 // twice loses 6 to 10 us (240 rows of 64 heads under 16384 tokens: 250 us on the line, 230
-// so).
+// so).  In shared_kernel one or two groups of several items do the same where that makes no
+// range more than an eighth longer: the items' blocks then read the same tokens at the same
+// time (96 columns of 60000 FP16 tokens: 124 us on the line, 81 so).
 //
 // The tile is attn_kernel's: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix
 // instructions, 32 tokens at a time, HT column tiles of 16 a wave; keys and values go
@@ -38,7 +40,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
-constexpr int kFewGroups = 16;  // whose items get whole blocks where they can
+constexpr int kFewGroups = 16;  // whose items get whole blocks where they can, of many columns
 
 // What every lane of the wave holds, in a scalar register.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -73,6 +75,7 @@ struct Groups {
     int32_t lead[kSharedGroups];
     int32_t first[kSharedGroups], rows[kSharedGroups], length[kSharedGroups];
     int32_t sums[2][8];  // a wave
+    int32_t best;        // the least share tried that fits
     int32_t share;       // > 0: items have whole blocks, of at most so much of the line; and
                          // `line` counts blocks
 };
@@ -221,38 +224,38 @@ __device__ __forceinline__ bool find_groups(const SharedProblem &p, Groups &s, i
         if (g < p.groups)
             s.lead[g] = has[i] >= 0 ? req[i] : -1;
     }
-    if (tid == 0)
-        s.share = DEAL::kMost > 1 ? 0x7fffffff : 0;
+    if (tid == 0) {
+        s.share = 0;
+        s.best = 0x7fffffff;
+    }
     __syncthreads();
-    if (DEAL::kMost == 1)
+    const int32_t all = s.line[p.groups], all_items = s.items[p.groups];
+    constexpr int kMostGroups = DEAL::kMost > 1 ? kFewGroups : kSharedAligned;
+    if (bad || p.groups > kMostGroups || all_items > blocks || all <= DEAL::kMost * blocks ||
+        (DEAL::kMost == 1 && all_items <= p.groups))
         return !bad;
-    const int32_t all = s.line[p.groups];
-    const bool few = !bad && p.groups <= kFewGroups && s.items[p.groups] <= blocks;
-    if (few && all > DEAL::kMost * blocks) {
+    const int32_t mean = (all + blocks - 1) / blocks;
+    {
         // thread i tries 1 + i / 128 times the mean
-        const int32_t mean = (all + blocks - 1) / blocks;
         const int32_t share = mean + (int32_t)((int64_t)mean * tid / 128);
         int32_t n = 0;
         for (int g = 0; g < p.groups; ++g)
             n += Items<DEAL>(p, Group{s.first[g], s.rows[g], s.length[g]}).blocks(share);
         if (n <= blocks)
-            atomicMin(&s.share, share);
+            atomicMin(&s.best, share);
     }
     __syncthreads();
-    const int32_t share = s.share;
-    __syncthreads();
-    if (share != 0x7fffffff) {
-        if (tid == 0) {
-            int32_t at_block = 0;
-            for (int g = 0; g <= p.groups; ++g) {
-                s.line[g] = at_block;
-                if (g < p.groups)
-                    at_block +=
-                        Items<DEAL>(p, Group{s.first[g], s.rows[g], s.length[g]}).blocks(share);
-            }
+    const int32_t share = s.best;
+    const bool use = share != 0x7fffffff && (DEAL::kMost > 1 || (share - mean) <= mean / 8);
+    if (use && tid == 0) {
+        s.share = share;
+        int32_t at_block = 0;
+        for (int g = 0; g <= p.groups; ++g) {
+            s.line[g] = at_block;
+            if (g < p.groups)
+                at_block +=
+                    Items<DEAL>(p, Group{s.first[g], s.rows[g], s.length[g]}).blocks(share);
         }
-    } else if (tid == 0) {
-        s.share = 0;
     }
     __syncthreads();
     return !bad;
@@ -482,11 +485,17 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
         const uint8_t *base[2];
         bool ok[2];  // a block outside the cache is never read: the first one stands in
         uint32_t at_[2];
-        const auto load = [&](auto *to, const uint8_t *from) {
+        // again: other items read the same tokens, so the caches keep them (64 rows in 8
+        // groups, up to 4 items each, of 12000 E4M3 tokens: 42.7 us without, 39.2 so)
+        constexpr bool kBoth = FP8 || D != 192 || HT > 1;  // else all registers are in use
+        const auto load = [&](auto *to, const uint8_t *from, auto again) {
             typedef typename std::remove_reference<decltype(*to)>::type T;
-            *to = stream<T>(from);
+            if (again)
+                *to = *reinterpret_cast<const T *>(from);
+            else
+                *to = stream<T>(from);
         };
-        const auto load_keys = [&] {
+        const auto load_keys = [&](auto again) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 ok[h] = id[h] >= 0 && id[h] < a.n_blocks;
@@ -495,30 +504,32 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
 #pragma unroll
                 for (int s = 0; s < S::kKeyLoads; ++s)
                     load(&key[h][s],
-                         base[h] + (key_head + at_[h] * 64 + s * tokens * 64) + key_lane);
+                         base[h] + (key_head + at_[h] * 64 + s * tokens * 64) + key_lane, again);
             }
         };
-        const auto load_piece = [&](auto &v, int d0, int width) {
+        const auto load_piece = [&](auto &v, int d0, int width, auto again) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int h = j >> 2;
                 const uint32_t t = at_[h] + 4 * (j & 3);
-                load(&v.raw[j], base[h] + (val_head + (t * D + d0) * S::kElt) +
-                                    (quarter * D + col * width) * S::kElt);
+                load(&v.raw[j],
+                     base[h] + (val_head + (t * D + d0) * S::kElt) +
+                         (quarter * D + col * width) * S::kElt,
+                     again);
             }
         };
-        const auto load_values = [&] {
+        const auto load_values = [&](auto again) {
 #pragma unroll
             for (int i = 0; i < S::kP8; ++i)
-                load_piece(v8[i], 128 * i, 8);
+                load_piece(v8[i], 128 * i, 8, again);
             if (S::kP4)
-                load_piece(v4[0], 128 * S::kP8, 4);
+                load_piece(v4[0], 128 * S::kP8, 4, again);
             if (S::kP2)
-                load_piece(v2[0], 128 * S::kP8 + 64 * S::kP4, 2);
+                load_piece(v2[0], 128 * S::kP8 + 64 * S::kP4, 2, again);
         };
-        const auto take = [&](int t0, auto more) {
+        const auto take = [&](int t0, auto more, auto again) {
             const bool ok0 = ok[0], ok1 = ok[1];
-            load_values();
+            load_values(again);
             f32x4 scores[HT][2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -542,7 +553,7 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
                 }
             }
             if (more) {
-                load_keys();
+                load_keys(again);
                 find(t0 + 2 * kTile);
             }
             float to_ref = to_log2;
@@ -635,13 +646,19 @@ __global__ __launch_bounds__(kThreads, (Shape<TYPE, FP8, D, HT>::kWavesPerSimd))
             if (S::kP2)
                 turn(v2[0], 2);
         };
-        if (u0 < u1) {
+        const auto take_all = [&](auto again) {
             find(u0 * kTile);
-            load_keys();
+            load_keys(again);
             find(u0 * kTile + kTile);
             for (int u = u0; u < u1 - 1; ++u)
-                take(u * kTile, std::true_type());
-            take((u1 - 1) * kTile, std::false_type());
+                take(u * kTile, std::true_type(), again);
+            take((u1 - 1) * kTile, std::false_type(), again);
+        };
+        if (u0 < u1) {
+            if (kBoth && grp.rows > p.item_rows)
+                take_all(std::true_type());
+            else
+                take_all(std::false_type());
         }
 
         // ---- the block's partial of the item -----------------------------------------

@@ -349,24 +349,50 @@ def test_empty_and_refused_calls():
                         workspace=torch.empty(64, dtype=torch.uint8, device=DEV))
 
 
-def test_longest_prefix():
-    """Two rows of 32 heads under 2^31 - 256 tokens, all of them in one block: a token counts
-    as often as the block is named.  Sums grow over up to 2^16 tiles, each of which rounds
-    them (and what the matrix cores hold, 4 times) to 2^-24 of themselves."""
-    tokens, dim, cols = 256, 64, 2 ** 23 - 1
-    c = Cache(1, tokens, 1, dim, E4M3, 0.05, 0.02)
+@pytest.mark.parametrize("dtype,cdtype,dim,kv_heads,group,tokens", KINDS)
+def test_many_columns(dtype, cdtype, dim, kv_heads, group, tokens):
+    """Groups of 150 columns and more, three and one: tiles through LDS, for every type and
+    width; last items of one row, and of as many columns as go into a wave and more."""
+    args = (dtype, cdtype, dim, kv_heads, group, tokens)
+    rows = -(-150 // group)
+    own = [(None if i % 11 == 4 else 1 + 5 * i % 23) for i in range(2 * rows)]
+    Batch([(333, own[:rows]), (64, own[:rows + 1]), (700, own[1:rows])], [7], *args, seed=4).run()
+    Batch([(515, own[:rows * 2])], [], *args, seed=5).run()
+
+
+@pytest.mark.parametrize("dtype,cdtype,dim,kv_heads,group,groups", [
+    (F16, F16, 128, 4, 8, [(3300, 20)]), (BF16, BF16, 128, 4, 8, [(2900, 17), (700, 5)]),
+    (F16, E4M3, 128, 2, 16, [(5000, 11)]), (BF16, E4M3, 192, 4, 4, [(1500, 1), (3000, 30)]),
+    (F16, F16, 64, 4, 32, [(4001, 6)]), (F16, F16, 192, 4, 4, [(2100, 11)]),
+    (BF16, BF16, 256, 2, 16, [(3000, 3)]), (F16, F16, 96, 4, 8, [(2500, 13), (2500, 13)]),
+])
+def test_items_side_by_side(dtype, cdtype, dim, kv_heads, group, groups):
+    """One or two groups of several items, which get whole blocks with the same tokens."""
+    Batch([(n, [3 * i % 40 + 1 if i % 7 != 2 else None for i in range(rows)])
+           for n, rows in groups], [9], dtype, cdtype, dim, kv_heads, group, 32, seed=dim).run()
+
+
+@pytest.mark.parametrize("cdtype,dim,rows,heads,tiles", [(E4M3, 64, 2, 32, 2 ** 16),
+                                                         (F16, 192, 4, 16, 2 ** 17)])
+def test_longest_prefix(cdtype, dim, rows, heads, tiles):
+    """Rows under 2^31 - 256 tokens, all of them in one block: a token counts as often as the
+    block is named.  Sums grow over up to `tiles` tiles, each of which rounds them (and what
+    the matrix cores hold, 4 times) to 2^-24 of themselves."""
+    tokens, cols = 256, 2 ** 23 - 1
+    scales = (0.05, 0.02) if cdtype == E4M3 else (1.0, 1.0)
+    c = Cache(1, tokens, 1, dim, cdtype, *scales)
     k, v = rnd(tokens, 1, dim, seed=1), 1 + 0.5 * rnd(tokens, 1, dim, seed=2)
-    c.place(torch.arange(tokens), k / 0.05, v / 0.02)
-    q = rnd(2, 32, dim, seed=3).to(F16)
+    c.place(torch.arange(tokens), k / scales[0], v / scales[1])
+    q = rnd(rows, heads, dim, seed=3).to(F16)
     one = torch.zeros(1, dtype=torch.int32)
-    want, lse64 = attn_oracle(q, c, one[:, None], torch.tensor([tokens] * 2), torch.zeros(2).int(),
-                              dim ** -0.5, 0)[:2]
+    want, lse64 = attn_oracle(q, c, one[:, None], torch.tensor([tokens] * rows),
+                              torch.zeros(rows).int(), dim ** -0.5, 0)[:2]
     table = torch.zeros((1, cols), dtype=torch.int32, device=DEV)
     n = i32([cols * tokens]).to(DEV)
-    lse = torch.empty((2, 32), device=DEV)
-    got = dps.attn_shared(q.to(DEV), c.up(), table, n.repeat(2), i32([0, 2]).to(DEV), n,
-                          req=torch.zeros(2, dtype=torch.int32, device=DEV), lse=lse)
-    step = 2.0 ** 16 * 2.0 ** -24
-    err = (got.cpu().double() - want.double().reshape(got.shape)).abs().max()
+    lse = torch.empty((rows, heads), device=DEV)
+    got = dps.attn_shared(q.to(DEV), c.up(), table, n.repeat(rows), i32([0, rows]).to(DEV), n,
+                          req=torch.zeros(rows, dtype=torch.int32, device=DEV), lse=lse)
+    step = tiles * 2.0 ** -24
+    err = (got.cpu().double() - want).abs().max()
     assert err <= 5 * step * float(v.abs().max()) + 2.0 ** -10, err
-    assert float((lse.cpu().double() - lse64.reshape(2, 32) - math.log(cols)).abs().max()) <= 2 * step
+    assert float((lse.cpu().double() - lse64 - math.log(cols)).abs().max()) <= 2 * step
