@@ -16,7 +16,7 @@ replayed while requests grow.
 Run as a program (python -m paper_2609_34380_amd.decode), it decodes with a small
 layer until KV blocks push the residuals out, goes on in fast mode, and returns
 to full mode once the requests end and the residuals are restored; with the argument
-"beams" the requests are beams of one prompt, and blocks that end up scattered over the
+"beams" the requests are beams of two prompts, and blocks that end up scattered over the
 units are moved together so that the residuals can return.
 """
 import sys
@@ -413,26 +413,28 @@ def main(steps=1600):
     shared.close()
 
 
-def main_beams(steps=900, beams=8, vocab=32000, prompt=400):
-    """One prompt of `prompt` tokens, then beams over a vocabulary."""
-    shared = SharedLayer(batch=beams, groups=1)
+def main_beams(steps=2000, requests=2, beams=4, vocab=32000, prompt=400):
+    """Prompts of `prompt` tokens, then beams over a vocabulary until their blocks evict a
+    residual, and one beam that is left."""
+    slots = requests * beams
+    shared = SharedLayer(batch=slots, groups=requests)
     gen = torch.Generator(device="cuda").manual_seed(1)
     head = torch.randn((vocab, SharedLayer.HIDDEN), device="cuda", generator=gen).to(torch.float16)
     embed = torch.randn((vocab, SharedLayer.HIDDEN), device="cuda", generator=gen).to(torch.float16)
     names = {dps.MODE_FULL: "full", dps.MODE_FAST: "fast"}
     search, batch, mode = Beams(shared.batch, [shared.cache], beams, vocab), shared.batch, None
-    x = torch.zeros((beams, SharedLayer.HIDDEN), dtype=torch.float16, device="cuda")
-    for t in range(prompt):   # in the first slot
-        x[0] = embed[t % vocab]
-        y = shared.decode(x, [1] + [0] * (beams - 1))
-    batch.fork([0] * beams, [shared.cache])
-    y = y[:1].repeat(beams, 1)
+    x = torch.zeros((slots, SharedLayer.HIDDEN), dtype=torch.float16, device="cuda")
+    for t in range(prompt):   # in each request's first slot
+        x[:requests] = embed[t % vocab:t % vocab + requests]
+        y = shared.decode(x, ([1] + [0] * (beams - 1)) * requests)
+    batch.fork([r // beams * beams for r in range(slots)], [shared.cache])
+    y = y[:requests].repeat_interleave(beams, 0)
     for t in range(steps):
         token = search.pick(y @ head.t())
         if token is None:
             print("step %d: no room for more KV blocks" % t)
             break
-        y = shared.decode(embed[token.long().clamp(min=0)], [1] * beams)
+        y = shared.decode(embed[token.long().clamp(min=0)], [1] * slots)
         if y is None:
             print("step %d: no room for more KV blocks" % t)
             break
@@ -441,9 +443,9 @@ def main_beams(steps=900, beams=8, vocab=32000, prompt=400):
             print("step %d: %s mode, %s" % (t, names[mode], shared.sums.counts()))
     torch.cuda.synchronize()
     print("%d beams of %d tokens in %d blocks, %d of them shared" %
-          (beams, batch.lengths[0], len({b for x in batch.blocks for b in x}),
-           int(batch.shared_len[0]) // batch.block_tokens))
-    wake = any([batch.end(r) for r in range(1, beams)])
+          (slots, batch.lengths[0], len({b for x in batch.blocks for b in x}),
+           int(batch.shared_len.sum()) // batch.block_tokens))
+    wake = any([batch.end(r) for r in range(1, slots)])
     if batch.compact([shared.cache]) or wake:
         shared.worker.kick()
     shared.worker.wait_idle()
