@@ -465,7 +465,9 @@ typedef struct {
     int32_t *tokens;    /* [rows] ... its first tokens[i] tokens; -1 in all three past
                            the last copy                                                */
     int32_t *freed;     /* [n_freed] blocks of the old tables that no new one holds,
-                           ascending; -1 past the last                                  */
+                           ascending; -1 past the last.  Every entry of an old table
+                           counts, those past its row's length too: a caller whose rows
+                           still name blocks that were given back frees by its own lists */
     int64_t n_freed;    /* room in freed; what does not fit is counted and left out     */
     int32_t *counts;    /* [2] copies, which is also the blocks taken off `fresh`, and
                            blocks freed, in all; the step fits if the first is at most

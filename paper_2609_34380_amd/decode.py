@@ -190,23 +190,23 @@ class PagedBatch:
             parents = torch.tensor(host, dtype=torch.int32, device=self.table.device)
         here = self._after_steps()
         i32 = dict(dtype=torch.int32, device=self.table.device)
-        held = sorted({b for blocks in self.blocks for b in blocks})
-        out = dps.make_kv_fork(len(host), self.table.shape[1], len(held), self.table.device)
+        # no blocks for kv_fork to list: a table row names what its slot's earlier requests held,
+        # too, which may be another holder's by now; what nothing holds any more is known here
+        out = dps.make_kv_fork(len(host), self.table.shape[1], 0, self.table.device)
         out = out._replace(table=self.table)    # where captured steps look for it
         f = dps.kv_fork(parents, torch.tensor(self.lengths, **i32), self.table.clone(),
-                        torch.tensor(taken, **i32), self.block_tokens,
-                        max(held + taken, default=-1) + 1, out=out)
+                        torch.tensor(taken, **i32), self.block_tokens, 0, out=out)
         for cache in caches:
             dps.kv_copy(cache, f.src, f.dst, tokens=f.tokens, count=f.counts)
         fresh = dict(zip(copied, taken))
         blocks = [list(self.blocks[p]) if p >= 0 else [] for p in host]
         for r, block in fresh.items():
             blocks[r][-1] = block
+        freed = {b for x in self.blocks for b in x} - {b for x in blocks for b in x}
         self.lengths = [self.lengths[p] if p >= 0 else 0 for p in host]
         self.blocks, self._forks = blocks, self._forks + 1
         here.synchronize()
-        freed = f.freed[:int(f.counts[1])].tolist()
-        self.wake = self.sums.free(freed) if freed else False
+        self.wake = self.sums.free(sorted(freed)) if freed else False
         return True
 
     def compact(self, caches, max_moves=1 << 16):
