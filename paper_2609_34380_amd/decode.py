@@ -211,11 +211,18 @@ class PagedBatch:
 
     def compact(self, caches, max_moves=1 << 16):
         """Moves blocks of nearly empty units together (dps.SumManager.compact), in each of
-        `caches`, so that units become free: True when residuals wait for them.  Waits for
-        the steps before and for the moves."""
+        `caches`, so that units become free: True when residuals wait for them.  Units in
+        which others than this batch have blocks stay as they are.  Waits for the steps before
+        and for the moves."""
         self._mapped()
         self._ours(caches)
-        src, dst = self.sums.compact(max_moves)
+        ours, per = {b for blocks in self.blocks for b in blocks}, self.sums.blocks_per_unit
+        moves = list(zip(*self.sums.compact(max_moves)))
+        others = {s // per for s, _ in moves if s not in ours}
+        left = [d for s, d in moves if s // per in others]
+        if left:
+            self.sums.free(left)
+        src, dst = ([m[i] for m in moves if m[0] // per not in others] for i in range(2))
         if not src:
             return False
         here = self._after_steps()

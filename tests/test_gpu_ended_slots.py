@@ -79,6 +79,28 @@ def test_another_holder_of_the_manager():
         s.shared.close()
 
 
+def test_moves_beside_another_holder():
+    """Another holder's blocks in the unit that is nearly empty: they and their bytes stay."""
+    s = Slots(4, 3)
+    try:
+        sums, pool = s.shared.sums, s.shared.pool
+        per = sums.blocks_per_unit
+        for _ in range(16 * per // 4):
+            s.step([1, 1, 1, 1])                        # one unit
+        theirs = sums.alloc(3)                          # the next one's first
+        block = pool.numel() // (sums.n_units * per)
+        for b in theirs:
+            pool[b * block:(b + 1) * block] = 0x5A
+        s.end(0)
+        assert not s.batch.compact([s.shared.cache])
+        s.step([0, 1, 1, 1])
+        assert all(bool((pool[b * block:(b + 1) * block] == 0x5A).all()) for b in theirs)
+        assert not set(sums.alloc(20)) & (set(theirs) | {b for x in s.batch.blocks for b in x})
+    finally:
+        torch.cuda.synchronize()
+        s.shared.close()
+
+
 @pytest.mark.parametrize("seed", range(3))
 def test_random_ends_and_forks(seed):
     """Ends, forks, moves and steps in any order, with none or several of a kind together."""

@@ -243,3 +243,77 @@ def test_random_lives(host, seed):
         elif all(n < a.batch.max_tokens for n in a.batch.lengths):
             a.step([int(rng.random() < 0.8) for _ in range(slots)])
         check(sums, *lives)
+
+
+# ---- moves, beside other holders of blocks ----------------------------------------------
+
+
+def test_compact_leaves_another_holders_blocks(host):
+    """The unit to empty holds another batch's blocks: they stay where its table says, and the
+    places that the plan had taken for them are free again."""
+    sums = dps.SumManager(2, 8, 0)
+    a, b = Life(sums, 2), Life(sums, 1)
+    for new, n in (([1, 0], 20), ([0, 1], 12)):    # blocks 0 .. 4 and 5 .. 7
+        for _ in range(n):
+            a.step(new)
+    for _ in range(8):
+        b.step([1])                                # 8 and 9
+    a.end(1)
+    before = sums.counts()
+    assert not a.batch.compact([a.cache])
+    assert sums.counts() == before and b.batch.blocks == [[8, 9]]
+    check(sums, a, b)
+    assert "copy" not in host.log
+    assert not set(sums.alloc(9)) & {0, 1, 2, 3, 4, 8, 9}
+
+
+def test_compact_moves_the_units_that_are_its_own(host):
+    """Of two units to empty one holds another batch's block: the other is emptied, and the
+    residual that waits for it is reported."""
+    sums = dps.SumManager(3, 8, 1)
+    a, b = Life(sums, 3), Life(sums, 1)
+    for r, n in ((0, 20), (1, 12), (2, 8), (1, 24)):   # 8 .. 12, 13 .. 15, 16 and 17, 18 .. 23
+        for _ in range(n):
+            a.step([int(i == r) for i in range(3)])
+    b.step([1])                                    # 0, where the residual was
+    assert sums.mode == dps.MODE_FAST and b.batch.blocks == [[0]]
+    a.end(1)
+    assert a.batch.compact([a.cache])
+    assert a.batch.blocks[2] == [14, 15] and b.batch.blocks == [[0]]
+    check(sums, a, b)
+    assert sums.unit_state(2) == dps.UNIT_FREE
+    assert not set(sums.alloc(9)) & (held(a)[0] | {0})
+
+
+def test_compact_of_one_batch_frees_whole_units(host):
+    sums = dps.SumManager(3, 8, 1)
+    a = Life(sums, 3)
+    for _ in range(32):
+        a.step([1, 1, 1])
+    assert sums.mode == dps.MODE_FAST
+    a.end(0)
+    a.end(2)
+    assert sums.counts()["free"] == 0
+    assert a.batch.compact([a.cache])
+    check(sums, a)
+    assert sums.counts()["free"] == 2
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_random_lives_with_moves(host, seed):
+    rng = random.Random(1000 + seed)
+    sums = dps.SumManager(rng.randint(2, 5), rng.choice((4, 8)), rng.randint(0, 2))
+    lives = [Life(sums, rng.randint(1, 4)) for _ in range(rng.randint(1, 3))]
+    for _ in range(200):
+        a = rng.choice(lives)
+        slots = len(a.want)
+        op = rng.random()
+        if op < 0.15:
+            a.fork([rng.choice([-1] + list(range(slots)) * 2) for _ in range(slots)])
+        elif op < 0.3:
+            a.end(rng.randrange(slots))
+        elif op < 0.45:
+            a.batch.compact([a.cache], rng.choice((1, 3, 1000)))
+        elif all(n < a.batch.max_tokens for n in a.batch.lengths):
+            a.step([int(rng.random() < 0.8) for _ in range(slots)])
+        check(sums, *lives)
