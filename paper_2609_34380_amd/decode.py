@@ -39,10 +39,11 @@ class PagedBatch:
 
     Steps may run on other streams than grow(): its copies wait for the work of every
     stream that map() was called on, also to capture it, and are complete when it
-    returns.  Before the next grow() a caller waits for a graph replayed elsewhere than
-    on the stream of its capture.
+    returns.  Before the next grow(), fork() or compact() a caller waits for a graph replayed
+    elsewhere than on the stream of its capture.
 
-    fork() lets slots go on from other slots, sharing their whole blocks.  With groups > 0
+    fork() lets slots go on from other slots, sharing their whole blocks.  It and compact()
+    come between steps, after all that reads self.step is enqueued.  With groups > 0
     (the most groups of rows that one step's attention treats as one) grow() also finds
     which neighbouring rows share their first blocks: self.group_start and
     self.shared_len, for dps.attn_shared."""
@@ -55,14 +56,18 @@ class PagedBatch:
         self.max_tokens = columns * block_tokens
         i32 = dict(dtype=torch.int32, device=device)
         self.table = torch.full((batch, columns), -1, **i32)
-        self.ctx_len, self.new_len = torch.zeros(batch, **i32), torch.zeros(batch, **i32)
+        # a step's lengths, and the counts that its map() writes: below 0 before it has run
+        self._lengths = torch.zeros(2 * batch + 2, **i32)
+        self.ctx_len, self.new_len = self._lengths[:batch], self._lengths[batch:2 * batch]
         self.rows = batch if rows is None else rows
         # a step never takes more than a block a slot and what its rows fill
         self.fresh = torch.full((batch + self.rows // block_tokens + 1,), -1, **i32)
         self.step = dps.make_kv_map(batch, self.rows, self.ctx_len.device)
+        self.step = self.step._replace(counts=self._lengths[2 * batch:])
         # that the buffers were filled on, or map() was called on
         self._streams = [torch.cuda.current_stream(self.table.device)]
         self._unmapped = set()               # slots that grew since the last map()
+        self._grown = set()                  # slots of the last step, whoever mapped it
         self._captured = False               # map() is in a graph: replays are not seen here
         self._forks = 0                      # > 0: slots may have blocks in common
         self._group_key = None               # of the groups that are on the device
@@ -93,8 +98,7 @@ class PagedBatch:
         self._after_steps()
         if self.groups:
             self._group([r for r, n in enumerate(new) for _ in range(n)])
-        self.ctx_len.copy_(torch.tensor(self.lengths, dtype=torch.int32))
-        self.new_len.copy_(torch.tensor(new, dtype=torch.int32))
+        self._lengths.copy_(torch.tensor([*self.lengths, *new, -1, -1], dtype=torch.int32))
         if taken:
             self.fresh[:len(taken)].copy_(torch.tensor(taken, dtype=torch.int32))
         at = 0
@@ -103,6 +107,7 @@ class PagedBatch:
             at += n
             self.lengths[r] += new[r]
         self._unmapped = {r for r, n in enumerate(new) if n}
+        self._grown = set(self._unmapped)
         return True
 
     def _after_steps(self):
@@ -144,6 +149,15 @@ class PagedBatch:
         if self._unmapped and not self._captured:
             raise RuntimeError("the tokens of the last grow() are not mapped")
 
+    def _between_steps(self):
+        """Refuses what would come between a step's grow() and its map(), which may be in a
+        graph: the step's blocks are in no table yet.  Returns the current stream."""
+        self._mapped()
+        here = self._after_steps()
+        if self._captured and self._grown and int(self.step.counts[0]) < 0:
+            raise RuntimeError("the tokens of the last grow() are not mapped")
+        return here
+
     def map(self):
         """Enqueue the step's block tables and slot maps."""
         stream = torch.cuda.current_stream(self.table.device)
@@ -169,7 +183,7 @@ class PagedBatch:
         back those that no slot holds any more; self.wake says then whether residuals wait
         for the units that became free.  Waits for the steps before, as grow() does, and
         for the copies."""
-        self._mapped()
+        here = self._between_steps()
         self._ours(caches)
         given = torch.is_tensor(parents)
         if given and not (parents.dtype == torch.int32 and parents.device == self.table.device and
@@ -188,7 +202,6 @@ class PagedBatch:
             return False
         if not given:
             parents = torch.tensor(host, dtype=torch.int32, device=self.table.device)
-        here = self._after_steps()
         i32 = dict(dtype=torch.int32, device=self.table.device)
         # no blocks for kv_fork to list: a table row names what its slot's earlier requests held,
         # too, which may be another holder's by now; what nothing holds any more is known here
@@ -214,7 +227,7 @@ class PagedBatch:
         `caches`, so that units become free: True when residuals wait for them.  Units in
         which others than this batch have blocks stay as they are.  Waits for the steps before
         and for the moves."""
-        self._mapped()
+        here = self._between_steps()
         self._ours(caches)
         ours, per = {b for blocks in self.blocks for b in blocks}, self.sums.blocks_per_unit
         moves = list(zip(*self.sums.compact(max_moves)))
@@ -225,7 +238,6 @@ class PagedBatch:
         src, dst = ([m[i] for m in moves if m[0] // per not in others] for i in range(2))
         if not src:
             return False
-        here = self._after_steps()
         i32 = dict(dtype=torch.int32, device=self.table.device)
         s, d = torch.tensor(src, **i32), torch.tensor(dst, **i32)
         for cache in caches:
@@ -248,6 +260,7 @@ class PagedBatch:
             others = {b for blocks in self.blocks for b in blocks}
             mine = [b for b in mine if b not in others]
         self._unmapped.discard(slot)
+        self._grown.discard(slot)
         return self.sums.free(mine) if mine else False
 
 

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from gpu_helpers import DEV
-from paper_2609_34380_amd import decode, dps
+from paper_2609_34380_amd import decode, dps, graphs
 from test_gpu_beams import check_blocks, fork_ref
 from test_gpu_decode import Layer64, close
 
@@ -126,6 +126,49 @@ def test_random_ends_and_forks(seed):
                 ended = False
             check_blocks(s.batch)
         assert after_end > 1
+    finally:
+        torch.cuda.synchronize()
+        s.shared.close()
+
+
+def test_fork_and_compact_wait_for_the_replay():
+    """A step is grown, and its map() and layer are in a graph: until the replay its blocks
+    are in no table, and fork and compact are refused; after it they do what they always do."""
+    s = Slots(3, 4, groups=2)
+    try:
+        batch, shared = s.batch, s.shared
+        x = torch.zeros(3, 1024, dtype=torch.float16, device=DEV)
+        y = {m: torch.zeros_like(x) for m in graphs.ModeGraphs.MODES}
+
+        def step(m, mode):
+            batch.map()
+            shared.layer(x, batch, mode, out=y[mode])
+
+        steps = graphs.ModeGraphs(step, (3,))
+        steps.capture()
+        torch.cuda.synchronize()
+        for t in range(60):
+            assert batch.grow([1, 1, 1])
+            table, lengths, counts = batch.table.clone(), list(batch.lengths), shared.sums.counts()
+            for call in (lambda: batch.fork([0, 0, 2], [shared.cache]),
+                         lambda: batch.compact([shared.cache])):
+                with pytest.raises(RuntimeError):
+                    call()
+            assert torch.equal(table, batch.table) and lengths == batch.lengths
+            assert counts == shared.sums.counts()
+            x.copy_(torch.randn(3, 1024, generator=s.gen).to(torch.float16))
+            steps.stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(steps.stream):
+                steps.replay(3, shared.sums.mode)
+            torch.cuda.synchronize()
+            close(y[shared.sums.mode], s.ref.step(x.cpu(), [0, 1, 2], shared.sums.mode))
+            check_blocks(batch)
+            if t % 7 == 6:
+                s.fork([t % 3, 1, 0])
+            elif t % 11 == 10:
+                s.end(t % 3)
+                batch.compact([shared.cache])
+            check_blocks(batch)
     finally:
         torch.cuda.synchronize()
         s.shared.close()

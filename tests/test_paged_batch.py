@@ -317,3 +317,99 @@ def test_random_lives_with_moves(host, seed):
         elif all(n < a.batch.max_tokens for n in a.batch.lengths):
             a.step([int(rng.random() < 0.8) for _ in range(slots)])
         check(sums, *lives)
+
+
+# ---- between a step's grow() and the replay of its captured map() --------------------------
+
+
+class Captured(Life):
+    """Its map() is captured once; a step replays it."""
+
+    def capture(self, host):
+        host.recorded = self.recorded = []
+        self.batch.map()
+        host.recorded = None
+
+    def replay(self):
+        for run in self.recorded:
+            run()
+        self.store()
+
+
+def same_again(a, host):
+    """Nothing has changed when a call is refused."""
+    b, log = a.batch, list(host.log)
+    state = lambda: (list(b.lengths), [list(x) for x in b.blocks], b.table.tolist(),
+                     b.sums.counts(), a.cache.tokens.tolist(), b.ctx_len.tolist(),
+                     b.new_len.tolist())
+    before = state()
+    for call in (lambda: b.fork([0, 0, 1], [a.cache]), lambda: b.compact([a.cache])):
+        with pytest.raises(RuntimeError):
+            call()
+        assert state() == before and host.log == log
+
+
+@pytest.mark.parametrize("eager_first", [True, False])
+def test_fork_and_compact_wait_for_the_replay(host, eager_first):
+    sums = dps.SumManager(3, 8, 0)
+    a = Captured(sums, 3)
+    if eager_first:
+        for _ in range(3):
+            a.step([1, 1, 1])
+    a.capture(host)
+    for t in range(30):
+        assert a.batch.grow([1, int(t < 20), 1])
+        same_again(a, host)
+        a.replay()
+        check(sums, a)
+        if t == 20:
+            a.end(1)
+            a.batch.compact([a.cache])
+        elif t % 3 == 0:
+            assert a.fork([0, 2, 0])
+        check(sums, a)
+
+
+def test_capture_after_grow(host):
+    """The step that was grown before the capture still has to be replayed."""
+    a = Captured(dps.SumManager(2, 8, 0), 3)
+    assert a.batch.grow([1, 1, 0])
+    a.capture(host)
+    same_again(a, host)
+    a.replay()
+    assert a.fork([0, 1, 0])
+    a.check()
+
+
+def test_an_eager_map_beside_a_capture(host):
+    a = Captured(dps.SumManager(2, 8, 0), 3)
+    a.capture(host)
+    assert a.step([1, 0, 1])
+    assert a.fork([0, 2, 0])
+    a.check()
+    assert a.batch.grow([0, 0, 0])          # nothing to map
+    assert a.fork([0, 0, 0])
+    a.check()
+
+
+def test_the_same_lengths_as_in_the_step_before(host):
+    """A slot whose new length is what the last step left in the step's arrays."""
+    a = Captured(dps.SumManager(2, 8, 0), 3)
+    a.capture(host)
+    for new in ([1, 1, 1], [1, 0, 0]):
+        assert a.batch.grow(new)
+        a.replay()
+    assert a.fork([1, 1, 2])                # lengths 1, 1, 1; the step's arrays say 2, 1, 1
+    assert a.batch.grow([1, 0, 0])
+    same_again(a, host)
+    a.replay()
+    check(a.batch.sums, a)
+
+
+def test_the_slot_that_grew_has_ended(host):
+    a = Captured(dps.SumManager(2, 8, 0), 3)
+    a.capture(host)
+    assert a.batch.grow([1, 0, 0])
+    a.end(0)
+    assert a.fork([0, 1, 2])
+    a.check()
