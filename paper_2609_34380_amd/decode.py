@@ -200,17 +200,23 @@ class PagedBatch:
         taken = self.sums.alloc(len(copied))
         if taken is None:
             return False
-        if not given:
-            parents = torch.tensor(host, dtype=torch.int32, device=self.table.device)
         i32 = dict(dtype=torch.int32, device=self.table.device)
-        # no blocks for kv_fork to list: a table row names what its slot's earlier requests held,
-        # too, which may be another holder's by now; what nothing holds any more is known here
-        out = dps.make_kv_fork(len(host), self.table.shape[1], 0, self.table.device)
-        out = out._replace(table=self.table)    # where captured steps look for it
-        f = dps.kv_fork(parents, torch.tensor(self.lengths, **i32), self.table.clone(),
-                        torch.tensor(taken, **i32), self.block_tokens, 0, out=out)
-        for cache in caches:
-            dps.kv_copy(cache, f.src, f.dst, tokens=f.tokens, count=f.counts)
+        try:
+            if not given:
+                parents = torch.tensor(host, **i32)
+            # no blocks for kv_fork to list: a table row names what its slot's earlier requests
+            # held, too, which may be another holder's by now; what nothing holds any more is
+            # known here
+            out = dps.make_kv_fork(len(host), self.table.shape[1], 0, self.table.device)
+            f = dps.kv_fork(parents, torch.tensor(self.lengths, **i32), self.table,
+                            torch.tensor(taken, **i32), self.block_tokens, 0, out=out)
+            for cache in caches:
+                dps.kv_copy(cache, f.src, f.dst, tokens=f.tokens, count=f.counts)
+            self.table.copy_(f.table)      # where captured steps look for it
+        except Exception:
+            here.synchronize()             # copies may be under way
+            self.sums.free(taken)
+            raise
         fresh = dict(zip(copied, taken))
         blocks = [list(self.blocks[p]) if p >= 0 else [] for p in host]
         for r, block in fresh.items():
@@ -239,10 +245,15 @@ class PagedBatch:
         if not src:
             return False
         i32 = dict(dtype=torch.int32, device=self.table.device)
-        s, d = torch.tensor(src, **i32), torch.tensor(dst, **i32)
-        for cache in caches:
-            dps.kv_copy(cache, s, d)
-        dps.kv_remap(self.table, s, d)
+        try:
+            s, d = torch.tensor(src, **i32), torch.tensor(dst, **i32)
+            for cache in caches:
+                dps.kv_copy(cache, s, d)
+            dps.kv_remap(self.table, s, d)
+        except Exception:
+            here.synchronize()
+            self.sums.free(dst)
+            raise
         to = dict(zip(src, dst))
         self.blocks = [[to.get(b, b) for b in blocks] for blocks in self.blocks]
         here.synchronize()

@@ -413,3 +413,31 @@ def test_the_slot_that_grew_has_ended(host):
     a.end(0)
     assert a.fork([0, 1, 2])
     a.check()
+
+
+# ---- calls that are refused below -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("name", ["fork", "copy", "remap"])
+def test_a_refused_call_changes_nothing(host, name):
+    """An entry point that refuses its arguments (tensors of another device than the current
+    one, too many rows): tables, lists and the manager's blocks are what they were."""
+    sums = dps.SumManager(2, 8, 0)
+    a = Life(sums, 3)
+    for t in range(22):
+        a.step([1, int(t < 13), 1])
+    a.end(2)
+    b = a.batch
+    state = lambda: (list(b.lengths), [list(x) for x in b.blocks], b.table.tolist(), sums.counts())
+    before = state()
+    host.fail = name
+    calls = [lambda: b.fork([0, 0, 1], [a.cache]), lambda: b.compact([a.cache])]
+    for call in {"fork": calls[:1], "copy": calls, "remap": calls[1:]}[name]:
+        with pytest.raises(ValueError):
+            call()
+        assert state() == before
+    host.fail = None
+    assert a.fork([0, 0, 1])
+    check(sums, a)
+    b.compact([a.cache])
+    check(sums, a)
