@@ -426,6 +426,7 @@ def test_a_refused_call_changes_nothing(host, name):
     a = Life(sums, 3)
     for t in range(22):
         a.step([1, int(t < 13), 1])
+    a.end(1)
     a.end(2)
     b = a.batch
     state = lambda: (list(b.lengths), [list(x) for x in b.blocks], b.table.tolist(), sums.counts())
