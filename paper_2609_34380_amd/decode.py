@@ -71,7 +71,7 @@ class PagedBatch:
         self._captured = False               # map() is in a graph: replays are not seen here
         self._forks = 0                      # > 0: slots may have blocks in common
         self._group_key = None               # of the groups that are on the device
-        self.wake = False                    # what fork() freed lets residuals return
+        self.wake = False                    # what forks have freed lets residuals return
         self.group_start, self.shared_len = (torch.zeros(n, **i32) for n in (groups + 1, groups))
 
     def grow(self, new):
@@ -180,9 +180,9 @@ class PagedBatch:
         slot is empty from now on), for all slots at once: shared whole blocks, and a copy
         of a last block that has room, in each of `caches` (every layer's).  Takes the
         blocks of the copies (False, with nothing changed, if no room is left) and gives
-        back those that no slot holds any more; self.wake says then whether residuals wait
-        for the units that became free.  Waits for the steps before, as grow() does, and
-        for the copies."""
+        back those that no slot holds any more; where residuals wait for units that became
+        free, self.wake turns True, and stays so until the caller, who wakes their restore, has
+        set it back.  Waits for the steps before, as grow() does, and for the copies."""
         here = self._between_steps()
         self._ours(caches)
         given = torch.is_tensor(parents)
@@ -215,7 +215,7 @@ class PagedBatch:
             self.table.copy_(f.table)      # where captured steps look for it
         except Exception:
             here.synchronize()             # copies may be under way
-            self.sums.free(taken)
+            self.wake = self.sums.free(taken) or self.wake
             raise
         fresh = dict(zip(copied, taken))
         blocks = [list(self.blocks[p]) if p >= 0 else [] for p in host]
@@ -225,7 +225,7 @@ class PagedBatch:
         self.lengths = [self.lengths[p] if p >= 0 else 0 for p in host]
         self.blocks, self._forks = blocks, self._forks + 1
         here.synchronize()
-        self.wake = self.sums.free(sorted(freed)) if freed else False
+        self.wake = (bool(freed) and self.sums.free(sorted(freed))) or self.wake
         return True
 
     def compact(self, caches, max_moves=1 << 16):
@@ -329,10 +329,10 @@ class AttentionLayer:
 class Beams:
     """Beam search over the slots of a PagedBatch, `beams` slots a request: pick() takes
     the logits of a step's rows (a new token in every slot), gives every slot the beam it
-    goes on with, and returns the tokens of the next step.  caches: every layer's.  end:
-    the token that ends a beam (-1: none).  Ended beams keep their slots, and slots for
-    which there is no beam are empty and have no score; both take tokens like the others,
-    whose logits do not count."""
+    goes on with (PagedBatch.fork: look at the batch's wake then), and returns the tokens of
+    the next step.  caches: every layer's.  end: the token that ends a beam (-1: none).
+    Ended beams keep their slots, and slots for which there is no beam are empty and have no
+    score; both take tokens like the others, whose logits do not count."""
 
     def __init__(self, batch, caches, beams, vocab, end=-1):
         slots = len(batch.lengths)
@@ -465,6 +465,9 @@ def main_beams(steps=2000, requests=2, beams=4, vocab=32000, prompt=400):
         if token is None:
             print("step %d: no room for more KV blocks" % t)
             break
+        if batch.wake:
+            batch.wake = False
+            shared.worker.kick()
         y = shared.decode(embed[token.long().clamp(min=0)], [1] * slots)
         if y is None:
             print("step %d: no room for more KV blocks" % t)
@@ -477,7 +480,7 @@ def main_beams(steps=2000, requests=2, beams=4, vocab=32000, prompt=400):
           (slots, batch.lengths[0], len({b for x in batch.blocks for b in x}),
            int(batch.shared_len.sum()) // batch.block_tokens))
     wake = any([batch.end(r) for r in range(1, slots)])
-    if batch.compact([shared.cache]) or wake:
+    if batch.compact([shared.cache]) or wake or batch.wake:
         shared.worker.kick()
     shared.worker.wait_idle()
     print("one beam is left, its blocks together: %s mode, %s" %

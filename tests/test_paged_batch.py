@@ -442,3 +442,25 @@ def test_a_refused_call_changes_nothing(host, name):
     check(sums, a)
     b.compact([a.cache])
     check(sums, a)
+
+
+# ---- residuals that wait ----------------------------------------------------------------------
+
+
+def test_wake_stays_until_it_is_looked_at(host):
+    """A fork frees a unit that an evicted residual waits for; the ones after it free none."""
+    sums = dps.SumManager(2, 4, 2)
+    a = Life(sums, 2)
+    for _ in range(16):
+        a.step([1, 1])
+    assert sums.mode == dps.MODE_FAST and not a.batch.wake
+    assert a.fork([-1, 1])
+    assert not a.batch.wake              # every other block: no whole unit
+    a.batch.compact([a.cache])
+    for _ in range(16):
+        a.step([1, 0])
+    assert a.fork([-1, 1]) and a.batch.wake
+    for _ in range(3):
+        assert a.fork([-1, 1]) and a.batch.wake
+    a.batch.wake = False
+    assert a.fork([-1, 1]) and not a.batch.wake
