@@ -87,14 +87,10 @@ class PagedBatch:
             if had + n > self.max_tokens:
                 raise ValueError("a request outgrows its table row")
             need.append(-(-(had + n) // self.block_tokens) - -(-had // self.block_tokens))
+        self._mapped()
         taken = self.sums.alloc(sum(need))
         if taken is None:
             return False
-        try:
-            self._mapped()
-        except RuntimeError:
-            self.sums.free(taken)
-            raise
         self._after_steps()
         if self.groups:
             self._group([r for r, n in enumerate(new) for _ in range(n)])

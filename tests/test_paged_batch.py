@@ -464,3 +464,15 @@ def test_wake_stays_until_it_is_looked_at(host):
         assert a.fork([-1, 1]) and a.batch.wake
     a.batch.wake = False
     assert a.fork([-1, 1]) and not a.batch.wake
+
+
+def test_a_grow_that_is_refused_evicts_nothing(host):
+    """A step that is refused takes no blocks, and so evicts nothing."""
+    sums = dps.SumManager(2, 4, 1)
+    a = Life(sums, 2)
+    for _ in range(15):
+        a.step([1, 0])
+    assert a.batch.grow([1, 0]) and sums.mode == dps.MODE_FULL
+    with pytest.raises(RuntimeError):
+        a.batch.grow([0, 1])
+    assert sums.mode == dps.MODE_FULL and a.batch.lengths == [16, 0]
