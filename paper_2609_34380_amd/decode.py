@@ -355,7 +355,7 @@ class Beams:
             return None
         self.score.copy_(step.score)
         self.done.copy_(step.done.view(-1))
-        parents, tokens = step.parent.view(-1).tolist(), step.token.view(-1)
+        parents, tokens = step.parent.view(-1).tolist(), step.token.view(-1).clone()
         self.tokens = [self.tokens[p] + [t] if p >= 0 else []
                        for p, t in zip(parents, tokens.tolist())]
         return tokens

@@ -476,3 +476,34 @@ def test_a_grow_that_is_refused_evicts_nothing(host):
     with pytest.raises(RuntimeError):
         a.batch.grow([0, 1])
     assert sums.mode == dps.MODE_FULL and a.batch.lengths == [16, 0]
+
+
+# ---- beams ------------------------------------------------------------------------------------
+
+
+class Picks:
+    """beam_select that hands out given parents and tokens, in the buffers it is given."""
+
+    def __init__(self, picks):
+        self.picks = list(picks)
+
+    def __call__(self, logits, score, beams, keep=None, done=None, end=-1, out=None, workspace=None):
+        parent, token = self.picks.pop(0)
+        out.score.fill_(-1.0)
+        out.parent.copy_(torch.tensor(parent, dtype=torch.int32).view(out.parent.shape))
+        out.token.copy_(torch.tensor(token, dtype=torch.int32).view(out.token.shape))
+        out.done.zero_()
+        return out
+
+
+def test_picked_tokens_stay(host, monkeypatch):
+    """What pick() returned is still what it was after the next pick()."""
+    monkeypatch.setattr(dps, "beam_select", Picks([([0, 0], [5, 6]), ([1, 0], [7, 8])]))
+    a = Life(dps.SumManager(2, 8, 0), 2)
+    search = decode.Beams(a.batch, [a.cache], 2, 100)
+    a.step([1, 1])
+    first = search.pick(torch.zeros(2, 100))
+    a.step([1, 1])
+    second = search.pick(torch.zeros(2, 100))
+    assert first.tolist() == [5, 6] and second.tolist() == [7, 8]
+    assert search.tokens == [[6, 7], [5, 8]]
