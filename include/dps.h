@@ -563,7 +563,7 @@ size_t dps_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t vocab, int
 /* The next beams of each request: token t after beam w scores score_w + x_wt -
  * log(sum_t exp(x_wt)); the `keep` highest of all beams and tokens of the request,
  * of equal ones those of the lowest (w, t), go to the outputs in that order.  Scores
- * are compared in 64 bits (sums of exponentials good to 2^-21 of themselves) and
+ * are compared in 64 bits (sums of exponentials good to 2^-19 of themselves) and
  * rounded once to fp32.  A beam that has ended counts as one candidate, its score
  * with the token `end` (which has to be given with `done`).  A logit of -inf is never
  * picked; a beam with a NaN or +inf among its logits, or whose score is not

@@ -22,9 +22,12 @@
 // Precision: exponentials in fp32 of differences from the wave's largest (of which
 // none is above 0), the values of a 16-byte vector added in fp32, in pairs; their
 // sums, log and scores in 64 bits, since candidates of different beams may lie closer
-// than fp32 tells apart.  A sum is good to 2^-21 of itself: 3 roundings of 2^-24 in
-// the pairs, 2^-23 of the exponential, and 3 of 2^-24 |d| e^d (at most 0.37 of that) in
-// its argument d.
+// than fp32 tells apart.  A sum is good to 2^-19.8 of itself (fp32 logits 2^-20), in units of
+// 2^-24: 3 (2) for the pairs' roundings, 2 for the exponential, and 2.23 |d| for its
+// argument (the difference d and the product are rounded, log2 e is 0.23 off), where the mean
+// of |d| under the weights e^d is at most 5.6 of a wave's 4096 values (5.0 of 2048): (n - 1) t /
+// (e^t + n - 1), which is what one value and n - 1 others t below it have.  Such rows came
+// out up to 8.2 units off (16 bits: 6.5).
 #include <type_traits>
 
 #include "dps_internal.h"
