@@ -237,9 +237,12 @@ DPS_EXPORT dps_status dps_sum_compact(dps_sum *s, int64_t max_moves, int64_t *sr
                                    to * s->blocks_per_unit + to_index);
             }
         }
-        for (int64_t u : units)
-            if (s->used[u] == s->blocks_per_unit)
-                move_unit(s, u, DPS_UNIT_FULL);
+        for (int64_t u : units) {
+            if (s->used[u] == s->blocks_per_unit) {  // the set's node goes along: no allocation
+                s->full.insert(s->avail.extract(u));
+                s->state[u] = DPS_UNIT_FULL;
+            }
+        }
         std::sort(moves.begin(), moves.end());
         for (const auto &m : moves) {
             src[*n] = m.first;
