@@ -564,7 +564,9 @@ size_t dps_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t vocab, int
  * log(sum_t exp(x_wt)); the `keep` highest of all beams and tokens of the request,
  * of equal ones those of the lowest (w, t), go to the outputs in that order.  Scores
  * are compared in 64 bits (sums of exponentials good to 2^-19 of themselves) and
- * rounded once to fp32.  A beam that has ended counts as one candidate, its score
+ * rounded once to fp32.  Of different logits of one beam that are so near to each other
+ * that their scores are equal in 64 bits (2^-53 of the beam's score, or of the sum's log)
+ * any may be taken.  A beam that has ended counts as one candidate, its score
  * with the token `end` (which has to be given with `done`).  A logit of -inf is never
  * picked; a beam with a NaN or +inf among its logits, or whose score is not
  * finite, has no candidates.  Where there are fewer than `keep`, the rest is score

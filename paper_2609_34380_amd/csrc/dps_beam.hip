@@ -3,7 +3,9 @@
 // Beam w of a batch item, token t:  score = cum_w + (x_wt - log sum_t exp x_wt).
 // The `keep` best over all beams and tokens, of equal ones those with the lowest
 // (w, t).  Within a beam the order is that of the logits alone, so a piece of a
-// row can give up all but its `keep` best before the row's sum is known.
+// row can give up all but its `keep` best before the row's sum is known.  (Where different
+// logits end in the same 64-bit score, which of them were given up depends on their
+// pieces: the lowest tokens among those that were not are taken.)
 //
 // Two launches.  The first reads every logit once: a block of threads holds a piece
 // of a row in registers, sums its exponentials (a wave each) and lists its best.  The second, a

@@ -993,7 +993,9 @@ def beam_select(logits, score, beams, keep=None, done=None, end=-1, out=None, wo
     log_softmax(logits[row])[token] for each request, best first, of equal ones those
     of the lowest row and token.  score: float32, one a row; done: uint8, one a row:
     the beam has ended and stands for itself with the token `end`.  Returns a BeamStep
-    (out); places without a candidate have score -inf, parent and token -1."""
+    (out); places without a candidate have score -inf, parent and token -1.  (Different
+    logits of a row count as equal ones in any order where 64 bits cannot tell their scores
+    apart.)"""
     lib = _lib or load_library()
     kind = _BEAM_TYPES.get(logits.dtype)
     if kind is None or logits.dim() != 2 or not logits.is_cuda:

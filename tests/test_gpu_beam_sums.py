@@ -1,5 +1,6 @@
 """How near beam_select's sums of exponentials are to the exact ones, where their roundings
-weigh most: one peak, and as many equal values as a wave holds some way below it."""
+weigh most: one peak, and as many equal values as a wave holds some way below it; and what it
+picks where 64 bits cannot tell scores apart."""
 import math
 
 import numpy as np
@@ -57,3 +58,20 @@ def test_a_peak_over_equal_values(dtype, per):
     print("%s: %.2f of 2^-24, at most %.2f" % (dtype, off.max() / UNIT, limit / UNIT))
     assert off.max() <= limit
     assert limit < 2.0 ** -19
+
+
+@pytest.mark.parametrize("vocab,keep", [(50, 4), (70000, 4), (70000, 256)])
+def test_scores_that_swallow_the_logits(vocab, keep):
+    """A score so large that every token's is the same in 64 bits: different tokens of the
+    first beam, all of that score; equal logits still by their tokens."""
+    rng = np.random.default_rng(vocab + keep)
+    x = torch.from_numpy(rng.normal(size=(4, vocab)).astype(np.float32))
+    x[2:] = 1.5
+    score = np.array([-1e20, -1e20, -1e20, -1e20], np.float32)
+    got = dps.beam_select(x.to(DEV), torch.from_numpy(score).to(DEV), 2, keep=keep)
+    token, parent = got.token.tolist(), got.parent.tolist()
+    n = min(keep, vocab)
+    assert parent[0][:n] == [0] * n and len(set(token[0][:n])) == n
+    assert all(0 <= t < vocab for t in token[0][:n])
+    assert parent[1][:n] == [2] * n and token[1][:n] == list(range(n))
+    assert bool((got.score == float(score[0])).all())
