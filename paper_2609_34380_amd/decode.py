@@ -306,13 +306,13 @@ class AttentionLayer:
         rows, step = x.shape[0], batch.step
         if rows != step.pos.shape[0]:
             raise ValueError("x has %d rows, the step's map %d" % (rows, step.pos.shape[0]))
+        if self.groups != batch.groups:
+            raise ValueError("the layer is for %d groups, the batch has %d" %
+                             (self.groups, batch.groups))
         qkv, q, a = self._qkv[:rows], self._q[:rows], self._a[:rows]
         dps.linear(x, self.qkv, mode, out=qkv, workspace=self._ws)
         dps.kv_store(qkv, self.cache, step.slot, self.heads, pos=step.pos, rope=self.rope,
                      q_weight=self.q_weight, k_weight=self.k_weight, q_out=q)
-        if self.groups != batch.groups:
-            raise ValueError("the layer is for %d groups, the batch has %d" %
-                             (self.groups, batch.groups))
         if self.groups:
             dps.attn_shared(q, self.cache, batch.table, step.kv_len, batch.group_start,
                             batch.shared_len, req=step.req, out=a, workspace=self._ws)
