@@ -87,7 +87,13 @@ class PagedBatch:
             if had + n > self.max_tokens:
                 raise ValueError("a request outgrows its table row")
             need.append(-(-(had + n) // self.block_tokens) - -(-had // self.block_tokens))
-        self._mapped()
+        try:
+            self._mapped()
+        except RuntimeError:
+            c = self.sums.counts()
+            if sum(need) > (c["free"] + c["backed"]) * self.sums.blocks_per_unit + c["free_blocks"]:
+                return False
+            raise
         taken = self.sums.alloc(sum(need))
         if taken is None:
             return False

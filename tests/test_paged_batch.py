@@ -110,9 +110,9 @@ class Life:
 
     count = 0
 
-    def __init__(self, sums, slots, columns=16, groups=0):
-        self.batch = decode.PagedBatch(sums, slots, columns * TOKENS, TOKENS, device="cpu",
-                                       groups=groups)
+    def __init__(self, sums, slots, columns=16, groups=0, rows=None):
+        self.batch = decode.PagedBatch(sums, slots, columns * TOKENS, TOKENS, rows=rows,
+                                       device="cpu", groups=groups)
         self.cache = Cache(sums.n_units * sums.blocks_per_unit)
         self.want = [[] for _ in range(slots)]
 
@@ -469,12 +469,14 @@ def test_wake_stays_until_it_is_looked_at(host):
 def test_a_grow_that_is_refused_evicts_nothing(host):
     """A step that is refused takes no blocks, and so evicts nothing."""
     sums = dps.SumManager(2, 4, 1)
-    a = Life(sums, 2)
+    a = Life(sums, 2, rows=20)
     for _ in range(15):
         a.step([1, 0])
     assert a.batch.grow([1, 0]) and sums.mode == dps.MODE_FULL
     with pytest.raises(RuntimeError):
         a.batch.grow([0, 1])
+    assert sums.mode == dps.MODE_FULL and a.batch.lengths == [16, 0]
+    assert not a.batch.grow([0, 17])         # no room for it anyway
     assert sums.mode == dps.MODE_FULL and a.batch.lengths == [16, 0]
 
 
