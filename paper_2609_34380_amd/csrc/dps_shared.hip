@@ -22,7 +22,10 @@
 // twice loses 6 to 10 us (240 rows of 64 heads under 16384 tokens: 250 us on the line, 230
 // so).  In shared_kernel one or two groups of several items do the same where that makes no
 // range more than an eighth longer: the items' blocks then read the same tokens at the same
-// time (96 columns of 60000 FP16 tokens: 124 us on the line, 81 so).
+// time (96 columns of 60000 FP16 tokens, 8 key/value heads: 123 us on the line, 77 so; of
+// 16384 50 and 40, and 51 with a bound of a sixteenth).  Longer ranges go either way: 192
+// columns of 16384 tokens and 16 key/value heads 81 us on the line, 94 with whole blocks, 84
+// columns of each of two prefixes of 9000 and 24 heads 134 and 87.
 //
 // The tile is attn_kernel's: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix
 // instructions, 32 tokens at a time, HT column tiles of 16 a wave; keys and values go
@@ -795,6 +798,10 @@ shared_wide_kernel(const SharedProblem p, const int32_t *__restrict__ tables)
     const int first_head = kvh * a.group + sub * a.group_step;
     const int n_heads = min(a.group_step, a.group - sub * a.group_step);
 
+    // of a tile's time 3 of 8 parts are its own, the rest goes with its columns: 300 rows of 8
+    // heads under 20 FP16 prefixes of up to 4000 tokens take 155 us with 0 of 8, 118 with 2, 111
+    // with 3, 110 with 4 and 122 with 6, under 30 prefixes 179, 142, 145, 139 and 153, 256 rows
+    // under 7 E4M3 prefixes of 12000 238, 188, 199, 196 and 206
     typedef Deal<kWideWaves, 32, kWideWaves, kWideWaves * 3 / 8> DealT;
     const bool good = find_groups<DealT>(p, s_groups, blocks);
     const int32_t share = uniform(s_groups.share);
