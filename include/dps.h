@@ -615,7 +615,9 @@ dps_status dps_sum_free(dps_sum *s, const int64_t *blocks, int64_t n, int32_t *w
 /* Moves that empty whole units: for AVAIL units from the one with the fewest blocks on
  * (the lowest id of equals), all of its blocks go to free places of the other AVAIL
  * units, the fullest first, as long as they fit there and in max_moves in all.  The
- * *n moves go to src[i] -> dst[i] (room for max_moves each), src ascending.  The dst
+ * *n moves go to src[i] -> dst[i] (room for max_moves each), src ascending; whoever
+ * holds the blocks (a caller that is not the only one frees the dst of moves that it
+ * leaves out, and never their src).  The dst
  * blocks are allocated by this call and the src blocks stay so: the caller copies
  * the blocks and changes its tables (dps_kv_copy, dps_kv_remap) and then frees src
  * (dps_sum_free), which makes their units FREE. */

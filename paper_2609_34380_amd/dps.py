@@ -1079,9 +1079,9 @@ class SumManager:
 
     def compact(self, max_moves):
         """Moves that empty whole units (dps_sum_compact): two lists of block ids, src
-        (ascending) and dst.  dst is allocated from now on; src is freed by the caller,
-        with free(), once the blocks are copied (kv_copy) and no table names it
-        (kv_remap)."""
+        (ascending) and dst, whoever holds them.  dst is allocated from now on; src is freed
+        by the caller, with free(), once the blocks are copied (kv_copy) and no table names
+        it (kv_remap); of a move that the caller leaves out, dst is."""
         arr = ctypes.c_int64 * max(max_moves, 1)
         src, dst, n = arr(), arr(), ctypes.c_int64(0)
         _check(_lib.dps_sum_compact(self._h, max_moves, src, dst, ctypes.byref(n)))
